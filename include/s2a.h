@@ -1,4 +1,4 @@
-/* S2A 4-bit activation stash for GELU and softmax -- C ABI of libs2a.so (sm_100a).
+/* S2A 4-bit activation stash for GELU and softmax, and the layers around them -- C ABI of libs2a.so (sm_100a).
  *
  * The library implements the "Non-Parametric Layers" part (Section 3.2) of
  * "Structure to Activation" (arXiv 2503.08154): in the forward pass a fused kernel
@@ -65,7 +65,8 @@ typedef enum {
   S2A_ERR_CUDA = 5,   /* the CUDA runtime refused the launch                     */
   S2A_ERR_DEVICE = 6, /* a kernel gave up on a bounded wait (see s2a_device_error) */
   S2A_ERR_TOO_LARGE = 7, /* beyond the built-in scratch of s2a_gelu_fwd_tensor_range_static */
-  S2A_ERR_OVERLAP = 8 /* the output overlaps the input without being the same tensor   */
+  S2A_ERR_OVERLAP = 8, /* the output overlaps the input without being the same tensor  */
+  S2A_ERR_VALUE = 9   /* a scalar argument (eps, p, a distance) is outside its range   */
 } s2a_status;
 
 /* Bytes of packed codes for n_elems elements: (n_elems + 1) / 2. */
@@ -245,6 +246,134 @@ int s2a_cap_bwd(const void* grad_out, void* grad_in, size_t n_rows, size_t chann
  */
 int s2a_lrp_fwd(const void* x, const float* A, const float* B, void* y, size_t batch, size_t tokens,
                 size_t channels, size_t rank, int dt, void* cuda_stream);
+
+/* ---- The layers between the stash kernels of a transformer block --------------------------
+ * Layer norm, dropout and the bucketed relative position bias, with their backward passes.
+ * They belong to no equation of the paper; they are here because a block's remaining layers
+ * would otherwise keep for backward what the stash saves: of these, layer norm keeps 8 bytes
+ * a row and the other two keep nothing.  The conventions at the top hold, but for what is said
+ * here.  `wdt` is the element type of learned parameters and of their gradients (S2A_F32 or
+ * S2A_BF16, whatever dt is).  Sums are binary32 and in a fixed order: no atomics, so a call
+ * repeated on the same inputs writes the same bits.  Non-finite inputs are allowed and go where
+ * the formulas take them.
+ *
+ * A `scratch` argument is device memory that the caller owns, 16-byte aligned, of the size that
+ * the *_scratch_bytes helper gives for the same shape; its contents on entry are ignored, and no
+ * other work may use it until the call's kernels have finished.  Two captured graphs that may
+ * run at the same time need a scratch each.
+ */
+
+/* Bytes of scratch for the weights' gradients of s2a_layernorm_bwd (0 where row_len is 0 or
+ * above 2^31-1): at most 592 * row_len * 4. */
+size_t s2a_layernorm_scratch_bytes(size_t n_rows, size_t row_len);
+
+/* Layer norm forward.  Per row: mean = sum(x) / row_len, var = sum((x - mean)^2) / row_len,
+ * rstd = 1 / sqrt(var + eps), y = (x - mean) * rstd * gamma + beta.
+ *   x      in   n_rows rows of row_len elements of type dt, x_stride elements apart
+ *   gamma  in   row_len elements of type wdt, or NULL (ones)
+ *   beta   in   row_len elements of type wdt, or NULL (zeros)
+ *   y      out  n_rows rows, y_stride elements apart; may be x with the same stride
+ *   stats  out  2 * n_rows floats, (mean, rstd) of each row for the backward call, 8-byte
+ *               aligned; or NULL (inference)
+ * Pointers need the alignment of their element type only (stats: 8 bytes); rows that all start
+ * on 16-byte boundaries with row_len a multiple of 8 are read in whole vectors, others element
+ * by element.  y_stride must be at least row_len; the bytes between rows are not touched.
+ * x_stride is free (0 repeats one row).  eps: finite, not negative.  An output whose rows
+ * overlap x's rows without being the same rows returns S2A_ERR_OVERLAP (rows of one stride may
+ * interleave); gamma, beta and stats must not overlap an output (not checked).
+ */
+int s2a_layernorm_fwd(const void* x, const void* gamma, const void* beta, void* y, float* stats, size_t n_rows,
+                      size_t row_len, size_t x_stride, size_t y_stride, float eps, int dt, int wdt, void* cuda_stream);
+
+/* Layer norm backward, from x and the (mean, rstd) that the forward call kept.  With
+ * a = grad_out * gamma and xhat = (x - mean) * rstd:
+ *   grad_in    = rstd * (a - sum(a) / row_len - xhat * sum(a * xhat) / row_len)
+ *   grad_gamma = sum over rows of grad_out * xhat,  grad_beta = sum over rows of grad_out
+ *   grad_out, x, grad_in   rows of type dt with a stride each; grad_in may be grad_out or x (same
+ *                          stride)
+ *   stats                  in   as written by s2a_layernorm_fwd
+ *   grad_gamma, grad_beta  out  row_len elements of type wdt, or NULL each (frozen weights); they
+ *                               are overwritten, not added to, and zeros where n_rows is 0
+ *   scratch                s2a_layernorm_scratch_bytes(n_rows, row_len) bytes; may be NULL where
+ *                          both weight gradients are
+ * Everything else as for s2a_layernorm_fwd.
+ */
+int s2a_layernorm_bwd(const void* grad_out, const void* x, const void* gamma, const float* stats, void* grad_in,
+                      void* grad_gamma, void* grad_beta, void* scratch, size_t n_rows, size_t row_len,
+                      size_t grad_out_stride, size_t x_stride, size_t grad_in_stride, int dt, int wdt, void* cuda_stream);
+
+/* The dropout threshold T = round_half_even(65536 p), 0 .. 65536: p is used to a resolution of
+ * 2^-16.  Host-only. */
+uint32_t s2a_dropout_threshold(double p);
+
+/* Dropout forward, y = dropout(x) or y = residual + dropout(x).  The mask is a function of
+ * (rng, site, element) and is stored nowhere: element e of the flat tensor owns 16 bits of
+ * Philox4x32-10 under key rng[0] (low word first) at counter (e / 8, rng[1] + site) (two 64-bit
+ * numbers, low words first); of the four output words, word w holds element 2w of the eight in its
+ * low half and element 2w + 1 in its high half.  The element is kept when its bits are at least
+ * T = s2a_dropout_threshold(p) and then scaled by 65536 / (65536 - T) (binary32), which makes
+ * the expectation x exactly; a dropped element counts as 0 whatever it holds.  T = 65536 drops
+ * everything.
+ *   x         in   n_elems elements of type dt
+ *   residual  in   n_elems elements of type dt, or NULL
+ *   y         out  n_elems elements of type dt; may be x or residual
+ *   rng       in   two 64-bit words in DEVICE memory, (seed, offset), 8-byte aligned: read when
+ *                  the kernel runs, so a captured graph draws a new mask on every replay if the
+ *                  offset is advanced in between.  Forward and backward must see the same words.
+ *   site      added to the offset (modulo 2^64); give each call of a step its own, and advance
+ *             the offset by more than the largest site from step to step
+ *   p         0 <= p <= 1
+ * The mask does not depend on dt, on p's effect on other elements, or on the launch shape.
+ */
+int s2a_dropout_fwd(const void* x, const void* residual, void* y, size_t n_elems, const uint64_t* rng, uint64_t site,
+                    double p, int dt, void* cuda_stream);
+
+/* Dropout backward: the same mask and scale applied to grad_out (the gradient to the residual is
+ * grad_out itself and needs no call).  grad_in may be grad_out.
+ */
+int s2a_dropout_bwd(const void* grad_out, void* grad_in, size_t n_elems, const uint64_t* rng, uint64_t site, double p, int dt,
+                    void* cuda_stream);
+
+/* Learned relative position bias, added to attention scores: y[b, h, q, k] = x[b, h, q, k] +
+ * table[bucket(q, k)][h].
+ *   x        in   [batch, heads, tq, tk] elements of type dt
+ *   table    in   [n_buckets, heads] elements of type wdt
+ *   buckets  in   int32, 4-byte aligned.  by_distance == 0: a map [tq, tk] (2-D windows).
+ *                 Otherwise a vector of tq + tk - 1 entries over the distance, bucket(q, k) =
+ *                 buckets[k - q + tq - 1]: a sequence whose bucket depends on k - q only; for one
+ *                 new token against a cache, tq = 1 and the vector is a window of a longer one.
+ *                 An entry outside 0 .. n_buckets - 1 adds nothing and has no gradient.
+ *   y        out  like x; may be x
+ * heads: 1 .. 65535, n_buckets: 1 .. 32768, tq * tk at most 2^40.  Scores of -inf (masked) stay
+ * -inf, rows of them included.  The gradient to x is grad_out itself and needs no call.
+ */
+int s2a_relbias_fwd(const void* x, const void* table, const int32_t* buckets, int by_distance, void* y, size_t batch,
+                    size_t heads, size_t tq, size_t tk, size_t n_buckets, int dt, int wdt, void* cuda_stream);
+
+/* Bytes of scratch for s2a_relbias_bwd (0 for a shape it refuses, and for an empty one). */
+size_t s2a_relbias_scratch_bytes(size_t batch, size_t heads, size_t tq, size_t tk, size_t n_buckets);
+
+/* The table's gradient: grad_table[u][h] = the sum of grad_out[b, h, q, k] over b and over the (q, k)
+ * of bucket u.
+ *   grad_out    in   [batch, heads, tq, tk] elements of type dt
+ *   grad_table  out  [n_buckets, heads] elements of type wdt; overwritten, zeros where there is
+ *                    nothing to add
+ *   scratch     s2a_relbias_scratch_bytes(...) bytes
+ */
+int s2a_relbias_bwd(const void* grad_out, const int32_t* buckets, int by_distance, void* grad_table, void* scratch,
+                    size_t batch, size_t heads, size_t tq, size_t tk, size_t n_buckets, int dt, int wdt, void* cuda_stream);
+
+/* Buckets over the distance d = k - q for `by_distance`, written to HOST memory: entry i is the bucket
+ * of d = first_distance + i, i < count.  A side has n_buckets buckets (half of them where
+ * `bidirectional`: keys ahead of the query then use the upper half, otherwise they all fall in bucket
+ * 0).  With n = |d| and e = side / 2: n itself for n < e, beyond that
+ * e + floor(log(n / e) / log(max_distance / e) * (side - e)), at most side - 1, with the borders in
+ * exact arithmetic.  n_buckets: at least 2 a side, even where bidirectional; max_distance above e;
+ * |first_distance| and count at most 2^40.  For tq queries against tk keys of which the last tq are
+ * the queries, first_distance = 1 - tk and count = tq + tk - 1.
+ */
+int s2a_relbias_log_buckets(int32_t* buckets, int64_t first_distance, size_t count, size_t n_buckets, size_t max_distance,
+                            int bidirectional);
 
 /* The pipelined kernels wait on shared-memory barriers with an iteration limit; a
  * wait that runs out records a bit in a per-device word and the kernel returns early.

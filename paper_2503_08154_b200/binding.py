@@ -29,6 +29,9 @@ EXPORTS = (
     "s2a_selftest_wait_expiry",
     "s2a_selftest_exp2_monotone",
     "s2a_codes_bytes_bits", "s2a_gelu_fwd_bits", "s2a_gelu_bwd_bits", "s2a_softmax_fwd_bits", "s2a_softmax_bwd_bits",
+    "s2a_layernorm_scratch_bytes", "s2a_layernorm_fwd", "s2a_layernorm_bwd",
+    "s2a_dropout_threshold", "s2a_dropout_fwd", "s2a_dropout_bwd",
+    "s2a_relbias_scratch_bytes", "s2a_relbias_fwd", "s2a_relbias_bwd", "s2a_relbias_log_buckets",
 )
 
 _lib = None
@@ -102,6 +105,20 @@ def lib() -> ctypes.CDLL:
             f = getattr(L, name)
             f.argtypes = [c.c_void_p, c.c_void_p, c.c_void_p, c.c_size_t, c.c_int, c.c_void_p]
             f.restype = c.c_int
+        ptr, size = c.c_void_p, c.c_size_t
+        for name, res, args in (
+                ("s2a_layernorm_scratch_bytes", size, [size, size]),
+                ("s2a_layernorm_fwd", c.c_int, [ptr] * 5 + [size] * 4 + [c.c_float, c.c_int, c.c_int, ptr]),
+                ("s2a_layernorm_bwd", c.c_int, [ptr] * 8 + [size] * 5 + [c.c_int, c.c_int, ptr]),
+                ("s2a_dropout_threshold", c.c_uint32, [c.c_double]),
+                ("s2a_dropout_fwd", c.c_int, [ptr, ptr, ptr, size, ptr, c.c_uint64, c.c_double, c.c_int, ptr]),
+                ("s2a_dropout_bwd", c.c_int, [ptr, ptr, size, ptr, c.c_uint64, c.c_double, c.c_int, ptr]),
+                ("s2a_relbias_scratch_bytes", size, [size] * 5),
+                ("s2a_relbias_fwd", c.c_int, [ptr, ptr, ptr, c.c_int, ptr] + [size] * 5 + [c.c_int, c.c_int, ptr]),
+                ("s2a_relbias_bwd", c.c_int, [ptr, ptr, c.c_int, ptr, ptr] + [size] * 5 + [c.c_int, c.c_int, ptr]),
+                ("s2a_relbias_log_buckets", c.c_int, [ptr, c.c_int64, size, size, size, c.c_int])):
+            f = getattr(L, name)
+            f.argtypes, f.restype = args, res
         L.s2a_device_error.argtypes = [c.POINTER(c.c_uint), c.c_int]
         L.s2a_device_error.restype = c.c_int
         L.s2a_describe_plan.argtypes = [c.c_int, c.c_size_t, c.c_size_t, c.c_int, c.c_char_p, c.c_size_t]
@@ -332,6 +349,189 @@ def s2a_relu_bwd(grad_out, mask, grad_in) -> None:
         raise S2AError("mask must be uint8 with at least mask_bytes(n) elements")
     check(lib().s2a_relu_bwd(grad_out.data_ptr(), mask.data_ptr(), grad_in.data_ptr(), n,
                              dtype_code(grad_out), _stream_ptr()))
+
+
+# ------------------------------------------------- layer norm, dropout, relative position bias
+def _on_device(first: torch.Tensor, *others) -> None:
+    """One device for all tensors of a call, None aside, and that device current: a launch goes to
+    the current device, whatever memory its pointers name."""
+    dev = first.device
+    if dev.type != "cuda":
+        raise S2AError("CUDA tensors are needed")
+    for t in others:
+        if t is not None and t.device != dev:
+            raise S2AError("all tensors of a call must be on one device")
+    if dev.index != torch.cuda.current_device():
+        raise S2AError("the tensors' device must be the current one (torch.cuda.device)")
+
+
+def _rows(t: torch.Tensor, n_rows: int, row_len: int, what: str) -> int:
+    """The stride in elements between the rows of a tensor that holds n_rows rows of row_len: a
+    contiguous one of any shape, or one whose last dimension is a row and whose leading dimensions
+    are evenly spaced (a slice such as x[:, 0])."""
+    if t.numel() != n_rows * row_len:
+        raise S2AError("%s must hold %d rows of %d elements" % (what, n_rows, row_len))
+    if t.is_contiguous():
+        return row_len
+    if t.dim() == 0 or t.shape[-1] != row_len or (row_len > 1 and t.stride(-1) != 1):
+        raise S2AError("%s: the elements of a row must be contiguous" % what)
+    dims = [(n, s) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n != 1]
+    for (_, outer), (n, inner) in zip(dims, dims[1:]):
+        if outer != n * inner:
+            raise S2AError("%s: its rows must be evenly spaced" % what)
+    return dims[-1][1] if dims else row_len
+
+
+def _param(t, n: int, what: str):
+    """The address of a learned parameter (or of its gradient) of n elements, None for none."""
+    if t is None:
+        return None
+    if not t.is_contiguous() or t.numel() != n:
+        raise S2AError("%s must be contiguous with %d elements" % (what, n))
+    return t.data_ptr()
+
+
+def _param_dtype(*ts) -> int:
+    codes = {dtype_code(t) for t in ts if t is not None}
+    if len(codes) > 1:
+        raise S2AError("learned parameters and their gradients must have one dtype")
+    return codes.pop() if codes else F32
+
+
+def _scratch(t, need: int):
+    if t is None:
+        raise S2AError("scratch is needed")
+    if not t.is_contiguous() or t.numel() * t.element_size() < need:
+        raise S2AError("scratch must be contiguous with at least %d bytes" % need)
+    return t.data_ptr()
+
+
+def _stats(t, n_rows: int):
+    if t is None:
+        return None
+    if t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != 2 * n_rows:
+        raise S2AError("stats must be contiguous float32 with 2 elements a row")
+    return t.data_ptr()
+
+
+def layernorm_scratch_bytes(n_rows: int, row_len: int) -> int:
+    return int(lib().s2a_layernorm_scratch_bytes(n_rows, row_len))
+
+
+def s2a_layernorm_fwd(x, gamma, beta, y, stats, row_len: int, eps: float) -> None:
+    """Layer norm over rows of row_len elements.  gamma, beta and stats ([n_rows, 2] float32, what the
+    backward call needs) may be None; x and y may be slices with evenly spaced rows."""
+    _on_device(x, gamma, beta, y, stats)
+    if row_len <= 0 or x.numel() % row_len:
+        raise S2AError("x must hold whole rows of row_len elements")
+    if y.dtype != x.dtype:
+        raise S2AError("y must match x in dtype")
+    n = x.numel() // row_len
+    check(lib().s2a_layernorm_fwd(x.data_ptr(), _param(gamma, row_len, "gamma"), _param(beta, row_len, "beta"), y.data_ptr(),
+                                  _stats(stats, n), n, row_len, _rows(x, n, row_len, "x"), _rows(y, n, row_len, "y"), eps,
+                                  dtype_code(x), _param_dtype(gamma, beta), _stream_ptr(x)))
+
+
+def s2a_layernorm_bwd(grad_out, x, gamma, stats, grad_in, grad_gamma, grad_beta, scratch, row_len: int) -> None:
+    """Layer norm's backward pass.  grad_gamma and grad_beta may be None (frozen weights; without both,
+    scratch may be None too); scratch holds layernorm_scratch_bytes(n_rows, row_len) bytes."""
+    _on_device(x, grad_out, gamma, stats, grad_in, grad_gamma, grad_beta, scratch)
+    if row_len <= 0 or x.numel() % row_len:
+        raise S2AError("x must hold whole rows of row_len elements")
+    if grad_out.dtype != x.dtype or grad_in.dtype != x.dtype:
+        raise S2AError("grad_out and grad_in must match x in dtype")
+    if stats is None:
+        raise S2AError("stats of the forward call are needed")
+    n = x.numel() // row_len
+    sums = grad_gamma is not None or grad_beta is not None
+    check(lib().s2a_layernorm_bwd(
+        grad_out.data_ptr(), x.data_ptr(), _param(gamma, row_len, "gamma"), _stats(stats, n), grad_in.data_ptr(),
+        _param(grad_gamma, row_len, "grad_gamma"), _param(grad_beta, row_len, "grad_beta"),
+        _scratch(scratch, layernorm_scratch_bytes(n, row_len)) if sums else None, n, row_len,
+        _rows(grad_out, n, row_len, "grad_out"), _rows(x, n, row_len, "x"), _rows(grad_in, n, row_len, "grad_in"),
+        dtype_code(x), _param_dtype(gamma, grad_gamma, grad_beta), _stream_ptr(x)))
+
+
+def dropout_threshold(p: float) -> int:
+    return int(lib().s2a_dropout_threshold(p))
+
+
+def _dropout_args(x, y, rng, site):
+    _dev(x, "x"), _dev(y, "y"), _dev(rng, "rng")
+    if y.numel() != x.numel() or y.dtype != x.dtype:
+        raise S2AError("the output must match the input in size and dtype")
+    if rng.dtype != torch.int64 or rng.numel() != 2:
+        raise S2AError("rng must be int64 with 2 elements, (seed, offset)")
+    return site & 0xFFFFFFFFFFFFFFFF
+
+
+def s2a_dropout_fwd(x, residual, y, rng, site: int, p: float) -> None:
+    """y = dropout(x), or residual + dropout(x).  rng is an int64 CUDA tensor (seed, offset) that the kernel
+    reads; `site` tells the calls of one step apart."""
+    _on_device(x, residual, y, rng)
+    site = _dropout_args(x, y, rng, site)
+    if residual is not None:
+        _dev(residual, "residual")
+        if residual.numel() != x.numel() or residual.dtype != x.dtype:
+            raise S2AError("residual must match x in size and dtype")
+    check(lib().s2a_dropout_fwd(x.data_ptr(), residual.data_ptr() if residual is not None else None, y.data_ptr(), x.numel(),
+                                rng.data_ptr(), site, p, dtype_code(x), _stream_ptr(x)))
+
+
+def s2a_dropout_bwd(grad_out, grad_in, rng, site: int, p: float) -> None:
+    _on_device(grad_out, grad_in, rng)
+    site = _dropout_args(grad_out, grad_in, rng, site)
+    check(lib().s2a_dropout_bwd(grad_out.data_ptr(), grad_in.data_ptr(), grad_out.numel(), rng.data_ptr(), site, p,
+                                dtype_code(grad_out), _stream_ptr(grad_out)))
+
+
+def _bias_args(scores, buckets, table, batch, heads, tq, tk):
+    _dev(scores, "the scores"), _dev(buckets, "buckets"), _dev(table, "the table")
+    if min(batch, heads, tq, tk) < 0 or scores.numel() != batch * heads * tq * tk:
+        raise S2AError("the scores must be [batch, heads, tq, tk]")
+    if table.dim() != 2 or table.shape[1] != heads:
+        raise S2AError("the table must be [n_buckets, heads]")
+    if buckets.dtype != torch.int32:
+        raise S2AError("buckets must be int32")
+    if buckets.dim() == 2 and tuple(buckets.shape) == (tq, tk):
+        return 0
+    if buckets.dim() == 1 and buckets.numel() == max(tq + tk - 1, 0):
+        return 1
+    raise S2AError("buckets must be a map [tq, tk] or a vector [tq + tk - 1]")
+
+
+def s2a_relbias_fwd(x, table, buckets, y, batch: int, heads: int, tq: int, tk: int) -> None:
+    """y = x + table[bucket(q, k)] over scores [batch, heads, tq, tk].  buckets: int32, a map [tq, tk], or a
+    vector [tq + tk - 1] over the distance k - q + tq - 1."""
+    _on_device(x, table, buckets, y)
+    by_distance = _bias_args(x, buckets, table, batch, heads, tq, tk)
+    _dev(y, "y")
+    if y.numel() != x.numel() or y.dtype != x.dtype:
+        raise S2AError("y must match x in size and dtype")
+    check(lib().s2a_relbias_fwd(x.data_ptr(), table.data_ptr(), buckets.data_ptr(), by_distance, y.data_ptr(), batch, heads, tq,
+                                tk, table.shape[0], dtype_code(x), dtype_code(table), _stream_ptr(x)))
+
+
+def relbias_scratch_bytes(batch: int, heads: int, tq: int, tk: int, n_buckets: int) -> int:
+    return int(lib().s2a_relbias_scratch_bytes(batch, heads, tq, tk, n_buckets))
+
+
+def s2a_relbias_bwd(grad_out, buckets, grad_table, scratch, batch: int, heads: int, tq: int, tk: int) -> None:
+    """The table's gradient; scratch holds relbias_scratch_bytes(batch, heads, tq, tk, n_buckets) bytes."""
+    _on_device(grad_out, buckets, grad_table, scratch)
+    by_distance = _bias_args(grad_out, buckets, grad_table, batch, heads, tq, tk)
+    n = grad_table.shape[0]
+    need = relbias_scratch_bytes(batch, heads, tq, tk, n)
+    check(lib().s2a_relbias_bwd(grad_out.data_ptr(), buckets.data_ptr(), by_distance, grad_table.data_ptr(),
+                                _scratch(scratch, need) if need else None, batch, heads, tq, tk, n, dtype_code(grad_out),
+                                dtype_code(grad_table), _stream_ptr(grad_out)))
+
+
+def log_buckets(first_distance: int, count: int, n_buckets: int, max_distance: int, bidirectional: bool) -> torch.Tensor:
+    """Buckets of the distances first_distance, first_distance + 1, ... as a CPU int32 tensor (s2a_relbias_log_buckets)."""
+    out = torch.empty(count, dtype=torch.int32)
+    check(lib().s2a_relbias_log_buckets(out.data_ptr(), first_distance, count, n_buckets, max_distance, int(bidirectional)))
+    return out
 
 
 def s2a_device_error(clear: bool = False) -> int:

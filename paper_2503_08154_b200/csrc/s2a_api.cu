@@ -1,4 +1,5 @@
 // extern "C" entry points of libs2a.so: argument checks, choice of kernel path, launch.
+#include <math.h>
 #include <stdio.h>
 #include <string.h>
 
@@ -75,6 +76,7 @@ const char* s2a_status_string(int status) {
       return "S2A_ERR_TOO_LARGE: n_elems exceeds the built-in scratch of the allocation-free entry point "
              "(536,870,912 elements); use s2a_gelu_fwd_tensor_range with your own scratch";
     case S2A_ERR_OVERLAP: return "S2A_ERR_OVERLAP: the output overlaps the input without being the same tensor";
+    case S2A_ERR_VALUE: return "S2A_ERR_VALUE: a scalar argument is outside its range";
     default: return "unknown s2a status";
   }
 }
@@ -232,6 +234,165 @@ int s2a_softmax_bwd_bits(const void* grad_out, const uint8_t* codes, const float
                          size_t n_elems, size_t row_len, int bits, int dt, void* cuda_stream) {
   return run_bits(kSoftmaxBwd, grad_out, grad_in, const_cast<uint8_t*>(codes), const_cast<float*>(meta), n_elems,
                   row_len, bits, dt, cuda_stream);
+}
+
+// ---- layer norm, dropout, relative position bias
+
+static size_t elem_bytes(int dt) { return dt == S2A_F32 ? 4 : 2; }
+
+// Whether n_rows rows of row_bytes, row_stride bytes apart, reach into another such set (in place, with equal rows, is
+// asked separately).  Two sets of one stride may interleave: slices of one buffer side by side.
+static bool rows_overlap(const void* a, size_t a_stride, const void* b, size_t b_stride, size_t n_rows, size_t row_bytes) {
+  const uintptr_t pa = (uintptr_t)a, pb = (uintptr_t)b;
+  const uintptr_t span_a = (n_rows - 1) * a_stride + row_bytes, span_b = (n_rows - 1) * b_stride + row_bytes;
+  if (pa + span_a <= pb || pb + span_b <= pa) return false;
+  if (a_stride == b_stride && n_rows > 1 && a_stride >= row_bytes) {
+    const uintptr_t d = pa < pb ? (pb - pa) % a_stride : (pa - pb) % a_stride;
+    return d < row_bytes || a_stride - d < row_bytes;
+  }
+  return true;
+}
+
+// The layout rules of one output of a row-wise call against one of its inputs: the same rows, or apart.
+static bool bad_rows(const void* in, size_t in_stride, const void* out, size_t out_stride, size_t n_rows, size_t row_bytes) {
+  if (in == out && (in_stride == out_stride || n_rows == 1)) return false;
+  return rows_overlap(in, in_stride, out, out_stride, n_rows, row_bytes);
+}
+
+static bool bytes_overlap(const void* a, size_t a_bytes, const void* b, size_t b_bytes) {
+  return (uintptr_t)a < (uintptr_t)b + b_bytes && (uintptr_t)b < (uintptr_t)a + a_bytes;
+}
+
+// n_rows rows of row_len elements, `stride` apart, must be addressable.
+static bool bad_stride(size_t n_rows, size_t row_len, size_t stride) {
+  return n_rows > 1 && stride != 0 && (n_rows - 1) > (((size_t)1 << 60) - row_len) / stride;
+}
+
+size_t s2a_layernorm_scratch_bytes(size_t n_rows, size_t row_len) {
+  return row_len == 0 || row_len > 0x7fffffffull ? 0 : (size_t)layernorm_scratch_bytes(n_rows, (uint32_t)row_len);
+}
+
+int s2a_layernorm_fwd(const void* x, const void* gamma, const void* beta, void* y, float* stats, size_t n_rows,
+                      size_t row_len, size_t x_stride, size_t y_stride, float eps, int dt, int wdt, void* cuda_stream) {
+  if ((dt != S2A_F32 && dt != S2A_BF16) || (wdt != S2A_F32 && wdt != S2A_BF16)) return S2A_ERR_DTYPE;
+  if (row_len == 0 || row_len > 0x7fffffffull || (n_rows > 1 && y_stride < row_len) ||
+      bad_stride(n_rows, row_len, x_stride) || bad_stride(n_rows, row_len, y_stride))
+    return S2A_ERR_SHAPE;
+  if (!(eps >= 0.0f) || eps > 3.4028234e38f) return S2A_ERR_VALUE;
+  if (n_rows == 0) return S2A_OK;
+  if (!x || !y) return S2A_ERR_NULL;
+  const size_t es = elem_bytes(dt);
+  if (misaligned(x, es) || misaligned(y, es) || misaligned(gamma, elem_bytes(wdt)) || misaligned(beta, elem_bytes(wdt)) ||
+      misaligned(stats, 8))
+    return S2A_ERR_ALIGN;
+  if (bad_rows(x, x_stride * es, y, y_stride * es, n_rows, row_len * es)) return S2A_ERR_OVERLAP;
+  return launch_layernorm_fwd(dt, wdt, x, gamma, beta, y, stats, n_rows, (uint32_t)row_len, x_stride, y_stride, eps,
+                              (cudaStream_t)cuda_stream) == cudaSuccess ? S2A_OK : S2A_ERR_CUDA;
+}
+
+int s2a_layernorm_bwd(const void* grad_out, const void* x, const void* gamma, const float* stats, void* grad_in,
+                      void* grad_gamma, void* grad_beta, void* scratch, size_t n_rows, size_t row_len,
+                      size_t grad_out_stride, size_t x_stride, size_t grad_in_stride, int dt, int wdt, void* cuda_stream) {
+  if ((dt != S2A_F32 && dt != S2A_BF16) || (wdt != S2A_F32 && wdt != S2A_BF16)) return S2A_ERR_DTYPE;
+  if (row_len == 0 || row_len > 0x7fffffffull || (n_rows > 1 && grad_in_stride < row_len) ||
+      bad_stride(n_rows, row_len, x_stride) || bad_stride(n_rows, row_len, grad_out_stride) ||
+      bad_stride(n_rows, row_len, grad_in_stride))
+    return S2A_ERR_SHAPE;
+  const bool sums = grad_gamma || grad_beta;
+  if (n_rows > 0 && (!grad_out || !x || !stats || !grad_in || (sums && !scratch))) return S2A_ERR_NULL;
+  const size_t es = elem_bytes(dt), ws = elem_bytes(wdt);
+  if (misaligned(grad_out, es) || misaligned(x, es) || misaligned(grad_in, es) || misaligned(stats, 8) ||
+      misaligned(gamma, ws) || misaligned(grad_gamma, ws) || misaligned(grad_beta, ws) || misaligned(scratch, 16))
+    return S2A_ERR_ALIGN;
+  if (n_rows > 0 && (bad_rows(grad_out, grad_out_stride * es, grad_in, grad_in_stride * es, n_rows, row_len * es) ||
+                     bad_rows(x, x_stride * es, grad_in, grad_in_stride * es, n_rows, row_len * es)))
+    return S2A_ERR_OVERLAP;
+  return launch_layernorm_bwd(dt, wdt, grad_out, x, gamma, stats, grad_in, grad_gamma, grad_beta, (float*)scratch, n_rows,
+                              (uint32_t)row_len, grad_out_stride, x_stride, grad_in_stride, (cudaStream_t)cuda_stream) ==
+                 cudaSuccess ? S2A_OK : S2A_ERR_CUDA;
+}
+
+static int run_dropout(const void* x, const void* residual, void* y, size_t n, const uint64_t* rng, uint64_t site, double p,
+                       int dt, void* stream) {
+  if (dt != S2A_F32 && dt != S2A_BF16) return S2A_ERR_DTYPE;
+  if (!(p >= 0.0 && p <= 1.0)) return S2A_ERR_VALUE;
+  if (n > ((size_t)1 << 60)) return S2A_ERR_SHAPE;
+  if (n == 0) return S2A_OK;
+  if (!x || !y || !rng) return S2A_ERR_NULL;
+  if (misaligned(x, 16) || misaligned(residual, 16) || misaligned(y, 16) || misaligned(rng, 8)) return S2A_ERR_ALIGN;
+  const size_t bytes = n * elem_bytes(dt);
+  if ((x != y && bytes_overlap(x, bytes, y, bytes)) || (residual && residual != y && bytes_overlap(residual, bytes, y, bytes)))
+    return S2A_ERR_OVERLAP;
+  return launch_dropout(dt, x, residual, y, n, rng, site, s2a_dropout_threshold(p), (cudaStream_t)stream) == cudaSuccess
+             ? S2A_OK : S2A_ERR_CUDA;
+}
+
+uint32_t s2a_dropout_threshold(double p) { return !(p > 0.0) ? 0u : (p >= 1.0 ? 65536u : (uint32_t)nearbyint(65536.0 * p)); }
+
+int s2a_dropout_fwd(const void* x, const void* residual, void* y, size_t n_elems, const uint64_t* rng, uint64_t site,
+                    double p, int dt, void* cuda_stream) {
+  return run_dropout(x, residual, y, n_elems, rng, site, p, dt, cuda_stream);
+}
+
+int s2a_dropout_bwd(const void* grad_out, void* grad_in, size_t n_elems, const uint64_t* rng, uint64_t site, double p, int dt,
+                    void* cuda_stream) {
+  return run_dropout(grad_out, nullptr, grad_in, n_elems, rng, site, p, dt, cuda_stream);
+}
+
+static bool bad_bias_shape(size_t batch, size_t heads, size_t tq, size_t tk, size_t n_buckets) {
+  if (batch > 0x7fffffffull || heads == 0 || heads > 65535u || tq > 0x7fffffffull || tk > 0x7fffffffull || n_buckets == 0 ||
+      n_buckets > kMaxBuckets)
+    return true;
+  const size_t slab = tq * tk;
+  return slab > ((size_t)1 << 40) || (slab != 0 && batch * heads > ((size_t)1 << 60) / slab);
+}
+
+size_t s2a_relbias_scratch_bytes(size_t batch, size_t heads, size_t tq, size_t tk, size_t n_buckets) {
+  if (bad_bias_shape(batch, heads, tq, tk, n_buckets) || batch * tq * tk == 0) return 0;
+  return (size_t)relbias_bwd_ctas((uint32_t)batch, (uint32_t)heads, (uint32_t)tq, (uint32_t)tk, (uint32_t)n_buckets) *
+         n_buckets * sizeof(float);
+}
+
+int s2a_relbias_fwd(const void* x, const void* table, const int32_t* buckets, int by_distance, void* y, size_t batch,
+                    size_t heads, size_t tq, size_t tk, size_t n_buckets, int dt, int wdt, void* cuda_stream) {
+  if ((dt != S2A_F32 && dt != S2A_BF16) || (wdt != S2A_F32 && wdt != S2A_BF16)) return S2A_ERR_DTYPE;
+  if (bad_bias_shape(batch, heads, tq, tk, n_buckets)) return S2A_ERR_SHAPE;
+  if (batch * tq * tk == 0) return S2A_OK;
+  if (!x || !table || !buckets || !y) return S2A_ERR_NULL;
+  if (misaligned(x, 16) || misaligned(y, 16) || misaligned(table, elem_bytes(wdt)) || misaligned(buckets, 4))
+    return S2A_ERR_ALIGN;
+  const size_t bytes = batch * heads * tq * tk * elem_bytes(dt);
+  if (x != y && bytes_overlap(x, bytes, y, bytes)) return S2A_ERR_OVERLAP;
+  return launch_relbias_fwd(dt, wdt, x, table, buckets, by_distance != 0, y, (uint32_t)batch, (uint32_t)heads, (uint32_t)tq,
+                            (uint32_t)tk, (uint32_t)n_buckets, (cudaStream_t)cuda_stream) == cudaSuccess
+             ? S2A_OK : S2A_ERR_CUDA;
+}
+
+int s2a_relbias_bwd(const void* grad_out, const int32_t* buckets, int by_distance, void* grad_table, void* scratch,
+                    size_t batch, size_t heads, size_t tq, size_t tk, size_t n_buckets, int dt, int wdt, void* cuda_stream) {
+  if ((dt != S2A_F32 && dt != S2A_BF16) || (wdt != S2A_F32 && wdt != S2A_BF16)) return S2A_ERR_DTYPE;
+  if (bad_bias_shape(batch, heads, tq, tk, n_buckets)) return S2A_ERR_SHAPE;
+  const bool empty = batch * tq * tk == 0;
+  if (!grad_table || (!empty && (!grad_out || !buckets || !scratch))) return S2A_ERR_NULL;
+  if (misaligned(grad_out, 16) || misaligned(buckets, 4) || misaligned(grad_table, elem_bytes(wdt)) || misaligned(scratch, 16))
+    return S2A_ERR_ALIGN;
+  return launch_relbias_bwd(dt, wdt, grad_out, buckets, by_distance != 0, grad_table, (float*)scratch, (uint32_t)batch,
+                            (uint32_t)heads, (uint32_t)tq, (uint32_t)tk, (uint32_t)n_buckets, (cudaStream_t)cuda_stream) ==
+                 cudaSuccess ? S2A_OK : S2A_ERR_CUDA;
+}
+
+int s2a_relbias_log_buckets(int32_t* buckets, int64_t first_distance, size_t count, size_t n_buckets, size_t max_distance,
+                            int bidirectional) {
+  const size_t side = bidirectional ? n_buckets / 2 : n_buckets;
+  if (n_buckets > kMaxBuckets || side < 2 || (bidirectional && n_buckets % 2 != 0)) return S2A_ERR_SHAPE;
+  if (max_distance <= side / 2 || max_distance > 0x7fffffffull || count > ((size_t)1 << 40) ||
+      first_distance < -((int64_t)1 << 40) || first_distance > ((int64_t)1 << 40))
+    return S2A_ERR_VALUE;
+  if (count == 0) return S2A_OK;
+  if (!buckets) return S2A_ERR_NULL;
+  if (misaligned(buckets, 4)) return S2A_ERR_ALIGN;
+  log_buckets(buckets, first_distance, count, (uint32_t)n_buckets, (uint32_t)max_distance, bidirectional != 0);
+  return S2A_OK;
 }
 
 int s2a_device_error(unsigned int* flags, int clear) {

@@ -6,6 +6,9 @@
 
 namespace s2a {
 
+// SMs of the current device (148 where none is visible).
+int sm_count();
+
 // Per-device host-side caches (attribute set-up, symbol addresses, SM counts) are tables of
 // this many entries indexed by the CUDA device ordinal.
 constexpr int kMaxDevices = 64;
@@ -55,6 +58,35 @@ cudaError_t launch_gelu_fwd_tensor_range_static(int dt, const void* x, void* y, 
 cudaError_t launch_cap(bool fwd, int dt, const void* in, void* out, uint64_t n_out, uint32_t r, cudaStream_t st);
 cudaError_t launch_lrp_fwd(int dt, const void* x, const float* A, const float* B, void* y, uint32_t batch,
                            uint32_t tokens, uint32_t channels, uint32_t rank, cudaStream_t st);
+
+// Layer norm.  Strides are in elements between the starts of neighbouring rows.  stats: (mean, rstd) per row; gamma,
+// beta, stats (forward), grad_gamma and grad_beta may be NULL; scratch: layernorm_scratch_bytes(n_rows, row_len),
+// needed where a weight gradient is asked for.
+uint64_t layernorm_scratch_bytes(uint64_t n_rows, uint32_t row_len);
+cudaError_t launch_layernorm_fwd(int dt, int wdt, const void* x, const void* gamma, const void* beta, void* y, float* stats,
+                                 uint64_t n_rows, uint32_t row_len, uint64_t x_stride, uint64_t y_stride, float eps,
+                                 cudaStream_t st);
+cudaError_t launch_layernorm_bwd(int dt, int wdt, const void* g, const void* x, const void* gamma, const float* stats,
+                                 void* grad_in, void* grad_gamma, void* grad_beta, float* scratch, uint64_t n_rows,
+                                 uint32_t row_len, uint64_t g_stride, uint64_t x_stride, uint64_t out_stride,
+                                 cudaStream_t st);
+
+// Dropout (x = grad_out for the backward pass): an element is dropped when its 16 random bits are below `threshold`
+// (0 .. 65536).  rng: two device words, (seed, offset).  residual may be NULL.
+cudaError_t launch_dropout(int dt, const void* x, const void* residual, void* y, uint64_t n, const uint64_t* rng,
+                           uint64_t site, uint32_t threshold, cudaStream_t st);
+
+// Relative position bias.  buckets: [tq, tk], or [tq + tk - 1] over k - q + tq - 1 where by_distance is set.  scratch of the
+// backward call: relbias_bwd_ctas(...) * n_buckets floats.  log_buckets runs on the host.
+constexpr uint32_t kMaxBuckets = 32768;
+uint32_t relbias_bwd_ctas(uint32_t batch, uint32_t heads, uint32_t tq, uint32_t tk, uint32_t n_buckets);
+cudaError_t launch_relbias_fwd(int dt, int wdt, const void* x, const void* table, const int32_t* buckets, int by_distance,
+                               void* y, uint32_t batch, uint32_t heads, uint32_t tq, uint32_t tk, uint32_t n_buckets,
+                               cudaStream_t st);
+cudaError_t launch_relbias_bwd(int dt, int wdt, const void* g, const int32_t* buckets, int by_distance, void* grad_table,
+                               float* scratch, uint32_t batch, uint32_t heads, uint32_t tq, uint32_t tk, uint32_t n_buckets,
+                               cudaStream_t st);
+void log_buckets(int32_t* out, int64_t first, uint64_t count, uint32_t n_buckets, uint32_t max_distance, bool bidirectional);
 
 // ---------------------------------------------------------------- pipelined tiles
 // A tile is `tile_rows` consecutive rows whose flat element span starts and ends on a

@@ -1,0 +1,76 @@
+// Eight consecutive elements of an I/O tensor in registers (16 bytes of bfloat16, 32 of binary32), and the
+// launch helper of the kernels built on them.
+#pragma once
+
+#include "s2a_common.cuh"
+
+namespace s2a {
+
+template <int DT> struct Eight;
+template <> struct Eight<kBF16> {
+  uint4 r;
+  __device__ __forceinline__ void zero() { r = make_uint4(0, 0, 0, 0); }
+  __device__ __forceinline__ void load(const void* p) { r = *(const uint4*)p; }
+  __device__ __forceinline__ void store(void* p) const { *(uint4*)p = r; }
+  __device__ __forceinline__ void get(F2* v) const {
+    v[0] = f2_from_bf16x2(r.x);
+    v[1] = f2_from_bf16x2(r.y);
+    v[2] = f2_from_bf16x2(r.z);
+    v[3] = f2_from_bf16x2(r.w);
+  }
+  __device__ __forceinline__ void set(const F2* v) {
+    r = make_uint4(f2_to_bf16x2(v[0]), f2_to_bf16x2(v[1]), f2_to_bf16x2(v[2]), f2_to_bf16x2(v[3]));
+  }
+};
+template <> struct Eight<kF32> {
+  float4 a, b;
+  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
+  __device__ __forceinline__ void load(const void* p) { a = ((const float4*)p)[0]; b = ((const float4*)p)[1]; }
+  __device__ __forceinline__ void store(void* p) const { ((float4*)p)[0] = a; ((float4*)p)[1] = b; }
+  __device__ __forceinline__ void get(F2* v) const {
+    v[0] = f2_pack(a.x, a.y);
+    v[1] = f2_pack(a.z, a.w);
+    v[2] = f2_pack(b.x, b.y);
+    v[3] = f2_pack(b.z, b.w);
+  }
+  __device__ __forceinline__ void set(const F2* v) {
+    f2_unpack(v[0], a.x, a.y);
+    f2_unpack(v[1], a.z, a.w);
+    f2_unpack(v[2], b.x, b.y);
+    f2_unpack(v[3], b.z, b.w);
+  }
+};
+
+// One element of a learned parameter (layer norm's weights, a bias table): binary32 or bfloat16 by `wdt`.
+__device__ __forceinline__ float load_param(const void* p, uint64_t i, int wdt) {
+  return wdt == kF32 ? ((const float*)p)[i] : __bfloat162float(((const __nv_bfloat16*)p)[i]);
+}
+__device__ __forceinline__ void store_param(void* p, uint64_t i, int wdt, float v) {
+  if (wdt == kF32) ((float*)p)[i] = v;
+  else ((__nv_bfloat16*)p)[i] = __float2bfloat16_rn(v);
+}
+
+// Programmatic dependent launch.  Every kernel launched through launch_overlapped calls enter_grid() before it
+// touches memory: the next kernel of the stream may then be scheduled, and this one goes on once its
+// predecessor has completed and its writes are visible.
+__device__ __forceinline__ void enter_grid() {
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
+  asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
+template <typename... P, typename... A>
+cudaError_t launch_overlapped(void (*kernel)(P...), dim3 grid, unsigned threads, size_t smem, cudaStream_t st, A... args) {
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(threads);
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = st;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, static_cast<P>(args)...);
+}
+
+}  // namespace s2a

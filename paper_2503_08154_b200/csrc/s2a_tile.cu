@@ -53,6 +53,8 @@ uint32_t gcd_u32(uint32_t a, uint32_t b) {
 
 uint32_t align_up(uint32_t v, uint32_t a) { return (v + a - 1) / a * a; }
 
+}  // namespace
+
 // SMs of the current device, looked up once per device.  Concurrent first calls may both
 // query and store the same value.
 int sm_count() {
@@ -67,6 +69,8 @@ int sm_count() {
   }
   return n;
 }
+
+namespace {
 
 unsigned int* error_word_address() {
   // one address per device; looked up on first use with that device current (two threads
