@@ -6,22 +6,27 @@
 //             grad_in = rstd (a - sum a / L - xhat sum(a xhat) / L),
 //             grad_gamma = sum over rows of g xhat, grad_beta = sum over rows of g
 //
-// A row belongs to a team of TW warps and stays in its registers between the one read and the one write: NO pieces
-// of eight elements a lane.  The variance is taken around the mean (two passes over registers, no difference of
-// squares); warps merge (count, mean, squared deviations) with one exchange through shared memory (Chan, Golub and
-// LeVeque's pairwise update).  All sums are binary32.
+// Both passes are bound by memory: a row is read once and written once.  A row belongs to a team of LANES threads (8 to
+// 512) that own NO pieces of eight consecutive elements each, and the next rows of a team are always on the way: every
+// thread copies its own pieces into a ring of STAGES rows in shared memory (cp.async), so the bytes in flight do not cost
+// registers, and since it reads back only what it copied itself the ring needs no barrier.  The variance is taken around
+// the mean (no difference of squares); the warps of a row merge (count, mean, squared deviations) with one exchange (Chan,
+// Golub and LeVeque's pairwise update).  All sums are binary32.
 //
-// The weights' gradients are sums over rows, so a team keeps one running sum per column in registers over all the
-// rows it walks; each CTA writes one partial pair of rows to the caller's scratch and a second kernel adds the
-// partials in a fixed order: no atomics, the same bits on every run.
+// Rows need not start on a 16-byte boundary.  A row's first element then sits s elements into a vector, pieces are the
+// vectors of the memory (piece v holds columns 8v - s .. 8v - s + 7), and the two at the row's ends are masked (EDGE).  A team keeps
+// to rows of one s, so that its pieces mean the same columns in every row.
+//
+// The weights' gradients are sums over rows: a thread keeps the sums of its own columns in registers over all the rows
+// of its team, a CTA adds its teams' sums in order and writes one pair of rows to the caller's scratch, and a second kernel
+// adds those in order: no atomics, the same bits on every run.
 #include "s2a_launch.h"
 #include "s2a_oct.cuh"
 
 namespace s2a {
 namespace {
 
-constexpr uint32_t kMaxRegisterRow = 16 * 32 * 32;  // 16 warps, 32 elements a lane
-constexpr uint32_t kMaxPartials = 296;              // partial sums of the weights' gradients: two CTAs per SM of a B200
+constexpr uint32_t kMaxPartials = 296;  // partial sums of the weights' gradients: two CTAs per SM of a B200
 
 struct NormArgs {
   const void* x;
@@ -32,66 +37,141 @@ struct NormArgs {
   const float* stats_in;
   float* stats_out;      // may be NULL
   float* partials;       // backward with weight gradients: [CTA][2][row_len]
+  const void* x_end;     // one past the last element of x, of g
+  const void* g_end;
   uint64_t n_rows;
   uint64_t x_stride, g_stride, out_stride;
   uint32_t row_len;
   int wdt;
   float eps;
+  int g_apart, out_apart;  // EDGE: g's (out's) rows do not sit on the 16-byte grid as x's do: element by element
 };
 
-// Which columns a lane owns.  VEC: piece j is the eight consecutive columns from (j * LANES + lane) * 8 (whole
-// 16-byte vectors).  Otherwise element i of piece j is column (j * 8 + i) * LANES + lane: neighbouring lanes on
-// neighbouring elements, for rows that do not start on a 16-byte boundary.
-template <bool VEC, int LANES>
-__device__ __forceinline__ uint32_t column(int j, int i, uint32_t lane) {
-  return VEC ? ((uint32_t)j * LANES + lane) * 8u + (uint32_t)i : (uint32_t)(j * 8 + i) * LANES + lane;
+template <int DT> constexpr int kVec = DT == kF32 ? 4 : 8;  // elements in 16 bytes
+
+__host__ __device__ constexpr int threads_of(int lanes) { return lanes > 256 ? lanes : 256; }
+// Rows in flight per team: what keeps two CTAs of an SM (one of 512 threads) within its shared memory.
+__host__ __device__ constexpr int stages_of(int stage_bytes) {
+  return stage_bytes <= 24 * 1024 ? 4 : (stage_bytes <= 32 * 1024 ? 3 : (stage_bytes <= 100 * 1024 ? 2 : 1));
+}
+__host__ __device__ constexpr int stage_bytes(int dt, int no, int lanes, int tensors) {
+  return threads_of(lanes) * no * (dt == kF32 ? 32 : 16) * tensors + (tensors == 2 ? threads_of(lanes) * 8 : 0);
 }
 
-// A lane's share of a row as read.
-template <int DT, bool VEC, int NO, int LANES>
-struct Share {
-  Eight<DT> p[NO];
-  __device__ __forceinline__ void load(const typename Io<DT>::T* row, uint32_t lane, uint32_t L) {
+// A thread's pieces of one tensor in one stage of the ring: [piece][half][thread] of 16 bytes.
+template <int DT, int NO, int THREADS>
+struct Slot {
+  static constexpr int kHalves = DT == kF32 ? 2 : 1;
+  static constexpr int kBytes = NO * kHalves * THREADS * 16;
+  char* base;  // of the stage, at this thread's column
+  __device__ __forceinline__ char* at(int j, int half) const { return base + (j * kHalves + half) * THREADS * 16; }
+  __device__ __forceinline__ Eight<DT> read(int j) const;
+  __device__ __forceinline__ void write(int j, const Eight<DT>& v) const;
+};
+template <int DT, int NO, int THREADS>
+__device__ __forceinline__ Eight<DT> Slot<DT, NO, THREADS>::read(int j) const {
+  Eight<DT> v;
+  if constexpr (DT == kF32) {
+    v.a = *(const float4*)at(j, 0);
+    v.b = *(const float4*)at(j, 1);
+  } else {
+    v.r = *(const uint4*)at(j, 0);
+  }
+  return v;
+}
+template <int DT, int NO, int THREADS>
+__device__ __forceinline__ void Slot<DT, NO, THREADS>::write(int j, const Eight<DT>& v) const {
+  if constexpr (DT == kF32) {
+    *(float4*)at(j, 0) = v.a;
+    *(float4*)at(j, 1) = v.b;
+  } else {
+    *(uint4*)at(j, 0) = v.r;
+  }
+}
+
+// Where a thread's pieces lie: piece j begins at column (j * LANES + lane) * 8 - s (s = 0 without EDGE).
+template <int LANES>
+__device__ __forceinline__ int piece_column(int j, uint32_t lane, int s) { return (int)((j * LANES + lane) * 8u) - s; }
+
+template <bool EDGE>
+__device__ __forceinline__ bool piece_on(int c, int L) { return EDGE ? (c < L && c + 8 > 0) : c < L; }
+
+// Starts the copies of a row's pieces.  `end`: of the tensor.  A vector that the tensor does not wholly contain (only at the
+// tensor's two ends), and every piece of a tensor that sits on another grid (`apart`), is read element by element.
+template <int DT, bool EDGE, int NO, int LANES, int THREADS>
+__device__ __forceinline__ void fetch(const Slot<DT, NO, THREADS>& slot, const void* tensor, const void* end, uint64_t row,
+                                      uint64_t stride, uint32_t lane, int L, int s, bool apart) {
+  using T = typename Io<DT>::T;
+  const T* p = (const T*)tensor + row * stride;
 #pragma unroll
-    for (int j = 0; j < NO; ++j) {
-      if (VEC) {
-        const uint32_t c = column<VEC, LANES>(j, 0, lane);
-        if (c < L) p[j].load(row + c);
-        else p[j].zero();
-      } else {
-        float v[8];
+  for (int j = 0; j < NO; ++j) {
+    const int c = piece_column<LANES>(j, lane, s);
+    if (!piece_on<EDGE>(c, L)) continue;
+    if (!EDGE || (!apart && p + c >= (const T*)tensor && p + c + 8 <= (const T*)end)) {
+      copy_async<16>(slot.at(j, 0), p + c);
+      if (DT == kF32) copy_async<16>(slot.at(j, Slot<DT, NO, THREADS>::kHalves - 1), p + c + 4);
+    } else {
+      float f[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t c = column<VEC, LANES>(j, i, lane);
-          v[i] = c < L ? Io<DT>::widen(row[c]) : 0.0f;
-        }
-        F2 w[4];
+      for (int i = 0; i < 8; ++i) f[i] = c + i >= 0 && c + i < L ? Io<DT>::widen(p[c + i]) : 0.0f;
+      F2 w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = f2_pack(v[2 * i], v[2 * i + 1]);
-        p[j].set(w);
-      }
+      for (int i = 0; i < 4; ++i) w[i] = f2_pack(f[2 * i], f[2 * i + 1]);
+      Eight<DT> v;
+      v.set(w);
+      slot.write(j, v);
     }
   }
-};
+}
 
-template <int DT, bool VEC, int LANES>
-__device__ __forceinline__ void store_piece(typename Io<DT>::T* row, int j, uint32_t lane, uint32_t L, const F2* v) {
-  if (VEC) {
-    const uint32_t c = column<VEC, LANES>(j, 0, lane);
-    if (c < L) {
-      Eight<DT> o;
-      o.set(v);
-      o.store(row + c);
-    }
+// Elements of a piece outside the row become zero.
+__device__ __forceinline__ void mask_ends(F2* v, int c, int L) {
+  if (c >= 0 && c + 8 <= L) return;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float lo, hi;
+    f2_unpack(v[i], lo, hi);
+    const int k = c + 2 * i;
+    v[i] = f2_pack(k >= 0 && k < L ? lo : 0.0f, k + 1 >= 0 && k + 1 < L ? hi : 0.0f);
+  }
+}
+
+template <int DT, bool EDGE>
+__device__ __forceinline__ void put_piece(typename Io<DT>::T* row, int c, int L, bool apart, const F2* v) {
+  if (!EDGE || (!apart && c >= 0 && c + 8 <= L)) {
+    Eight<DT> o;
+    o.set(v);
+    o.store(row + c);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t c = column<VEC, LANES>(j, i, lane);
       float lo, hi;
       f2_unpack(v[i / 2], lo, hi);
-      if (c < L) row[c] = Io<DT>::narrow(i % 2 ? hi : lo);
+      if (c + i >= 0 && c + i < L) row[c + i] = Io<DT>::narrow(i % 2 ? hi : lo);
     }
   }
+}
+
+// Eight learned parameters from column c on; `fill` where there are none.
+__device__ __forceinline__ void load_weights(const void* p, int c, int L, int wdt, float fill, F2* v) {
+  const char* at = (const char*)p + (int64_t)c * (wdt == kF32 ? 4 : 2);
+  if (p && c >= 0 && c + 8 <= L && ((uintptr_t)at & 15u) == 0) {
+    if (wdt == kF32) {
+      Eight<kF32> w;
+      w.load(at);
+      w.get(v);
+    } else {
+      Eight<kBF16> w;
+      w.load(at);
+      w.get(v);
+    }
+    return;
+  }
+  float f[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) f[i] = p && c + i >= 0 && c + i < L ? load_param(p, (uint64_t)(c + i), wdt) : fill;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = f2_pack(f[2 * i], f[2 * i + 1]);
 }
 
 __device__ __forceinline__ float f2_sum(F2 a) {
@@ -100,12 +180,12 @@ __device__ __forceinline__ float f2_sum(F2 a) {
   return lo + hi;
 }
 
-// Whether both elements of pair i of piece j lie inside the row; in the vector form pieces are all in or all out.
-template <bool VEC, int LANES>
-__device__ __forceinline__ F2 masked(F2 v, int j, int i, uint32_t lane, uint32_t L) {
-  float lo, hi;
-  f2_unpack(v, lo, hi);
-  return f2_pack(column<VEC, LANES>(j, 2 * i, lane) < L ? lo : 0.0f, column<VEC, LANES>(j, 2 * i + 1, lane) < L ? hi : 0.0f);
+// Sum over the lanes of a team that lie in one warp (or over groups of W lanes).
+template <int W>
+__device__ __forceinline__ float lanes_sum(float v) {
+#pragma unroll
+  for (int o = W / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  return v;
 }
 
 template <int LANES>
@@ -113,138 +193,168 @@ __device__ __forceinline__ void team_barrier(uint32_t team) {
   if (LANES > 32) asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(LANES) : "memory");
 }
 
-__host__ __device__ constexpr int threads_of(int tw) { return tw > 8 ? tw * 32 : 256; }
+// The shift s of a row: how many elements of its first vector lie before it.
+template <int DT, bool EDGE>
+__device__ __forceinline__ int row_shift(const NormArgs& a, uint64_t row) {
+  using T = typename Io<DT>::T;
+  return EDGE ? (int)((((uintptr_t)a.x / sizeof(T)) + row * a.x_stride) % kVec<DT>) : 0;
+}
 
 // ---------------------------------------------------------------- forward
-template <int DT, bool VEC, int NO, int TW>
-__global__ void __launch_bounds__(threads_of(TW)) norm_fwd_kernel(NormArgs a) {
+template <int DT, bool EDGE, int NO, int LANES>
+__global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : (NO == 1 ? 4 : 2)) norm_fwd_kernel(NormArgs a) {
   using T = typename Io<DT>::T;
-  constexpr int LANES = TW * 32, TEAMS = threads_of(TW) / LANES;
-  __shared__ float merge[2][TEAMS][TW][2];
+  constexpr int THREADS = threads_of(LANES), TEAMS = THREADS / LANES, WARPS = LANES / 32 > 1 ? LANES / 32 : 1;
+  constexpr int GROUP = LANES < 32 ? LANES : 32;
+  constexpr int BYTES = stage_bytes(DT, NO, LANES, 1), STAGES = stages_of(BYTES);
+  extern __shared__ __align__(16) char ring[];
+  __shared__ float4 merge[2][TEAMS][WARPS];  // (mean, deviations, count) of each warp of a row, two rows' worth
   enter_grid();
-  const uint32_t team = threadIdx.x / LANES, lane = threadIdx.x % LANES, warp = lane / 32, L = a.row_len;
+  const uint32_t team = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+  const int L = (int)a.row_len;
   const float inv_l = 1.0f / (float)L;
+  const uint64_t step = (uint64_t)gridDim.x * TEAMS, first = (uint64_t)blockIdx.x * TEAMS + team;
+  const int s = row_shift<DT, EDGE>(a, first);
+  using Ring = Slot<DT, NO, THREADS>;
+#pragma unroll
+  for (int k = 0; k < STAGES; ++k) {
+    if (first + k * step < a.n_rows)
+      fetch<DT, EDGE, NO, LANES, THREADS>(Ring{ring + k * BYTES + threadIdx.x * 16}, a.x, a.x_end, first + k * step, a.x_stride, lane, L, s, false);
+    copy_commit();
+  }
   F2 gamma[NO][4], beta[NO][4];
   float count = 0.0f;  // elements of the row that this warp holds
 #pragma unroll
-  for (int j = 0; j < NO; ++j)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t c0 = column<VEC, LANES>(j, 2 * i, lane), c1 = column<VEC, LANES>(j, 2 * i + 1, lane);
-      gamma[j][i] = f2_pack(a.gamma && c0 < L ? load_param(a.gamma, c0, a.wdt) : 1.0f,
-                            a.gamma && c1 < L ? load_param(a.gamma, c1, a.wdt) : 1.0f);
-      beta[j][i] = f2_pack(a.beta && c0 < L ? load_param(a.beta, c0, a.wdt) : 0.0f,
-                           a.beta && c1 < L ? load_param(a.beta, c1, a.wdt) : 0.0f);
-      count += (float)(c0 < L) + (float)(c1 < L);
-    }
-  count = warp_sum(count);
-  const float inv_count = count > 0.0f ? 1.0f / count : 0.0f;
-  const uint64_t step = (uint64_t)gridDim.x * TEAMS;
-  uint32_t parity = 0;
-  for (uint64_t r = (uint64_t)blockIdx.x * TEAMS + team; r < a.n_rows; r += step) {
-    Share<DT, VEC, NO, LANES> raw;
-    raw.load((const T*)a.x + r * a.x_stride, lane, L);
+  for (int j = 0; j < NO; ++j) {
+    const int c = piece_column<LANES>(j, lane, s);
+    load_weights(a.gamma, c, L, a.wdt, 1.0f, gamma[j]);
+    load_weights(a.beta, c, L, a.wdt, 0.0f, beta[j]);
+    if (piece_on<EDGE>(c, L)) count += (float)(min(c + 8, L) - max(c, 0));
+  }
+  if (WARPS > 1) count = lanes_sum<32>(count);
+  const float inv_count = WARPS > 1 ? (count > 0.0f ? 1.0f / count : 0.0f) : inv_l;
+  uint32_t parity = 0, stage = 0;
+  // the lanes of a warp that serve several rows keep together: a row past the end is computed on whatever the ring holds
+  // and written nowhere
+  for (uint64_t base = (uint64_t)blockIdx.x * TEAMS; base < a.n_rows; base += step) {
+    const uint64_t r = base + team;
+    if (LANES >= 32 && r >= a.n_rows) break;
+    copy_wait<STAGES - 1>();
+    const Ring slot{ring + stage * BYTES + threadIdx.x * 16};
     F2 v[NO][4], sum = f2_both(0.0f);
 #pragma unroll
     for (int j = 0; j < NO; ++j) {
-      raw.p[j].get(v[j]);
+      const int c = piece_column<LANES>(j, lane, s);
+      if (piece_on<EDGE>(c, L)) {
+        slot.read(j).get(v[j]);
+        if (EDGE) mask_ends(v[j], c, L);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[j][i] = f2_both(0.0f);
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) sum = f2_add(sum, v[j][i]);
     }
-    float mean = warp_sum(f2_sum(sum)) * (TW == 1 ? inv_l : inv_count);
+    if (r + STAGES * step < a.n_rows)
+      fetch<DT, EDGE, NO, LANES, THREADS>(slot, a.x, a.x_end, r + STAGES * step, a.x_stride, lane, L, s, false);
+    copy_commit();
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
+    float mean = lanes_sum<GROUP>(f2_sum(sum)) * inv_count;
     F2 sq = f2_both(0.0f);
 #pragma unroll
-    for (int j = 0; j < NO; ++j)
+    for (int j = 0; j < NO; ++j) {
+      const int c = piece_column<LANES>(j, lane, s);
+      if (!piece_on<EDGE>(c, L)) continue;
+      F2 d[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const F2 d = masked<VEC, LANES>(f2_sub(v[j][i], f2_both(mean)), j, i, lane, L);
-        sq = f2_fma(d, d, sq);
-      }
-    float dev = warp_sum(f2_sum(sq));
-    if (TW > 1) {
-      if (lane % 32 == 0) {
-        merge[parity][team][warp][0] = mean * count;
-        merge[parity][team][warp][1] = dev;
-      }
+      for (int i = 0; i < 4; ++i) d[i] = f2_sub(v[j][i], f2_both(mean));
+      if (EDGE) mask_ends(d, c, L);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sq = f2_fma(d[i], d[i], sq);
+    }
+    float dev = lanes_sum<GROUP>(f2_sum(sq));
+    if (WARPS > 1) {
+      if (lane % 32 == 0) merge[parity][team][lane / 32] = make_float4(mean, dev, count, 0.0f);
       // the two buffers alternate: a warp writes one of them again only after the next row's barrier, which every
       // warp of the team reaches after it has read this row's values
       team_barrier<LANES>(team);
-      float total = 0.0f;
-#pragma unroll
-      for (int w = 0; w < TW; ++w) total += merge[parity][team][w][0];
-      mean = total * inv_l;
-      dev = 0.0f;
-#pragma unroll
-      for (int w = 0; w < TW; ++w) {
-        // elements of warp w, as counted above
-        uint32_t n = 0;
-        if (VEC) {
-#pragma unroll
-          for (int j = 0; j < NO; ++j) {
-            const uint32_t c = ((uint32_t)j * LANES + (uint32_t)w * 32) * 8;
-            n += c < L ? min(L - c, 256u) : 0u;
-          }
-        } else {
-#pragma unroll
-          for (int j = 0; j < NO * 8; ++j) {
-            const uint32_t c = (uint32_t)j * LANES + (uint32_t)w * 32;
-            n += c < L ? min(L - c, 32u) : 0u;
-          }
-        }
-        const float nw = (float)n;
-        const float off = n ? merge[parity][team][w][0] / nw - mean : 0.0f;
-        dev += merge[parity][team][w][1] + nw * off * off;
-      }
+      const float4 m = merge[parity][team][lane % WARPS];
+      mean = lanes_sum<WARPS>(m.z * m.x) * inv_l;
+      dev = lanes_sum<WARPS>(m.y + m.z * (m.x - mean) * (m.x - mean));
       parity ^= 1;
     }
     const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(dev * inv_l + a.eps));
+    if (LANES < 32 && r >= a.n_rows) continue;
     if (a.stats_out && lane == 0) ((float2*)a.stats_out)[r] = make_float2(mean, rstd);
     T* out = (T*)a.out + r * a.out_stride;
 #pragma unroll
     for (int j = 0; j < NO; ++j) {
+      const int c = piece_column<LANES>(j, lane, s);
+      if (!piece_on<EDGE>(c, L)) continue;
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         v[j][i] = f2_fma(f2_mul(f2_sub(v[j][i], f2_both(mean)), f2_both(rstd)), gamma[j][i], beta[j][i]);
-      store_piece<DT, VEC, LANES>(out, j, lane, L, v[j]);
+      put_piece<DT, EDGE>(out, c, L, EDGE && a.out_apart, v[j]);
     }
   }
 }
 
 // ---------------------------------------------------------------- backward
-template <int DT, bool VEC, int NO, int TW, bool WG>
-__global__ void __launch_bounds__(threads_of(TW)) norm_bwd_kernel(NormArgs a) {
+template <int DT, bool EDGE, int NO, int LANES, bool WG>
+__global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : 2) norm_bwd_kernel(NormArgs a) {
   using T = typename Io<DT>::T;
-  constexpr int LANES = TW * 32, TEAMS = threads_of(TW) / LANES;
-  __shared__ float2 merge[2][TEAMS][TW];
-  extern __shared__ float column_sums[];  // [2][row_len], when several teams share a CTA
+  constexpr int THREADS = threads_of(LANES), TEAMS = THREADS / LANES, WARPS = LANES / 32 > 1 ? LANES / 32 : 1;
+  constexpr int GROUP = LANES < 32 ? LANES : 32;
+  constexpr int BYTES = stage_bytes(DT, NO, LANES, 2), STAGES = stages_of(BYTES);
+  using Ring = Slot<DT, NO, THREADS>;
+  extern __shared__ __align__(16) char ring[];  // per stage: x's pieces, g's pieces, (mean, rstd) per thread
+  __shared__ float2 merge[2][TEAMS][WARPS];
   enter_grid();
-  const uint32_t team = threadIdx.x / LANES, lane = threadIdx.x % LANES, warp = lane / 32, L = a.row_len;
+  const uint32_t team = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+  const int L = (int)a.row_len;
   const float inv_l = 1.0f / (float)L;
+  const uint64_t step = (uint64_t)gridDim.x * TEAMS, first = (uint64_t)blockIdx.x * TEAMS + team;
+  const int s = row_shift<DT, EDGE>(a, first);
+  const auto start_row = [&](char* at, uint64_t r) {
+    if (r >= a.n_rows) return;
+    fetch<DT, EDGE, NO, LANES, THREADS>(Ring{at + threadIdx.x * 16}, a.x, a.x_end, r, a.x_stride, lane, L, s, false);
+    fetch<DT, EDGE, NO, LANES, THREADS>(Ring{at + Ring::kBytes + threadIdx.x * 16}, a.g, a.g_end, r, a.g_stride, lane, L, s, EDGE && a.g_apart);
+    copy_async<8>(at + 2 * Ring::kBytes + threadIdx.x * 8, a.stats_in + 2 * r);
+  };
+#pragma unroll
+  for (int k = 0; k < STAGES; ++k) {
+    start_row(ring + k * BYTES, first + k * step);
+    copy_commit();
+  }
   F2 gamma[NO][4], dgamma[NO][4], dbeta[NO][4];
 #pragma unroll
-  for (int j = 0; j < NO; ++j)
+  for (int j = 0; j < NO; ++j) {
+    load_weights(a.gamma, piece_column<LANES>(j, lane, s), L, a.wdt, 1.0f, gamma[j]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint32_t c0 = column<VEC, LANES>(j, 2 * i, lane), c1 = column<VEC, LANES>(j, 2 * i + 1, lane);
-      gamma[j][i] = f2_pack(a.gamma && c0 < L ? load_param(a.gamma, c0, a.wdt) : 1.0f,
-                            a.gamma && c1 < L ? load_param(a.gamma, c1, a.wdt) : 1.0f);
-      dgamma[j][i] = dbeta[j][i] = f2_both(0.0f);
-    }
-  const uint64_t step = (uint64_t)gridDim.x * TEAMS;
-  uint32_t parity = 0;
-  for (uint64_t r = (uint64_t)blockIdx.x * TEAMS + team; r < a.n_rows; r += step) {
-    Share<DT, VEC, NO, LANES> rx, rg;
-    rx.load((const T*)a.x + r * a.x_stride, lane, L);
-    rg.load((const T*)a.g + r * a.g_stride, lane, L);
-    const float2 st = ((const float2*)a.stats_in)[r];
+    for (int i = 0; i < 4; ++i) dgamma[j][i] = dbeta[j][i] = f2_both(0.0f);
+  }
+  uint32_t parity = 0, stage = 0;
+  for (uint64_t base = (uint64_t)blockIdx.x * TEAMS; base < a.n_rows; base += step) {
+    const uint64_t r = base + team;
+    if (LANES >= 32 && r >= a.n_rows) break;  // narrower teams share a warp and keep together
+    const bool on = LANES >= 32 || r < a.n_rows;
+    copy_wait<STAGES - 1>();
+    char* at = ring + stage * BYTES;
+    const Ring sx{at + threadIdx.x * 16}, sg{at + Ring::kBytes + threadIdx.x * 16};
+    const float2 st = *(const float2*)(at + 2 * Ring::kBytes + threadIdx.x * 8);
     const F2 mean2 = f2_both(st.x), rstd2 = f2_both(st.y);
     F2 s1 = f2_both(0.0f), s2 = f2_both(0.0f);
-    // elements past the row's end have g = 0, and so no share in any sum
 #pragma unroll
     for (int j = 0; j < NO; ++j) {
+      const int c = piece_column<LANES>(j, lane, s);
+      if (!on || !piece_on<EDGE>(c, L)) continue;
       F2 x[4], g[4];
-      rx.p[j].get(x);
-      rg.p[j].get(g);
+      sx.read(j).get(x);
+      sg.read(j).get(g);
+      if (EDGE) {
+        mask_ends(x, c, L);
+        mask_ends(g, c, L);
+      }
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const F2 xhat = f2_mul(f2_sub(x[i], mean2), rstd2), w = f2_mul(g[i], gamma[j][i]);
@@ -256,80 +366,90 @@ __global__ void __launch_bounds__(threads_of(TW)) norm_bwd_kernel(NormArgs a) {
         }
       }
     }
-    float c1 = warp_sum(f2_sum(s1)), c2 = warp_sum(f2_sum(s2));
-    if (TW > 1) {
-      if (lane % 32 == 0) merge[parity][team][warp] = make_float2(c1, c2);
+    float c1 = lanes_sum<GROUP>(f2_sum(s1)), c2 = lanes_sum<GROUP>(f2_sum(s2));
+    if (WARPS > 1) {
+      if (lane % 32 == 0) merge[parity][team][lane / 32] = make_float2(c1, c2);
       team_barrier<LANES>(team);  // alternating buffers, as in the forward kernel
-      c1 = c2 = 0.0f;
-#pragma unroll
-      for (int w = 0; w < TW; ++w) {
-        const float2 m = merge[parity][team][w];
-        c1 += m.x;
-        c2 += m.y;
-      }
+      const float2 m = merge[parity][team][lane % WARPS];
+      c1 = lanes_sum<WARPS>(m.x);
+      c2 = lanes_sum<WARPS>(m.y);
       parity ^= 1;
     }
     const F2 m1 = f2_both(c1 * inv_l), m2 = f2_both(-c2 * inv_l);
     T* out = (T*)a.out + r * a.out_stride;
 #pragma unroll
     for (int j = 0; j < NO; ++j) {
+      const int c = piece_column<LANES>(j, lane, s);
+      if (!on || !piece_on<EDGE>(c, L)) continue;
       F2 x[4], g[4];
-      rx.p[j].get(x);
-      rg.p[j].get(g);
+      sx.read(j).get(x);
+      sg.read(j).get(g);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const F2 xhat = f2_mul(f2_sub(x[i], mean2), rstd2);
         g[i] = f2_mul(f2_fma(xhat, m2, f2_sub(f2_mul(g[i], gamma[j][i]), m1)), rstd2);
       }
-      store_piece<DT, VEC, LANES>(out, j, lane, L, g);
+      put_piece<DT, EDGE>(out, c, L, EDGE && a.out_apart, g);
     }
+    start_row(at, r + STAGES * step);
+    copy_commit();
+    stage = stage + 1 == STAGES ? 0 : stage + 1;
   }
-  if (!WG) return;
-  // The teams of a CTA add their columns one after the other, in order.
-  float* part = a.partials + (uint64_t)blockIdx.x * 2 * L;
-  for (uint32_t t = 0; t < TEAMS; ++t) {
-    if (team == t) {
+  if constexpr (WG) {
+    // The CTA's teams, column by column, in order.  The ring holds their sums by piece: [team][2][half][piece][lane] of four
+    // columns, which threads write and read without bank conflicts.
+    copy_wait<0>();
+    __syncthreads();
+    float4* sums = (float4*)ring;
+    constexpr int kRow = 2 * NO * LANES;  // float4s of one of a team's two rows
 #pragma unroll
-      for (int j = 0; j < NO; ++j)
+    for (int j = 0; j < NO; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const uint32_t c = column<VEC, LANES>(j, i, lane);
-          if (c >= L) continue;
-          float dg[2], db[2];
-          f2_unpack(dgamma[j][i / 2], dg[0], dg[1]);
-          f2_unpack(dbeta[j][i / 2], db[0], db[1]);
-          const float before_g = t ? column_sums[c] : 0.0f, before_b = t ? column_sums[L + c] : 0.0f;
-          if (t + 1 < TEAMS) {
-            column_sums[c] = before_g + dg[i % 2];
-            column_sums[L + c] = before_b + db[i % 2];
-          } else {
-            part[c] = before_g + dg[i % 2];
-            part[L + c] = before_b + db[i % 2];
-          }
-        }
+      for (int half = 0; half < 2; ++half) {
+        float4 w;
+        f2_unpack(dgamma[j][2 * half], w.x, w.y);
+        f2_unpack(dgamma[j][2 * half + 1], w.z, w.w);
+        sums[(team * 2 + 0) * kRow + (half * NO + j) * LANES + lane] = w;
+        f2_unpack(dbeta[j][2 * half], w.x, w.y);
+        f2_unpack(dbeta[j][2 * half + 1], w.z, w.w);
+        sums[(team * 2 + 1) * kRow + (half * NO + j) * LANES + lane] = w;
+      }
+    __syncthreads();
+    float* part = a.partials + (uint64_t)blockIdx.x * 2 * L;
+    const float* flat = (const float*)ring;
+    for (uint32_t k = threadIdx.x; k < 2u * (uint32_t)L; k += THREADS) {
+      const uint32_t which = k >= (uint32_t)L, c = which ? k - L : k;
+      float t = 0.0f;
+#pragma unroll 4
+      for (int m = 0; m < TEAMS; ++m) {
+        const uint32_t p = c + (EDGE ? (uint32_t)row_shift<DT, EDGE>(a, (uint64_t)blockIdx.x * TEAMS + m) : 0u);
+        t += flat[((m * 2 + which) * kRow + ((p / 4) % 2) * NO * LANES + p / 8) * 4 + p % 4];
+      }
+      part[k] = t;
     }
-    if (t + 1 < TEAMS) __syncthreads();
   }
 }
 
 // Adds the partial rows: [n_part][2][row_len] -> grad_gamma, grad_beta (either may be NULL).  A CTA owns 32 columns
-// of one of the two; its eight warps take every eighth partial.
-__global__ void __launch_bounds__(256) norm_reduce_kernel(const float* partials, uint32_t n_part, uint32_t L, void* dgamma,
-                                                          void* dbeta, int wdt) {
-  __shared__ float sums[8][32];
+// of one of the two; its warps take every 32nd partial.
+constexpr int kReduceWarps = 32;
+__global__ void __launch_bounds__(kReduceWarps * 32) norm_reduce_kernel(const float* partials, uint32_t n_part, uint32_t L,
+                                                                        void* dgamma, void* dbeta, int wdt) {
+  __shared__ float sums[kReduceWarps][33];
   enter_grid();
   const uint32_t which = blockIdx.y, w = threadIdx.x / 32, c = blockIdx.x * 32 + threadIdx.x % 32;
   float acc = 0.0f;
-  if (c < L)
-    for (uint32_t p = w; p < n_part; p += 8) acc += partials[((uint64_t)p * 2 + which) * L + c];
+  if (c < L) {
+#pragma unroll 5
+    for (uint32_t p = w; p < n_part; p += kReduceWarps) acc += partials[((uint64_t)p * 2 + which) * L + c];
+  }
   sums[w][threadIdx.x % 32] = acc;
   __syncthreads();
+  // warp w adds up column w: lane k holds the sum of warp k
+  acc = warp_sum(sums[threadIdx.x % 32][w]);
   void* out = which ? dbeta : dgamma;
-  if (w == 0 && c < L && out) {
-#pragma unroll
-    for (int k = 1; k < 8; ++k) acc += sums[k][threadIdx.x];
-    store_param(out, c, wdt, acc);
-  }
+  const uint32_t mine = blockIdx.x * 32 + w;
+  if (threadIdx.x % 32 == 0 && mine < L && out) store_param(out, mine, wdt, acc);
 }
 
 // ---------------------------------------------------------------- rows too long for registers
@@ -420,96 +540,123 @@ __global__ void __launch_bounds__(256) norm_columns_long_kernel(NormArgs a) {
 }
 
 // ---------------------------------------------------------------- host side
-// The team that takes a row: one warp up to 1024 elements (one to four pieces of eight a lane), then twice the
-// warps for each doubling (three or four pieces).
-struct Team {
-  int warps, pieces;
-};
-Team team_of(uint32_t L) {
-  int tw = 1;
-  while (L > (uint32_t)tw * 1024u) tw *= 2;
-  return {tw, (int)((L + tw * 256 - 1) / (tw * 256))};
-}
-
-uint32_t partial_count(uint64_t n_rows, uint32_t L) {
-  uint64_t want;
-  if (L <= kMaxRegisterRow) {
-    const int tw = team_of(L).warps;
-    const uint64_t teams = threads_of(tw) / (tw * 32);
-    want = (n_rows + teams - 1) / teams;
-  } else {
-    want = (n_rows + 63) / 64;
+uint64_t gcd64(uint64_t a, uint64_t b) {
+  while (b) {
+    const uint64_t t = a % b;
+    a = b;
+    b = t;
   }
-  return (uint32_t)(want < 1 ? 1 : (want < kMaxPartials ? want : kMaxPartials));
+  return a;
 }
 
-template <int DT, bool VEC, int NO, int TW>
-cudaError_t launch_norm(bool fwd, bool wg, const NormArgs& a, cudaStream_t st) {
-  constexpr int TEAMS = threads_of(TW) / (TW * 32);
+uint32_t partial_cap(uint64_t n_rows) { return (uint32_t)(n_rows < 1 ? 1 : (n_rows < kMaxPartials ? n_rows : kMaxPartials)); }
+
+template <int DT, bool EDGE, int NO, int LANES>
+cudaError_t launch_norm(bool fwd, bool wg, const NormArgs& a, uint32_t& parts, cudaStream_t st) {
+  static std::atomic<uint64_t> ready[3] = {};
+  constexpr int THREADS = threads_of(LANES), TEAMS = THREADS / LANES;
+  constexpr int B1 = stage_bytes(DT, NO, LANES, 1), B2 = stage_bytes(DT, NO, LANES, 2);
+  constexpr size_t ring_fwd = (size_t)B1 * stages_of(B1), ring_bwd = (size_t)B2 * stages_of(B2);
+  constexpr size_t sums = (size_t)THREADS * NO * 64;  // the teams' column sums take the ring's place
+  constexpr size_t smem_wg = ring_bwd > sums ? ring_bwd : sums;
   const uint64_t want = (a.n_rows + TEAMS - 1) / TEAMS;
+  const uint64_t per_sm = LANES > 256 ? 1 : (fwd && NO == 1 ? 4 : 2);
+  uint64_t cap = fwd || !wg ? (uint64_t)sm_count() * per_sm : (LANES > 256 ? kMaxPartials / 2 : kMaxPartials);
+  if (EDGE) {  // a team's rows must all have one shift: the number of teams is a multiple of the shifts' period
+    const uint64_t period = kVec<DT> / gcd64(kVec<DT>, a.x_stride % kVec<DT>), unit = period / gcd64(period, TEAMS);
+    cap = cap / unit * unit;
+  }
+  const unsigned grid = (unsigned)(want < cap ? want : cap);
+  parts = grid;
+  cudaError_t e;
   if (fwd) {
-    const uint64_t cap = (uint64_t)sm_count() * 4;
-    return launch_overlapped(norm_fwd_kernel<DT, VEC, NO, TW>, dim3((unsigned)(want < cap ? want : cap)), threads_of(TW), 0, st, a);
+    e = allow_shared(norm_fwd_kernel<DT, EDGE, NO, LANES>, ring_fwd, ready[0]);
+    return e != cudaSuccess ? e : launch_overlapped(norm_fwd_kernel<DT, EDGE, NO, LANES>, dim3(grid), THREADS, ring_fwd, st, a);
   }
   if (!wg) {
-    const uint64_t cap = (uint64_t)sm_count() * 4;
-    return launch_overlapped(norm_bwd_kernel<DT, VEC, NO, TW, false>, dim3((unsigned)(want < cap ? want : cap)), threads_of(TW), 0, st, a);
+    e = allow_shared(norm_bwd_kernel<DT, EDGE, NO, LANES, false>, ring_bwd, ready[1]);
+    return e != cudaSuccess ? e : launch_overlapped(norm_bwd_kernel<DT, EDGE, NO, LANES, false>, dim3(grid), THREADS, ring_bwd, st, a);
   }
-  const size_t smem = TEAMS > 1 ? (size_t)a.row_len * 8 : 0;
-  return launch_overlapped(norm_bwd_kernel<DT, VEC, NO, TW, true>, dim3(partial_count(a.n_rows, a.row_len)), threads_of(TW), smem, st, a);
+  e = allow_shared(norm_bwd_kernel<DT, EDGE, NO, LANES, true>, smem_wg, ready[2]);
+  return e != cudaSuccess ? e : launch_overlapped(norm_bwd_kernel<DT, EDGE, NO, LANES, true>, dim3(grid), THREADS, smem_wg, st, a);
 }
 
-template <int DT, bool VEC>
-cudaError_t launch_norm_shape(bool fwd, bool wg, const NormArgs& a, cudaStream_t st) {
-  const Team t = team_of(a.row_len);
-  switch (t.warps * 8 + t.pieces) {
-    case 8 + 1: return launch_norm<DT, VEC, 1, 1>(fwd, wg, a, st);
-    case 8 + 2: return launch_norm<DT, VEC, 2, 1>(fwd, wg, a, st);
-    case 8 + 3: return launch_norm<DT, VEC, 3, 1>(fwd, wg, a, st);
-    case 8 + 4: return launch_norm<DT, VEC, 4, 1>(fwd, wg, a, st);
-    case 16 + 3: return launch_norm<DT, VEC, 3, 2>(fwd, wg, a, st);
-    case 16 + 4: return launch_norm<DT, VEC, 4, 2>(fwd, wg, a, st);
-    case 32 + 3: return launch_norm<DT, VEC, 3, 4>(fwd, wg, a, st);
-    case 32 + 4: return launch_norm<DT, VEC, 4, 4>(fwd, wg, a, st);
-    case 64 + 3: return launch_norm<DT, VEC, 3, 8>(fwd, wg, a, st);
-    case 64 + 4: return launch_norm<DT, VEC, 4, 8>(fwd, wg, a, st);
-    case 128 + 3: return launch_norm<DT, VEC, 3, 16>(fwd, wg, a, st);
-    case 128 + 4: return launch_norm<DT, VEC, 4, 16>(fwd, wg, a, st);
-  }
+// The smallest team that holds the row: one piece a lane up to a warp, two or three beyond.
+template <int DT, bool EDGE>
+cudaError_t launch_norm_shape(bool fwd, bool wg, const NormArgs& a, uint32_t vecs, uint32_t& parts, cudaStream_t st) {
+#define S2A_NORM(NO, LANES) \
+  if (vecs <= NO * LANES) return launch_norm<DT, EDGE, NO, LANES>(fwd, wg, a, parts, st);
+  S2A_NORM(1, 8)
+  S2A_NORM(1, 16)
+  S2A_NORM(1, 32)
+  S2A_NORM(2, 32)
+  S2A_NORM(3, 32)
+  S2A_NORM(2, 64)
+  S2A_NORM(3, 64)
+  S2A_NORM(2, 128)
+  S2A_NORM(3, 128)
+  S2A_NORM(2, 256)
+  S2A_NORM(3, 256)
+  S2A_NORM(2, 512)
+  S2A_NORM(3, 512)
+  S2A_NORM(4, 512)
+#undef S2A_NORM
   return cudaErrorInvalidValue;
 }
 
 template <int DT>
-cudaError_t launch_norm_dt(bool fwd, bool wg, const NormArgs& a, cudaStream_t st) {
-  if (a.row_len > kMaxRegisterRow) {
-    const uint64_t cap = (uint64_t)sm_count() * 4;
-    const dim3 grid((unsigned)(a.n_rows < cap ? a.n_rows : cap));
-    if (fwd) return launch_overlapped(norm_fwd_long_kernel<DT>, grid, kLongThreads, 0, st, a);
-    if (wg) {
-      const dim3 cols((a.row_len + 255) / 256, partial_count(a.n_rows, a.row_len));
-      const cudaError_t e = launch_overlapped(norm_columns_long_kernel<DT>, cols, 256, 0, st, a);
-      if (e != cudaSuccess) return e;
-    }
-    return launch_overlapped(norm_bwd_long_kernel<DT>, grid, kLongThreads, 0, st, a);
+cudaError_t launch_norm_dt(bool fwd, bool wg, NormArgs a, uint32_t& parts, cudaStream_t st) {
+  using T = typename Io<DT>::T;
+  constexpr uint64_t V = kVec<DT>;
+  if (a.n_rows == 1) a.x_stride = a.g_stride = a.out_stride = a.row_len;
+  // how far the rows of two tensors are apart on the 16-byte grid: nowhere, if their bases and strides agree modulo it
+  const auto apart = [&](const void* p, uint64_t stride) {
+    return p && (((uintptr_t)p / sizeof(T) - (uintptr_t)a.x / sizeof(T)) % V != 0 || (a.n_rows > 1 && (stride - a.x_stride) % V != 0));
+  };
+  a.g_apart = apart(a.g, a.g_stride);
+  a.out_apart = apart(a.out, a.out_stride);
+  a.x_end = (const T*)a.x + (a.n_rows - 1) * a.x_stride + a.row_len;
+  a.g_end = a.g ? (const T*)a.g + (a.n_rows - 1) * a.g_stride + a.row_len : nullptr;
+  const bool shifted = ((uintptr_t)a.x / sizeof(T)) % V != 0 || (a.n_rows > 1 && a.x_stride % V != 0);
+  const bool edge = shifted || a.row_len % 8 != 0 || a.g_apart || a.out_apart;
+  const uint32_t vecs = shifted ? (uint32_t)((a.row_len + V - 1 + 7) / 8) : (a.row_len + 7) / 8;
+  if (vecs <= 4 * 512)
+    return edge ? launch_norm_shape<DT, true>(fwd, wg, a, vecs, parts, st) : launch_norm_shape<DT, false>(fwd, wg, a, vecs, parts, st);
+  const uint64_t cap = (uint64_t)sm_count() * 4;
+  const dim3 grid((unsigned)(a.n_rows < cap ? a.n_rows : cap));
+  if (fwd) return launch_overlapped(norm_fwd_long_kernel<DT>, grid, kLongThreads, 0, st, a);
+  if (wg) {
+    const uint64_t want = (a.n_rows + 63) / 64;
+    parts = (uint32_t)(want < kMaxPartials ? want : kMaxPartials);
+    const cudaError_t e = launch_overlapped(norm_columns_long_kernel<DT>, dim3((a.row_len + 255) / 256, parts), 256, 0, st, a);
+    if (e != cudaSuccess) return e;
   }
-  // whole 16-byte vectors: eight elements a piece, every row starting on a 16-byte boundary
-  const uint64_t es = DT == kF32 ? 4 : 2;
-  const bool vec = a.row_len % 8 == 0 && (((uintptr_t)a.x | (uintptr_t)a.out | (uintptr_t)a.g) & 15u) == 0 &&
-                   ((a.n_rows == 1) || ((a.x_stride * es | a.out_stride * es | a.g_stride * es) & 15u) == 0);
-  return vec ? launch_norm_shape<DT, true>(fwd, wg, a, st) : launch_norm_shape<DT, false>(fwd, wg, a, st);
+  return launch_overlapped(norm_bwd_long_kernel<DT>, grid, kLongThreads, 0, st, a);
 }
 
 }  // namespace
 
 uint64_t layernorm_scratch_bytes(uint64_t n_rows, uint32_t row_len) {
-  return (uint64_t)partial_count(n_rows, row_len) * 2 * row_len * sizeof(float);
+  return (uint64_t)partial_cap(n_rows) * 2 * row_len * sizeof(float);
 }
 
 cudaError_t launch_layernorm_fwd(int dt, int wdt, const void* x, const void* gamma, const void* beta, void* y, float* stats,
                                  uint64_t n_rows, uint32_t row_len, uint64_t x_stride, uint64_t y_stride, float eps,
                                  cudaStream_t st) {
-  NormArgs a{x, nullptr, gamma, beta, y, nullptr, stats, nullptr, n_rows, x_stride, 0, y_stride, row_len, wdt, eps};
-  return dt == kF32 ? launch_norm_dt<kF32>(true, false, a, st) : launch_norm_dt<kBF16>(true, false, a, st);
+  NormArgs a = {};
+  a.x = x;
+  a.gamma = gamma;
+  a.beta = beta;
+  a.out = y;
+  a.stats_out = stats;
+  a.n_rows = n_rows;
+  a.x_stride = x_stride;
+  a.out_stride = y_stride;
+  a.row_len = row_len;
+  a.wdt = wdt;
+  a.eps = eps;
+  uint32_t parts = 0;
+  return dt == kF32 ? launch_norm_dt<kF32>(true, false, a, parts, st) : launch_norm_dt<kBF16>(true, false, a, parts, st);
 }
 
 cudaError_t launch_layernorm_bwd(int dt, int wdt, const void* g, const void* x, const void* gamma, const float* stats,
@@ -525,11 +672,24 @@ cudaError_t launch_layernorm_bwd(int dt, int wdt, const void* g, const void* x, 
     }
     return grad_beta ? cudaMemsetAsync(grad_beta, 0, bytes, st) : cudaSuccess;
   }
-  NormArgs a{x, g, gamma, nullptr, grad_in, stats, nullptr, scratch, n_rows, x_stride, g_stride, out_stride, row_len, wdt, 0.0f};
-  const cudaError_t e = dt == kF32 ? launch_norm_dt<kF32>(false, wg, a, st) : launch_norm_dt<kBF16>(false, wg, a, st);
+  NormArgs a = {};
+  a.x = x;
+  a.g = g;
+  a.gamma = gamma;
+  a.out = grad_in;
+  a.stats_in = stats;
+  a.partials = scratch;
+  a.n_rows = n_rows;
+  a.x_stride = x_stride;
+  a.g_stride = g_stride;
+  a.out_stride = out_stride;
+  a.row_len = row_len;
+  a.wdt = wdt;
+  uint32_t parts = 0;
+  const cudaError_t e = dt == kF32 ? launch_norm_dt<kF32>(false, wg, a, parts, st) : launch_norm_dt<kBF16>(false, wg, a, parts, st);
   if (e != cudaSuccess || !wg) return e;
-  return launch_overlapped(norm_reduce_kernel, dim3((row_len + 31) / 32, 2), 256, 0, st, scratch,
-                           partial_count(n_rows, row_len), row_len, grad_gamma, grad_beta, wdt);
+  return launch_overlapped(norm_reduce_kernel, dim3((row_len + 31) / 32, 2), kReduceWarps * 32, 0, st, scratch, parts, row_len,
+                           grad_gamma, grad_beta, wdt);
 }
 
 }  // namespace s2a

@@ -2,6 +2,8 @@
 // launch helper of the kernels built on them.
 #pragma once
 
+#include <atomic>
+
 #include "s2a_common.cuh"
 
 namespace s2a {
@@ -50,12 +52,39 @@ __device__ __forceinline__ void store_param(void* p, uint64_t i, int wdt, float 
   else ((__nv_bfloat16*)p)[i] = __float2bfloat16_rn(v);
 }
 
+// Asynchronous copies of a thread's own pieces into shared memory (16, 8 or 4 bytes, both sides aligned to that), in groups
+// that complete in order.  A thread that reads back only what it copied needs no barrier, just the wait.
+template <int BYTES>
+__device__ __forceinline__ void copy_async(void* smem, const void* global) {
+  const uint32_t s = (uint32_t)__cvta_generic_to_shared(smem);
+  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(s), "l"(global) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(s), "l"(global), "n"(BYTES) : "memory");
+}
+__device__ __forceinline__ void copy_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copy_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
 // Programmatic dependent launch.  Every kernel launched through launch_overlapped calls enter_grid() before it
 // touches memory: the next kernel of the stream may then be scheduled, and this one goes on once its
 // predecessor has completed and its writes are visible.
 __device__ __forceinline__ void enter_grid() {
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   asm volatile("griddepcontrol.wait;" ::: "memory");
+}
+
+// Lets a kernel use `bytes` of dynamic shared memory on the current device, once per device (`done`: one bit each, a
+// static of the caller per kernel; concurrent first calls may both set the attribute).
+template <typename... P>
+cudaError_t allow_shared(void (*kernel)(P...), size_t bytes, std::atomic<uint64_t>& done) {
+  if (bytes <= 40 * 1024) return cudaSuccess;  // within the 48 KB that need no leave, static arrays included
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
+  if (e != cudaSuccess) return e;
+  const uint64_t bit = 1ull << (dev & 63);
+  if (dev < 64 && (done.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+  e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+  if (e == cudaSuccess && dev < 64) done.fetch_or(bit, std::memory_order_release);
+  return e;
 }
 
 template <typename... P, typename... A>
