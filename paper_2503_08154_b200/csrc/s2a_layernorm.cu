@@ -7,14 +7,14 @@
 //             grad_gamma = sum over rows of g xhat, grad_beta = sum over rows of g
 //
 // Both passes are bound by memory: a row is read once and written once.  A row belongs to a team of LANES threads (8 to
-// 512) that own NO pieces of eight consecutive elements each, and the next rows of a team are always on the way: every
+// 512) that own NO * 8 elements each, in pieces of 16 bytes, and the next rows of a team are always on the way: every
 // thread copies its own pieces into a ring of STAGES rows in shared memory (cp.async), so the bytes in flight do not cost
 // registers, and since it reads back only what it copied itself the ring needs no barrier.  The variance is taken around
 // the mean (no difference of squares); the warps of a row merge (count, mean, squared deviations) with one exchange (Chan,
 // Golub and LeVeque's pairwise update).  All sums are binary32.
 //
 // Rows need not start on a 16-byte boundary.  A row's first element then sits s elements into a vector, pieces are the
-// vectors of the memory (piece v holds columns 8v - s .. 8v - s + 7), and the two at the row's ends are masked (EDGE).  A team keeps
+// vectors of the memory (piece v holds V columns from V v - s on), and the two at the row's ends are masked (EDGE).  A team keeps
 // to rows of one s, so that its pieces mean the same columns in every row.
 //
 // The weights' gradients are sums over rows: a thread keeps the sums of its own columns in registers over all the rows
@@ -47,7 +47,9 @@ struct NormArgs {
   int g_apart, out_apart;  // EDGE: g's (out's) rows do not sit on the 16-byte grid as x's do: element by element
 };
 
-template <int DT> constexpr int kVec = DT == kF32 ? 4 : 8;  // elements in 16 bytes
+template <int DT> constexpr int kVec = DT == kF32 ? 4 : 8;   // elements of a piece: 16 bytes
+template <int DT> constexpr int kPairs = kVec<DT> / 2;
+template <int DT, int NO> constexpr int kPieces = NO * 8 / kVec<DT>;  // pieces of a thread: NO * 8 elements
 
 __host__ __device__ constexpr int threads_of(int lanes) { return lanes > 256 ? lanes : 256; }
 // Rows in flight per team: what keeps two CTAs of an SM (one of 512 threads) within its shared memory.
@@ -58,77 +60,73 @@ __host__ __device__ constexpr int stage_bytes(int dt, int no, int lanes, int ten
   return threads_of(lanes) * no * (dt == kF32 ? 32 : 16) * tensors + (tensors == 2 ? threads_of(lanes) * 8 : 0);
 }
 
-// A thread's pieces of one tensor in one stage of the ring: [piece][half][thread] of 16 bytes.
-template <int DT, int NO, int THREADS>
-struct Slot {
-  static constexpr int kHalves = DT == kF32 ? 2 : 1;
-  static constexpr int kBytes = NO * kHalves * THREADS * 16;
-  char* base;  // of the stage, at this thread's column
-  __device__ __forceinline__ char* at(int j, int half) const { return base + (j * kHalves + half) * THREADS * 16; }
-  __device__ __forceinline__ Eight<DT> read(int j) const;
-  __device__ __forceinline__ void write(int j, const Eight<DT>& v) const;
-};
-template <int DT, int NO, int THREADS>
-__device__ __forceinline__ Eight<DT> Slot<DT, NO, THREADS>::read(int j) const {
-  Eight<DT> v;
+// A piece as it lies in memory.
+template <int DT>
+__device__ __forceinline__ void widen_piece(const uint4& r, F2* v) {
   if constexpr (DT == kF32) {
-    v.a = *(const float4*)at(j, 0);
-    v.b = *(const float4*)at(j, 1);
+    v[0] = f2_pack(__uint_as_float(r.x), __uint_as_float(r.y));
+    v[1] = f2_pack(__uint_as_float(r.z), __uint_as_float(r.w));
   } else {
-    v.r = *(const uint4*)at(j, 0);
+    v[0] = f2_from_bf16x2(r.x);
+    v[1] = f2_from_bf16x2(r.y);
+    v[2] = f2_from_bf16x2(r.z);
+    v[3] = f2_from_bf16x2(r.w);
   }
-  return v;
 }
-template <int DT, int NO, int THREADS>
-__device__ __forceinline__ void Slot<DT, NO, THREADS>::write(int j, const Eight<DT>& v) const {
+template <int DT>
+__device__ __forceinline__ uint4 narrow_piece(const F2* v) {
   if constexpr (DT == kF32) {
-    *(float4*)at(j, 0) = v.a;
-    *(float4*)at(j, 1) = v.b;
+    float a, b, c, d;
+    f2_unpack(v[0], a, b);
+    f2_unpack(v[1], c, d);
+    return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
   } else {
-    *(uint4*)at(j, 0) = v.r;
+    return make_uint4(f2_to_bf16x2(v[0]), f2_to_bf16x2(v[1]), f2_to_bf16x2(v[2]), f2_to_bf16x2(v[3]));
   }
 }
 
-// Where a thread's pieces lie: piece j begins at column (j * LANES + lane) * 8 - s (s = 0 without EDGE).
-template <int LANES>
-__device__ __forceinline__ int piece_column(int j, uint32_t lane, int s) { return (int)((j * LANES + lane) * 8u) - s; }
+// Where a thread's pieces lie: piece j begins at column (j * LANES + lane) * kVec - s (s = 0 without EDGE).
+template <int DT, int LANES>
+__device__ __forceinline__ int piece_column(int j, uint32_t lane, int s) { return (int)((j * LANES + lane) * (uint32_t)kVec<DT>) - s; }
 
-template <bool EDGE>
-__device__ __forceinline__ bool piece_on(int c, int L) { return EDGE ? (c < L && c + 8 > 0) : c < L; }
+template <int DT, bool EDGE>
+__device__ __forceinline__ bool piece_on(int c, int L) { return EDGE ? (c < L && c + kVec<DT> > 0) : c < L; }
+template <int DT>
+__device__ __forceinline__ bool piece_whole(int c, int L) { return c >= 0 && c + kVec<DT> <= L; }
 
-// Starts the copies of a row's pieces.  `end`: of the tensor.  A vector that the tensor does not wholly contain (only at the
-// tensor's two ends), and every piece of a tensor that sits on another grid (`apart`), is read element by element.
+// Starts the copies of a row's pieces into this thread's column of a stage, [piece][thread] of 16 bytes.  `end`: of the
+// tensor.  A vector that the tensor does not wholly contain (only at the tensor's two ends), and every piece of a
+// tensor that sits on another grid (`apart`), is read element by element.
 template <int DT, bool EDGE, int NO, int LANES, int THREADS>
-__device__ __forceinline__ void fetch(const Slot<DT, NO, THREADS>& slot, const void* tensor, const void* end, uint64_t row,
-                                      uint64_t stride, uint32_t lane, int L, int s, bool apart) {
+__device__ __forceinline__ void fetch(uint4* slot, const void* tensor, const void* end, uint64_t row, uint64_t stride,
+                                      uint32_t lane, int L, int s, bool apart) {
   using T = typename Io<DT>::T;
+  constexpr int V = kVec<DT>;
   const T* p = (const T*)tensor + row * stride;
 #pragma unroll
-  for (int j = 0; j < NO; ++j) {
-    const int c = piece_column<LANES>(j, lane, s);
-    if (!piece_on<EDGE>(c, L)) continue;
-    if (!EDGE || (!apart && p + c >= (const T*)tensor && p + c + 8 <= (const T*)end)) {
-      copy_async<16>(slot.at(j, 0), p + c);
-      if (DT == kF32) copy_async<16>(slot.at(j, Slot<DT, NO, THREADS>::kHalves - 1), p + c + 4);
+  for (int j = 0; j < kPieces<DT, NO>; ++j) {
+    const int c = piece_column<DT, LANES>(j, lane, s);
+    if (!piece_on<DT, EDGE>(c, L)) continue;
+    if (!EDGE || (!apart && p + c >= (const T*)tensor && p + c + V <= (const T*)end)) {
+      copy_async<16>(slot + j * THREADS, p + c);
     } else {
-      float f[8];
+      float f[V];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) f[i] = c + i >= 0 && c + i < L ? Io<DT>::widen(p[c + i]) : 0.0f;
-      F2 w[4];
+      for (int i = 0; i < V; ++i) f[i] = c + i >= 0 && c + i < L ? Io<DT>::widen(p[c + i]) : 0.0f;
+      F2 w[V / 2];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = f2_pack(f[2 * i], f[2 * i + 1]);
-      Eight<DT> v;
-      v.set(w);
-      slot.write(j, v);
+      for (int i = 0; i < V / 2; ++i) w[i] = f2_pack(f[2 * i], f[2 * i + 1]);
+      slot[j * THREADS] = narrow_piece<DT>(w);
     }
   }
 }
 
 // Elements of a piece outside the row become zero.
+template <int DT>
 __device__ __forceinline__ void mask_ends(F2* v, int c, int L) {
-  if (c >= 0 && c + 8 <= L) return;
+  if (piece_whole<DT>(c, L)) return;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < kPairs<DT>; ++i) {
     float lo, hi;
     f2_unpack(v[i], lo, hi);
     const int k = c + 2 * i;
@@ -138,13 +136,11 @@ __device__ __forceinline__ void mask_ends(F2* v, int c, int L) {
 
 template <int DT, bool EDGE>
 __device__ __forceinline__ void put_piece(typename Io<DT>::T* row, int c, int L, bool apart, const F2* v) {
-  if (!EDGE || (!apart && c >= 0 && c + 8 <= L)) {
-    Eight<DT> o;
-    o.set(v);
-    o.store(row + c);
+  if (!EDGE || (!apart && piece_whole<DT>(c, L))) {
+    *(uint4*)(row + c) = narrow_piece<DT>(v);
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < kVec<DT>; ++i) {
       float lo, hi;
       f2_unpack(v[i / 2], lo, hi);
       if (c + i >= 0 && c + i < L) row[c + i] = Io<DT>::narrow(i % 2 ? hi : lo);
@@ -152,26 +148,33 @@ __device__ __forceinline__ void put_piece(typename Io<DT>::T* row, int c, int L,
   }
 }
 
-// Eight learned parameters from column c on; `fill` where there are none.
+// A piece's learned parameters, from column c on; `fill` where there are none.
+template <int DT>
 __device__ __forceinline__ void load_weights(const void* p, int c, int L, int wdt, float fill, F2* v) {
-  const char* at = (const char*)p + (int64_t)c * (wdt == kF32 ? 4 : 2);
-  if (p && c >= 0 && c + 8 <= L && ((uintptr_t)at & 15u) == 0) {
-    if (wdt == kF32) {
-      Eight<kF32> w;
-      w.load(at);
-      w.get(v);
-    } else {
-      Eight<kBF16> w;
-      w.load(at);
-      w.get(v);
+  constexpr int V = kVec<DT>;
+  if (p && piece_whole<DT>(c, L)) {
+    const char* at = (const char*)p + (int64_t)c * (wdt == kF32 ? 4 : 2);
+    if (wdt == kF32 && ((uintptr_t)at & 15u) == 0) {
+#pragma unroll
+      for (int i = 0; i < V / 4; ++i) widen_piece<kF32>(((const uint4*)at)[i], v + 2 * i);
+      return;
     }
-    return;
+    if (wdt == kBF16 && ((uintptr_t)at & (2 * V - 1)) == 0) {
+      const uint2 a = *(const uint2*)at, b = V == 8 ? ((const uint2*)at)[1] : a;
+      v[0] = f2_from_bf16x2(a.x);
+      v[1] = f2_from_bf16x2(a.y);
+      if (V == 8) {
+        v[V / 2 - 2] = f2_from_bf16x2(b.x);
+        v[V / 2 - 1] = f2_from_bf16x2(b.y);
+      }
+      return;
+    }
   }
-  float f[8];
+  float f[V];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) f[i] = p && c + i >= 0 && c + i < L ? load_param(p, (uint64_t)(c + i), wdt) : fill;
+  for (int i = 0; i < V; ++i) f[i] = p && c + i >= 0 && c + i < L ? load_param(p, (uint64_t)(c + i), wdt) : fill;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = f2_pack(f[2 * i], f[2 * i + 1]);
+  for (int i = 0; i < V / 2; ++i) v[i] = f2_pack(f[2 * i], f[2 * i + 1]);
 }
 
 __device__ __forceinline__ float f2_sum(F2 a) {
@@ -215,21 +218,21 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : (NO == 1 
   const float inv_l = 1.0f / (float)L;
   const uint64_t step = (uint64_t)gridDim.x * TEAMS, first = (uint64_t)blockIdx.x * TEAMS + team;
   const int s = row_shift<DT, EDGE>(a, first);
-  using Ring = Slot<DT, NO, THREADS>;
+  constexpr int NP = kPieces<DT, NO>, PAIRS = kPairs<DT>;
 #pragma unroll
   for (int k = 0; k < STAGES; ++k) {
     if (first + k * step < a.n_rows)
-      fetch<DT, EDGE, NO, LANES, THREADS>(Ring{ring + k * BYTES + threadIdx.x * 16}, a.x, a.x_end, first + k * step, a.x_stride, lane, L, s, false);
+      fetch<DT, EDGE, NO, LANES, THREADS>((uint4*)(ring + k * BYTES) + threadIdx.x, a.x, a.x_end, first + k * step, a.x_stride, lane, L, s, false);
     copy_commit();
   }
-  F2 gamma[NO][4], beta[NO][4];
+  F2 gamma[NP][PAIRS], beta[NP][PAIRS];
   float count = 0.0f;  // elements of the row that this warp holds
 #pragma unroll
-  for (int j = 0; j < NO; ++j) {
-    const int c = piece_column<LANES>(j, lane, s);
-    load_weights(a.gamma, c, L, a.wdt, 1.0f, gamma[j]);
-    load_weights(a.beta, c, L, a.wdt, 0.0f, beta[j]);
-    if (piece_on<EDGE>(c, L)) count += (float)(min(c + 8, L) - max(c, 0));
+  for (int j = 0; j < NP; ++j) {
+    const int c = piece_column<DT, LANES>(j, lane, s);
+    load_weights<DT>(a.gamma, c, L, a.wdt, 1.0f, gamma[j]);
+    load_weights<DT>(a.beta, c, L, a.wdt, 0.0f, beta[j]);
+    if (piece_on<DT, EDGE>(c, L)) count += (float)(min(c + kVec<DT>, L) - max(c, 0));
   }
   if (WARPS > 1) count = lanes_sum<32>(count);
   const float inv_count = WARPS > 1 ? (count > 0.0f ? 1.0f / count : 0.0f) : inv_l;
@@ -240,20 +243,20 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : (NO == 1 
     const uint64_t r = base + team;
     if (LANES >= 32 && r >= a.n_rows) break;
     copy_wait<STAGES - 1>();
-    const Ring slot{ring + stage * BYTES + threadIdx.x * 16};
-    F2 v[NO][4], sum = f2_both(0.0f);
+    uint4* slot = (uint4*)(ring + stage * BYTES) + threadIdx.x;
+    F2 v[NP][PAIRS], sum = f2_both(0.0f);
 #pragma unroll
-    for (int j = 0; j < NO; ++j) {
-      const int c = piece_column<LANES>(j, lane, s);
-      if (piece_on<EDGE>(c, L)) {
-        slot.read(j).get(v[j]);
-        if (EDGE) mask_ends(v[j], c, L);
+    for (int j = 0; j < NP; ++j) {
+      const int c = piece_column<DT, LANES>(j, lane, s);
+      if (piece_on<DT, EDGE>(c, L)) {
+        widen_piece<DT>(slot[j * THREADS], v[j]);
+        if (EDGE) mask_ends<DT>(v[j], c, L);
       } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) v[j][i] = f2_both(0.0f);
+        for (int i = 0; i < PAIRS; ++i) v[j][i] = f2_both(0.0f);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sum = f2_add(sum, v[j][i]);
+      for (int i = 0; i < PAIRS; ++i) sum = f2_add(sum, v[j][i]);
     }
     if (r + STAGES * step < a.n_rows)
       fetch<DT, EDGE, NO, LANES, THREADS>(slot, a.x, a.x_end, r + STAGES * step, a.x_stride, lane, L, s, false);
@@ -262,15 +265,15 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : (NO == 1 
     float mean = lanes_sum<GROUP>(f2_sum(sum)) * inv_count;
     F2 sq = f2_both(0.0f);
 #pragma unroll
-    for (int j = 0; j < NO; ++j) {
-      const int c = piece_column<LANES>(j, lane, s);
-      if (!piece_on<EDGE>(c, L)) continue;
-      F2 d[4];
+    for (int j = 0; j < NP; ++j) {
+      const int c = piece_column<DT, LANES>(j, lane, s);
+      if (!piece_on<DT, EDGE>(c, L)) continue;
+      F2 d[PAIRS];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) d[i] = f2_sub(v[j][i], f2_both(mean));
-      if (EDGE) mask_ends(d, c, L);
+      for (int i = 0; i < PAIRS; ++i) d[i] = f2_sub(v[j][i], f2_both(mean));
+      if (EDGE) mask_ends<DT>(d, c, L);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) sq = f2_fma(d[i], d[i], sq);
+      for (int i = 0; i < PAIRS; ++i) sq = f2_fma(d[i], d[i], sq);
     }
     float dev = lanes_sum<GROUP>(f2_sum(sq));
     if (WARPS > 1) {
@@ -288,11 +291,11 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : (NO == 1 
     if (a.stats_out && lane == 0) ((float2*)a.stats_out)[r] = make_float2(mean, rstd);
     T* out = (T*)a.out + r * a.out_stride;
 #pragma unroll
-    for (int j = 0; j < NO; ++j) {
-      const int c = piece_column<LANES>(j, lane, s);
-      if (!piece_on<EDGE>(c, L)) continue;
+    for (int j = 0; j < NP; ++j) {
+      const int c = piece_column<DT, LANES>(j, lane, s);
+      if (!piece_on<DT, EDGE>(c, L)) continue;
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < PAIRS; ++i)
         v[j][i] = f2_fma(f2_mul(f2_sub(v[j][i], f2_both(mean)), f2_both(rstd)), gamma[j][i], beta[j][i]);
       put_piece<DT, EDGE>(out, c, L, EDGE && a.out_apart, v[j]);
     }
@@ -306,7 +309,7 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : 2) norm_b
   constexpr int THREADS = threads_of(LANES), TEAMS = THREADS / LANES, WARPS = LANES / 32 > 1 ? LANES / 32 : 1;
   constexpr int GROUP = LANES < 32 ? LANES : 32;
   constexpr int BYTES = stage_bytes(DT, NO, LANES, 2), STAGES = stages_of(BYTES);
-  using Ring = Slot<DT, NO, THREADS>;
+  constexpr int NP = kPieces<DT, NO>, PAIRS = kPairs<DT>, TENSOR = NP * THREADS * 16;
   extern __shared__ __align__(16) char ring[];  // per stage: x's pieces, g's pieces, (mean, rstd) per thread
   __shared__ float2 merge[2][TEAMS][WARPS];
   enter_grid();
@@ -317,21 +320,21 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : 2) norm_b
   const int s = row_shift<DT, EDGE>(a, first);
   const auto start_row = [&](char* at, uint64_t r) {
     if (r >= a.n_rows) return;
-    fetch<DT, EDGE, NO, LANES, THREADS>(Ring{at + threadIdx.x * 16}, a.x, a.x_end, r, a.x_stride, lane, L, s, false);
-    fetch<DT, EDGE, NO, LANES, THREADS>(Ring{at + Ring::kBytes + threadIdx.x * 16}, a.g, a.g_end, r, a.g_stride, lane, L, s, EDGE && a.g_apart);
-    copy_async<8>(at + 2 * Ring::kBytes + threadIdx.x * 8, a.stats_in + 2 * r);
+    fetch<DT, EDGE, NO, LANES, THREADS>((uint4*)at + threadIdx.x, a.x, a.x_end, r, a.x_stride, lane, L, s, false);
+    fetch<DT, EDGE, NO, LANES, THREADS>((uint4*)(at + TENSOR) + threadIdx.x, a.g, a.g_end, r, a.g_stride, lane, L, s, EDGE && a.g_apart);
+    copy_async<8>(at + 2 * TENSOR + threadIdx.x * 8, a.stats_in + 2 * r);
   };
 #pragma unroll
   for (int k = 0; k < STAGES; ++k) {
     start_row(ring + k * BYTES, first + k * step);
     copy_commit();
   }
-  F2 gamma[NO][4], dgamma[NO][4], dbeta[NO][4];
+  F2 gamma[NP][PAIRS], dgamma[NP][PAIRS], dbeta[NP][PAIRS];
 #pragma unroll
-  for (int j = 0; j < NO; ++j) {
-    load_weights(a.gamma, piece_column<LANES>(j, lane, s), L, a.wdt, 1.0f, gamma[j]);
+  for (int j = 0; j < NP; ++j) {
+    load_weights<DT>(a.gamma, piece_column<DT, LANES>(j, lane, s), L, a.wdt, 1.0f, gamma[j]);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) dgamma[j][i] = dbeta[j][i] = f2_both(0.0f);
+    for (int i = 0; i < PAIRS; ++i) dgamma[j][i] = dbeta[j][i] = f2_both(0.0f);
   }
   uint32_t parity = 0, stage = 0;
   for (uint64_t base = (uint64_t)blockIdx.x * TEAMS; base < a.n_rows; base += step) {
@@ -340,23 +343,23 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : 2) norm_b
     const bool on = LANES >= 32 || r < a.n_rows;
     copy_wait<STAGES - 1>();
     char* at = ring + stage * BYTES;
-    const Ring sx{at + threadIdx.x * 16}, sg{at + Ring::kBytes + threadIdx.x * 16};
-    const float2 st = *(const float2*)(at + 2 * Ring::kBytes + threadIdx.x * 8);
+    const uint4 *sx = (const uint4*)at + threadIdx.x, *sg = (const uint4*)(at + TENSOR) + threadIdx.x;
+    const float2 st = *(const float2*)(at + 2 * TENSOR + threadIdx.x * 8);
     const F2 mean2 = f2_both(st.x), rstd2 = f2_both(st.y);
     F2 s1 = f2_both(0.0f), s2 = f2_both(0.0f);
 #pragma unroll
-    for (int j = 0; j < NO; ++j) {
-      const int c = piece_column<LANES>(j, lane, s);
-      if (!on || !piece_on<EDGE>(c, L)) continue;
-      F2 x[4], g[4];
-      sx.read(j).get(x);
-      sg.read(j).get(g);
+    for (int j = 0; j < NP; ++j) {
+      const int c = piece_column<DT, LANES>(j, lane, s);
+      if (!on || !piece_on<DT, EDGE>(c, L)) continue;
+      F2 x[PAIRS], g[PAIRS];
+      widen_piece<DT>(sx[j * THREADS], x);
+      widen_piece<DT>(sg[j * THREADS], g);
       if (EDGE) {
-        mask_ends(x, c, L);
-        mask_ends(g, c, L);
+        mask_ends<DT>(x, c, L);
+        mask_ends<DT>(g, c, L);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < PAIRS; ++i) {
         const F2 xhat = f2_mul(f2_sub(x[i], mean2), rstd2), w = f2_mul(g[i], gamma[j][i]);
         s1 = f2_add(s1, w);
         s2 = f2_fma(w, xhat, s2);
@@ -378,14 +381,14 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : 2) norm_b
     const F2 m1 = f2_both(c1 * inv_l), m2 = f2_both(-c2 * inv_l);
     T* out = (T*)a.out + r * a.out_stride;
 #pragma unroll
-    for (int j = 0; j < NO; ++j) {
-      const int c = piece_column<LANES>(j, lane, s);
-      if (!on || !piece_on<EDGE>(c, L)) continue;
-      F2 x[4], g[4];
-      sx.read(j).get(x);
-      sg.read(j).get(g);
+    for (int j = 0; j < NP; ++j) {
+      const int c = piece_column<DT, LANES>(j, lane, s);
+      if (!on || !piece_on<DT, EDGE>(c, L)) continue;
+      F2 x[PAIRS], g[PAIRS];
+      widen_piece<DT>(sx[j * THREADS], x);
+      widen_piece<DT>(sg[j * THREADS], g);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < PAIRS; ++i) {
         const F2 xhat = f2_mul(f2_sub(x[i], mean2), rstd2);
         g[i] = f2_mul(f2_fma(xhat, m2, f2_sub(f2_mul(g[i], gamma[j][i]), m1)), rstd2);
       }
@@ -396,23 +399,23 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : 2) norm_b
     stage = stage + 1 == STAGES ? 0 : stage + 1;
   }
   if constexpr (WG) {
-    // The CTA's teams, column by column, in order.  The ring holds their sums by piece: [team][2][half][piece][lane] of four
+    // The CTA's teams, column by column, in order.  The ring holds their sums by piece: [team][2][quarter][piece][lane] of four
     // columns, which threads write and read without bank conflicts.
     copy_wait<0>();
     __syncthreads();
     float4* sums = (float4*)ring;
-    constexpr int kRow = 2 * NO * LANES;  // float4s of one of a team's two rows
+    constexpr int QUADS = kVec<DT> / 4, kRow = QUADS * NP * LANES;  // float4s of a piece; of one of a team's two rows
 #pragma unroll
-    for (int j = 0; j < NO; ++j)
+    for (int j = 0; j < NP; ++j)
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
+      for (int q = 0; q < QUADS; ++q) {
         float4 w;
-        f2_unpack(dgamma[j][2 * half], w.x, w.y);
-        f2_unpack(dgamma[j][2 * half + 1], w.z, w.w);
-        sums[(team * 2 + 0) * kRow + (half * NO + j) * LANES + lane] = w;
-        f2_unpack(dbeta[j][2 * half], w.x, w.y);
-        f2_unpack(dbeta[j][2 * half + 1], w.z, w.w);
-        sums[(team * 2 + 1) * kRow + (half * NO + j) * LANES + lane] = w;
+        f2_unpack(dgamma[j][2 * q], w.x, w.y);
+        f2_unpack(dgamma[j][2 * q + 1], w.z, w.w);
+        sums[(team * 2 + 0) * kRow + (q * NP + j) * LANES + lane] = w;
+        f2_unpack(dbeta[j][2 * q], w.x, w.y);
+        f2_unpack(dbeta[j][2 * q + 1], w.z, w.w);
+        sums[(team * 2 + 1) * kRow + (q * NP + j) * LANES + lane] = w;
       }
     __syncthreads();
     float* part = a.partials + (uint64_t)blockIdx.x * 2 * L;
@@ -423,7 +426,7 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : 2) norm_b
 #pragma unroll 4
       for (int m = 0; m < TEAMS; ++m) {
         const uint32_t p = c + (EDGE ? (uint32_t)row_shift<DT, EDGE>(a, (uint64_t)blockIdx.x * TEAMS + m) : 0u);
-        t += flat[((m * 2 + which) * kRow + ((p / 4) % 2) * NO * LANES + p / 8) * 4 + p % 4];
+        t += flat[((m * 2 + which) * kRow + ((p / 4) % QUADS) * NP * LANES + p / kVec<DT>) * 4 + p % 4];
       }
       part[k] = t;
     }
@@ -583,9 +586,9 @@ cudaError_t launch_norm(bool fwd, bool wg, const NormArgs& a, uint32_t& parts, c
 
 // The smallest team that holds the row: one piece a lane up to a warp, two or three beyond.
 template <int DT, bool EDGE>
-cudaError_t launch_norm_shape(bool fwd, bool wg, const NormArgs& a, uint32_t vecs, uint32_t& parts, cudaStream_t st) {
+cudaError_t launch_norm_shape(bool fwd, bool wg, const NormArgs& a, uint32_t elems, uint32_t& parts, cudaStream_t st) {
 #define S2A_NORM(NO, LANES) \
-  if (vecs <= NO * LANES) return launch_norm<DT, EDGE, NO, LANES>(fwd, wg, a, parts, st);
+  if (elems <= NO * LANES * 8) return launch_norm<DT, EDGE, NO, LANES>(fwd, wg, a, parts, st);
   S2A_NORM(1, 8)
   S2A_NORM(1, 16)
   S2A_NORM(1, 32)
@@ -618,10 +621,10 @@ cudaError_t launch_norm_dt(bool fwd, bool wg, NormArgs a, uint32_t& parts, cudaS
   a.x_end = (const T*)a.x + (a.n_rows - 1) * a.x_stride + a.row_len;
   a.g_end = a.g ? (const T*)a.g + (a.n_rows - 1) * a.g_stride + a.row_len : nullptr;
   const bool shifted = ((uintptr_t)a.x / sizeof(T)) % V != 0 || (a.n_rows > 1 && a.x_stride % V != 0);
-  const bool edge = shifted || a.row_len % 8 != 0 || a.g_apart || a.out_apart;
-  const uint32_t vecs = shifted ? (uint32_t)((a.row_len + V - 1 + 7) / 8) : (a.row_len + 7) / 8;
-  if (vecs <= 4 * 512)
-    return edge ? launch_norm_shape<DT, true>(fwd, wg, a, vecs, parts, st) : launch_norm_shape<DT, false>(fwd, wg, a, vecs, parts, st);
+  const bool edge = shifted || a.row_len % V != 0 || a.g_apart || a.out_apart;
+  const uint32_t elems = (uint32_t)(a.row_len + (shifted ? V - 1 : 0));  // with what lies before the row in its first vector
+  if (elems <= 4 * 512 * 8)
+    return edge ? launch_norm_shape<DT, true>(fwd, wg, a, elems, parts, st) : launch_norm_shape<DT, false>(fwd, wg, a, elems, parts, st);
   const uint64_t cap = (uint64_t)sm_count() * 4;
   const dim3 grid((unsigned)(a.n_rows < cap ? a.n_rows : cap));
   if (fwd) return launch_overlapped(norm_fwd_long_kernel<DT>, grid, kLongThreads, 0, st, a);
