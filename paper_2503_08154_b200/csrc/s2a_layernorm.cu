@@ -47,8 +47,6 @@ struct NormArgs {
   int g_apart, out_apart;  // EDGE: g's (out's) rows do not sit on the 16-byte grid as x's do: element by element
 };
 
-template <int DT> constexpr int kVec = DT == kF32 ? 4 : 8;   // elements of a piece: 16 bytes
-template <int DT> constexpr int kPairs = kVec<DT> / 2;
 template <int DT, int NO> constexpr int kPieces = NO * 8 / kVec<DT>;  // pieces of a thread: NO * 8 elements
 
 __host__ __device__ constexpr int threads_of(int lanes) { return lanes > 256 ? lanes : 256; }
@@ -58,31 +56,6 @@ __host__ __device__ constexpr int stages_of(int stage_bytes) {
 }
 __host__ __device__ constexpr int stage_bytes(int dt, int no, int lanes, int tensors) {
   return threads_of(lanes) * no * (dt == kF32 ? 32 : 16) * tensors + (tensors == 2 ? threads_of(lanes) * 8 : 0);
-}
-
-// A piece as it lies in memory.
-template <int DT>
-__device__ __forceinline__ void widen_piece(const uint4& r, F2* v) {
-  if constexpr (DT == kF32) {
-    v[0] = f2_pack(__uint_as_float(r.x), __uint_as_float(r.y));
-    v[1] = f2_pack(__uint_as_float(r.z), __uint_as_float(r.w));
-  } else {
-    v[0] = f2_from_bf16x2(r.x);
-    v[1] = f2_from_bf16x2(r.y);
-    v[2] = f2_from_bf16x2(r.z);
-    v[3] = f2_from_bf16x2(r.w);
-  }
-}
-template <int DT>
-__device__ __forceinline__ uint4 narrow_piece(const F2* v) {
-  if constexpr (DT == kF32) {
-    float a, b, c, d;
-    f2_unpack(v[0], a, b);
-    f2_unpack(v[1], c, d);
-    return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
-  } else {
-    return make_uint4(f2_to_bf16x2(v[0]), f2_to_bf16x2(v[1]), f2_to_bf16x2(v[2]), f2_to_bf16x2(v[3]));
-  }
 }
 
 // Where a thread's pieces lie: piece j begins at column (j * LANES + lane) * kVec - s (s = 0 without EDGE).

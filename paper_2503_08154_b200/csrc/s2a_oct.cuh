@@ -1,5 +1,5 @@
-// Eight consecutive elements of an I/O tensor in registers (16 bytes of bfloat16, 32 of binary32), and the
-// launch helper of the kernels built on them.
+// Consecutive elements of an I/O tensor in registers: eight (16 bytes of bfloat16, 32 of binary32), or the piece of 16
+// bytes; asynchronous copies, and the launch helpers of the kernels built on them.
 #pragma once
 
 #include <atomic>
@@ -42,6 +42,34 @@ template <> struct Eight<kF32> {
     f2_unpack(v[3], b.z, b.w);
   }
 };
+
+template <int DT> constexpr int kVec = DT == kF32 ? 4 : 8;  // elements of a piece: 16 bytes
+template <int DT> constexpr int kPairs = kVec<DT> / 2;
+
+// A piece as it lies in memory.
+template <int DT>
+__device__ __forceinline__ void widen_piece(const uint4& r, F2* v) {
+  if constexpr (DT == kF32) {
+    v[0] = f2_pack(__uint_as_float(r.x), __uint_as_float(r.y));
+    v[1] = f2_pack(__uint_as_float(r.z), __uint_as_float(r.w));
+  } else {
+    v[0] = f2_from_bf16x2(r.x);
+    v[1] = f2_from_bf16x2(r.y);
+    v[2] = f2_from_bf16x2(r.z);
+    v[3] = f2_from_bf16x2(r.w);
+  }
+}
+template <int DT>
+__device__ __forceinline__ uint4 narrow_piece(const F2* v) {
+  if constexpr (DT == kF32) {
+    float a, b, c, d;
+    f2_unpack(v[0], a, b);
+    f2_unpack(v[1], c, d);
+    return make_uint4(__float_as_uint(a), __float_as_uint(b), __float_as_uint(c), __float_as_uint(d));
+  } else {
+    return make_uint4(f2_to_bf16x2(v[0]), f2_to_bf16x2(v[1]), f2_to_bf16x2(v[2]), f2_to_bf16x2(v[3]));
+  }
+}
 
 // One element of a learned parameter (layer norm's weights, a bias table): binary32 or bfloat16 by `wdt`.
 __device__ __forceinline__ float load_param(const void* p, uint64_t i, int wdt) {
