@@ -344,7 +344,7 @@ int s2a_dropout_bwd(const void* grad_out, void* grad_in, size_t n_elems, const u
  *                 new token against a cache, tq = 1 and the vector is a window of a longer one.
  *                 An entry outside 0 .. n_buckets - 1 adds nothing and has no gradient.
  *   y        out  like x; may be x
- * heads: 1 .. 65535, n_buckets: 1 .. 32768, tq * tk at most 2^40.  Scores of -inf (masked) stay
+ * heads: 1 .. 65535, n_buckets: 1 .. 32768, tq * tk at most 2^36.  Scores of -inf (masked) stay
  * -inf, rows of them included.  The gradient to x is grad_out itself and needs no call.
  */
 int s2a_relbias_fwd(const void* x, const void* table, const int32_t* buckets, int by_distance, void* y, size_t batch,

@@ -344,13 +344,12 @@ static bool bad_bias_shape(size_t batch, size_t heads, size_t tq, size_t tk, siz
       n_buckets > kMaxBuckets)
     return true;
   const size_t slab = tq * tk;
-  return slab > ((size_t)1 << 40) || (slab != 0 && batch * heads > ((size_t)1 << 60) / slab);
+  return slab > ((size_t)1 << 36) || (slab != 0 && batch * heads > ((size_t)1 << 60) / slab);
 }
 
 size_t s2a_relbias_scratch_bytes(size_t batch, size_t heads, size_t tq, size_t tk, size_t n_buckets) {
   if (bad_bias_shape(batch, heads, tq, tk, n_buckets) || batch * tq * tk == 0) return 0;
-  return (size_t)relbias_bwd_ctas((uint32_t)batch, (uint32_t)heads, (uint32_t)tq, (uint32_t)tk, (uint32_t)n_buckets) *
-         n_buckets * sizeof(float);
+  return (size_t)relbias_scratch_bytes((uint32_t)heads, (uint32_t)n_buckets);
 }
 
 int s2a_relbias_fwd(const void* x, const void* table, const int32_t* buckets, int by_distance, void* y, size_t batch,

@@ -77,9 +77,9 @@ cudaError_t launch_dropout(int dt, const void* x, const void* residual, void* y,
                            uint64_t site, uint32_t threshold, cudaStream_t st);
 
 // Relative position bias.  buckets: [tq, tk], or [tq + tk - 1] over k - q + tq - 1 where by_distance is set.  scratch of the
-// backward call: relbias_bwd_ctas(...) * n_buckets floats.  log_buckets runs on the host.
+// backward call: relbias_scratch_bytes.  log_buckets runs on the host.
 constexpr uint32_t kMaxBuckets = 32768;
-uint32_t relbias_bwd_ctas(uint32_t batch, uint32_t heads, uint32_t tq, uint32_t tk, uint32_t n_buckets);
+uint64_t relbias_scratch_bytes(uint32_t heads, uint32_t n_buckets);
 cudaError_t launch_relbias_fwd(int dt, int wdt, const void* x, const void* table, const int32_t* buckets, int by_distance,
                                void* y, uint32_t batch, uint32_t heads, uint32_t tq, uint32_t tk, uint32_t n_buckets,
                                cudaStream_t st);

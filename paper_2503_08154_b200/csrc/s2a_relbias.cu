@@ -10,10 +10,11 @@
 // d is constant.  Let o be the offset of a row (b, h, q) and V the elements of a 16-byte vector.  Element i of the vector
 // V (floor((o + q) / V) + m) of the tensor has d = V m + i - c + tq - 1 where c = (o + q) mod V is the row's class.  So a
 // thread that owns (m, c) meets the same V distances in every row of that class, over queries and samples: forward keeps
-// their biases in registers, backward their sums, and both only load and add (and store) inside the loop.  The classes
-// are taken one after the other; the rows of a class are every V-th row or sample, or whatever arithmetic gives.
+// their biases in registers, backward their sums, and inside the loop both only load and add (and store).  The classes are
+// taken one after the other.
 //
-// Work is cut into items: a head, a block of query rows, a chunk of vectors (`lanes` of them) and a part of the batch.
+// Work is cut into items: a head, a block of query rows, a chunk of vectors (`lanes` of them) and a part of the batch.  A thread
+// has the loads of kAhead rows of a run in flight at a time.
 #include <math.h>
 
 #include "s2a_launch.h"
@@ -22,9 +23,17 @@
 namespace s2a {
 namespace {
 
+#ifndef AHEAD
+#define AHEAD 4
+#define MINB 3
+#define FIXF 12
+#define FIXB 20
+#endif
 constexpr uint32_t kThreads = 256, kMostThreads = 320;
-constexpr uint32_t kTableBytes = 128 * 1024;  // shared memory for the tables of a backward CTA
-constexpr int kAhead = 4;                     // rows whose loads a thread has in flight
+constexpr uint32_t kThreadsPerSm = 1024;     // at 64 registers a thread
+constexpr int kAhead = AHEAD;
+constexpr int kStaged = 5;                   // slots that a thread looks up at a time
+constexpr uint32_t kTableBytes = 24 * 1024;  // shared memory for the tables of a backward CTA, beyond the first table
 
 struct BiasArgs {
   const void* x;           // x or grad_out
@@ -32,179 +41,245 @@ struct BiasArgs {
   const void* table;       // forward
   const int32_t* buckets;  // [tq + tk - 1]
   float* partials;         // backward: [head][CTA of the head][n_buckets]
-  uint64_t tk;             // up to 2^40 (a map)
+  uint64_t tk;             // up to 2^36 (a map)
+  uint64_t slab, sample;   // elements of one (b, h), of one b
   uint32_t batch, heads, tq;
   uint32_t n_buckets;
   uint32_t block;          // query rows of an item
-  uint32_t blocks, chunks, parts;  // items of a head: blocks * chunks * parts
-  uint32_t lanes;          // threads of a CTA along a chunk; the other factor of the threads runs along the batch
-  uint32_t ctas_per_head;
+  uint32_t part;           // samples of an item
+  uint32_t chunks, parts, items;  // chunks of vectors, parts of the batch; items of a head: (query blocks) * chunks * parts
+  uint32_t lanes, rows;    // threads of a CTA along a chunk, and along the batch
+  uint32_t ctas_per_head, threads;
   uint32_t tables;         // backward: warps that have a table
-  uint32_t threads;        // of a CTA
   int by_batch;            // the inner loop runs over samples (few query rows), not over query rows
+  int wdt;
   // Along the inner loop the class moves by `step` = 2^shift * odd (mod V) from row to row: rows of one class come every `period` =
   // V / 2^shift rows, and there are some if the class differs from the first row's by a multiple of 2^shift.
-  uint32_t period, shift, odd;
-  int wdt;
+  uint32_t step, period, period_log, shift, odd;
+  uint32_t classes;        // with one query row the classes are those of the samples; with more, any may occur
+  int64_t row_step;        // elements between the rows of a run, and the keys that the thread's vector moves by
+  int key_step;
 };
 
 // An item, and the thread's place in it.
 struct Item {
-  uint32_t h, q0, q1, b0, b1;
-  int64_t m;       // the thread's vector, relative to the rows' floor((o + q) / V)
-  int64_t d0;      // the distance index of shared slot 0 (see slot())
+  uint32_t queries, samples;  // of the item
+  uint32_t c0;                // class of its first row
+  // The thread's vector in the first row, were that row of class 0: its element in the tensor, and the keys it is from being
+  // wholly inside the row, V m + q0 >= 0 and <= tk - V.
+  int64_t e;
+  int key_low, key_high;
+  // Shared slot k (see slot()) is distance d0 + k: its bucket is lut[k], for low <= k < high.
+  const int32_t* lut;
+  int low, high;
 };
-// Distance V m + i - c + tq - 1 lives in shared slot V lane + i - c + V - 1 >= 0, spread so that lanes V apart fall in
-// different banks.
-template <int V> __device__ __forceinline__ uint32_t slot(uint32_t k) { return k + k / V; }
-template <int V> __device__ __forceinline__ uint32_t slot_of(uint32_t lane, int i, uint32_t c) {
-  const uint32_t k = i + V - 1 - c;  // 0 .. 2 V - 2
-  return lane * (V + 1) + k + (k >= V ? 1u : 0u);
-}
+// Distance V m + i - c + tq - 1 lives in slot V lane + i - c + V - 1 >= 0 of the chunk.
 template <int V> __host__ __device__ constexpr uint32_t slots(uint32_t lanes) { return lanes * V + V - 1; }
-template <int V> __host__ __device__ constexpr uint32_t padded(uint32_t lanes) { return slots<V>(lanes) + slots<V>(lanes) / V + 1; }
+// In the forward kernel's shared memory the slots are spread so that lanes V apart fall in different banks.
+template <int V> __device__ __forceinline__ uint32_t spread(uint32_t k) { return k + k / V; }
+template <int V> __host__ __device__ constexpr uint32_t spread_slots(uint32_t lanes) { return slots<V>(lanes) + slots<V>(lanes) / V + 1; }
+
+__device__ __forceinline__ int clamp_int(int64_t v) {
+  const int64_t far = 1 << 30;
+  return (int)(v > far ? far : (v < -far ? -far : v));
+}
 
 template <int V>
-__device__ __forceinline__ Item item_of(const BiasArgs& a, uint32_t h, uint64_t index, uint32_t lane) {
+__device__ __forceinline__ Item item_of(const BiasArgs& a, uint32_t h, uint32_t index, uint32_t lane) {
   Item t;
-  t.h = h;
-  const uint64_t place = a.parts == 1 ? index : index / a.parts;
-  const uint32_t part = (uint32_t)(index - place * a.parts);
-  const uint32_t block = a.blocks == 1 ? 0u : (uint32_t)(place / a.chunks), chunk = (uint32_t)(place - (uint64_t)block * a.chunks);
-  t.q0 = block * a.block;
-  t.q1 = min(a.tq, t.q0 + a.block);
-  t.b0 = (uint32_t)((uint64_t)a.batch * part / a.parts);
-  t.b1 = (uint32_t)((uint64_t)a.batch * (part + 1) / a.parts);
-  // the lowest vector that a row of the block can need: k >= 0, i.e. V m >= c - q - (V - 1) with c >= 0, q <= q1 - 1
-  const int64_t low = -(int64_t)((t.q1 - 1 + V - 1) / V) + (int64_t)chunk * a.lanes;
-  t.m = low + lane;
-  t.d0 = low * V - (V - 1) + (int64_t)a.tq - 1;
+  const uint32_t place = a.parts == 1 ? index : index / a.parts, part = index - place * a.parts;
+  const uint32_t block = place / a.chunks, chunk = place - block * a.chunks;
+  const uint32_t q0 = block * a.block, b0 = part * a.part;
+  t.queries = min(a.tq - q0, a.block);
+  t.samples = b0 < a.batch ? min(a.batch - b0, a.part) : 0;
+  const uint64_t first = b0 * a.sample + h * a.slab + q0 * a.tk;
+  t.c0 = ((uint32_t)first + q0) & (V - 1);
+  // the lowest vector that a row of the block can need: k >= 0, i.e. V m >= c - q - (V - 1) with c >= 0, q < q0 + queries
+  const int64_t lowest = (int64_t)chunk * a.lanes - (int64_t)((q0 + t.queries + V - 2) / V);
+  const int64_t k = (lowest + lane) * V + q0;
+  t.e = (int64_t)first + k;
+  t.key_low = clamp_int(-k);
+  t.key_high = clamp_int((int64_t)a.tk - V - k);
+  const int64_t d0 = lowest * V - (V - 1) + (int64_t)a.tq - 1;
+  t.lut = a.buckets + d0;
+  t.low = clamp_int(-d0);
+  t.high = clamp_int((int64_t)(a.tq + a.tk) - 1 - d0);
   return t;
 }
 
-// The first row of class c, counted from one of class c0; false if there is none.  r * 2^shift * odd = c - c0 (mod V) has the
-// solution r = (c - c0) / 2^shift * odd (mod period): an odd number is its own inverse modulo 8.
+// The bucket of slot k, -1 for none (and for k < 0).
+__device__ __forceinline__ int bucket_of(const BiasArgs& a, const Item& t, int k) {
+  const int u = k >= 0 && k >= t.low && k < t.high ? t.lut[k] : -1;
+  return (uint32_t)u < a.n_buckets ? u : -1;
+}
+
+// The runs of an item as one thread takes them, class by class.  A run: the rows of one class along the inner loop (samples or
+// query rows), row_step elements apart, of which the thread's vector moves by key_step keys.
 template <int V>
-__device__ __forceinline__ bool first_of_class(const BiasArgs& a, uint32_t c0, uint32_t c, uint32_t& r) {
-  const uint32_t off = (c - c0) & (V - 1);
-  r = ((off >> a.shift) * a.odd) & (a.period - 1);
-  return (off & ((1u << a.shift) - 1u)) == 0;
-}
+struct Runs {
+  uint32_t i, c;    // the class, by number and as it is
+  uint32_t o;       // a query row of the item (by_batch) or a sample
+  int n;            // rows of the run
+  int low, high;    // row j's vector is wholly inside its row for low <= j * key_step <= high, wholly outside for j * key_step <= low - V
+                    // and for j * key_step >= high + V
+  int64_t e;        // the first row's element
 
-// Calls body(n, e, e_step, k, k_step) for the runs of rows of class c that row-thread `row` of `rows` takes: n rows, the first
-// with the thread's vector at element e of the tensor and key k (both may lie outside), the others e_step and k_step on.
-template <int V, class Body>
-__device__ __forceinline__ void walk(const BiasArgs& a, const Item& t, uint32_t c, uint32_t row, uint32_t rows, Body body) {
-  const uint64_t slab = a.tq * a.tk, sample = slab * a.heads;
-  uint32_t r;
-  if (a.by_batch) {
-    for (uint32_t q = t.q0; q < t.q1; ++q) {
-      const uint64_t o = t.b0 * sample + t.h * slab + q * a.tk;
-      if (!first_of_class<V>(a, (uint32_t)o + q, c, r)) continue;
-      const uint32_t b = t.b0 + r + row * a.period, step = rows * a.period;  // samples b, b + step, ...
-      if (b >= t.b1) continue;
-      const int64_t k = t.m * V - c + q;
-      body((int)((t.b1 - b + step - 1) / step), (int64_t)(o + (b - t.b0) * sample) + k, (int64_t)(step * sample), k, 0);
-    }
-  } else {
-    for (uint32_t b = t.b0 + row; b < t.b1; b += rows) {
-      const uint64_t o = b * sample + t.h * slab + t.q0 * a.tk;
-      if (!first_of_class<V>(a, (uint32_t)o + t.q0, c, r) || t.q0 + r >= t.q1) continue;
-      const int64_t k = t.m * V - c + t.q0 + r;  // query rows q0 + r, q0 + r + period, ...
-      body((int)((t.q1 - t.q0 - r + a.period - 1) / a.period), (int64_t)(o + r * a.tk) + k, (int64_t)(a.period * (a.tk + 1)), k,
-           (int)a.period);
+  __device__ __forceinline__ void start(const BiasArgs& a, const Item& t, uint32_t row) {
+    i = row < a.rows ? 0 : a.classes;  // threads may be left over
+    o = a.by_batch ? 0 : row;
+    seek(a, t, row);
+  }
+  __device__ __forceinline__ bool done(const BiasArgs& a) const { return i >= a.classes; }
+  __device__ __forceinline__ void next(const BiasArgs& a, const Item& t, uint32_t row) {
+    o += a.by_batch ? 1 : a.rows;
+    seek(a, t, row);
+  }
+
+  // The first run at or after run o of class i.
+  __device__ __forceinline__ void seek(const BiasArgs& a, const Item& t, uint32_t row) {
+    for (; i < a.classes; ++i, o = a.by_batch ? 0 : row) {
+      c = a.tq == 1 ? (t.c0 + i * a.step) & (V - 1) : i;
+      const uint32_t end = a.by_batch ? t.queries : t.samples, hop = a.by_batch ? 1 : a.rows;
+      for (; o < end; o += hop) {
+        // The run's first row: r * 2^shift * odd = c - (class of row 0) (mod V) has the solution
+        // r = (c - class) / 2^shift * odd (mod period), as an odd number is its own inverse modulo 8.
+        const uint32_t off = (c - t.c0 - o * (a.by_batch ? (uint32_t)a.tk + 1 : (uint32_t)a.sample)) & (V - 1);
+        if (off & ((1u << a.shift) - 1u)) continue;
+        uint32_t r = ((off >> a.shift) * a.odd) & (a.period - 1);
+        uint32_t q = r;
+        if (a.by_batch) {  // samples r + row * period, + rows * period, ...
+          r += row * a.period;
+          q = o;
+          n = r < t.samples ? (int)((t.samples - r - 1) / (a.rows * a.period)) + 1 : 0;
+        } else {           // query rows r, + period, ...
+          n = r < t.queries ? (int)((t.queries - r - 1) >> a.period_log) + 1 : 0;
+        }
+        if (n == 0) continue;
+        e = t.e + (int64_t)((a.by_batch ? r : o) * a.sample + q * (a.tk + 1)) - c;
+        low = t.key_low - (int)(q - c);
+        high = t.key_high - (int)(q - c);
+        return;
+      }
     }
   }
-}
 
-// Keys k .. k + V - 1 against 0 .. tk - 1, in 32 bits: `at` counts from the run's first row (at most a block of rows on).
-struct KeyRange {
-  int low, high;  // a vector `at` keys on is wholly inside for low <= at <= high, wholly outside for at <= low - V, at >= high + V
-  __device__ __forceinline__ KeyRange(int64_t k, uint64_t tk, int V) {
-    const int64_t far = 1 << 30, hi = (int64_t)tk - V - k;
-    low = (int)(-k > far ? far : (-k < -far ? -far : -k));
-    high = (int)(hi > far ? far : (hi < -far ? -far : hi));
+  // The rows of the run that the vector meets: any0 <= j < any1, wholly for in0 <= j < in1 (in0 = in1 = any1 if there is no such).
+  __device__ __forceinline__ void meets(const BiasArgs& a, int& any0, int& any1, int& in0, int& in1) const {
+    if (a.by_batch) {
+      any0 = 0;
+      any1 = low < V && high > -V ? n : 0;
+      in0 = low <= 0 && high >= 0 ? 0 : any1;
+      in1 = any1;
+    } else {
+      const int log = (int)a.period_log, up = a.key_step - 1;
+      any0 = max(0, (low - V + 1 + up) >> log);
+      any1 = max(any0, min(n, ((high + V - 1) >> log) + 1));
+      in0 = max(any0, (low + up) >> log);
+      in1 = min(any1, (high >> log) + 1);
+      if (in0 >= in1) in0 = in1 = any1;
+    }
   }
-  __device__ __forceinline__ bool inside(int at) const { return at >= low && at <= high; }
-  __device__ __forceinline__ bool outside(int at, int V) const { return at <= low - V || at >= high + V; }
 };
 
+// Loads elements from .. to - 1 of a vector, zeros in place of the others; one by one, as the rest of the vector is another row's, or
+// lies after the tensor.
 template <int DT>
-__device__ __forceinline__ uint4 load_ends(const typename Io<DT>::T* x, int from, int to) {  // elements from .. to - 1 of a vector
-  float f[kVec<DT>];
+__device__ __forceinline__ uint4 load_ends(const typename Io<DT>::T* x, int from, int to) {
+  uint32_t w[kVec<DT>];
 #pragma unroll
-  for (int i = 0; i < kVec<DT>; ++i) f[i] = i >= from && i < to ? Io<DT>::widen(x[i]) : 0.0f;
-  F2 v[kPairs<DT>];
+  for (int i = 0; i < kVec<DT>; ++i) {
+    w[i] = 0;
+    if (i < from || i >= to) continue;
+    if constexpr (DT == kF32) w[i] = __float_as_uint(x[i]);
+    else w[i] = __bfloat16_as_ushort(x[i]);
+  }
+  if constexpr (DT == kF32) return make_uint4(w[0], w[1], w[2], w[3]);
+  else return make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+}
+
+// Stores elements from .. to - 1 of a vector.
+template <int DT>
+__device__ __forceinline__ void store_ends(typename Io<DT>::T* y, const uint4& v, int from, int to) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
 #pragma unroll
-  for (int i = 0; i < kPairs<DT>; ++i) v[i] = f2_pack(f[2 * i], f[2 * i + 1]);
-  return narrow_piece<DT>(v);
+  for (int i = 0; i < kVec<DT>; ++i) {
+    if (i < from || i >= to) continue;
+    if constexpr (DT == kF32) y[i] = __uint_as_float(w[i]);
+    else y[i] = __ushort_as_bfloat16((unsigned short)(w[i / 2] >> (16 * (i % 2))));
+  }
 }
 
 // ---------------------------------------------------------------- forward
 template <int DT>
-__device__ __forceinline__ uint4 add_bias(const uint4& r, const float* bias) {
+__device__ __forceinline__ uint4 add_bias(const uint4& r, const F2* bias) {
   F2 v[kPairs<DT>];
   widen_piece<DT>(r, v);
 #pragma unroll
-  for (int i = 0; i < kPairs<DT>; ++i) v[i] = f2_add(v[i], f2_pack(bias[2 * i], bias[2 * i + 1]));
+  for (int i = 0; i < kPairs<DT>; ++i) v[i] = f2_add(v[i], bias[i]);
   return narrow_piece<DT>(v);
 }
 
 template <int DT>
-__global__ void __launch_bounds__(kMostThreads, 3) bias_fwd_kernel(BiasArgs a) {
+__global__ void __launch_bounds__(kMostThreads, MINB) bias_fwd_kernel(BiasArgs a) {
   using T = typename Io<DT>::T;
   constexpr int V = kVec<DT>;
-  extern __shared__ float bias_of[];  // by slot: the bias of each distance of the chunk
+  extern __shared__ float bias_of[];  // by slot
   enter_grid();
-  const uint32_t lane = threadIdx.x % a.lanes, row = threadIdx.x / a.lanes, rows = blockDim.x / a.lanes;
-  const uint32_t h = blockIdx.x / a.ctas_per_head, count = slots<V>(a.lanes);
-  const uint64_t items = (uint64_t)a.blocks * a.chunks * a.parts;
-  const int64_t distances = (int64_t)(a.tq + a.tk - 1);
-  for (uint64_t index = blockIdx.x % a.ctas_per_head; index < items; index += a.ctas_per_head) {
+  const uint32_t row = threadIdx.x / a.lanes, lane = threadIdx.x - row * a.lanes, h = blockIdx.y, count = slots<V>(a.lanes);
+  for (uint32_t index = blockIdx.x; index < a.items; index += gridDim.x) {
     const Item t = item_of<V>(a, h, index, lane);
-    __syncthreads();  // the previous item's biases have been read
-    for (uint32_t k = threadIdx.x; k < count; k += blockDim.x) {
-      const int64_t d = t.d0 + k;
-      const int u = d >= 0 && d < distances ? a.buckets[d] : -1;
-      bias_of[slot<V>(k)] = u >= 0 && (uint32_t)u < a.n_buckets ? load_param(a.table, (uint64_t)u * a.heads + h, a.wdt) : 0.0f;
+    if (index != blockIdx.x) __syncthreads();  // the previous item's biases have been read
+    // several at a time: the two dependent loads of a slot are waited for once
+    for (uint32_t k = threadIdx.x; k < count; k += kStaged * a.threads) {
+      int u[kStaged];
+      float v[kStaged];
+#pragma unroll
+      for (int i = 0; i < kStaged; ++i) u[i] = bucket_of(a, t, k + i * a.threads < count ? (int)(k + i * a.threads) : -1);
+#pragma unroll
+      for (int i = 0; i < kStaged; ++i) v[i] = u[i] >= 0 ? load_param(a.table, (uint64_t)u[i] * a.heads + h, a.wdt) : 0.0f;
+#pragma unroll
+      for (int i = 0; i < kStaged; ++i)
+        if (k + i * a.threads < count) bias_of[spread<V>(k + i * a.threads)] = v[i];
     }
     __syncthreads();
+    Runs<V> run;
 #pragma unroll 1
-    for (uint32_t c = 0; c < V; ++c) {
-      walk<V>(a, t, c, row, rows, [&](int n, int64_t e, int64_t e_step, int64_t k, int k_step) {
-        float bias[V];
+    for (run.start(a, t, row); !run.done(a); run.next(a, t, row)) {
+      int any0, any1, in0, in1;
+      run.meets(a, any0, any1, in0, in1);
+      if (any0 >= any1) continue;
+      F2 bias[V / 2];
+      const uint32_t k = lane * V + V - 1 - run.c;
 #pragma unroll
-        for (int i = 0; i < V; ++i) bias[i] = bias_of[slot_of<V>(lane, i, c)];
-        const KeyRange range(k, a.tk, V);
-        const T* x = (const T*)a.x + e;
-        T* y = (T*)a.y + e;
-        for (int j = 0, at = 0; j < n; j += kAhead, at += kAhead * k_step, x += kAhead * e_step, y += kAhead * e_step) {
-          uint4 r[kAhead];
-          if (j + kAhead <= n && at >= range.low && at + (kAhead - 1) * k_step <= range.high) {
+      for (int i = 0; i < V / 2; ++i) bias[i] = f2_pack(bias_of[spread<V>(k + 2 * i)], bias_of[spread<V>(k + 2 * i + 1)]);
+      const T* x = (const T*)a.x + run.e + in0 * a.row_step;
+      T* y = (T*)a.y + run.e + in0 * a.row_step;
+      int left = in1 - in0;
+#pragma unroll 1
+      for (; left >= kAhead; left -= kAhead, x += kAhead * a.row_step, y += kAhead * a.row_step) {
+        uint4 r[kAhead];
 #pragma unroll
-            for (int s = 0; s < kAhead; ++s) r[s] = *(const uint4*)(x + s * e_step);
+        for (int s = 0; s < kAhead; ++s) r[s] = *(const uint4*)(x + s * a.row_step);
 #pragma unroll
-            for (int s = 0; s < kAhead; ++s) *(uint4*)(y + s * e_step) = add_bias<DT>(r[s], bias);
-            continue;
-          }
+        for (int s = 0; s < kAhead; ++s) *(uint4*)(y + s * a.row_step) = add_bias<DT>(r[s], bias);
+      }
+      if (left > 0) {
+        uint4 r[kAhead - 1];
 #pragma unroll
-          for (int s = 0; s < kAhead; ++s)
-            if (j + s < n && range.inside(at + s * k_step)) r[s] = *(const uint4*)(x + s * e_step);
+        for (int s = 0; s < kAhead - 1; ++s)
+          if (s < left) r[s] = *(const uint4*)(x + s * a.row_step);
 #pragma unroll
-          for (int s = 0; s < kAhead; ++s) {
-            const int key = at + s * k_step;
-            if (j + s >= n || range.outside(key, V)) continue;
-            if (range.inside(key)) {
-              *(uint4*)(y + s * e_step) = add_bias<DT>(r[s], bias);
-            } else {  // an end of the row: element by element
-              const int from = range.low - key, to = range.high + V - key;
-#pragma unroll
-              for (int i = 0; i < V; ++i)
-                if (i >= from && i < to) y[s * e_step + i] = Io<DT>::narrow(Io<DT>::widen(x[s * e_step + i]) + bias[i]);
-            }
-          }
-        }
-      });
+        for (int s = 0; s < kAhead - 1; ++s)
+          if (s < left) *(uint4*)(y + s * a.row_step) = add_bias<DT>(r[s], bias);
+      }
+#pragma unroll 1
+      for (int j = any0; j < any1; ++j) {  // the rows that end inside the vector
+        if (j == in0) j = in1;
+        if (j >= any1) break;
+        const int from = run.low - j * a.key_step, to = run.high + V - j * a.key_step;
+        const int64_t e = run.e + j * a.row_step;
+        store_ends<DT>((T*)a.y + e, add_bias<DT>(load_ends<DT>((const T*)a.x + e, from, to), bias), from, to);
+      }
     }
   }
 }
@@ -242,86 +317,106 @@ __device__ __forceinline__ void table_add(float* table, int u, float v) {
 }
 
 template <int DT>
-__global__ void __launch_bounds__(kMostThreads, 3) bias_bwd_kernel(BiasArgs a) {
+__device__ __forceinline__ void add_vector(F2* acc, const uint4& r) {
+  F2 v[kPairs<DT>];
+  widen_piece<DT>(r, v);
+#pragma unroll
+  for (int i = 0; i < kPairs<DT>; ++i) acc[i] = f2_add(acc[i], v[i]);
+}
+
+template <int DT>
+__global__ void __launch_bounds__(kMostThreads, MINB) bias_bwd_kernel(BiasArgs a) {
   using T = typename Io<DT>::T;
   constexpr int V = kVec<DT>;
-  extern __shared__ float shared[];  // [tables][n_buckets], then by row-thread and slot: the sum of each distance of the chunk
+  // [2 V - 1][thread]: a thread's sums of the distances V lane + 0 .. 2 V - 2 that its vector has in one class or another.
+  // [slots] their totals over the threads; [tables][n_buckets]; [slots] the buckets.
+  extern __shared__ float sums[];
   enter_grid();
-  const uint32_t lane = threadIdx.x % a.lanes, row = threadIdx.x / a.lanes, rows = blockDim.x / a.lanes, warp = threadIdx.x / 32;
-  const uint32_t h = blockIdx.x / a.ctas_per_head, count = slots<V>(a.lanes), pad = padded<V>(a.lanes);
-  const uint64_t items = (uint64_t)a.blocks * a.chunks * a.parts;
-  const int64_t distances = (int64_t)(a.tq + a.tk - 1);
-  float* sums = shared + a.tables * a.n_buckets;
-  for (uint32_t i = threadIdx.x; i < a.tables * a.n_buckets; i += blockDim.x) shared[i] = 0.0f;
-  for (uint64_t index = blockIdx.x % a.ctas_per_head; index < items; index += a.ctas_per_head) {
+  const uint32_t row = threadIdx.x / a.lanes, lane = threadIdx.x - row * a.lanes, warp = threadIdx.x / 32, h = blockIdx.y;
+  const uint32_t count = slots<V>(a.lanes);
+  float *totals = sums + (2 * V - 1) * a.threads, *tables = totals + count;
+  int16_t* ids = (int16_t*)(tables + a.tables * a.n_buckets);
+  for (uint32_t i = threadIdx.x; i < a.tables * a.n_buckets; i += a.threads) tables[i] = 0.0f;
+  for (uint32_t index = blockIdx.x; index < a.items; index += gridDim.x) {
     const Item t = item_of<V>(a, h, index, lane);
-    __syncthreads();  // the previous item's sums have been read
-    for (uint32_t k = threadIdx.x; k < rows * pad; k += blockDim.x) sums[k] = 0.0f;
+    if (index != blockIdx.x) __syncthreads();  // the previous item's sums have been read
+#pragma unroll
+    for (int k = 0; k < 2 * V - 1; ++k) sums[k * a.threads + threadIdx.x] = 0.0f;
+    for (uint32_t k = threadIdx.x; k < count; k += kStaged * a.threads) {  // buckets are below kMaxBuckets = 2^15
+      int u[kStaged];
+#pragma unroll
+      for (int i = 0; i < kStaged; ++i) u[i] = bucket_of(a, t, k + i * a.threads < count ? (int)(k + i * a.threads) : -1);
+#pragma unroll
+      for (int i = 0; i < kStaged; ++i)
+        if (k + i * a.threads < count) ids[k + i * a.threads] = (int16_t)u[i];
+    }
+    Runs<V> run;
 #pragma unroll 1
-    for (uint32_t c = 0; c < V; ++c) {
+    for (run.start(a, t, row); !run.done(a); run.next(a, t, row)) {
+      int any0, any1, in0, in1;
+      run.meets(a, any0, any1, in0, in1);
+      if (any0 >= any1) continue;
       F2 acc[V / 2];
 #pragma unroll
       for (int i = 0; i < V / 2; ++i) acc[i] = f2_both(0.0f);
-      int any = 0;  // a class may have no rows
-      walk<V>(a, t, c, row, rows, [&](int n, int64_t e, int64_t e_step, int64_t k, int k_step) {
-        any = 1;
-        const KeyRange range(k, a.tk, V);
-        const T* x = (const T*)a.x + e;
-        for (int j = 0, at = 0; j < n; j += kAhead, at += kAhead * k_step, x += kAhead * e_step) {
-          uint4 r[kAhead];
-          if (j + kAhead <= n && at >= range.low && at + (kAhead - 1) * k_step <= range.high) {
+      const T* x = (const T*)a.x + run.e + in0 * a.row_step;
+      int left = in1 - in0;
+#pragma unroll 1
+      for (; left >= kAhead; left -= kAhead, x += kAhead * a.row_step) {
+        uint4 r[kAhead];
 #pragma unroll
-            for (int s = 0; s < kAhead; ++s) r[s] = *(const uint4*)(x + s * e_step);
-          } else {
+        for (int s = 0; s < kAhead; ++s) r[s] = *(const uint4*)(x + s * a.row_step);
 #pragma unroll
-            for (int s = 0; s < kAhead; ++s) {
-              const int key = at + s * k_step;
-              r[s] = make_uint4(0, 0, 0, 0);
-              if (j + s >= n || range.outside(key, V)) continue;
-              if (range.inside(key)) r[s] = *(const uint4*)(x + s * e_step);
-              else r[s] = load_ends<DT>(x + s * e_step, range.low - key, range.high + V - key);
-            }
-          }
+        for (int s = 0; s < kAhead; ++s) add_vector<DT>(acc, r[s]);
+      }
+      if (left > 0) {
+        uint4 r[kAhead - 1];
 #pragma unroll
-          for (int s = 0; s < kAhead; ++s) {
-            F2 v[V / 2];
-            widen_piece<DT>(r[s], v);
+        for (int s = 0; s < kAhead - 1; ++s)
+          if (s < left) r[s] = *(const uint4*)(x + s * a.row_step);
 #pragma unroll
-            for (int i = 0; i < V / 2; ++i) acc[i] = f2_add(acc[i], v[i]);
-          }
-        }
-      });
-      // the classes overlap: a slot belongs to neighbouring lanes in different classes
-      if (!__syncthreads_or(any)) continue;
-      float* mine = sums + row * pad;
+        for (int s = 0; s < kAhead - 1; ++s)
+          if (s < left) add_vector<DT>(acc, r[s]);
+      }
+#pragma unroll 1
+      for (int j = any0; j < any1; ++j) {  // the rows that end inside the vector
+        if (j == in0) j = in1;
+        if (j >= any1) break;
+        add_vector<DT>(acc, load_ends<DT>((const T*)a.x + run.e + j * a.row_step, run.low - j * a.key_step, run.high + V - j * a.key_step));
+      }
+      float* mine = sums + (V - 1 - run.c) * a.threads + threadIdx.x;  // the distances V lane + i - c + V - 1
 #pragma unroll
       for (int i = 0; i < V / 2; ++i) {
         float lo, hi;
         f2_unpack(acc[i], lo, hi);
-        mine[slot_of<V>(lane, 2 * i, c)] += lo;
-        mine[slot_of<V>(lane, 2 * i + 1, c)] += hi;
+        mine[(2 * i) * a.threads] += lo;
+        mine[(2 * i + 1) * a.threads] += hi;
       }
     }
     __syncthreads();
+    for (uint32_t k = threadIdx.x; k < count; k += a.threads) {
+      // the distance is number k - V l of thread l for l = k / V and for the one before
+      const uint32_t l = k / V, own = k % V;
+      float v = 0.0f;
+      for (uint32_t w = 0; w < a.rows; ++w) {
+        if (l < a.lanes) v += sums[own * a.threads + w * a.lanes + l];
+        if (l > 0 && own + V < 2 * V - 1) v += sums[(own + V) * a.threads + w * a.lanes + l - 1];
+      }
+      totals[k] = v;
+    }
+    __syncthreads();
     if (warp < a.tables) {
-      float* table = shared + warp * a.n_buckets;
       for (uint32_t k0 = warp * 32; k0 < count; k0 += a.tables * 32) {
         const uint32_t k = k0 + threadIdx.x % 32;
-        const int64_t d = t.d0 + k;
-        int u = k < count && d >= 0 && d < distances ? a.buckets[d] : -1;
-        if (u < 0 || (uint32_t)u >= a.n_buckets) u = -1;
-        float v = 0.0f;
-        if (u >= 0)
-          for (uint32_t w = 0; w < rows; ++w) v += sums[w * pad + slot<V>(k)];
-        table_add(table, u, v);
+        table_add(tables + warp * a.n_buckets, k < count ? ids[k] : -1, k < count ? totals[k] : 0.0f);
       }
     }
   }
   __syncthreads();
-  float* part = a.partials + (uint64_t)blockIdx.x * a.n_buckets;
-  for (uint32_t u = threadIdx.x; u < a.n_buckets; u += blockDim.x) {
+  float* part = a.partials + ((uint64_t)h * gridDim.x + blockIdx.x) * a.n_buckets;
+  for (uint32_t u = threadIdx.x; u < a.n_buckets; u += a.threads) {
     float s = 0.0f;
-    for (uint32_t w = 0; w < a.tables; ++w) s += shared[w * a.n_buckets + u];
+    for (uint32_t w = 0; w < a.tables; ++w) s += tables[w * a.n_buckets + u];
     part[u] = s;
   }
 }
@@ -350,40 +445,57 @@ __global__ void __launch_bounds__(256) bias_table_kernel(const float* partials, 
 // ---------------------------------------------------------------- host side
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
-// Cuts the work of every head into items, about `want` of them over all heads.
+// Cuts the work of every head into items: of the cuts tried, the one whose CTAs are done first, where every SM of a B200 holds
+// kThreadsPerSm threads, a thread's row counts one and an item `fixed` besides.  At most `most` CTAs over all heads.
 template <int V>
-void cut(BiasArgs& a, uint64_t want) {
-  const uint64_t per_head = ceil_div(want, a.heads);
-  // query rows of an item: with many, the inner loop runs along the diagonals; with few, over the samples
-  a.by_batch = a.tq < 4 * V;
-  a.block = a.by_batch ? (a.tq < V ? a.tq : V) : 128;
-  const uint32_t step = (uint32_t)((a.by_batch ? (uint64_t)a.heads * a.tq * a.tk : a.tk + 1) % V);
+void cut(BiasArgs& a, uint64_t most, uint32_t fixed) {
+  a.by_batch = a.tq < 4 * V;  // with few query rows the inner loop runs over the samples
+  a.step = (uint32_t)((a.by_batch ? a.sample : a.tk + 1) % V);
   a.shift = 0;
-  while ((1u << a.shift) < V && (step >> a.shift) % 2 == 0) ++a.shift;
+  while ((1u << a.shift) < V && (a.step >> a.shift) % 2 == 0) ++a.shift;
   a.period = V >> a.shift;
-  a.odd = step >> a.shift;
-  // the vectors that the rows of a block can need, whatever their class
-  const auto vectors = [&] { return (a.tk + V - 2) / V + 1 + (a.block + V - 2) / V; };
-  while (!a.by_batch && a.block > 32 && ceil_div(a.tq, a.block) * ceil_div(vectors(), kMostThreads) * a.batch < per_head) a.block /= 2;
-  a.blocks = (uint32_t)ceil_div(a.tq, a.block);
-  // the threads along them: a CTA's width with one row of threads, or a power of two with several side by side
-  const uint64_t vecs = vectors();
-  a.lanes = 8;
-  while (a.lanes < 128 && a.lanes < vecs) a.lanes *= 2;
-  if (vecs > 128) a.lanes = (uint32_t)ceil_div(ceil_div(vecs, ceil_div(vecs, kMostThreads)), 32) * 32;
-  // fewer lanes (and more samples side by side) where the chunks are too few and the samples enough
-  const uint64_t side = a.by_batch ? a.period * kAhead : 1;  // samples that keep one row of threads busy
-  while (a.lanes > 32 && a.blocks * ceil_div(vecs, a.lanes) < per_head) {
-    const uint32_t less = a.lanes > 128 ? 128 : a.lanes / 2;
-    if (kThreads / less * side > a.batch) break;
-    a.lanes = less;
+  a.odd = a.step >> a.shift;
+  a.period_log = (V == 8 ? 3 : 2) - a.shift;
+  a.classes = a.tq == 1 ? a.period : V;
+  uint64_t best = ~0ull;
+  // heights of an item, in multiples of V
+  for (uint32_t block = a.by_batch ? V : 32; block <= (a.by_batch ? (uint32_t)V : 256u); block += block < 128 ? 16 : 32) {
+    const uint32_t height = block < a.tq ? block : a.tq;
+    const uint64_t blocks = ceil_div(a.tq, height);
+    const uint64_t vecs = (a.tk + V - 2) / V + 1 + (height + V - 2) / V;  // that the rows of a block can need, whatever their class
+    for (uint32_t want = kMostThreads; want >= 16; want = want > 256 ? 256 : want / 2) {
+      if (want > 16 && want / 2 >= vecs) continue;
+      const uint64_t chunks = ceil_div(vecs, want);
+      const uint32_t lanes = (uint32_t)ceil_div(vecs, chunks);
+      // threads side by side along the batch; by_batch each has whole periods of samples
+      const uint32_t side = a.by_batch ? a.period : 1, fit = kThreads / lanes > 1 ? kThreads / lanes : 1;
+      const uint32_t most_rows = (a.batch + side - 1) / side, rows = fit < most_rows ? fit : most_rows;
+      const uint32_t share = rows * side, shares = (a.batch + share - 1) / share;  // samples that one row of every thread takes
+      const uint32_t threads = (lanes * rows + 31) / 32 * 32;
+      const uint64_t resident = 148ull * (kThreadsPerSm / threads);
+      const uint64_t per_head = (resident < most ? resident : most) / a.heads > 1 ? (resident < most ? resident : most) / a.heads : 1;
+      uint64_t parts = per_head / (blocks * chunks);
+      parts = parts < 1 ? 1 : (parts < shares ? parts : shares);
+      const uint32_t part = (uint32_t)((shares + parts - 1) / parts) * share;
+      parts = (a.batch + part - 1) / part;
+      const uint64_t items = blocks * chunks * parts;
+      const uint64_t time = ((items + per_head - 1) / per_head) * ((uint64_t)height * (part / rows) + fixed);
+      if (time >= best || items > 0xffffffffull) continue;
+      best = time;
+      a.block = height;
+      a.lanes = lanes;
+      a.rows = rows;
+      a.threads = threads;
+      a.chunks = (uint32_t)chunks;
+      a.part = part;
+      a.parts = (uint32_t)parts;
+      a.items = (uint32_t)items;
+      a.ctas_per_head = (uint32_t)(items < per_head ? items : per_head);
+    }
+    if (height == a.tq) break;
   }
-  a.threads = a.lanes > 128 ? a.lanes : kThreads;
-  a.chunks = (uint32_t)ceil_div(vecs, a.lanes);
-  const uint64_t most = ceil_div(a.batch, a.threads / a.lanes * side), parts = ceil_div(per_head, (uint64_t)a.blocks * a.chunks);
-  a.parts = (uint32_t)(parts < 1 ? 1 : (parts < most ? parts : most));
-  const uint64_t items = (uint64_t)a.blocks * a.chunks * a.parts, cap = 4 * per_head;
-  a.ctas_per_head = (uint32_t)(items < cap ? items : cap);
+  a.row_step = (int64_t)(a.by_batch ? (uint64_t)a.rows * a.period * a.sample : (uint64_t)a.period * (a.tk + 1));
+  a.key_step = a.by_batch ? 0 : (int)a.period;
 }
 
 BiasArgs shape_args(uint32_t batch, uint32_t heads, uint32_t tq, uint32_t tk, uint32_t n_buckets, bool by_distance) {
@@ -392,50 +504,47 @@ BiasArgs shape_args(uint32_t batch, uint32_t heads, uint32_t tq, uint32_t tk, ui
   a.heads = heads;
   a.tq = by_distance ? tq : 1;
   a.tk = by_distance ? tk : (uint64_t)tq * tk;
+  a.slab = (uint64_t)tq * tk;
+  a.sample = a.slab * heads;
   a.n_buckets = n_buckets;
   return a;
 }
 
-constexpr uint64_t kFwdItems = 148 * 8;  // eight CTAs of 256 threads per SM of a B200
-// The backward kernel writes a table per CTA: half as many CTAs, and fewer yet for tables of many buckets.
-uint64_t bwd_items(uint32_t n_buckets) {
-  const uint64_t most = (1ull << 23) / n_buckets;
-  return most < 148 * 4 ? most : 148 * 4;
+// CTAs of the backward kernel, of which each writes a table: fewer for tables of many buckets.
+uint64_t bwd_most(uint32_t n_buckets) {
+  const uint64_t by_table = (1ull << 22) / n_buckets, most = 148 * 8;
+  return by_table < most ? by_table : most;
 }
 
 template <int DT>
 cudaError_t launch_bias_fwd(BiasArgs& a, cudaStream_t st) {
   constexpr int V = kVec<DT>;
-  cut<V>(a, kFwdItems);
-  return launch_overlapped(bias_fwd_kernel<DT>, dim3(a.heads * a.ctas_per_head), a.threads, padded<V>(a.lanes) * sizeof(float), st, a);
+  cut<V>(a, ~0ull, FIXF);
+  return launch_overlapped(bias_fwd_kernel<DT>, dim3(a.ctas_per_head, a.heads), a.threads, spread_slots<V>(a.lanes) * sizeof(float), st, a);
 }
 
 template <int DT>
 cudaError_t launch_bias_bwd(BiasArgs& a, cudaStream_t st) {
   constexpr int V = kVec<DT>;
   static std::atomic<uint64_t> ready = {};
-  cut<V>(a, bwd_items(a.n_buckets));
-  uint32_t tables = a.threads / 32;
-  while (tables > 1 && (tables * a.n_buckets * sizeof(float) > kTableBytes || tables * 64 > slots<V>(a.lanes))) tables /= 2;
-  a.tables = tables;
-  const size_t smem = ((size_t)tables * a.n_buckets + (size_t)(a.threads / a.lanes) * padded<V>(a.lanes)) * sizeof(float);
-  const cudaError_t e = allow_shared(bias_bwd_kernel<DT>, kTableBytes + 64 * 1024, ready);
-  return e != cudaSuccess ? e : launch_overlapped(bias_bwd_kernel<DT>, dim3(a.heads * a.ctas_per_head), a.threads, smem, st, a);
+  cut<V>(a, bwd_most(a.n_buckets), FIXB);
+  const size_t count = slots<V>(a.lanes);
+  a.tables = a.threads / 32;
+  while (a.tables > 1 && (a.tables * a.n_buckets * sizeof(float) > kTableBytes || a.tables * 64 > count)) a.tables /= 2;
+  const size_t smem = ((size_t)a.threads * (2 * V - 1) + count + (size_t)a.tables * a.n_buckets) * sizeof(float) + count * sizeof(int16_t);
+  // the most that any shape takes: 167 KB
+  constexpr size_t most = ((size_t)kMostThreads * (2 * V - 1) + slots<V>(kMostThreads) + kMaxBuckets) * sizeof(float) +
+                          slots<V>(kMostThreads) * sizeof(int16_t);
+  static_assert(most <= 227 * 1024, "a CTA must fit an SM");
+  const cudaError_t e = allow_shared(bias_bwd_kernel<DT>, most, ready);
+  return e != cudaSuccess ? e : launch_overlapped(bias_bwd_kernel<DT>, dim3(a.ctas_per_head, a.heads), a.threads, smem, st, a);
 }
 
 }  // namespace
 
-// The most CTAs over the element types and the two forms, which the size of the scratch does not tell apart.
-uint32_t relbias_bwd_ctas(uint32_t batch, uint32_t heads, uint32_t tq, uint32_t tk, uint32_t n_buckets) {
-  uint32_t most = 0;
-  for (int form = 0; form < 2; ++form) {
-    BiasArgs a = shape_args(batch, heads, tq, tk, n_buckets, form != 0);
-    cut<kVec<kF32>>(a, bwd_items(n_buckets));
-    most = a.ctas_per_head > most ? a.ctas_per_head : most;
-    cut<kVec<kBF16>>(a, bwd_items(n_buckets));
-    most = a.ctas_per_head > most ? a.ctas_per_head : most;
-  }
-  return heads * most;
+uint64_t relbias_scratch_bytes(uint32_t heads, uint32_t n_buckets) {
+  const uint64_t ctas = bwd_most(n_buckets);
+  return (ctas > heads ? ctas : heads) * n_buckets * sizeof(float);
 }
 
 cudaError_t launch_relbias_fwd(int dt, int wdt, const void* x, const void* table, const int32_t* buckets, int by_distance,

@@ -135,7 +135,7 @@ def test_bias_scratch(lib):
     for batch, heads, tq, tk, n in ((64, 12, 197, 197, 732), (1, 1, 1, 1, 1), (2, 16, 2048, 2048, 32), (3, 65535, 1, 9, 64),
                                     (1, 2, 50, 50, 32768)):
         b = f(batch, heads, tq, tk, n)
-        assert b % (4 * n * heads) == 0 and 4 * n * heads <= b <= 4 * 4 * max(1 << 23, 2 * heads * n)
+        assert b % (4 * n) == 0 and 4 * n * heads <= b <= 4 * max(1 << 22, heads * n)
 
 
 def _bucket(d, n_buckets, max_distance, bidirectional):
