@@ -13,8 +13,7 @@
 // their biases in registers, backward their sums, and inside the loop both only load and add (and store).  The classes are
 // taken one after the other.
 //
-// Work is cut into items: a head, a block of query rows, a chunk of vectors (`lanes` of them) and a part of the batch.  A thread
-// has the loads of kAhead rows of a run in flight at a time.
+// Work is cut into items: a head, a block of query rows, a chunk of vectors (`lanes` of them) and a part of the batch.
 #include <math.h>
 
 #include "s2a_launch.h"
@@ -23,17 +22,11 @@
 namespace s2a {
 namespace {
 
-#ifndef AHEAD
-#define AHEAD 4
-#define MINB 3
-#define FIXF 12
-#define FIXB 20
-#endif
+constexpr int kAheadFwd = 4, kAheadBwd = 4, kAheadCut = 4;  // rows of a run whose loads a thread has in flight
 constexpr uint32_t kThreads = 256, kMostThreads = 320;
 constexpr uint32_t kThreadsPerSm = 1024;     // at 64 registers a thread
-constexpr int kAhead = AHEAD;
 constexpr int kStaged = 5;                   // slots that a thread looks up at a time
-constexpr uint32_t kTableBytes = 24 * 1024;  // shared memory for the tables of a backward CTA, beyond the first table
+constexpr uint32_t kTableBytes = 64 * 1024;  // shared memory for the tables of a backward CTA, beyond the first table
 
 struct BiasArgs {
   const void* x;           // x or grad_out
@@ -163,13 +156,13 @@ struct Runs {
     }
   }
 
-  // The rows of the run that the vector meets: any0 <= j < any1, wholly for in0 <= j < in1 (in0 = in1 = any1 if there is no such).
-  __device__ __forceinline__ void meets(const BiasArgs& a, int& any0, int& any1, int& in0, int& in1) const {
+  // The rows of the run that the vector meets.  Along the samples (key_step 0) all of them, in one way: j = 0 .. in1 - 1, all
+  // whole or all cut.  Along the query rows whole ones, in0 <= j < in1, and cut ones, the other j of any0 <= j < any1.
+  __device__ __forceinline__ void meets(const BiasArgs& a, int& any0, int& any1, int& in0, int& in1, bool& cut) const {
     if (a.by_batch) {
-      any0 = 0;
-      any1 = low < V && high > -V ? n : 0;
-      in0 = low <= 0 && high >= 0 ? 0 : any1;
-      in1 = any1;
+      any0 = any1 = in0 = 0;
+      in1 = low < V && high > -V ? n : 0;
+      cut = low > 0 || high < 0;
     } else {
       const int log = (int)a.period_log, up = a.key_step - 1;
       any0 = max(0, (low - V + 1 + up) >> log);
@@ -177,6 +170,7 @@ struct Runs {
       in0 = max(any0, (low + up) >> log);
       in1 = min(any1, (high >> log) + 1);
       if (in0 >= in1) in0 = in1 = any1;
+      cut = false;
     }
   }
 };
@@ -195,6 +189,22 @@ __device__ __forceinline__ uint4 load_ends(const typename Io<DT>::T* x, int from
   }
   if constexpr (DT == kF32) return make_uint4(w[0], w[1], w[2], w[3]);
   else return make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+}
+
+// The vector at x, of which elements from .. to - 1 count: whole where the tensor holds it whole (the rest is another row's), the
+// tensor's last one element by element.
+template <int DT>
+__device__ __forceinline__ uint4 load_cut(const typename Io<DT>::T* x, const typename Io<DT>::T* end, int from, int to) {
+  return x + kVec<DT> <= end ? *(const uint4*)x : load_ends<DT>(x, from, to);
+}
+// Elements from .. to - 1 of a vector, zeros in place of the others.
+template <int DT>
+__device__ __forceinline__ uint4 keep_elements(const uint4& v, int from, int to) {
+  uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < kVec<DT>; ++i)
+    if (i < from || i >= to) w[DT == kF32 ? i : i / 2] &= DT == kF32 ? 0u : (i % 2 ? 0x0000ffffu : 0xffff0000u);
+  return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
 // Stores elements from .. to - 1 of a vector.
@@ -220,11 +230,12 @@ __device__ __forceinline__ uint4 add_bias(const uint4& r, const F2* bias) {
 }
 
 template <int DT>
-__global__ void __launch_bounds__(kMostThreads, MINB) bias_fwd_kernel(BiasArgs a) {
+__global__ void __launch_bounds__(kMostThreads, 3) bias_fwd_kernel(BiasArgs a) {
   using T = typename Io<DT>::T;
   constexpr int V = kVec<DT>;
   extern __shared__ float bias_of[];  // by slot
   enter_grid();
+  const int64_t to_y = (const T*)a.y - (const T*)a.x;  // both on the 16-byte grid
   const uint32_t row = threadIdx.x / a.lanes, lane = threadIdx.x - row * a.lanes, h = blockIdx.y, count = slots<V>(a.lanes);
   for (uint32_t index = blockIdx.x; index < a.items; index += gridDim.x) {
     const Item t = item_of<V>(a, h, index, lane);
@@ -246,39 +257,44 @@ __global__ void __launch_bounds__(kMostThreads, MINB) bias_fwd_kernel(BiasArgs a
 #pragma unroll 1
     for (run.start(a, t, row); !run.done(a); run.next(a, t, row)) {
       int any0, any1, in0, in1;
-      run.meets(a, any0, any1, in0, in1);
-      if (any0 >= any1) continue;
+      bool cut;
+      run.meets(a, any0, any1, in0, in1, cut);
+      if (any0 >= any1 && in0 >= in1) continue;
       F2 bias[V / 2];
       const uint32_t k = lane * V + V - 1 - run.c;
 #pragma unroll
       for (int i = 0; i < V / 2; ++i) bias[i] = f2_pack(bias_of[spread<V>(k + 2 * i)], bias_of[spread<V>(k + 2 * i + 1)]);
-      const T* x = (const T*)a.x + run.e + in0 * a.row_step;
-      T* y = (T*)a.y + run.e + in0 * a.row_step;
-      int left = in1 - in0;
+      const T *x = (const T*)a.x + run.e + in0 * a.row_step, *end = (const T*)a.x + a.batch * a.sample;
 #pragma unroll 1
-      for (; left >= kAhead; left -= kAhead, x += kAhead * a.row_step, y += kAhead * a.row_step) {
-        uint4 r[kAhead];
+      for (int left = in1 - in0; left > 0; left -= kAheadFwd, x += kAheadFwd * a.row_step) {
+        uint4 r[kAheadFwd];
 #pragma unroll
-        for (int s = 0; s < kAhead; ++s) r[s] = *(const uint4*)(x + s * a.row_step);
+        for (int s = 0; s < kAheadFwd; ++s)
+          if (s < left) r[s] = cut ? load_cut<DT>(x + s * a.row_step, end, run.low, run.high + V) : *(const uint4*)(x + s * a.row_step);
 #pragma unroll
-        for (int s = 0; s < kAhead; ++s) *(uint4*)(y + s * a.row_step) = add_bias<DT>(r[s], bias);
+        for (int s = 0; s < kAheadFwd; ++s) {
+          if (s >= left) break;
+          const uint4 w = add_bias<DT>(r[s], bias);
+          T* y = (T*)(x + s * a.row_step + to_y);
+          if (cut) store_ends<DT>(y, w, run.low, run.high + V);
+          else *(uint4*)y = w;
+        }
       }
-      if (left > 0) {
-        uint4 r[kAhead - 1];
-#pragma unroll
-        for (int s = 0; s < kAhead - 1; ++s)
-          if (s < left) r[s] = *(const uint4*)(x + s * a.row_step);
-#pragma unroll
-        for (int s = 0; s < kAhead - 1; ++s)
-          if (s < left) *(uint4*)(y + s * a.row_step) = add_bias<DT>(r[s], bias);
-      }
+      // the cut rows: a few before the whole ones and a few after
+      const int before = in0 - any0, cuts = before + any1 - in1;
 #pragma unroll 1
-      for (int j = any0; j < any1; ++j) {  // the rows that end inside the vector
-        if (j == in0) j = in1;
-        if (j >= any1) break;
-        const int from = run.low - j * a.key_step, to = run.high + V - j * a.key_step;
-        const int64_t e = run.e + j * a.row_step;
-        store_ends<DT>((T*)a.y + e, add_bias<DT>(load_ends<DT>((const T*)a.x + e, from, to), bias), from, to);
+      for (int j0 = 0; j0 < cuts; j0 += 2) {
+        uint4 r[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const int j = j0 + s < before ? any0 + j0 + s : in1 + j0 + s - before, moved = j * a.key_step;
+          if (j < any1) r[s] = load_cut<DT>((const T*)a.x + run.e + j * a.row_step, end, run.low - moved, run.high + V - moved);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const int j = j0 + s < before ? any0 + j0 + s : in1 + j0 + s - before, moved = j * a.key_step;
+          if (j < any1) store_ends<DT>((T*)a.y + run.e + j * a.row_step, add_bias<DT>(r[s], bias), run.low - moved, run.high + V - moved);
+        }
       }
     }
   }
@@ -286,15 +302,17 @@ __global__ void __launch_bounds__(kMostThreads, MINB) bias_fwd_kernel(BiasArgs a
 
 // ---------------------------------------------------------------- backward
 // Adds one value per lane (bucket u, none for u < 0) to a warp's table.  Neighbouring lanes of one bucket are added up first
-// (a segmented scan), then the last lane of each run adds its sum; runs of one bucket apart from each other take turns
-// in lane order.  No atomics: the order is always the same.
-__device__ __forceinline__ void table_add(float* table, int u, float v) {
+// (a segmented scan), and the last lane of each run adds its sum; runs of one bucket apart from each other take turns in
+// lane order.  No atomics: the order is always the same.  Whether two runs meet is found by writing: each lane leaves its number at
+// its bucket's tag and looks whether it is still there (__match_any_sync on 32 different buckets takes about 480 cycles, this about
+// 50).  Which of two lanes a tag keeps does not matter.
+__device__ __forceinline__ void table_add(float* table, uint8_t* tags, int u, float v) {
   const unsigned all = 0xffffffffu;
   const uint32_t lane = threadIdx.x % 32;
   const int before = __shfl_up_sync(all, u, 1), after = __shfl_down_sync(all, u, 1);
   const bool head = lane == 0 || before != u, tail = lane == 31 || after != u;
-  if (__any_sync(all, !head)) {
-    const uint32_t heads = __ballot_sync(all, head);
+  const uint32_t heads = __ballot_sync(all, head);
+  if (heads != all) {
     const uint32_t start = 31 - __clz(heads & (0xffffffffu >> (31 - lane)));  // where this lane's run begins
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -303,12 +321,15 @@ __device__ __forceinline__ void table_add(float* table, int u, float v) {
     }
   }
   const bool mine = tail && u >= 0;
-  const unsigned peers = __match_any_sync(all, mine ? u : -1 - (int)lane);
-  if (__all_sync(all, peers == (1u << lane))) {
+  if (mine) tags[u] = (uint8_t)lane;
+  __syncwarp();
+  const bool met = mine && tags[u] != lane;
+  if (!__any_sync(all, met)) {
     if (mine) table[u] += v;
     __syncwarp();
     return;
   }
+  const unsigned peers = __match_any_sync(all, mine ? u : -1 - (int)lane);
   const int turn = __popc(peers & ((1u << lane) - 1u)), turns = __reduce_max_sync(all, turn);
   for (int k = 0; k <= turns; ++k) {
     if (mine && turn == k) table[u] += v;
@@ -325,17 +346,18 @@ __device__ __forceinline__ void add_vector(F2* acc, const uint4& r) {
 }
 
 template <int DT>
-__global__ void __launch_bounds__(kMostThreads, MINB) bias_bwd_kernel(BiasArgs a) {
+__global__ void __launch_bounds__(kMostThreads, 3) bias_bwd_kernel(BiasArgs a) {
   using T = typename Io<DT>::T;
   constexpr int V = kVec<DT>;
   // [2 V - 1][thread]: a thread's sums of the distances V lane + 0 .. 2 V - 2 that its vector has in one class or another.
-  // [slots] their totals over the threads; [tables][n_buckets]; [slots] the buckets.
+  // [tables][n_buckets]; [slots] the buckets; [tables][n_buckets] the tables' tags.
   extern __shared__ float sums[];
   enter_grid();
   const uint32_t row = threadIdx.x / a.lanes, lane = threadIdx.x - row * a.lanes, warp = threadIdx.x / 32, h = blockIdx.y;
   const uint32_t count = slots<V>(a.lanes);
-  float *totals = sums + (2 * V - 1) * a.threads, *tables = totals + count;
+  float* tables = sums + (2 * V - 1) * a.threads;
   int16_t* ids = (int16_t*)(tables + a.tables * a.n_buckets);
+  uint8_t* tags = (uint8_t*)(ids + count);
   for (uint32_t i = threadIdx.x; i < a.tables * a.n_buckets; i += a.threads) tables[i] = 0.0f;
   for (uint32_t index = blockIdx.x; index < a.items; index += gridDim.x) {
     const Item t = item_of<V>(a, h, index, lane);
@@ -354,35 +376,50 @@ __global__ void __launch_bounds__(kMostThreads, MINB) bias_bwd_kernel(BiasArgs a
 #pragma unroll 1
     for (run.start(a, t, row); !run.done(a); run.next(a, t, row)) {
       int any0, any1, in0, in1;
-      run.meets(a, any0, any1, in0, in1);
-      if (any0 >= any1) continue;
+      bool cut;
+      run.meets(a, any0, any1, in0, in1, cut);
+      if (any0 >= any1 && in0 >= in1) continue;
       F2 acc[V / 2];
 #pragma unroll
       for (int i = 0; i < V / 2; ++i) acc[i] = f2_both(0.0f);
-      const T* x = (const T*)a.x + run.e + in0 * a.row_step;
+      const T *x = (const T*)a.x + run.e + in0 * a.row_step, *end = (const T*)a.x + a.batch * a.sample;
       int left = in1 - in0;
+      if (!cut) {
 #pragma unroll 1
-      for (; left >= kAhead; left -= kAhead, x += kAhead * a.row_step) {
-        uint4 r[kAhead];
+        for (; left >= kAheadBwd; left -= kAheadBwd, x += kAheadBwd * a.row_step) {
+          uint4 r[kAheadBwd];
 #pragma unroll
-        for (int s = 0; s < kAhead; ++s) r[s] = *(const uint4*)(x + s * a.row_step);
+          for (int s = 0; s < kAheadBwd; ++s) r[s] = *(const uint4*)(x + s * a.row_step);
 #pragma unroll
-        for (int s = 0; s < kAhead; ++s) add_vector<DT>(acc, r[s]);
-      }
-      if (left > 0) {
-        uint4 r[kAhead - 1];
-#pragma unroll
-        for (int s = 0; s < kAhead - 1; ++s)
-          if (s < left) r[s] = *(const uint4*)(x + s * a.row_step);
-#pragma unroll
-        for (int s = 0; s < kAhead - 1; ++s)
-          if (s < left) add_vector<DT>(acc, r[s]);
+          for (int s = 0; s < kAheadBwd; ++s) add_vector<DT>(acc, r[s]);
+        }
       }
 #pragma unroll 1
-      for (int j = any0; j < any1; ++j) {  // the rows that end inside the vector
-        if (j == in0) j = in1;
-        if (j >= any1) break;
-        add_vector<DT>(acc, load_ends<DT>((const T*)a.x + run.e + j * a.row_step, run.low - j * a.key_step, run.high + V - j * a.key_step));
+      for (; left > 0; left -= kAheadCut, x += kAheadCut * a.row_step) {
+        uint4 r[kAheadCut];
+#pragma unroll
+        for (int s = 0; s < kAheadCut; ++s) {
+          r[s] = make_uint4(0, 0, 0, 0);
+          if (s < left) r[s] = cut ? load_cut<DT>(x + s * a.row_step, end, run.low, run.high + V) : *(const uint4*)(x + s * a.row_step);
+        }
+#pragma unroll
+        for (int s = 0; s < kAheadCut; ++s) add_vector<DT>(acc, cut ? keep_elements<DT>(r[s], run.low, run.high + V) : r[s]);
+      }
+      // the cut rows: a few before the whole ones and a few after
+      const int before = in0 - any0, cuts = before + any1 - in1;
+#pragma unroll 1
+      for (int j0 = 0; j0 < cuts; j0 += 2) {
+        uint4 r[2];
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const int j = j0 + s < before ? any0 + j0 + s : in1 + j0 + s - before, moved = j * a.key_step;
+          r[s] = make_uint4(0, 0, 0, 0);
+          if (j < any1)
+            r[s] = keep_elements<DT>(load_cut<DT>((const T*)a.x + run.e + j * a.row_step, end, run.low - moved, run.high + V - moved),
+                                     run.low - moved, run.high + V - moved);
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) add_vector<DT>(acc, r[s]);
       }
       float* mine = sums + (V - 1 - run.c) * a.threads + threadIdx.x;  // the distances V lane + i - c + V - 1
 #pragma unroll
@@ -394,21 +431,17 @@ __global__ void __launch_bounds__(kMostThreads, MINB) bias_bwd_kernel(BiasArgs a
       }
     }
     __syncthreads();
-    for (uint32_t k = threadIdx.x; k < count; k += a.threads) {
-      // the distance is number k - V l of thread l for l = k / V and for the one before
-      const uint32_t l = k / V, own = k % V;
-      float v = 0.0f;
-      for (uint32_t w = 0; w < a.rows; ++w) {
-        if (l < a.lanes) v += sums[own * a.threads + w * a.lanes + l];
-        if (l > 0 && own + V < 2 * V - 1) v += sums[(own + V) * a.threads + w * a.lanes + l - 1];
-      }
-      totals[k] = v;
-    }
-    __syncthreads();
     if (warp < a.tables) {
       for (uint32_t k0 = warp * 32; k0 < count; k0 += a.tables * 32) {
         const uint32_t k = k0 + threadIdx.x % 32;
-        table_add(tables + warp * a.n_buckets, k < count ? ids[k] : -1, k < count ? totals[k] : 0.0f);
+        // the distance is number k - V l of thread l for l = k / V and for the one before
+        const uint32_t l = k / V, own = k % V;
+        float v = 0.0f;
+        if (l < a.lanes)
+          for (uint32_t w = 0; w < a.rows; ++w) v += sums[own * a.threads + w * a.lanes + l];
+        if (l > 0 && l <= a.lanes && own + V < 2 * V - 1)
+          for (uint32_t w = 0; w < a.rows; ++w) v += sums[(own + V) * a.threads + w * a.lanes + l - 1];
+        table_add(tables + warp * a.n_buckets, tags + warp * a.n_buckets, k < count ? ids[k] : -1, v);
       }
     }
   }
@@ -463,35 +496,36 @@ void cut(BiasArgs& a, uint64_t most, uint32_t fixed) {
     const uint32_t height = block < a.tq ? block : a.tq;
     const uint64_t blocks = ceil_div(a.tq, height);
     const uint64_t vecs = (a.tk + V - 2) / V + 1 + (height + V - 2) / V;  // that the rows of a block can need, whatever their class
-    for (uint32_t want = kMostThreads; want >= 16; want = want > 256 ? 256 : want / 2) {
-      if (want > 16 && want / 2 >= vecs) continue;
-      const uint64_t chunks = ceil_div(vecs, want);
-      const uint32_t lanes = (uint32_t)ceil_div(vecs, chunks);
-      // threads side by side along the batch; by_batch each has whole periods of samples
-      const uint32_t side = a.by_batch ? a.period : 1, fit = kThreads / lanes > 1 ? kThreads / lanes : 1;
-      const uint32_t most_rows = (a.batch + side - 1) / side, rows = fit < most_rows ? fit : most_rows;
-      const uint32_t share = rows * side, shares = (a.batch + share - 1) / share;  // samples that one row of every thread takes
-      const uint32_t threads = (lanes * rows + 31) / 32 * 32;
-      const uint64_t resident = 148ull * (kThreadsPerSm / threads);
-      const uint64_t per_head = (resident < most ? resident : most) / a.heads > 1 ? (resident < most ? resident : most) / a.heads : 1;
-      uint64_t parts = per_head / (blocks * chunks);
-      parts = parts < 1 ? 1 : (parts < shares ? parts : shares);
-      const uint32_t part = (uint32_t)((shares + parts - 1) / parts) * share;
-      parts = (a.batch + part - 1) / part;
-      const uint64_t items = blocks * chunks * parts;
-      const uint64_t time = ((items + per_head - 1) / per_head) * ((uint64_t)height * (part / rows) + fixed);
-      if (time >= best || items > 0xffffffffull) continue;
-      best = time;
-      a.block = height;
-      a.lanes = lanes;
-      a.rows = rows;
-      a.threads = threads;
-      a.chunks = (uint32_t)chunks;
-      a.part = part;
-      a.parts = (uint32_t)parts;
-      a.items = (uint32_t)items;
-      a.ctas_per_head = (uint32_t)(items < per_head ? items : per_head);
-    }
+    for (uint32_t width : {kMostThreads, kThreads, 160u})
+      for (uint32_t side = 1; side <= 16; side *= 2) {  // threads of a CTA; how many of them side by side along the batch
+        if (side > 1 && width / side * 2 < 16) break;
+        const uint64_t chunks = ceil_div(vecs, width / side);
+        const uint32_t lanes = (uint32_t)ceil_div(vecs, chunks);
+        // along the samples each row of threads has whole periods of them
+        const uint32_t least = a.by_batch ? a.period : 1, fit = width / lanes, most_rows = (a.batch + least - 1) / least;
+        const uint32_t rows = fit < most_rows ? fit : most_rows;
+        const uint32_t share = rows * least, shares = (a.batch + share - 1) / share;  // samples that one row of every thread takes
+        const uint32_t threads = (lanes * rows + 31) / 32 * 32;
+        const uint64_t resident = 148u * (kThreadsPerSm / threads), ctas = resident < most ? resident : most;
+        const uint64_t per_head = ctas > a.heads ? ctas / a.heads : 1;
+        uint64_t parts = per_head / (blocks * chunks);
+        parts = parts < 1 ? 1 : (parts < shares ? parts : shares);
+        const uint32_t part = (uint32_t)((shares + parts - 1) / parts) * share;
+        parts = (a.batch + part - 1) / part;
+        const uint64_t items = blocks * chunks * parts;
+        const uint64_t time = ((items + per_head - 1) / per_head) * ((uint64_t)height * (part / rows) + fixed);
+        if (time >= best || items > 0xffffffffull) continue;
+        best = time;
+        a.block = height;
+        a.lanes = lanes;
+        a.rows = rows;
+        a.threads = threads;
+        a.chunks = (uint32_t)chunks;
+        a.part = part;
+        a.parts = (uint32_t)parts;
+        a.items = (uint32_t)items;
+        a.ctas_per_head = (uint32_t)(items < per_head ? items : per_head);
+      }
     if (height == a.tq) break;
   }
   a.row_step = (int64_t)(a.by_batch ? (uint64_t)a.rows * a.period * a.sample : (uint64_t)a.period * (a.tk + 1));
@@ -519,7 +553,7 @@ uint64_t bwd_most(uint32_t n_buckets) {
 template <int DT>
 cudaError_t launch_bias_fwd(BiasArgs& a, cudaStream_t st) {
   constexpr int V = kVec<DT>;
-  cut<V>(a, ~0ull, FIXF);
+  cut<V>(a, ~0ull, 12);
   return launch_overlapped(bias_fwd_kernel<DT>, dim3(a.ctas_per_head, a.heads), a.threads, spread_slots<V>(a.lanes) * sizeof(float), st, a);
 }
 
@@ -527,14 +561,18 @@ template <int DT>
 cudaError_t launch_bias_bwd(BiasArgs& a, cudaStream_t st) {
   constexpr int V = kVec<DT>;
   static std::atomic<uint64_t> ready = {};
-  cut<V>(a, bwd_most(a.n_buckets), FIXB);
+  cut<V>(a, bwd_most(a.n_buckets), 20);
   const size_t count = slots<V>(a.lanes);
-  a.tables = a.threads / 32;
-  while (a.tables > 1 && (a.tables * a.n_buckets * sizeof(float) > kTableBytes || a.tables * 64 > count)) a.tables /= 2;
-  const size_t smem = ((size_t)a.threads * (2 * V - 1) + count + (size_t)a.tables * a.n_buckets) * sizeof(float) + count * sizeof(int16_t);
-  // the most that any shape takes: 167 KB
-  constexpr size_t most = ((size_t)kMostThreads * (2 * V - 1) + slots<V>(kMostThreads) + kMaxBuckets) * sizeof(float) +
-                          slots<V>(kMostThreads) * sizeof(int16_t);
+  // a table for each warp, unless they take too much shared memory, or a warp has less than two rows of slots to add
+  const uint32_t room = (uint32_t)(kTableBytes / (a.n_buckets * (sizeof(float) + 1))), use = (uint32_t)(count / 64);
+  a.tables = a.threads / 32 < room ? a.threads / 32 : room;
+  a.tables = a.tables < use ? a.tables : use;
+  if (a.tables < 1) a.tables = 1;
+  const size_t smem = ((size_t)a.threads * (2 * V - 1) + (size_t)a.tables * a.n_buckets) * sizeof(float) + count * sizeof(int16_t) +
+                      (size_t)a.tables * a.n_buckets;
+  // the most that any shape takes: 184 KB
+  constexpr size_t most = ((size_t)kMostThreads * (2 * V - 1) + kMaxBuckets) * sizeof(float) +
+                          slots<V>(kMostThreads) * sizeof(int16_t) + kMaxBuckets;
   static_assert(most <= 227 * 1024, "a CTA must fit an SM");
   const cudaError_t e = allow_shared(bias_bwd_kernel<DT>, most, ready);
   return e != cudaSuccess ? e : launch_overlapped(bias_bwd_kernel<DT>, dim3(a.ctas_per_head, a.heads), a.threads, smem, st, a);
