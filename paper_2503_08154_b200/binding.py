@@ -352,16 +352,20 @@ def s2a_relu_bwd(grad_out, mask, grad_in) -> None:
 
 
 # ------------------------------------------------- layer norm, dropout, relative position bias
+_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+_current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
+
+
 def _on_device(first: torch.Tensor, *others) -> None:
     """One device for all tensors of a call, None aside, and that device current: a launch goes to
     the current device, whatever memory its pointers name."""
-    dev = first.device
-    if dev.type != "cuda":
+    dev = first.get_device()
+    if dev < 0:
         raise S2AError("CUDA tensors are needed")
     for t in others:
-        if t is not None and t.device != dev:
+        if t is not None and t.get_device() != dev:
             raise S2AError("all tensors of a call must be on one device")
-    if dev.index != torch.cuda.current_device():
+    if dev != _current_device():
         raise S2AError("the tensors' device must be the current one (torch.cuda.device)")
 
 
@@ -373,9 +377,12 @@ def _rows(t: torch.Tensor, n_rows: int, row_len: int, what: str) -> int:
         raise S2AError("%s must hold %d rows of %d elements" % (what, n_rows, row_len))
     if t.is_contiguous():
         return row_len
-    if t.dim() == 0 or t.shape[-1] != row_len or (row_len > 1 and t.stride(-1) != 1):
+    shape, stride = t.shape, t.stride()
+    if not shape or shape[-1] != row_len or (row_len > 1 and stride[-1] != 1):
         raise S2AError("%s: the elements of a row must be contiguous" % what)
-    dims = [(n, s) for n, s in zip(t.shape[:-1], t.stride()[:-1]) if n != 1]
+    if len(shape) == 2:
+        return stride[0] if n_rows > 1 else row_len
+    dims = [(n, s) for n, s in zip(shape[:-1], stride[:-1]) if n != 1]
     for (_, outer), (n, inner) in zip(dims, dims[1:]):
         if outer != n * inner:
             raise S2AError("%s: its rows must be evenly spaced" % what)
@@ -386,16 +393,25 @@ def _param(t, n: int, what: str):
     """The address of a learned parameter (or of its gradient) of n elements, None for none."""
     if t is None:
         return None
-    if not t.is_contiguous() or t.numel() != n:
+    if t.numel() != n or not t.is_contiguous():
         raise S2AError("%s must be contiguous with %d elements" % (what, n))
     return t.data_ptr()
 
 
+def _code(t: torch.Tensor) -> int:
+    code = _CODES.get(t.dtype)
+    return dtype_code(t) if code is None else code
+
+
 def _param_dtype(*ts) -> int:
-    codes = {dtype_code(t) for t in ts if t is not None}
-    if len(codes) > 1:
-        raise S2AError("learned parameters and their gradients must have one dtype")
-    return codes.pop() if codes else F32
+    found = None
+    for t in ts:
+        if t is not None:
+            code = _code(t)
+            if found is not None and code != found:
+                raise S2AError("learned parameters and their gradients must have one dtype")
+            found = code
+    return F32 if found is None else found
 
 
 def _scratch(t, need: int):
@@ -409,7 +425,7 @@ def _scratch(t, need: int):
 def _stats(t, n_rows: int):
     if t is None:
         return None
-    if t.dtype != torch.float32 or not t.is_contiguous() or t.numel() != 2 * n_rows:
+    if t.dtype is not torch.float32 or t.numel() != 2 * n_rows or not t.is_contiguous():
         raise S2AError("stats must be contiguous float32 with 2 elements a row")
     return t.data_ptr()
 
@@ -429,7 +445,7 @@ def s2a_layernorm_fwd(x, gamma, beta, y, stats, row_len: int, eps: float) -> Non
     n = x.numel() // row_len
     check(lib().s2a_layernorm_fwd(x.data_ptr(), _param(gamma, row_len, "gamma"), _param(beta, row_len, "beta"), y.data_ptr(),
                                   _stats(stats, n), n, row_len, _rows(x, n, row_len, "x"), _rows(y, n, row_len, "y"), eps,
-                                  dtype_code(x), _param_dtype(gamma, beta), _stream_ptr(x)))
+                                  _code(x), _param_dtype(gamma, beta), _stream_ptr(x)))
 
 
 def s2a_layernorm_bwd(grad_out, x, gamma, stats, grad_in, grad_gamma, grad_beta, scratch, row_len: int) -> None:
@@ -449,7 +465,7 @@ def s2a_layernorm_bwd(grad_out, x, gamma, stats, grad_in, grad_gamma, grad_beta,
         _param(grad_gamma, row_len, "grad_gamma"), _param(grad_beta, row_len, "grad_beta"),
         _scratch(scratch, layernorm_scratch_bytes(n, row_len)) if sums else None, n, row_len,
         _rows(grad_out, n, row_len, "grad_out"), _rows(x, n, row_len, "x"), _rows(grad_in, n, row_len, "grad_in"),
-        dtype_code(x), _param_dtype(gamma, grad_gamma, grad_beta), _stream_ptr(x)))
+        _code(x), _param_dtype(gamma, grad_gamma, grad_beta), _stream_ptr(x)))
 
 
 def dropout_threshold(p: float) -> int:
@@ -475,14 +491,14 @@ def s2a_dropout_fwd(x, residual, y, rng, site: int, p: float) -> None:
         if residual.numel() != x.numel() or residual.dtype != x.dtype:
             raise S2AError("residual must match x in size and dtype")
     check(lib().s2a_dropout_fwd(x.data_ptr(), residual.data_ptr() if residual is not None else None, y.data_ptr(), x.numel(),
-                                rng.data_ptr(), site, p, dtype_code(x), _stream_ptr(x)))
+                                rng.data_ptr(), site, p, _code(x), _stream_ptr(x)))
 
 
 def s2a_dropout_bwd(grad_out, grad_in, rng, site: int, p: float) -> None:
     _on_device(grad_out, grad_in, rng)
     site = _dropout_args(grad_out, grad_in, rng, site)
     check(lib().s2a_dropout_bwd(grad_out.data_ptr(), grad_in.data_ptr(), grad_out.numel(), rng.data_ptr(), site, p,
-                                dtype_code(grad_out), _stream_ptr(grad_out)))
+                                _code(grad_out), _stream_ptr(grad_out)))
 
 
 def _bias_args(scores, buckets, table, batch, heads, tq, tk):
@@ -509,7 +525,7 @@ def s2a_relbias_fwd(x, table, buckets, y, batch: int, heads: int, tq: int, tk: i
     if y.numel() != x.numel() or y.dtype != x.dtype:
         raise S2AError("y must match x in size and dtype")
     check(lib().s2a_relbias_fwd(x.data_ptr(), table.data_ptr(), buckets.data_ptr(), by_distance, y.data_ptr(), batch, heads, tq,
-                                tk, table.shape[0], dtype_code(x), dtype_code(table), _stream_ptr(x)))
+                                tk, table.shape[0], _code(x), _code(table), _stream_ptr(x)))
 
 
 def relbias_scratch_bytes(batch: int, heads: int, tq: int, tk: int, n_buckets: int) -> int:
@@ -523,8 +539,8 @@ def s2a_relbias_bwd(grad_out, buckets, grad_table, scratch, batch: int, heads: i
     n = grad_table.shape[0]
     need = relbias_scratch_bytes(batch, heads, tq, tk, n)
     check(lib().s2a_relbias_bwd(grad_out.data_ptr(), buckets.data_ptr(), by_distance, grad_table.data_ptr(),
-                                _scratch(scratch, need) if need else None, batch, heads, tq, tk, n, dtype_code(grad_out),
-                                dtype_code(grad_table), _stream_ptr(grad_out)))
+                                _scratch(scratch, need) if need else None, batch, heads, tq, tk, n, _code(grad_out),
+                                _code(grad_table), _stream_ptr(grad_out)))
 
 
 def log_buckets(first_distance: int, count: int, n_buckets: int, max_distance: int, bidirectional: bool) -> torch.Tensor:
