@@ -37,8 +37,6 @@ struct NormArgs {
   const float* stats_in;
   float* stats_out;      // may be NULL
   float* partials;       // backward with weight gradients: [CTA][2][row_len]
-  const void* x_end;     // one past the last element of x, of g
-  const void* g_end;
   uint64_t n_rows;
   uint64_t x_stride, g_stride, out_stride;
   uint32_t row_len;
@@ -62,26 +60,27 @@ __host__ __device__ constexpr int stage_bytes(int dt, int no, int lanes, int ten
 template <int DT, int LANES>
 __device__ __forceinline__ int piece_column(int j, uint32_t lane, int s) { return (int)((j * LANES + lane) * (uint32_t)kVec<DT>) - s; }
 
-template <int DT, bool EDGE>
-__device__ __forceinline__ bool piece_on(int c, int L) { return EDGE ? (c < L && c + kVec<DT> > 0) : c < L; }
 template <int DT>
 __device__ __forceinline__ bool piece_whole(int c, int L) { return c >= 0 && c + kVec<DT> <= L; }
 
-// Starts the copies of a row's pieces into this thread's column of a stage, [piece][thread] of 16 bytes.  `end`: of the
-// tensor.  A vector that the tensor does not wholly contain (only at the tensor's two ends), and every piece of a
-// tensor that sits on another grid (`apart`), is read element by element.
+// Starts the copies of a row's pieces into this thread's column of a stage, [piece][thread] of 16 bytes.  Elements after the row's end
+// come out as zeros; the elements before its beginning that share its first vector are another row's, and cut_head clears
+// them.  Where the tensor itself begins inside that vector, and in a tensor that sits on another grid (`apart`), pieces are read
+// element by element.
 template <int DT, bool EDGE, int NO, int LANES, int THREADS>
-__device__ __forceinline__ void fetch(uint4* slot, const void* tensor, const void* end, uint64_t row, uint64_t stride,
-                                      uint32_t lane, int L, int s, bool apart) {
+__device__ __forceinline__ void fetch(uint4* slot, const void* tensor, uint64_t row, uint64_t stride, uint32_t lane, int L, int s,
+                                      bool apart) {
   using T = typename Io<DT>::T;
   constexpr int V = kVec<DT>;
   const T* p = (const T*)tensor + row * stride;
 #pragma unroll
   for (int j = 0; j < kPieces<DT, NO>; ++j) {
     const int c = piece_column<DT, LANES>(j, lane, s);
-    if (!piece_on<DT, EDGE>(c, L)) continue;
-    if (!EDGE || (!apart && p + c >= (const T*)tensor && p + c + V <= (const T*)end)) {
+    if (c >= L) continue;
+    if (!EDGE) {
       copy_async<16>(slot + j * THREADS, p + c);
+    } else if (!apart && (j > 0 || p + c >= (const T*)tensor)) {
+      copy_async_front(slot + j * THREADS, p + c, min(L - c, V) * (int)sizeof(T));
     } else {
       float f[V];
 #pragma unroll
@@ -92,6 +91,27 @@ __device__ __forceinline__ void fetch(uint4* slot, const void* tensor, const voi
       slot[j * THREADS] = narrow_piece<DT>(w);
     }
   }
+}
+
+// What a thread's first piece keeps of its 16 bytes: all of it but for the first s elements of a row's first vector.
+template <int DT>
+__device__ __forceinline__ uint4 head_mask(uint32_t lane, int s) {
+  uint32_t m[4] = {~0u, ~0u, ~0u, ~0u};
+  if (lane == 0)
+#pragma unroll
+    for (int i = 0; i < kVec<DT>; ++i)
+      if (i < s) m[DT == kF32 ? i : i / 2] &= DT == kF32 ? 0u : (i % 2 ? 0x0000ffffu : 0xffff0000u);
+  return make_uint4(m[0], m[1], m[2], m[3]);
+}
+template <int DT, bool EDGE>
+__device__ __forceinline__ uint4 cut_head(uint4 r, int j, const uint4& mask) {
+  if (EDGE && j == 0) {
+    r.x &= mask.x;
+    r.y &= mask.y;
+    r.z &= mask.z;
+    r.w &= mask.w;
+  }
+  return r;
 }
 
 // Elements of a piece outside the row become zero.
@@ -191,11 +211,12 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : (NO == 1 
   const float inv_l = 1.0f / (float)L;
   const uint64_t step = (uint64_t)gridDim.x * TEAMS, first = (uint64_t)blockIdx.x * TEAMS + team;
   const int s = row_shift<DT, EDGE>(a, first);
+  const uint4 head = head_mask<DT>(lane, s);
   constexpr int NP = kPieces<DT, NO>, PAIRS = kPairs<DT>;
 #pragma unroll
   for (int k = 0; k < STAGES; ++k) {
     if (first + k * step < a.n_rows)
-      fetch<DT, EDGE, NO, LANES, THREADS>((uint4*)(ring + k * BYTES) + threadIdx.x, a.x, a.x_end, first + k * step, a.x_stride, lane, L, s, false);
+      fetch<DT, EDGE, NO, LANES, THREADS>((uint4*)(ring + k * BYTES) + threadIdx.x, a.x, first + k * step, a.x_stride, lane, L, s, false);
     copy_commit();
   }
   F2 gamma[NP][PAIRS], beta[NP][PAIRS];
@@ -205,7 +226,7 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : (NO == 1 
     const int c = piece_column<DT, LANES>(j, lane, s);
     load_weights<DT>(a.gamma, c, L, a.wdt, 1.0f, gamma[j]);
     load_weights<DT>(a.beta, c, L, a.wdt, 0.0f, beta[j]);
-    if (piece_on<DT, EDGE>(c, L)) count += (float)(min(c + kVec<DT>, L) - max(c, 0));
+    if (c < L) count += (float)(min(c + kVec<DT>, L) - max(c, 0));
   }
   if (WARPS > 1) count = lanes_sum<32>(count);
   const float inv_count = WARPS > 1 ? (count > 0.0f ? 1.0f / count : 0.0f) : inv_l;
@@ -221,9 +242,8 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : (NO == 1 
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
       const int c = piece_column<DT, LANES>(j, lane, s);
-      if (piece_on<DT, EDGE>(c, L)) {
-        widen_piece<DT>(slot[j * THREADS], v[j]);
-        if (EDGE) mask_ends<DT>(v[j], c, L);
+      if (c < L) {
+        widen_piece<DT>(cut_head<DT, EDGE>(slot[j * THREADS], j, head), v[j]);
       } else {
 #pragma unroll
         for (int i = 0; i < PAIRS; ++i) v[j][i] = f2_both(0.0f);
@@ -232,7 +252,7 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : (NO == 1 
       for (int i = 0; i < PAIRS; ++i) sum = f2_add(sum, v[j][i]);
     }
     if (r + STAGES * step < a.n_rows)
-      fetch<DT, EDGE, NO, LANES, THREADS>(slot, a.x, a.x_end, r + STAGES * step, a.x_stride, lane, L, s, false);
+      fetch<DT, EDGE, NO, LANES, THREADS>(slot, a.x, r + STAGES * step, a.x_stride, lane, L, s, false);
     copy_commit();
     stage = stage + 1 == STAGES ? 0 : stage + 1;
     float mean = lanes_sum<GROUP>(f2_sum(sum)) * inv_count;
@@ -240,36 +260,37 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : (NO == 1 
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
       const int c = piece_column<DT, LANES>(j, lane, s);
-      if (!piece_on<DT, EDGE>(c, L)) continue;
-      F2 d[PAIRS];
+      if (c >= L) continue;
 #pragma unroll
-      for (int i = 0; i < PAIRS; ++i) d[i] = f2_sub(v[j][i], f2_both(mean));
-      if (EDGE) mask_ends<DT>(d, c, L);
+      for (int i = 0; i < PAIRS; ++i) v[j][i] = f2_sub(v[j][i], f2_both(mean));
+      if (EDGE) mask_ends<DT>(v[j], c, L);  // elements outside the row have no deviation
 #pragma unroll
-      for (int i = 0; i < PAIRS; ++i) sq = f2_fma(d[i], d[i], sq);
+      for (int i = 0; i < PAIRS; ++i) sq = f2_fma(v[j][i], v[j][i], sq);
     }
-    float dev = lanes_sum<GROUP>(f2_sum(sq));
+    float dev = lanes_sum<GROUP>(f2_sum(sq)), shift = 0.0f;  // v holds x - mean, or x - mean of the warp: `shift` more
     if (WARPS > 1) {
       if (lane % 32 == 0) merge[parity][team][lane / 32] = make_float4(mean, dev, count, 0.0f);
       // the two buffers alternate: a warp writes one of them again only after the next row's barrier, which every
       // warp of the team reaches after it has read this row's values
       team_barrier<LANES>(team);
       const float4 m = merge[parity][team][lane % WARPS];
+      shift = mean;
       mean = lanes_sum<WARPS>(m.z * m.x) * inv_l;
+      shift -= mean;
       dev = lanes_sum<WARPS>(m.y + m.z * (m.x - mean) * (m.x - mean));
       parity ^= 1;
     }
-    const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(dev * inv_l + a.eps));
+    const float rstd = __frsqrt_rn(dev * inv_l + a.eps);
     if (LANES < 32 && r >= a.n_rows) continue;
     if (a.stats_out && lane == 0) ((float2*)a.stats_out)[r] = make_float2(mean, rstd);
     T* out = (T*)a.out + r * a.out_stride;
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
       const int c = piece_column<DT, LANES>(j, lane, s);
-      if (!piece_on<DT, EDGE>(c, L)) continue;
+      if (c >= L) continue;
 #pragma unroll
       for (int i = 0; i < PAIRS; ++i)
-        v[j][i] = f2_fma(f2_mul(f2_sub(v[j][i], f2_both(mean)), f2_both(rstd)), gamma[j][i], beta[j][i]);
+        v[j][i] = f2_fma(f2_mul(WARPS > 1 ? f2_add(v[j][i], f2_both(shift)) : v[j][i], f2_both(rstd)), gamma[j][i], beta[j][i]);
       put_piece<DT, EDGE>(out, c, L, EDGE && a.out_apart, v[j]);
     }
   }
@@ -291,10 +312,11 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : 2) norm_b
   const float inv_l = 1.0f / (float)L;
   const uint64_t step = (uint64_t)gridDim.x * TEAMS, first = (uint64_t)blockIdx.x * TEAMS + team;
   const int s = row_shift<DT, EDGE>(a, first);
+  const uint4 head = head_mask<DT>(lane, s);
   const auto start_row = [&](char* at, uint64_t r) {
     if (r >= a.n_rows) return;
-    fetch<DT, EDGE, NO, LANES, THREADS>((uint4*)at + threadIdx.x, a.x, a.x_end, r, a.x_stride, lane, L, s, false);
-    fetch<DT, EDGE, NO, LANES, THREADS>((uint4*)(at + TENSOR) + threadIdx.x, a.g, a.g_end, r, a.g_stride, lane, L, s, EDGE && a.g_apart);
+    fetch<DT, EDGE, NO, LANES, THREADS>((uint4*)at + threadIdx.x, a.x, r, a.x_stride, lane, L, s, false);
+    fetch<DT, EDGE, NO, LANES, THREADS>((uint4*)(at + TENSOR) + threadIdx.x, a.g, r, a.g_stride, lane, L, s, EDGE && a.g_apart);
     copy_async<8>(at + 2 * TENSOR + threadIdx.x * 8, a.stats_in + 2 * r);
   };
 #pragma unroll
@@ -323,21 +345,17 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : 2) norm_b
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
       const int c = piece_column<DT, LANES>(j, lane, s);
-      if (!on || !piece_on<DT, EDGE>(c, L)) continue;
+      if (!on || c >= L) continue;
       F2 x[PAIRS], g[PAIRS];
-      widen_piece<DT>(sx[j * THREADS], x);
-      widen_piece<DT>(sg[j * THREADS], g);
-      if (EDGE) {
-        mask_ends<DT>(x, c, L);
-        mask_ends<DT>(g, c, L);
-      }
+      widen_piece<DT>(cut_head<DT, EDGE>(sx[j * THREADS], j, head), x);
+      widen_piece<DT>(cut_head<DT, EDGE>(sg[j * THREADS], j, head), g);
 #pragma unroll
       for (int i = 0; i < PAIRS; ++i) {
-        const F2 xhat = f2_mul(f2_sub(x[i], mean2), rstd2), w = f2_mul(g[i], gamma[j][i]);
+        const F2 xc = f2_sub(x[i], mean2), w = f2_mul(g[i], gamma[j][i]);
         s1 = f2_add(s1, w);
-        s2 = f2_fma(w, xhat, s2);
+        s2 = f2_fma(w, xc, s2);
         if (WG) {
-          dgamma[j][i] = f2_fma(g[i], xhat, dgamma[j][i]);
+          dgamma[j][i] = f2_fma(f2_mul(g[i], rstd2), xc, dgamma[j][i]);
           dbeta[j][i] = f2_add(dbeta[j][i], g[i]);
         }
       }
@@ -351,19 +369,19 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : 2) norm_b
       c2 = lanes_sum<WARPS>(m.y);
       parity ^= 1;
     }
-    const F2 m1 = f2_both(c1 * inv_l), m2 = f2_both(-c2 * inv_l);
+    // with w = g gamma and xc = x - mean: grad_in = rstd w - rstd sum w / L - xc rstd^3 sum(w xc) / L
+    const F2 k1 = f2_both(-st.y * (c1 * inv_l)), k2 = f2_both(-(st.y * (c2 * inv_l)) * st.y * st.y);
     T* out = (T*)a.out + r * a.out_stride;
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
       const int c = piece_column<DT, LANES>(j, lane, s);
-      if (!on || !piece_on<DT, EDGE>(c, L)) continue;
+      if (!on || c >= L) continue;
       F2 x[PAIRS], g[PAIRS];
       widen_piece<DT>(sx[j * THREADS], x);
       widen_piece<DT>(sg[j * THREADS], g);
 #pragma unroll
       for (int i = 0; i < PAIRS; ++i) {
-        const F2 xhat = f2_mul(f2_sub(x[i], mean2), rstd2);
-        g[i] = f2_mul(f2_fma(xhat, m2, f2_sub(f2_mul(g[i], gamma[j][i]), m1)), rstd2);
+        g[i] = f2_fma(f2_mul(g[i], gamma[j][i]), rstd2, f2_fma(f2_sub(x[i], mean2), k2, k1));
       }
       put_piece<DT, EDGE>(out, c, L, EDGE && a.out_apart, g);
     }
@@ -396,10 +414,12 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : 2) norm_b
     for (uint32_t k = threadIdx.x; k < 2u * (uint32_t)L; k += THREADS) {
       const uint32_t which = k >= (uint32_t)L, c = which ? k - L : k;
       float t = 0.0f;
-#pragma unroll 4
+      const auto at = [&](uint32_t p) { return flat + (which * kRow + ((p / 4) % QUADS) * NP * LANES + p / kVec<DT>) * 4 + p % 4; };
+      const float* column = at(c);
+#pragma unroll 8
       for (int m = 0; m < TEAMS; ++m) {
-        const uint32_t p = c + (EDGE ? (uint32_t)row_shift<DT, EDGE>(a, (uint64_t)blockIdx.x * TEAMS + m) : 0u);
-        t += flat[((m * 2 + which) * kRow + ((p / 4) % QUADS) * NP * LANES + p / kVec<DT>) * 4 + p % 4];
+        if (EDGE) column = at(c + (uint32_t)row_shift<DT, EDGE>(a, (uint64_t)blockIdx.x * TEAMS + m));
+        t += column[m * 2 * kRow * 4];
       }
       part[k] = t;
     }
@@ -407,7 +427,8 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : 2) norm_b
 }
 
 // Adds the partial rows: [n_part][2][row_len] -> grad_gamma, grad_beta (either may be NULL).  A CTA owns 32 columns
-// of one of the two; its warps take every 32nd partial.
+// of one of the two; its warps take every 32nd partial, all loads of a thread at once.  (CTAs of 128 threads that fit beside
+// the main kernel's, with 8 columns each, take 1.6 us longer on [12608, 768].)
 constexpr int kReduceWarps = 32;
 __global__ void __launch_bounds__(kReduceWarps * 32) norm_reduce_kernel(const float* partials, uint32_t n_part, uint32_t L,
                                                                         void* dgamma, void* dbeta, int wdt) {
@@ -416,8 +437,15 @@ __global__ void __launch_bounds__(kReduceWarps * 32) norm_reduce_kernel(const fl
   const uint32_t which = blockIdx.y, w = threadIdx.x / 32, c = blockIdx.x * 32 + threadIdx.x % 32;
   float acc = 0.0f;
   if (c < L) {
-#pragma unroll 5
-    for (uint32_t p = w; p < n_part; p += kReduceWarps) acc += partials[((uint64_t)p * 2 + which) * L + c];
+    const float* p = partials + (uint64_t)which * L + c;
+    float v[kMaxPartials / kReduceWarps + 1];
+#pragma unroll
+    for (int k = 0; k <= kMaxPartials / kReduceWarps; ++k) {
+      const uint32_t at = w + k * kReduceWarps;
+      v[k] = at < n_part ? p[(uint64_t)at * 2 * L] : 0.0f;
+    }
+#pragma unroll
+    for (int k = 0; k <= kMaxPartials / kReduceWarps; ++k) acc += v[k];
   }
   sums[w][threadIdx.x % 32] = acc;
   __syncthreads();
@@ -460,7 +488,7 @@ __global__ void __launch_bounds__(kLongThreads) norm_fwd_long_kernel(NormArgs a)
       const float d = Io<DT>::widen(x[c]) - mean;
       s += d * d;
     }
-    const float rstd = __fdiv_rn(1.0f, __fsqrt_rn(cta_sum(s, buf) / (float)L + a.eps));
+    const float rstd = __frsqrt_rn(cta_sum(s, buf) / (float)L + a.eps);
     if (a.stats_out && threadIdx.x == 0) ((float2*)a.stats_out)[r] = make_float2(mean, rstd);
     for (uint32_t c = threadIdx.x; c < L; c += kLongThreads) {
       const float gm = a.gamma ? load_param(a.gamma, c, a.wdt) : 1.0f, bt = a.beta ? load_param(a.beta, c, a.wdt) : 0.0f;
@@ -591,8 +619,6 @@ cudaError_t launch_norm_dt(bool fwd, bool wg, NormArgs a, uint32_t& parts, cudaS
   };
   a.g_apart = apart(a.g, a.g_stride);
   a.out_apart = apart(a.out, a.out_stride);
-  a.x_end = (const T*)a.x + (a.n_rows - 1) * a.x_stride + a.row_len;
-  a.g_end = a.g ? (const T*)a.g + (a.n_rows - 1) * a.g_stride + a.row_len : nullptr;
   const bool shifted = ((uintptr_t)a.x / sizeof(T)) % V != 0 || (a.n_rows > 1 && a.x_stride % V != 0);
   const bool edge = shifted || a.row_len % V != 0 || a.g_apart || a.out_apart;
   const uint32_t elems = (uint32_t)(a.row_len + (shifted ? V - 1 : 0));  // with what lies before the row in its first vector
