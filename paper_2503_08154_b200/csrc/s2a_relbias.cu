@@ -22,7 +22,7 @@
 namespace s2a {
 namespace {
 
-constexpr int kAheadFwd = 4, kAheadBwd = 4, kAheadCut = 4;  // rows of a run whose loads a thread has in flight
+constexpr int kAheadFwd = 4, kAheadBwd = 4;  // rows of a run whose loads a thread has in flight
 constexpr uint32_t kThreads = 256, kMostThreads = 320;
 constexpr uint32_t kThreadsPerSm = 1024;     // at 64 registers a thread
 constexpr int kStaged = 5;                   // slots that a thread looks up at a time
@@ -265,12 +265,16 @@ __global__ void __launch_bounds__(kMostThreads, 3) bias_fwd_kernel(BiasArgs a) {
 #pragma unroll
       for (int i = 0; i < V / 2; ++i) bias[i] = f2_pack(bias_of[spread<V>(k + 2 * i)], bias_of[spread<V>(k + 2 * i + 1)]);
       const T *x = (const T*)a.x + run.e + in0 * a.row_step, *end = (const T*)a.x + a.batch * a.sample;
+      // A cut vector is read whole, as its other elements are a neighbouring row's; only the tensor's last may not lie in it.
+      int left = in1 - in0;
+      const bool beyond = cut && x + (left - 1) * a.row_step + V > end;
+      if (beyond) --left;
 #pragma unroll 1
-      for (int left = in1 - in0; left > 0; left -= kAheadFwd, x += kAheadFwd * a.row_step) {
+      for (; left > 0; left -= kAheadFwd, x += kAheadFwd * a.row_step) {
         uint4 r[kAheadFwd];
 #pragma unroll
         for (int s = 0; s < kAheadFwd; ++s)
-          if (s < left) r[s] = cut ? load_cut<DT>(x + s * a.row_step, end, run.low, run.high + V) : *(const uint4*)(x + s * a.row_step);
+          if (s < left) r[s] = *(const uint4*)(x + s * a.row_step);
 #pragma unroll
         for (int s = 0; s < kAheadFwd; ++s) {
           if (s >= left) break;
@@ -279,6 +283,10 @@ __global__ void __launch_bounds__(kMostThreads, 3) bias_fwd_kernel(BiasArgs a) {
           if (cut) store_ends<DT>(y, w, run.low, run.high + V);
           else *(uint4*)y = w;
         }
+      }
+      if (beyond) {
+        const T* last = (const T*)a.x + run.e + (in1 - 1) * a.row_step;
+        store_ends<DT>((T*)(last + to_y), add_bias<DT>(load_ends<DT>(last, run.low, run.high + V), bias), run.low, run.high + V);
       }
       // the cut rows: a few before the whole ones and a few after
       const int before = in0 - any0, cuts = before + any1 - in1;
@@ -349,29 +357,28 @@ template <int DT>
 __global__ void __launch_bounds__(kMostThreads, 3) bias_bwd_kernel(BiasArgs a) {
   using T = typename Io<DT>::T;
   constexpr int V = kVec<DT>;
-  // [2 V - 1][thread]: a thread's sums of the distances V lane + 0 .. 2 V - 2 that its vector has in one class or another.
+  // [2 V - 1][stride]: a thread's sums of the distances V lane + 0 .. 2 V - 2 that its vector has in one class or another.
   // [tables][n_buckets]; [slots] the buckets; [tables][n_buckets] the tables' tags.
   extern __shared__ float sums[];
   enter_grid();
   const uint32_t row = threadIdx.x / a.lanes, lane = threadIdx.x - row * a.lanes, warp = threadIdx.x / 32, h = blockIdx.y;
   const uint32_t count = slots<V>(a.lanes);
-  float* tables = sums + (2 * V - 1) * a.threads;
-  int16_t* ids = (int16_t*)(tables + a.tables * a.n_buckets);
+  const uint32_t stride = a.threads + 32 / V;  // so that the sums of 32 neighbouring distances lie in 32 banks
+  float* tables = sums + (2 * V - 1) * stride;
+  int32_t* ids = (int32_t*)(tables + a.tables * a.n_buckets);
   uint8_t* tags = (uint8_t*)(ids + count);
   for (uint32_t i = threadIdx.x; i < a.tables * a.n_buckets; i += a.threads) tables[i] = 0.0f;
   for (uint32_t index = blockIdx.x; index < a.items; index += gridDim.x) {
     const Item t = item_of<V>(a, h, index, lane);
     if (index != blockIdx.x) __syncthreads();  // the previous item's sums have been read
 #pragma unroll
-    for (int k = 0; k < 2 * V - 1; ++k) sums[k * a.threads + threadIdx.x] = 0.0f;
-    for (uint32_t k = threadIdx.x; k < count; k += kStaged * a.threads) {  // buckets are below kMaxBuckets = 2^15
-      int u[kStaged];
-#pragma unroll
-      for (int i = 0; i < kStaged; ++i) u[i] = bucket_of(a, t, k + i * a.threads < count ? (int)(k + i * a.threads) : -1);
-#pragma unroll
-      for (int i = 0; i < kStaged; ++i)
-        if (k + i * a.threads < count) ids[k + i * a.threads] = (int16_t)u[i];
+    for (int k = 0; k < 2 * V - 1; ++k) sums[k * stride + threadIdx.x] = 0.0f;
+    // the buckets come while the rows do
+    for (uint32_t k = threadIdx.x; k < count; k += a.threads) {
+      if ((int)k >= t.low && (int)k < t.high) copy_async<4>(ids + k, t.lut + k);
+      else ids[k] = -1;
     }
+    copy_commit();
     Runs<V> run;
 #pragma unroll 1
     for (run.start(a, t, row); !run.done(a); run.next(a, t, row)) {
@@ -383,28 +390,27 @@ __global__ void __launch_bounds__(kMostThreads, 3) bias_bwd_kernel(BiasArgs a) {
 #pragma unroll
       for (int i = 0; i < V / 2; ++i) acc[i] = f2_both(0.0f);
       const T *x = (const T*)a.x + run.e + in0 * a.row_step, *end = (const T*)a.x + a.batch * a.sample;
+      // A cut vector is added whole, and the sums of the elements outside the row dropped at the end; only the tensor's last
+      // vector may not lie in it.
       int left = in1 - in0;
-      if (!cut) {
+      const bool beyond = cut && x + (left - 1) * a.row_step + V > end;
+      if (beyond) --left;
 #pragma unroll 1
-        for (; left >= kAheadBwd; left -= kAheadBwd, x += kAheadBwd * a.row_step) {
-          uint4 r[kAheadBwd];
+      for (; left >= kAheadBwd; left -= kAheadBwd, x += kAheadBwd * a.row_step) {
+        uint4 r[kAheadBwd];
 #pragma unroll
-          for (int s = 0; s < kAheadBwd; ++s) r[s] = *(const uint4*)(x + s * a.row_step);
+        for (int s = 0; s < kAheadBwd; ++s) r[s] = *(const uint4*)(x + s * a.row_step);
 #pragma unroll
-          for (int s = 0; s < kAheadBwd; ++s) add_vector<DT>(acc, r[s]);
-        }
+        for (int s = 0; s < kAheadBwd; ++s) add_vector<DT>(acc, r[s]);
       }
-#pragma unroll 1
-      for (; left > 0; left -= kAheadCut, x += kAheadCut * a.row_step) {
-        uint4 r[kAheadCut];
+      if (left > 0) {
+        uint4 r[kAheadBwd - 1];
 #pragma unroll
-        for (int s = 0; s < kAheadCut; ++s) {
-          r[s] = make_uint4(0, 0, 0, 0);
-          if (s < left) r[s] = cut ? load_cut<DT>(x + s * a.row_step, end, run.low, run.high + V) : *(const uint4*)(x + s * a.row_step);
-        }
+        for (int s = 0; s < kAheadBwd - 1; ++s) r[s] = s < left ? *(const uint4*)(x + s * a.row_step) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (int s = 0; s < kAheadCut; ++s) add_vector<DT>(acc, cut ? keep_elements<DT>(r[s], run.low, run.high + V) : r[s]);
+        for (int s = 0; s < kAheadBwd - 1; ++s) add_vector<DT>(acc, r[s]);
       }
+      if (beyond) add_vector<DT>(acc, load_ends<DT>((const T*)a.x + run.e + (in1 - 1) * a.row_step, run.low, run.high + V));
       // the cut rows: a few before the whole ones and a few after
       const int before = in0 - any0, cuts = before + any1 - in1;
 #pragma unroll 1
@@ -421,15 +427,16 @@ __global__ void __launch_bounds__(kMostThreads, 3) bias_bwd_kernel(BiasArgs a) {
 #pragma unroll
         for (int s = 0; s < 2; ++s) add_vector<DT>(acc, r[s]);
       }
-      float* mine = sums + (V - 1 - run.c) * a.threads + threadIdx.x;  // the distances V lane + i - c + V - 1
+      float* mine = sums + (V - 1 - run.c) * stride + threadIdx.x;  // the distances V lane + i - c + V - 1
 #pragma unroll
-      for (int i = 0; i < V / 2; ++i) {
+      for (int i = 0; i < V; ++i) {
         float lo, hi;
-        f2_unpack(acc[i], lo, hi);
-        mine[(2 * i) * a.threads] += lo;
-        mine[(2 * i + 1) * a.threads] += hi;
+        f2_unpack(acc[i / 2], lo, hi);
+        const float v = i % 2 ? hi : lo;
+        mine[i * stride] += !cut || (i >= run.low && i < run.high + V) ? v : 0.0f;
       }
     }
+    copy_wait<0>();
     __syncthreads();
     if (warp < a.tables) {
       for (uint32_t k0 = warp * 32; k0 < count; k0 += a.tables * 32) {
@@ -438,10 +445,11 @@ __global__ void __launch_bounds__(kMostThreads, 3) bias_bwd_kernel(BiasArgs a) {
         const uint32_t l = k / V, own = k % V;
         float v = 0.0f;
         if (l < a.lanes)
-          for (uint32_t w = 0; w < a.rows; ++w) v += sums[own * a.threads + w * a.lanes + l];
+          for (uint32_t w = 0; w < a.rows; ++w) v += sums[own * stride + w * a.lanes + l];
         if (l > 0 && l <= a.lanes && own + V < 2 * V - 1)
-          for (uint32_t w = 0; w < a.rows; ++w) v += sums[(own + V) * a.threads + w * a.lanes + l - 1];
-        table_add(tables + warp * a.n_buckets, tags + warp * a.n_buckets, k < count ? ids[k] : -1, v);
+          for (uint32_t w = 0; w < a.rows; ++w) v += sums[(own + V) * stride + w * a.lanes + l - 1];
+        const int u = k < count ? ids[k] : -1;
+        table_add(tables + warp * a.n_buckets, tags + warp * a.n_buckets, (uint32_t)u < a.n_buckets ? u : -1, v);
       }
     }
   }
@@ -568,11 +576,11 @@ cudaError_t launch_bias_bwd(BiasArgs& a, cudaStream_t st) {
   a.tables = a.threads / 32 < room ? a.threads / 32 : room;
   a.tables = a.tables < use ? a.tables : use;
   if (a.tables < 1) a.tables = 1;
-  const size_t smem = ((size_t)a.threads * (2 * V - 1) + (size_t)a.tables * a.n_buckets) * sizeof(float) + count * sizeof(int16_t) +
+  const size_t smem = ((size_t)(a.threads + 32 / V) * (2 * V - 1) + (size_t)a.tables * a.n_buckets) * sizeof(float) + count * sizeof(int32_t) +
                       (size_t)a.tables * a.n_buckets;
-  // the most that any shape takes: 184 KB
-  constexpr size_t most = ((size_t)kMostThreads * (2 * V - 1) + kMaxBuckets) * sizeof(float) +
-                          slots<V>(kMostThreads) * sizeof(int16_t) + kMaxBuckets;
+  // the most that any shape takes: 189 KB
+  constexpr size_t most = ((size_t)(kMostThreads + 32 / V) * (2 * V - 1) + kMaxBuckets) * sizeof(float) +
+                          slots<V>(kMostThreads) * sizeof(int32_t) + kMaxBuckets;
   static_assert(most <= 227 * 1024, "a CTA must fit an SM");
   const cudaError_t e = allow_shared(bias_bwd_kernel<DT>, most, ready);
   return e != cudaSuccess ? e : launch_overlapped(bias_bwd_kernel<DT>, dim3(a.ctas_per_head, a.heads), a.threads, smem, st, a);
