@@ -22,9 +22,10 @@
 namespace s2a {
 namespace {
 
-constexpr int kAheadFwd = 4, kAheadBwd = 4;  // rows of a run whose loads a thread has in flight
+constexpr int kAheadFwd = 4, kAheadBwd = 6;  // rows of a run whose loads a thread has in flight
 constexpr uint32_t kThreads = 256, kMostThreads = 320;
 constexpr uint32_t kThreadsPerSm = 1024;     // at 64 registers a thread
+constexpr int kAnnounced = 8;                // rows of an item's first run that are asked for before its shared memory is set up
 constexpr int kStaged = 5;                   // slots that a thread looks up at a time
 constexpr uint32_t kTableBytes = 64 * 1024;  // shared memory for the tables of a backward CTA, beyond the first table
 
@@ -154,6 +155,15 @@ struct Runs {
         return;
       }
     }
+  }
+
+  // Asks for the run's first rows in L2, ahead of the loop that loads them.
+  template <typename T>
+  __device__ __forceinline__ void announce(const BiasArgs& a, const T* x) const {
+    if (done(a)) return;
+#pragma unroll 1
+    for (int j = 0; j < kAnnounced && j < n; ++j)
+      if (j * a.key_step >= low && j * a.key_step <= high) asm volatile("prefetch.global.L2 [%0];" ::"l"(x + e + j * a.row_step));
   }
 
   // The rows of the run that the vector meets.  Along the samples (key_step 0) all of them, in one way: j = 0 .. in1 - 1, all
@@ -359,7 +369,7 @@ __global__ void __launch_bounds__(kMostThreads, 3) bias_bwd_kernel(BiasArgs a) {
   constexpr int V = kVec<DT>;
   // [2 V - 1][stride]: a thread's sums of the distances V lane + 0 .. 2 V - 2 that its vector has in one class or another.
   // [tables][n_buckets]; [slots] the buckets; [tables][n_buckets] the tables' tags.
-  extern __shared__ float sums[];
+  extern __shared__ __align__(16) float sums[];
   enter_grid();
   const uint32_t row = threadIdx.x / a.lanes, lane = threadIdx.x - row * a.lanes, warp = threadIdx.x / 32, h = blockIdx.y;
   const uint32_t count = slots<V>(a.lanes);
@@ -367,21 +377,25 @@ __global__ void __launch_bounds__(kMostThreads, 3) bias_bwd_kernel(BiasArgs a) {
   float* tables = sums + (2 * V - 1) * stride;
   int32_t* ids = (int32_t*)(tables + a.tables * a.n_buckets);
   uint8_t* tags = (uint8_t*)(ids + count);
-  for (uint32_t i = threadIdx.x; i < a.tables * a.n_buckets; i += a.threads) tables[i] = 0.0f;
   for (uint32_t index = blockIdx.x; index < a.items; index += gridDim.x) {
     const Item t = item_of<V>(a, h, index, lane);
-    if (index != blockIdx.x) __syncthreads();  // the previous item's sums have been read
-#pragma unroll
-    for (int k = 0; k < 2 * V - 1; ++k) sums[k * stride + threadIdx.x] = 0.0f;
+    Runs<V> run;
+    run.start(a, t, row);
+    run.announce(a, (const T*)a.x);
+    const bool first = index == blockIdx.x;
+    if (!first) __syncthreads();  // the previous item's sums have been read
+    const uint32_t zeros = (2 * V - 1) * stride + (first ? a.tables * a.n_buckets : 0);  // the tables once, the sums each time
+    for (uint32_t i = threadIdx.x; i < zeros / 4; i += a.threads) ((float4*)sums)[i] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (threadIdx.x < zeros % 4) sums[zeros / 4 * 4 + threadIdx.x] = 0.0f;
     // the buckets come while the rows do
     for (uint32_t k = threadIdx.x; k < count; k += a.threads) {
       if ((int)k >= t.low && (int)k < t.high) copy_async<4>(ids + k, t.lut + k);
       else ids[k] = -1;
     }
     copy_commit();
-    Runs<V> run;
+    __syncthreads();
 #pragma unroll 1
-    for (run.start(a, t, row); !run.done(a); run.next(a, t, row)) {
+    for (; !run.done(a); run.next(a, t, row)) {
       int any0, any1, in0, in1;
       bool cut;
       run.meets(a, any0, any1, in0, in1, cut);
@@ -439,15 +453,18 @@ __global__ void __launch_bounds__(kMostThreads, 3) bias_bwd_kernel(BiasArgs a) {
     copy_wait<0>();
     __syncthreads();
     if (warp < a.tables) {
+      // the distance of slot k is number k - V l of thread l for l = k / V, and of the one before; 32 / V lanes each l
+      const uint32_t own = threadIdx.x % V, before = own + V < 2 * V - 1;
       for (uint32_t k0 = warp * 32; k0 < count; k0 += a.tables * 32) {
-        const uint32_t k = k0 + threadIdx.x % 32;
-        // the distance is number k - V l of thread l for l = k / V and for the one before
-        const uint32_t l = k / V, own = k % V;
-        float v = 0.0f;
-        if (l < a.lanes)
-          for (uint32_t w = 0; w < a.rows; ++w) v += sums[own * stride + w * a.lanes + l];
-        if (l > 0 && l <= a.lanes && own + V < 2 * V - 1)
-          for (uint32_t w = 0; w < a.rows; ++w) v += sums[(own + V) * stride + w * a.lanes + l - 1];
+        const uint32_t k = k0 + threadIdx.x % 32, l = k / V;
+        const float* at = sums + own * stride + l;
+        float v = l < a.lanes ? at[0] : 0.0f;
+        const bool other = l > 0 && l <= a.lanes && before;
+        if (other) v += at[V * stride - 1];
+        for (uint32_t w = 1; w < a.rows; ++w) {
+          if (l < a.lanes) v += at[w * a.lanes];
+          if (other) v += at[V * stride - 1 + w * a.lanes];
+        }
         const int u = k < count ? ids[k] : -1;
         table_add(tables + warp * a.n_buckets, tags + warp * a.n_buckets, (uint32_t)u < a.n_buckets ? u : -1, v);
       }
