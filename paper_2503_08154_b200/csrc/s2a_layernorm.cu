@@ -170,6 +170,49 @@ __device__ __forceinline__ void load_weights(const void* p, int c, int L, int wd
   for (int i = 0; i < V / 2; ++i) v[i] = f2_pack(f[2 * i], f[2 * i + 1]);
 }
 
+// Where several teams share a CTA, its weights come through shared memory, each loaded once for all teams.  The loads are
+// sent out before the rows' copies: behind those they take as long as the whole first filling of the ring (5.4 us instead
+// of about 1 on [12608, 768]).
+template <int LANES> constexpr bool kStaged = LANES <= 64;
+template <int NO, int LANES> constexpr int kStagedFloats = kStaged<LANES> ? NO * 8 * LANES : 0;
+template <int NO, int LANES>
+struct Staged {
+  static constexpr int kEach = NO * 8 * LANES / threads_of(LANES) > 0 ? NO * 8 * LANES / threads_of(LANES) : 1;
+  float v[kEach];
+  __device__ __forceinline__ void load(const void* p, int L, int wdt, float fill) {
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int c = k * threads_of(LANES) + (int)threadIdx.x;
+      v[k] = p && c < L ? load_param(p, (uint64_t)c, wdt) : fill;
+    }
+  }
+  __device__ __forceinline__ void put(float* row, int L) const {
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int c = k * threads_of(LANES) + (int)threadIdx.x;
+      if (c < L) row[c] = v[k];
+    }
+  }
+};
+// A piece of a staged row.
+template <int DT, bool EDGE>
+__device__ __forceinline__ void take_piece(const float* row, int c, int L, F2* v) {
+  if (!EDGE) {
+#pragma unroll
+    for (int i = 0; i < kVec<DT> / 4; ++i) {
+      const float4 w = c < L ? ((const float4*)(row + c))[i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      v[2 * i] = f2_pack(w.x, w.y);
+      v[2 * i + 1] = f2_pack(w.z, w.w);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kPairs<DT>; ++i) {
+      const int k = c + 2 * i;
+      v[i] = f2_pack(k >= 0 && k < L ? row[k] : 0.0f, k + 1 >= 0 && k + 1 < L ? row[k + 1] : 0.0f);
+    }
+  }
+}
+
 __device__ __forceinline__ float f2_sum(F2 a) {
   float lo, hi;
   f2_unpack(a, lo, hi);
@@ -213,19 +256,35 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : (NO == 1 
   const int s = row_shift<DT, EDGE>(a, first);
   const uint4 head = head_mask<DT>(lane, s);
   constexpr int NP = kPieces<DT, NO>, PAIRS = kPairs<DT>;
+  Staged<NO, LANES> sg, sb;
+  if (kStaged<LANES>) {
+    sg.load(a.gamma, L, a.wdt, 1.0f);
+    sb.load(a.beta, L, a.wdt, 0.0f);
+  }
 #pragma unroll
   for (int k = 0; k < STAGES; ++k) {
     if (first + k * step < a.n_rows)
       fetch<DT, EDGE, NO, LANES, THREADS>((uint4*)(ring + k * BYTES) + threadIdx.x, a.x, first + k * step, a.x_stride, lane, L, s, false);
     copy_commit();
   }
+  float *gamma_row = (float*)(ring + STAGES * BYTES), *beta_row = gamma_row + kStagedFloats<NO, LANES>;
+  if (kStaged<LANES>) {
+    sg.put(gamma_row, L);
+    sb.put(beta_row, L);
+    __syncthreads();
+  }
   F2 gamma[NP][PAIRS], beta[NP][PAIRS];
   float count = 0.0f;  // elements of the row that this warp holds
 #pragma unroll
   for (int j = 0; j < NP; ++j) {
     const int c = piece_column<DT, LANES>(j, lane, s);
-    load_weights<DT>(a.gamma, c, L, a.wdt, 1.0f, gamma[j]);
-    load_weights<DT>(a.beta, c, L, a.wdt, 0.0f, beta[j]);
+    if (kStaged<LANES>) {
+      take_piece<DT, EDGE>(gamma_row, c, L, gamma[j]);
+      take_piece<DT, EDGE>(beta_row, c, L, beta[j]);
+    } else {
+      load_weights<DT>(a.gamma, c, L, a.wdt, 1.0f, gamma[j]);
+      load_weights<DT>(a.beta, c, L, a.wdt, 0.0f, beta[j]);
+    }
     if (c < L) count += (float)(min(c + kVec<DT>, L) - max(c, 0));
   }
   if (WARPS > 1) count = lanes_sum<32>(count);
@@ -319,15 +378,24 @@ __global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : 2) norm_b
     fetch<DT, EDGE, NO, LANES, THREADS>((uint4*)(at + TENSOR) + threadIdx.x, a.g, r, a.g_stride, lane, L, s, EDGE && a.g_apart);
     copy_async<8>(at + 2 * TENSOR + threadIdx.x * 8, a.stats_in + 2 * r);
   };
+  Staged<NO, LANES> staged;
+  if (kStaged<LANES>) staged.load(a.gamma, L, a.wdt, 1.0f);
 #pragma unroll
   for (int k = 0; k < STAGES; ++k) {
     start_row(ring + k * BYTES, first + k * step);
     copy_commit();
   }
+  float* gamma_row = (float*)(ring + STAGES * BYTES);
+  if (kStaged<LANES>) {
+    staged.put(gamma_row, L);
+    __syncthreads();
+  }
   F2 gamma[NP][PAIRS], dgamma[NP][PAIRS], dbeta[NP][PAIRS];
 #pragma unroll
   for (int j = 0; j < NP; ++j) {
-    load_weights<DT>(a.gamma, piece_column<DT, LANES>(j, lane, s), L, a.wdt, 1.0f, gamma[j]);
+    const int c = piece_column<DT, LANES>(j, lane, s);
+    if (kStaged<LANES>) take_piece<DT, EDGE>(gamma_row, c, L, gamma[j]);
+    else load_weights<DT>(a.gamma, c, L, a.wdt, 1.0f, gamma[j]);
 #pragma unroll
     for (int i = 0; i < PAIRS; ++i) dgamma[j][i] = dbeta[j][i] = f2_both(0.0f);
   }
@@ -560,7 +628,8 @@ cudaError_t launch_norm(bool fwd, bool wg, const NormArgs& a, uint32_t& parts, c
   static std::atomic<uint64_t> ready[3] = {};
   constexpr int THREADS = threads_of(LANES), TEAMS = THREADS / LANES;
   constexpr int B1 = stage_bytes(DT, NO, LANES, 1), B2 = stage_bytes(DT, NO, LANES, 2);
-  constexpr size_t ring_fwd = (size_t)B1 * stages_of(B1), ring_bwd = (size_t)B2 * stages_of(B2);
+  constexpr size_t weights = kStagedFloats<NO, LANES> * sizeof(float);  // a row of them
+  constexpr size_t ring_fwd = (size_t)B1 * stages_of(B1) + 2 * weights, ring_bwd = (size_t)B2 * stages_of(B2) + weights;
   constexpr size_t sums = (size_t)THREADS * NO * 64;  // the teams' column sums take the ring's place
   constexpr size_t smem_wg = ring_bwd > sums ? ring_bwd : sums;
   const uint64_t want = (a.n_rows + TEAMS - 1) / TEAMS;
