@@ -20,6 +20,12 @@
 // The weights' gradients are sums over rows: a thread keeps the sums of its own columns in registers over all the rows
 // of its team, a CTA adds its teams' sums in order and writes one pair of rows to the caller's scratch, and a second kernel
 // adds those in order: no atomics, the same bits on every run.
+//
+// What it measures on a B200 (6.57 TB/s copy rate): [12608, 768] bfloat16 forward 8.1 us (4.8 TB/s), backward with weights
+// 14.8 us (3.9 TB/s), without 11.0 us (5.3 TB/s); of these about 2 us are the launch, 1.4 us the first rows' way from memory,
+// and 3 us the second kernel of the weights' gradients.  [65536, 4096] backward 262 us (6.1 TB/s).  Loads of a whole row into
+// registers instead of the ring: 17.3 and 49.8 us.  Odd row lengths cost instructions, not bytes: [4616, 1025] binary32 backward
+// 17.2 us (3.3 TB/s), [20000, 1025] bfloat16 forward 32 us (2.5 TB/s), bound by issue at 16 warps an SM.
 #include "s2a_launch.h"
 #include "s2a_oct.cuh"
 
@@ -654,7 +660,8 @@ cudaError_t launch_norm(bool fwd, bool wg, const NormArgs& a, uint32_t& parts, c
   return e != cudaSuccess ? e : launch_overlapped(norm_bwd_kernel<DT, EDGE, NO, LANES, true>, dim3(grid), THREADS, smem_wg, st, a);
 }
 
-// The smallest team that holds the row: one piece a lane up to a warp, two or three beyond.
+// The smallest team that holds the row: eight elements a lane up to 256, sixteen or twenty-four beyond.  (At 768 elements, one
+// warp with 24 a lane against two with 16: 8.1 and 9 us forward, as two warps meet at a barrier in every row.)
 template <int DT, bool EDGE>
 cudaError_t launch_norm_shape(bool fwd, bool wg, const NormArgs& a, uint32_t elems, uint32_t& parts, cudaStream_t st) {
 #define S2A_NORM(NO, LANES) \

@@ -14,6 +14,14 @@
 // taken one after the other.
 //
 // Work is cut into items: a head, a block of query rows, a chunk of vectors (`lanes` of them) and a part of the batch.
+//
+// What it measures on a B200 (6.57 TB/s copy rate), bfloat16: [64, 12, 197, 197] under a map of 732 buckets, forward 25.8 us (4.6 TB/s:
+// 18 us of walking, which is the copy rate, after 3 us in which the chunk's biases are looked up, and the launch), backward
+// 23.1 us (2.6 TB/s: 12.7 of walking, 2.3 before and 5 after it for the tables, 2.5 for the second kernel); by distance
+// 28 us; [2, 16, 2048, 2048] by distance, forward 107 us (5.0 TB/s), backward 58 us (4.6 TB/s).  Looking the bucket of
+// every element up where it is added costs 200 us there.  Measured and not kept: the rows through a ring of cp.async as in
+// layer norm (92 us: the bookkeeping of a row's place outweighs the add), eight rows ahead in forward (spills, 33 us), rows
+// asked for in L2 before the forward kernel's look-up (26.5 us).
 #include <math.h>
 
 #include "s2a_launch.h"
