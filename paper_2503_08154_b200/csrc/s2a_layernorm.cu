@@ -23,9 +23,9 @@
 //
 // What it measures on a B200 (6.57 TB/s copy rate): [12608, 768] bfloat16 forward 8.1 us (4.8 TB/s), backward with weights
 // 14.8 us (3.9 TB/s), without 11.0 us (5.3 TB/s); of these about 2 us are the launch, 1.4 us the first rows' way from memory,
-// and 3 us the second kernel of the weights' gradients.  [65536, 4096] backward 262 us (6.1 TB/s).  Loads of a whole row into
-// registers instead of the ring: 17.3 and 49.8 us.  Odd row lengths cost instructions, not bytes: [4616, 1025] binary32 backward
-// 17.2 us (3.3 TB/s), [20000, 1025] bfloat16 forward 32 us (2.5 TB/s), bound by issue at 16 warps an SM.
+// and 3 us the second kernel of the weights' gradients.  [65536, 4096] backward 262 us (6.1 TB/s).  The first kernels,
+// with rows loaded into registers one at a time, took 17.3 and 49.8 us.  Odd row lengths cost instructions, not bytes: [4616, 1025] binary32 backward
+// 17.2 us (3.3 TB/s), [20000, 1025] bfloat16 forward 32 us (2.5 TB/s), 54 % of the issue slots at 16 warps an SM.
 #include "s2a_launch.h"
 #include "s2a_oct.cuh"
 
@@ -54,6 +54,12 @@ struct NormArgs {
 template <int DT, int NO> constexpr int kPieces = NO * 8 / kVec<DT>;  // pieces of a thread: NO * 8 elements
 
 __host__ __device__ constexpr int threads_of(int lanes) { return lanes > 256 ? lanes : 256; }
+// CTAs of the forward kernel on an SM.  Three of them hide the meeting of a row's warps better where their registers (80 a
+// thread) suffice without spills: [65536, 4096] bfloat16 193 us against 199 with two and 242 with four; in binary32, with half
+// the elements to a byte, two are ahead ([12608, 2048] 38.4 us against 39.7).
+__host__ __device__ constexpr int fwd_ctas(int dt, bool edge, int no, int lanes) {
+  return lanes > 256 ? 1 : (no == 1 ? 4 : (no == 2 && dt == kBF16 && !edge ? 3 : 2));
+}
 // Rows in flight per team: what keeps two CTAs of an SM (one of 512 threads) within its shared memory.
 __host__ __device__ constexpr int stages_of(int stage_bytes) {
   return stage_bytes <= 24 * 1024 ? 4 : (stage_bytes <= 32 * 1024 ? 3 : (stage_bytes <= 100 * 1024 ? 2 : 1));
@@ -176,6 +182,8 @@ __device__ __forceinline__ void load_weights(const void* p, int c, int L, int wd
   for (int i = 0; i < V / 2; ++i) v[i] = f2_pack(f[2 * i], f[2 * i + 1]);
 }
 
+// A thread holds the weights of its columns in registers for all its rows (read from shared memory in every row instead, they cost
+// more than the occupancy gives: 10.5 us at four CTAs an SM against 8.1 on [12608, 768]).
 // Where several teams share a CTA, its weights come through shared memory, each loaded once for all teams.  The loads are
 // sent out before the rows' copies: behind those they take as long as the whole first filling of the ring (5.4 us instead
 // of about 1 on [12608, 768]).
@@ -247,7 +255,7 @@ __device__ __forceinline__ int row_shift(const NormArgs& a, uint64_t row) {
 
 // ---------------------------------------------------------------- forward
 template <int DT, bool EDGE, int NO, int LANES>
-__global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : (NO == 1 ? 4 : 2)) norm_fwd_kernel(NormArgs a) {
+__global__ void __launch_bounds__(threads_of(LANES), fwd_ctas(DT, EDGE, NO, LANES)) norm_fwd_kernel(NormArgs a) {
   using T = typename Io<DT>::T;
   constexpr int THREADS = threads_of(LANES), TEAMS = THREADS / LANES, WARPS = LANES / 32 > 1 ? LANES / 32 : 1;
   constexpr int GROUP = LANES < 32 ? LANES : 32;
@@ -639,7 +647,7 @@ cudaError_t launch_norm(bool fwd, bool wg, const NormArgs& a, uint32_t& parts, c
   constexpr size_t sums = (size_t)THREADS * NO * 64;  // the teams' column sums take the ring's place
   constexpr size_t smem_wg = ring_bwd > sums ? ring_bwd : sums;
   const uint64_t want = (a.n_rows + TEAMS - 1) / TEAMS;
-  const uint64_t per_sm = LANES > 256 ? 1 : (fwd && NO == 1 ? 4 : 2);
+  const uint64_t per_sm = fwd ? fwd_ctas(DT, EDGE, NO, LANES) : (LANES > 256 ? 1 : 2);
   uint64_t cap = fwd || !wg ? (uint64_t)sm_count() * per_sm : (LANES > 256 ? kMaxPartials / 2 : kMaxPartials);
   if (EDGE) {  // a team's rows must all have one shift: the number of teams is a multiple of the shifts' period
     const uint64_t period = kVec<DT> / gcd64(kVec<DT>, a.x_stride % kVec<DT>), unit = period / gcd64(period, TEAMS);
@@ -660,8 +668,7 @@ cudaError_t launch_norm(bool fwd, bool wg, const NormArgs& a, uint32_t& parts, c
   return e != cudaSuccess ? e : launch_overlapped(norm_bwd_kernel<DT, EDGE, NO, LANES, true>, dim3(grid), THREADS, smem_wg, st, a);
 }
 
-// The smallest team that holds the row: eight elements a lane up to 256, sixteen or twenty-four beyond.  (At 768 elements, one
-// warp with 24 a lane against two with 16: 8.1 and 9 us forward, as two warps meet at a barrier in every row.)
+// The smallest team that holds the row: eight elements a lane up to 256, sixteen or twenty-four beyond.
 template <int DT, bool EDGE>
 cudaError_t launch_norm_shape(bool fwd, bool wg, const NormArgs& a, uint32_t elems, uint32_t& parts, cudaStream_t st) {
 #define S2A_NORM(NO, LANES) \
