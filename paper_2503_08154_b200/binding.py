@@ -356,9 +356,13 @@ _CODES = {torch.float32: F32, torch.bfloat16: BF16}
 _current_device = torch._C._cuda_getDevice if hasattr(torch._C, "_cuda_getDevice") else torch.cuda.current_device
 
 
-def _on_device(first: torch.Tensor, *others) -> None:
+def _stream_on(dev: int) -> int:
+    return _raw_stream(dev) if _raw_stream is not None else torch.cuda.current_stream(dev).cuda_stream
+
+
+def _on_device(first: torch.Tensor, *others) -> int:
     """One device for all tensors of a call, None aside, and that device current: a launch goes to
-    the current device, whatever memory its pointers name."""
+    the current device, whatever memory its pointers name.  Returns its index."""
     dev = first.get_device()
     if dev < 0:
         raise S2AError("CUDA tensors are needed")
@@ -367,6 +371,7 @@ def _on_device(first: torch.Tensor, *others) -> None:
             raise S2AError("all tensors of a call must be on one device")
     if dev != _current_device():
         raise S2AError("the tensors' device must be the current one (torch.cuda.device)")
+    return dev
 
 
 def _rows(t: torch.Tensor, n_rows: int, row_len: int, what: str) -> int:
@@ -437,35 +442,42 @@ def layernorm_scratch_bytes(n_rows: int, row_len: int) -> int:
 def s2a_layernorm_fwd(x, gamma, beta, y, stats, row_len: int, eps: float) -> None:
     """Layer norm over rows of row_len elements.  gamma, beta and stats ([n_rows, 2] float32, what the
     backward call needs) may be None; x and y may be slices with evenly spaced rows."""
-    _on_device(x, gamma, beta, y, stats)
-    if row_len <= 0 or x.numel() % row_len:
+    dev = _on_device(x, gamma, beta, y, stats)
+    elems = x.numel()
+    if row_len <= 0 or elems % row_len:
         raise S2AError("x must hold whole rows of row_len elements")
-    if y.dtype != x.dtype:
+    if y.dtype is not x.dtype:
         raise S2AError("y must match x in dtype")
-    n = x.numel() // row_len
-    check(lib().s2a_layernorm_fwd(x.data_ptr(), _param(gamma, row_len, "gamma"), _param(beta, row_len, "beta"), y.data_ptr(),
-                                  _stats(stats, n), n, row_len, _rows(x, n, row_len, "x"), _rows(y, n, row_len, "y"), eps,
-                                  _code(x), _param_dtype(gamma, beta), _stream_ptr(x)))
+    n = elems // row_len
+    status = (_lib or lib()).s2a_layernorm_fwd(
+        x.data_ptr(), _param(gamma, row_len, "gamma"), _param(beta, row_len, "beta"), y.data_ptr(), _stats(stats, n), n, row_len,
+        row_len if x.is_contiguous() else _rows(x, n, row_len, "x"), _rows(y, n, row_len, "y"), eps, _code(x),
+        _param_dtype(gamma, beta), _stream_on(dev))
+    if status:
+        check(status)
 
 
 def s2a_layernorm_bwd(grad_out, x, gamma, stats, grad_in, grad_gamma, grad_beta, scratch, row_len: int) -> None:
     """Layer norm's backward pass.  grad_gamma and grad_beta may be None (frozen weights; without both,
     scratch may be None too); scratch holds layernorm_scratch_bytes(n_rows, row_len) bytes."""
-    _on_device(x, grad_out, gamma, stats, grad_in, grad_gamma, grad_beta, scratch)
-    if row_len <= 0 or x.numel() % row_len:
+    dev = _on_device(x, grad_out, gamma, stats, grad_in, grad_gamma, grad_beta, scratch)
+    elems = x.numel()
+    if row_len <= 0 or elems % row_len:
         raise S2AError("x must hold whole rows of row_len elements")
-    if grad_out.dtype != x.dtype or grad_in.dtype != x.dtype:
+    if grad_out.dtype is not x.dtype or grad_in.dtype is not x.dtype:
         raise S2AError("grad_out and grad_in must match x in dtype")
     if stats is None:
         raise S2AError("stats of the forward call are needed")
-    n = x.numel() // row_len
+    n = elems // row_len
     sums = grad_gamma is not None or grad_beta is not None
-    check(lib().s2a_layernorm_bwd(
+    status = (_lib or lib()).s2a_layernorm_bwd(
         grad_out.data_ptr(), x.data_ptr(), _param(gamma, row_len, "gamma"), _stats(stats, n), grad_in.data_ptr(),
         _param(grad_gamma, row_len, "grad_gamma"), _param(grad_beta, row_len, "grad_beta"),
         _scratch(scratch, layernorm_scratch_bytes(n, row_len)) if sums else None, n, row_len,
-        _rows(grad_out, n, row_len, "grad_out"), _rows(x, n, row_len, "x"), _rows(grad_in, n, row_len, "grad_in"),
-        _code(x), _param_dtype(gamma, grad_gamma, grad_beta), _stream_ptr(x)))
+        _rows(grad_out, n, row_len, "grad_out"), row_len if x.is_contiguous() else _rows(x, n, row_len, "x"),
+        _rows(grad_in, n, row_len, "grad_in"), _code(x), _param_dtype(gamma, grad_gamma, grad_beta), _stream_on(dev))
+    if status:
+        check(status)
 
 
 def dropout_threshold(p: float) -> int:
@@ -473,10 +485,11 @@ def dropout_threshold(p: float) -> int:
 
 
 def _dropout_args(x, y, rng, site):
-    _dev(x, "x"), _dev(y, "y"), _dev(rng, "rng")
-    if y.numel() != x.numel() or y.dtype != x.dtype:
+    if not (x.is_contiguous() and y.is_contiguous() and rng.is_contiguous()):
+        raise S2AError("the input, the output and rng must be contiguous")
+    if y.numel() != x.numel() or y.dtype is not x.dtype:
         raise S2AError("the output must match the input in size and dtype")
-    if rng.dtype != torch.int64 or rng.numel() != 2:
+    if rng.dtype is not torch.int64 or rng.numel() != 2:
         raise S2AError("rng must be int64 with 2 elements, (seed, offset)")
     return site & 0xFFFFFFFFFFFFFFFF
 
@@ -484,48 +497,57 @@ def _dropout_args(x, y, rng, site):
 def s2a_dropout_fwd(x, residual, y, rng, site: int, p: float) -> None:
     """y = dropout(x), or residual + dropout(x).  rng is an int64 CUDA tensor (seed, offset) that the kernel
     reads; `site` tells the calls of one step apart."""
-    _on_device(x, residual, y, rng)
+    dev = _on_device(x, residual, y, rng)
     site = _dropout_args(x, y, rng, site)
+    added = None
     if residual is not None:
-        _dev(residual, "residual")
-        if residual.numel() != x.numel() or residual.dtype != x.dtype:
-            raise S2AError("residual must match x in size and dtype")
-    check(lib().s2a_dropout_fwd(x.data_ptr(), residual.data_ptr() if residual is not None else None, y.data_ptr(), x.numel(),
-                                rng.data_ptr(), site, p, _code(x), _stream_ptr(x)))
+        if not residual.is_contiguous() or residual.numel() != x.numel() or residual.dtype is not x.dtype:
+            raise S2AError("residual must be contiguous and match x in size and dtype")
+        added = residual.data_ptr()
+    status = (_lib or lib()).s2a_dropout_fwd(x.data_ptr(), added, y.data_ptr(), x.numel(), rng.data_ptr(), site, p, _code(x),
+                                             _stream_on(dev))
+    if status:
+        check(status)
 
 
 def s2a_dropout_bwd(grad_out, grad_in, rng, site: int, p: float) -> None:
-    _on_device(grad_out, grad_in, rng)
+    dev = _on_device(grad_out, grad_in, rng)
     site = _dropout_args(grad_out, grad_in, rng, site)
-    check(lib().s2a_dropout_bwd(grad_out.data_ptr(), grad_in.data_ptr(), grad_out.numel(), rng.data_ptr(), site, p,
-                                _code(grad_out), _stream_ptr(grad_out)))
+    status = (_lib or lib()).s2a_dropout_bwd(grad_out.data_ptr(), grad_in.data_ptr(), grad_out.numel(), rng.data_ptr(), site, p,
+                                             _code(grad_out), _stream_on(dev))
+    if status:
+        check(status)
 
 
 def _bias_args(scores, buckets, table, batch, heads, tq, tk):
-    _dev(scores, "the scores"), _dev(buckets, "buckets"), _dev(table, "the table")
+    if not (scores.is_contiguous() and buckets.is_contiguous() and table.is_contiguous()):
+        raise S2AError("the scores, the buckets and the table must be contiguous")
     if min(batch, heads, tq, tk) < 0 or scores.numel() != batch * heads * tq * tk:
         raise S2AError("the scores must be [batch, heads, tq, tk]")
-    if table.dim() != 2 or table.shape[1] != heads:
+    shape = table.shape
+    if len(shape) != 2 or shape[1] != heads:
         raise S2AError("the table must be [n_buckets, heads]")
-    if buckets.dtype != torch.int32:
+    if buckets.dtype is not torch.int32:
         raise S2AError("buckets must be int32")
-    if buckets.dim() == 2 and tuple(buckets.shape) == (tq, tk):
-        return 0
-    if buckets.dim() == 1 and buckets.numel() == max(tq + tk - 1, 0):
-        return 1
+    size = buckets.shape
+    if len(size) == 1 and size[0] == max(tq + tk - 1, 0):
+        return 1, shape[0]
+    if len(size) == 2 and size[0] == tq and size[1] == tk:
+        return 0, shape[0]
     raise S2AError("buckets must be a map [tq, tk] or a vector [tq + tk - 1]")
 
 
 def s2a_relbias_fwd(x, table, buckets, y, batch: int, heads: int, tq: int, tk: int) -> None:
     """y = x + table[bucket(q, k)] over scores [batch, heads, tq, tk].  buckets: int32, a map [tq, tk], or a
     vector [tq + tk - 1] over the distance k - q + tq - 1."""
-    _on_device(x, table, buckets, y)
-    by_distance = _bias_args(x, buckets, table, batch, heads, tq, tk)
-    _dev(y, "y")
-    if y.numel() != x.numel() or y.dtype != x.dtype:
-        raise S2AError("y must match x in size and dtype")
-    check(lib().s2a_relbias_fwd(x.data_ptr(), table.data_ptr(), buckets.data_ptr(), by_distance, y.data_ptr(), batch, heads, tq,
-                                tk, table.shape[0], _code(x), _code(table), _stream_ptr(x)))
+    dev = _on_device(x, table, buckets, y)
+    by_distance, n = _bias_args(x, buckets, table, batch, heads, tq, tk)
+    if not y.is_contiguous() or y.numel() != x.numel() or y.dtype is not x.dtype:
+        raise S2AError("y must be contiguous and match x in size and dtype")
+    status = (_lib or lib()).s2a_relbias_fwd(x.data_ptr(), table.data_ptr(), buckets.data_ptr(), by_distance, y.data_ptr(), batch,
+                                             heads, tq, tk, n, _code(x), _code(table), _stream_on(dev))
+    if status:
+        check(status)
 
 
 def relbias_scratch_bytes(batch: int, heads: int, tq: int, tk: int, n_buckets: int) -> int:
@@ -534,13 +556,14 @@ def relbias_scratch_bytes(batch: int, heads: int, tq: int, tk: int, n_buckets: i
 
 def s2a_relbias_bwd(grad_out, buckets, grad_table, scratch, batch: int, heads: int, tq: int, tk: int) -> None:
     """The table's gradient; scratch holds relbias_scratch_bytes(batch, heads, tq, tk, n_buckets) bytes."""
-    _on_device(grad_out, buckets, grad_table, scratch)
-    by_distance = _bias_args(grad_out, buckets, grad_table, batch, heads, tq, tk)
-    n = grad_table.shape[0]
+    dev = _on_device(grad_out, buckets, grad_table, scratch)
+    by_distance, n = _bias_args(grad_out, buckets, grad_table, batch, heads, tq, tk)
     need = relbias_scratch_bytes(batch, heads, tq, tk, n)
-    check(lib().s2a_relbias_bwd(grad_out.data_ptr(), buckets.data_ptr(), by_distance, grad_table.data_ptr(),
-                                _scratch(scratch, need) if need else None, batch, heads, tq, tk, n, _code(grad_out),
-                                _code(grad_table), _stream_ptr(grad_out)))
+    status = (_lib or lib()).s2a_relbias_bwd(grad_out.data_ptr(), buckets.data_ptr(), by_distance, grad_table.data_ptr(),
+                                             _scratch(scratch, need) if need else None, batch, heads, tq, tk, n, _code(grad_out),
+                                             _code(grad_table), _stream_on(dev))
+    if status:
+        check(status)
 
 
 def log_buckets(first_distance: int, count: int, n_buckets: int, max_distance: int, bidirectional: bool) -> torch.Tensor:
