@@ -15,13 +15,12 @@
 //
 // Work is cut into items: a head, a block of query rows, a chunk of vectors (`lanes` of them) and a part of the batch.
 //
-// What it measures on a B200 (6.57 TB/s copy rate), bfloat16: [64, 12, 197, 197] under a map of 732 buckets, forward 25.8 us (4.6 TB/s:
-// 18 us of walking, which is the copy rate, after 3 us in which the chunk's biases are looked up, and the launch), backward
-// 23.1 us (2.6 TB/s: 12.7 of walking, 2.3 before and 5 after it for the tables, 2.5 for the second kernel); by distance
-// 28 us; [2, 16, 2048, 2048] by distance, forward 107 us (5.0 TB/s), backward 58 us (4.6 TB/s).  Looking the bucket of
-// every element up where it is added costs 200 us there.  Measured and not kept: the rows through a ring of cp.async as in
-// layer norm (92 us: the bookkeeping of a row's place outweighs the add), eight rows ahead in forward (spills, 33 us), rows
-// asked for in L2 before the forward kernel's look-up (26.5 us).
+// What it measures on a B200 (6.57 TB/s copy rate), bfloat16: [64, 12, 197, 197] under a map of 732 buckets, forward 25.0 us (4.8 TB/s:
+// 18 us of walking, which is the copy rate, after the look-up of the chunk's biases, and the launch), backward 19.3 us (3.1 TB/s:
+// about 13 of walking, the rest setup, tables and the second kernel); by distance 28 us; [2, 16, 2048, 2048] by distance,
+// forward 106 us (5.1 TB/s), backward 53 us (5.1 TB/s).  Looking the bucket of every element up where it is added costs 200 us
+// there.  Measured and not kept: the rows through a ring of cp.async as in layer norm (92 us: the bookkeeping of a row's place
+// outweighs the add), eight rows ahead in forward (spills, 33 us), rows asked for in L2 before the forward kernel's look-up (no gain).
 #include <math.h>
 
 #include "s2a_launch.h"
@@ -511,10 +510,20 @@ __global__ void __launch_bounds__(256) bias_table_kernel(const float* partials, 
 // ---------------------------------------------------------------- host side
 uint64_t ceil_div(uint64_t a, uint64_t b) { return (a + b - 1) / b; }
 
+// What things cost a thread, in rows walked: an item; a slot whose bucket it looks up or adds; a run along the query rows, whose cut
+// rows are a wait of their own.
+struct Costs {
+  uint32_t item, slot, run;
+};
+// Counting the slots makes chunks narrower and puts threads side by side along the batch: [64, 12, 197, 197] under a map backward
+// 23.2 -> 19.3 us, forward 25.8 -> 25.0; [2, 16, 2048, 2048] backward 58 -> 53.  Counting the runs makes blocks taller: [16, 16, 577, 577]
+// by distance backward 50 -> 41; forward does not gain by it (81 -> 88).
+constexpr Costs kFwdCosts = {8, 1, 0}, kBwdCosts = {12, 2, 6};
+
 // Cuts the work of every head into items: of the cuts tried, the one whose CTAs are done first, where every SM of a B200 holds
-// kThreadsPerSm threads, a thread's row counts one and an item `fixed` besides.  At most `most` CTAs over all heads.
+// kThreadsPerSm threads.  At most `most` CTAs over all heads.
 template <int V>
-void cut(BiasArgs& a, uint64_t most, uint32_t fixed) {
+void cut(BiasArgs& a, uint64_t most, const Costs& cost) {
   a.by_batch = a.tq < 4 * V;  // with few query rows the inner loop runs over the samples
   a.step = (uint32_t)((a.by_batch ? a.sample : a.tk + 1) % V);
   a.shift = 0;
@@ -546,7 +555,9 @@ void cut(BiasArgs& a, uint64_t most, uint32_t fixed) {
         const uint32_t part = (uint32_t)((shares + parts - 1) / parts) * share;
         parts = (a.batch + part - 1) / part;
         const uint64_t items = blocks * chunks * parts;
-        const uint64_t time = ((items + per_head - 1) / per_head) * ((uint64_t)height * (part / rows) + fixed);
+        const uint64_t time = ((items + per_head - 1) / per_head) *
+                              ((uint64_t)(height + (a.by_batch ? 0 : cost.run * a.period)) * (part / rows) + cost.item +
+                               cost.slot * ((lanes * V + threads - 1) / threads));
         if (time >= best || items > 0xffffffffull) continue;
         best = time;
         a.block = height;
@@ -586,7 +597,7 @@ uint64_t bwd_most(uint32_t n_buckets) {
 template <int DT>
 cudaError_t launch_bias_fwd(BiasArgs& a, cudaStream_t st) {
   constexpr int V = kVec<DT>;
-  cut<V>(a, ~0ull, 12);
+  cut<V>(a, ~0ull, kFwdCosts);
   return launch_overlapped(bias_fwd_kernel<DT>, dim3(a.ctas_per_head, a.heads), a.threads, spread_slots<V>(a.lanes) * sizeof(float), st, a);
 }
 
@@ -594,7 +605,7 @@ template <int DT>
 cudaError_t launch_bias_bwd(BiasArgs& a, cudaStream_t st) {
   constexpr int V = kVec<DT>;
   static std::atomic<uint64_t> ready = {};
-  cut<V>(a, bwd_most(a.n_buckets), 20);
+  cut<V>(a, bwd_most(a.n_buckets), kBwdCosts);
   const size_t count = slots<V>(a.lanes);
   // a table for each warp, unless they take too much shared memory, or a warp has less than two rows of slots to add
   const uint32_t room = (uint32_t)(kTableBytes / (a.n_buckets * (sizeof(float) + 1))), use = (uint32_t)(count / 64);
