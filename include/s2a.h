@@ -264,7 +264,7 @@ int s2a_lrp_fwd(const void* x, const float* A, const float* B, void* y, size_t b
  */
 
 /* Bytes of scratch for the weights' gradients of s2a_layernorm_bwd (0 where row_len is 0 or
- * above 2^31-1): at most 592 * row_len * 4. */
+ * above 2^31-1): at most 888 * row_len * 4. */
 size_t s2a_layernorm_scratch_bytes(size_t n_rows, size_t row_len);
 
 /* Layer norm forward.  Per row: mean = sum(x) / row_len, var = sum((x - mean)^2) / row_len,

@@ -32,7 +32,7 @@
 namespace s2a {
 namespace {
 
-constexpr uint32_t kMaxPartials = 296;  // partial sums of the weights' gradients: two CTAs per SM of a B200
+constexpr uint32_t kMaxPartials = 444;  // partial sums of the weights' gradients: three CTAs per SM of a B200
 
 struct NormArgs {
   const void* x;
@@ -60,6 +60,9 @@ __host__ __device__ constexpr int threads_of(int lanes) { return lanes > 256 ? l
 __host__ __device__ constexpr int fwd_ctas(int dt, bool edge, int no, int lanes) {
   return lanes > 256 ? 1 : (no == 1 ? 4 : (no == 2 && dt == kBF16 && !edge ? 3 : 2));
 }
+// And of the backward kernel: three for short rows ([300000, 64] bfloat16 23.4 us against 32 with two), two for longer ones
+// ([65536, 4096] 263 us against 281 with three).
+__host__ __device__ constexpr int bwd_ctas(bool edge, int no, int lanes) { return lanes > 256 ? 1 : (no == 1 && !edge ? 3 : 2); }
 // Rows in flight per team: what keeps two CTAs of an SM (one of 512 threads) within its shared memory.
 __host__ __device__ constexpr int stages_of(int stage_bytes) {
   return stage_bytes <= 24 * 1024 ? 4 : (stage_bytes <= 32 * 1024 ? 3 : (stage_bytes <= 100 * 1024 ? 2 : 1));
@@ -371,7 +374,7 @@ __global__ void __launch_bounds__(threads_of(LANES), fwd_ctas(DT, EDGE, NO, LANE
 
 // ---------------------------------------------------------------- backward
 template <int DT, bool EDGE, int NO, int LANES, bool WG>
-__global__ void __launch_bounds__(threads_of(LANES), LANES > 256 ? 1 : 2) norm_bwd_kernel(NormArgs a) {
+__global__ void __launch_bounds__(threads_of(LANES), bwd_ctas(EDGE, NO, LANES)) norm_bwd_kernel(NormArgs a) {
   using T = typename Io<DT>::T;
   constexpr int THREADS = threads_of(LANES), TEAMS = THREADS / LANES, WARPS = LANES / 32 > 1 ? LANES / 32 : 1;
   constexpr int GROUP = LANES < 32 ? LANES : 32;
@@ -647,8 +650,8 @@ cudaError_t launch_norm(bool fwd, bool wg, const NormArgs& a, uint32_t& parts, c
   constexpr size_t sums = (size_t)THREADS * NO * 64;  // the teams' column sums take the ring's place
   constexpr size_t smem_wg = ring_bwd > sums ? ring_bwd : sums;
   const uint64_t want = (a.n_rows + TEAMS - 1) / TEAMS;
-  const uint64_t per_sm = fwd ? fwd_ctas(DT, EDGE, NO, LANES) : (LANES > 256 ? 1 : 2);
-  uint64_t cap = fwd || !wg ? (uint64_t)sm_count() * per_sm : (LANES > 256 ? kMaxPartials / 2 : kMaxPartials);
+  const uint64_t per_sm = fwd ? fwd_ctas(DT, EDGE, NO, LANES) : bwd_ctas(EDGE, NO, LANES);
+  uint64_t cap = fwd || !wg ? (uint64_t)sm_count() * per_sm : 148ull * bwd_ctas(EDGE, NO, LANES);
   if (EDGE) {  // a team's rows must all have one shift: the number of teams is a multiple of the shifts' period
     const uint64_t period = kVec<DT> / gcd64(kVec<DT>, a.x_stride % kVec<DT>), unit = period / gcd64(period, TEAMS);
     cap = cap / unit * unit;

@@ -77,7 +77,7 @@ def test_norm_scratch(lib):
         last = 0
         for rows in (0, 1, 7, 8, 9, 100, 1000, 10 ** 6):
             n = f(rows, L)
-            assert n % (8 * L) == 0 and last <= n <= 592 * L * 4 and n >= 8 * L
+            assert n % (8 * L) == 0 and last <= n <= 888 * L * 4 and n >= 8 * L
             last = n
 
 
