@@ -21,11 +21,11 @@
 // of its team, a CTA adds its teams' sums in order and writes one pair of rows to the caller's scratch, and a second kernel
 // adds those in order: no atomics, the same bits on every run.
 //
-// What it measures on a B200 (6.57 TB/s copy rate): [12608, 768] bfloat16 forward 8.1 us (4.8 TB/s), backward with weights
-// 14.8 us (3.9 TB/s), without 11.0 us (5.3 TB/s); of these about 2 us are the launch, 1.4 us the first rows' way from memory,
+// What it measures on a B200 (6.57 TB/s copy rate): [12608, 768] bfloat16 forward 8.0 us (4.9 TB/s), backward with weights
+// 14.7 us (4.0 TB/s), without 10.8 us (5.4 TB/s); of these about 2 us are the launch, 1.4 us the first rows' way from memory,
 // and 3 us the second kernel of the weights' gradients.  [65536, 4096] backward 262 us (6.1 TB/s).  The first kernels,
 // with rows loaded into registers one at a time, took 17.3 and 49.8 us.  Odd row lengths cost instructions, not bytes: [4616, 1025] binary32 backward
-// 17.2 us (3.3 TB/s), [20000, 1025] bfloat16 forward 32 us (2.5 TB/s), 54 % of the issue slots at 16 warps an SM.
+// 16.9 us (3.4 TB/s), [20000, 1025] bfloat16 forward 31 us (2.7 TB/s), half of the issue slots at 16 warps an SM.
 #include "s2a_launch.h"
 #include "s2a_oct.cuh"
 
@@ -75,6 +75,10 @@ __host__ __device__ constexpr int stage_bytes(int dt, int no, int lanes, int ten
 template <int DT, int LANES>
 __device__ __forceinline__ int piece_column(int j, uint32_t lane, int s) { return (int)((j * LANES + lane) * (uint32_t)kVec<DT>) - s; }
 
+// A team is the smallest that holds the row, so the row's last vector lies in one of a thread's last two pieces (three of the
+// shorter ones of binary32): only from piece kSure on may a piece end after the row, or begin after it.
+template <int DT, int NO> constexpr int kSure = kPieces<DT, NO> - (DT == kF32 ? 3 : 2);
+
 template <int DT>
 __device__ __forceinline__ bool piece_whole(int c, int L) { return c >= 0 && c + kVec<DT> <= L; }
 
@@ -91,8 +95,9 @@ __device__ __forceinline__ void fetch(uint4* slot, const void* tensor, uint64_t 
 #pragma unroll
   for (int j = 0; j < kPieces<DT, NO>; ++j) {
     const int c = piece_column<DT, LANES>(j, lane, s);
-    if (c >= L) continue;
-    if (!EDGE) {
+    const bool sure = j < kSure<DT, NO>;
+    if (!sure && c >= L) continue;
+    if (!EDGE || (sure && j > 0 && !apart)) {
       copy_async<16>(slot + j * THREADS, p + c);
     } else if (!apart && (j > 0 || p + c >= (const T*)tensor)) {
       copy_async_front(slot + j * THREADS, p + c, min(L - c, V) * (int)sizeof(T));
@@ -143,8 +148,8 @@ __device__ __forceinline__ void mask_ends(F2* v, int c, int L) {
 }
 
 template <int DT, bool EDGE>
-__device__ __forceinline__ void put_piece(typename Io<DT>::T* row, int c, int L, bool apart, const F2* v) {
-  if (!EDGE || (!apart && piece_whole<DT>(c, L))) {
+__device__ __forceinline__ void put_piece(typename Io<DT>::T* row, int c, int L, bool whole, bool apart, const F2* v) {
+  if (!EDGE || (!apart && (whole || piece_whole<DT>(c, L)))) {
     *(uint4*)(row + c) = narrow_piece<DT>(v);
   } else {
 #pragma unroll
@@ -318,7 +323,7 @@ __global__ void __launch_bounds__(threads_of(LANES), fwd_ctas(DT, EDGE, NO, LANE
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
       const int c = piece_column<DT, LANES>(j, lane, s);
-      if (c < L) {
+      if (j < kSure<DT, NO> || c < L) {
         widen_piece<DT>(cut_head<DT, EDGE>(slot[j * THREADS], j, head), v[j]);
       } else {
 #pragma unroll
@@ -336,10 +341,10 @@ __global__ void __launch_bounds__(threads_of(LANES), fwd_ctas(DT, EDGE, NO, LANE
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
       const int c = piece_column<DT, LANES>(j, lane, s);
-      if (c >= L) continue;
+      if (j >= kSure<DT, NO> && c >= L) continue;
 #pragma unroll
       for (int i = 0; i < PAIRS; ++i) v[j][i] = f2_sub(v[j][i], f2_both(mean));
-      if (EDGE) mask_ends<DT>(v[j], c, L);  // elements outside the row have no deviation
+      if (EDGE && (j == 0 || j >= kSure<DT, NO>)) mask_ends<DT>(v[j], c, L);  // elements outside the row have no deviation
 #pragma unroll
       for (int i = 0; i < PAIRS; ++i) sq = f2_fma(v[j][i], v[j][i], sq);
     }
@@ -363,11 +368,11 @@ __global__ void __launch_bounds__(threads_of(LANES), fwd_ctas(DT, EDGE, NO, LANE
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
       const int c = piece_column<DT, LANES>(j, lane, s);
-      if (c >= L) continue;
+      if (j >= kSure<DT, NO> && c >= L) continue;
 #pragma unroll
       for (int i = 0; i < PAIRS; ++i)
         v[j][i] = f2_fma(f2_mul(WARPS > 1 ? f2_add(v[j][i], f2_both(shift)) : v[j][i], f2_both(rstd)), gamma[j][i], beta[j][i]);
-      put_piece<DT, EDGE>(out, c, L, EDGE && a.out_apart, v[j]);
+      put_piece<DT, EDGE>(out, c, L, j > 0 && j < kSure<DT, NO>, EDGE && a.out_apart, v[j]);
     }
   }
 }
@@ -430,7 +435,7 @@ __global__ void __launch_bounds__(threads_of(LANES), bwd_ctas(EDGE, NO, LANES)) 
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
       const int c = piece_column<DT, LANES>(j, lane, s);
-      if (!on || c >= L) continue;
+      if (!on || (j >= kSure<DT, NO> && c >= L)) continue;
       F2 x[PAIRS], g[PAIRS];
       widen_piece<DT>(cut_head<DT, EDGE>(sx[j * THREADS], j, head), x);
       widen_piece<DT>(cut_head<DT, EDGE>(sg[j * THREADS], j, head), g);
@@ -460,7 +465,7 @@ __global__ void __launch_bounds__(threads_of(LANES), bwd_ctas(EDGE, NO, LANES)) 
 #pragma unroll
     for (int j = 0; j < NP; ++j) {
       const int c = piece_column<DT, LANES>(j, lane, s);
-      if (!on || c >= L) continue;
+      if (!on || (j >= kSure<DT, NO> && c >= L)) continue;
       F2 x[PAIRS], g[PAIRS];
       widen_piece<DT>(sx[j * THREADS], x);
       widen_piece<DT>(sg[j * THREADS], g);
@@ -468,7 +473,7 @@ __global__ void __launch_bounds__(threads_of(LANES), bwd_ctas(EDGE, NO, LANES)) 
       for (int i = 0; i < PAIRS; ++i) {
         g[i] = f2_fma(f2_mul(g[i], gamma[j][i]), rstd2, f2_fma(f2_sub(x[i], mean2), k2, k1));
       }
-      put_piece<DT, EDGE>(out, c, L, EDGE && a.out_apart, g);
+      put_piece<DT, EDGE>(out, c, L, j > 0 && j < kSure<DT, NO>, EDGE && a.out_apart, g);
     }
     start_row(at, r + STAGES * step);
     copy_commit();
