@@ -275,9 +275,10 @@ size_t s2a_layernorm_scratch_bytes(size_t n_rows, size_t row_len);
  *   y      out  n_rows rows, y_stride elements apart; may be x with the same stride
  *   stats  out  2 * n_rows floats, (mean, rstd) of each row for the backward call, 8-byte
  *               aligned; or NULL (inference)
- * Pointers need the alignment of their element type only (stats: 8 bytes); rows that all start
- * on 16-byte boundaries with row_len a multiple of 8 are read in whole vectors, others element
- * by element.  y_stride must be at least row_len; the bytes between rows are not touched.
+ * Pointers need the alignment of their element type only (stats: 8 bytes); tensors whose rows lie
+ * alike on the 16-byte grid are read in whole vectors, fastest where rows begin and end on it.
+ * Rows of which one tensor's lie differently on the grid from x's are taken element by element in
+ * that tensor.  y_stride must be at least row_len; the bytes between rows are not touched.
  * x_stride is free (0 repeats one row).  eps: finite, not negative.  An output whose rows
  * overlap x's rows without being the same rows returns S2A_ERR_OVERLAP (rows of one stride may
  * interleave); gamma, beta and stats must not overlap an output (not checked).
