@@ -16,8 +16,10 @@
 // Work is cut into items: a head, a block of query rows, a chunk of vectors (`lanes` of them) and a part of the batch.
 //
 // What it measures on a B200 (6.57 TB/s copy rate), bfloat16: [64, 12, 197, 197] under a map of 732 buckets, forward 25.0 us (4.8 TB/s:
-// 18 us of walking, which is the copy rate, after the look-up of the chunk's biases, and the launch), backward 19.3 us (3.1 TB/s:
-// about 13 of walking, the rest setup, tables and the second kernel); by distance 28 us; [2, 16, 2048, 2048] by distance,
+// 18 us of walking, which is the copy rate, after the look-up of the chunk's biases, and the launch), one sample of [16, 1025, 1025] 25 us
+// (2.9 TB/s: bias_fwd_few_kernel, bound by its instructions per element), backward 19.3 us (3.1 TB/s:
+// about 13 of walking, the rest setup, tables and the second kernel), one sample of [16, 1025, 1025] 100 us (the tables' turns); by
+// distance [64, 12, 197, 197] 28 us; [2, 16, 2048, 2048] by distance,
 // forward 106 us (5.1 TB/s), backward 53 us (5.1 TB/s).  Looking the bucket of every element up where it is added costs 200 us
 // there.  Measured and not kept: the rows through a ring of cp.async as in layer norm (92 us: the bookkeeping of a row's place
 // outweighs the add), eight rows ahead in forward (spills, 33 us), rows asked for in L2 before the forward kernel's look-up (no gain).
@@ -34,6 +36,15 @@ constexpr uint32_t kThreads = 256, kMostThreads = 320;
 constexpr uint32_t kThreadsPerSm = 1024;     // at 64 registers a thread
 constexpr int kAnnounced = 8;                // rows of an item's first run that are asked for before its shared memory is set up
 constexpr int kStaged = 5;                   // slots that a thread looks up at a time
+// bias_fwd_few_kernel and bias_bwd_few_kernel.  Up to so many samples they are faster than the diagonals, beyond that not always.
+// Forward, [B, 12, 401, 401] bfloat16: B = 2: 8.4 us against 14.4, 4: 12.3 against 15.6, 8: 20.2 against 18.7; [1, 16, 1025, 1025] 25 against
+// 75.  Backward, the same: 2: 18 against 34, 4: 21 against 35, 8: 26 against 37; [64, 12, 197, 197] 27.5 against 19.3; [1, 16, 1025, 1025] 100
+// against 243.
+constexpr uint32_t kFewSamplesFwd = 4, kFewSamplesBwd = 8;
+constexpr uint32_t kFewThreads = 512, kFewPerSm = 2;  // four keys and three or four CTAs an SM: 28 to 30 us
+constexpr int kFewKeys = 8;                           // keys of a thread in flight
+constexpr uint32_t kColumnBuckets = 12288;            // of a column in 48 KB
+constexpr uint32_t kFewTableBytes = 220 * 1024;       // shared memory of an SM for the tables of bias_bwd_few_kernel
 constexpr uint32_t kTableBytes = 64 * 1024;  // shared memory for the tables of a backward CTA, beyond the first table
 
 struct BiasArgs {
@@ -52,6 +63,7 @@ struct BiasArgs {
   uint32_t lanes, rows;    // threads of a CTA along a chunk, and along the batch
   uint32_t ctas_per_head, threads;
   uint32_t tables;         // backward: warps that have a table
+  int column;              // bias_fwd_few_kernel: the head's column of the table comes into shared memory first
   int by_batch;            // the inner loop runs over samples (few query rows), not over query rows
   int wdt;
   // Along the inner loop the class moves by `step` = 2^shift * odd (mod V) from row to row: rows of one class come every `period` =
@@ -325,6 +337,52 @@ __global__ void __launch_bounds__(kMostThreads, 3) bias_fwd_kernel(BiasArgs a) {
   }
 }
 
+// Maps with few samples: there is little for a bias to be kept for, and the way of a chunk through shared memory and the classes
+// costs more than the elements.  Here neighbouring threads take neighbouring keys, one by one, whatever their alignment, and look
+// a key's bias up once for all samples.  The buckets of neighbouring keys are mostly neighbours too, but their places in the table
+// are `heads` apart, a line for every lane or two: so a CTA that looks up more keys than the table has buckets copies its
+// head's column into shared memory first.
+template <int DT>
+__global__ void __launch_bounds__(kFewThreads, kFewPerSm) bias_fwd_few_kernel(BiasArgs a) {
+  using T = typename Io<DT>::T;
+  extern __shared__ float column[];  // by bucket
+  enter_grid();
+  const uint32_t h = blockIdx.y;
+  if (a.column) {
+#pragma unroll 4
+    for (uint32_t u = threadIdx.x; u < a.n_buckets; u += kFewThreads) column[u] = load_param(a.table, (uint64_t)u * a.heads + h, a.wdt);
+    __syncthreads();
+  }
+  for (uint64_t k0 = (uint64_t)blockIdx.x * kFewKeys * kFewThreads; k0 < a.tk; k0 += (uint64_t)gridDim.x * kFewKeys * kFewThreads) {
+    const uint64_t k = k0 + threadIdx.x, first = h * a.slab + k;
+    const int left = clamp_int((int64_t)(a.tk - k0) - threadIdx.x);  // key k + i * kFewThreads is there if i * kFewThreads < left
+    const T* x = (const T*)a.x + first;
+    T* y = (T*)a.y + first;
+    int u[kFewKeys];
+    T v[kFewKeys];
+    float bias[kFewKeys];
+#pragma unroll
+    for (int i = 0; i < kFewKeys; ++i) u[i] = i * (int)kFewThreads < left ? a.buckets[k + i * kFewThreads] : -1;
+#pragma unroll
+    for (int i = 0; i < kFewKeys; ++i)
+      if (i * (int)kFewThreads < left) v[i] = x[i * kFewThreads];
+#pragma unroll
+    for (int i = 0; i < kFewKeys; ++i)
+      bias[i] = (uint32_t)u[i] >= a.n_buckets ? 0.0f : (a.column ? column[u[i]] : load_param(a.table, (uint64_t)u[i] * a.heads + h, a.wdt));
+    for (uint32_t b = 0;;) {
+#pragma unroll
+      for (int i = 0; i < kFewKeys; ++i)
+        if (i * (int)kFewThreads < left) y[i * kFewThreads] = Io<DT>::narrow(Io<DT>::widen(v[i]) + bias[i]);
+      if (++b == a.batch) break;
+      x += a.sample;
+      y += a.sample;
+#pragma unroll
+      for (int i = 0; i < kFewKeys; ++i)
+        if (i * (int)kFewThreads < left) v[i] = x[i * kFewThreads];
+    }
+  }
+}
+
 // ---------------------------------------------------------------- backward
 // Adds one value per lane (bucket u, none for u < 0) to a warp's table.  Neighbouring lanes of one bucket are added up first
 // (a segmented scan), and the last lane of each run adds its sum; runs of one bucket apart from each other take turns in
@@ -359,6 +417,16 @@ __device__ __forceinline__ void table_add(float* table, uint8_t* tags, int u, fl
   for (int k = 0; k <= turns; ++k) {
     if (mine && turn == k) table[u] += v;
     __syncwarp();
+  }
+}
+
+// The sum of a CTA's tables, for bias_table_kernel.
+__device__ __forceinline__ void write_partials(const BiasArgs& a, const float* tables) {
+  float* part = a.partials + ((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * a.n_buckets;
+  for (uint32_t u = threadIdx.x; u < a.n_buckets; u += a.threads) {
+    float s = 0.0f;
+    for (uint32_t w = 0; w < a.tables; ++w) s += tables[w * a.n_buckets + u];
+    part[u] = s;
   }
 }
 
@@ -478,12 +546,46 @@ __global__ void __launch_bounds__(kMostThreads, 3) bias_bwd_kernel(BiasArgs a) {
     }
   }
   __syncthreads();
-  float* part = a.partials + ((uint64_t)h * gridDim.x + blockIdx.x) * a.n_buckets;
-  for (uint32_t u = threadIdx.x; u < a.n_buckets; u += a.threads) {
-    float s = 0.0f;
-    for (uint32_t w = 0; w < a.tables; ++w) s += tables[w * a.n_buckets + u];
-    part[u] = s;
+  write_partials(a, tables);
+}
+
+// As bias_fwd_few_kernel: a warp takes 32 neighbouring keys at a time, adds the samples up and the sums into its own table.  It is
+// bound by the turns at that table, so as many warps run as have room for one (asking for the next keys ahead of the turns: no
+// gain).
+template <int DT>
+__global__ void __launch_bounds__(kFewThreads, kFewPerSm) bias_bwd_few_kernel(BiasArgs a) {
+  using T = typename Io<DT>::T;
+  extern __shared__ __align__(16) float sums[];  // [tables][n_buckets]; [tables][n_buckets] their tags
+  enter_grid();
+  const uint32_t warp = threadIdx.x / 32, lane = threadIdx.x % 32, h = blockIdx.y;
+  for (uint32_t i = threadIdx.x; i < a.tables * a.n_buckets; i += a.threads) sums[i] = 0.0f;
+  __syncthreads();
+  float* table = sums + warp * a.n_buckets;
+  uint8_t* tags = (uint8_t*)(sums + a.tables * a.n_buckets) + warp * a.n_buckets;
+  const uint64_t hop = (uint64_t)gridDim.x * a.tables * (32 * kFewKeys);
+  for (uint64_t k0 = ((uint64_t)blockIdx.x * a.tables + warp) * (32 * kFewKeys); k0 < a.tk; k0 += hop) {
+    const uint64_t k = k0 + lane;
+    const int all = clamp_int((int64_t)(a.tk - k0)), left = all - (int)lane;
+    const T* x = (const T*)a.x + h * a.slab + k;
+    int u[kFewKeys];
+    float v[kFewKeys];
+#pragma unroll
+    for (int i = 0; i < kFewKeys; ++i) {
+      u[i] = i * 32 < left ? a.buckets[k + i * 32] : -1;
+      v[i] = i * 32 < left ? Io<DT>::widen(x[i * 32]) : 0.0f;
+    }
+    for (uint32_t b = 1; b < a.batch; ++b) {
+      x += a.sample;
+#pragma unroll
+      for (int i = 0; i < kFewKeys; ++i)
+        if (i * 32 < left) v[i] += Io<DT>::widen(x[i * 32]);
+    }
+#pragma unroll
+    for (int i = 0; i < kFewKeys; ++i)
+      if (i * 32 < all) table_add(table, tags, (uint32_t)u[i] < a.n_buckets ? u[i] : -1, v[i]);
   }
+  __syncthreads();
+  write_partials(a, sums);
 }
 
 // [head][CTA of the head][n_buckets] -> grad_table[n_buckets][heads].  A CTA owns 32 buckets of one head; its eight
@@ -597,6 +699,13 @@ uint64_t bwd_most(uint32_t n_buckets) {
 template <int DT>
 cudaError_t launch_bias_fwd(BiasArgs& a, cudaStream_t st) {
   constexpr int V = kVec<DT>;
+  if (a.tq == 1 && a.batch <= kFewSamplesFwd) {
+    const uint64_t resident = 148u * kFewPerSm, fit = resident > a.heads ? resident / a.heads : 1, want = ceil_div(a.tk, kFewKeys * kFewThreads);
+    const uint64_t ctas = want < fit ? want : fit;
+    a.column = a.n_buckets <= kColumnBuckets && a.tk >= (uint64_t)a.n_buckets * ctas;
+    static_assert(kColumnBuckets * sizeof(float) <= 48 * 1024, "what a CTA has without asking");
+    return launch_overlapped(bias_fwd_few_kernel<DT>, dim3((unsigned)ctas, a.heads), kFewThreads, a.column ? a.n_buckets * sizeof(float) : 0, st, a);
+  }
   cut<V>(a, ~0ull, kFwdCosts);
   return launch_overlapped(bias_fwd_kernel<DT>, dim3(a.ctas_per_head, a.heads), a.threads, spread_slots<V>(a.lanes) * sizeof(float), st, a);
 }
@@ -604,7 +713,19 @@ cudaError_t launch_bias_fwd(BiasArgs& a, cudaStream_t st) {
 template <int DT>
 cudaError_t launch_bias_bwd(BiasArgs& a, cudaStream_t st) {
   constexpr int V = kVec<DT>;
-  static std::atomic<uint64_t> ready = {};
+  static std::atomic<uint64_t> ready = {}, few_ready = {};
+  const uint32_t few_tables = kFewTableBytes / (a.n_buckets * (uint32_t)(sizeof(float) + 1));
+  if (a.tq == 1 && a.batch <= kFewSamplesBwd && few_tables >= 4) {
+    a.tables = few_tables < kFewThreads / 32 ? few_tables : kFewThreads / 32;
+    a.threads = a.tables * 32;
+    const size_t smem = (size_t)a.tables * a.n_buckets * (sizeof(float) + 1);
+    const uint64_t per_sm = few_tables / a.tables < kFewPerSm ? few_tables / a.tables : kFewPerSm;
+    const uint64_t resident = 148 * per_sm, most = resident < bwd_most(a.n_buckets) ? resident : bwd_most(a.n_buckets);
+    const uint64_t fit = most > a.heads ? most / a.heads : 1, want = ceil_div(a.tk, (uint64_t)a.threads * kFewKeys);
+    a.ctas_per_head = (uint32_t)(want < fit ? want : fit);
+    const cudaError_t e = allow_shared(bias_bwd_few_kernel<DT>, kFewTableBytes, few_ready);
+    return e != cudaSuccess ? e : launch_overlapped(bias_bwd_few_kernel<DT>, dim3(a.ctas_per_head, a.heads), a.threads, smem, st, a);
+  }
   cut<V>(a, bwd_most(a.n_buckets), kBwdCosts);
   const size_t count = slots<V>(a.lanes);
   // a table for each warp, unless they take too much shared memory, or a warp has less than two rows of slots to add

@@ -218,3 +218,57 @@ print("same")
 def test_first_calls_of_a_process_may_be_captured():
     r = subprocess.run([sys.executable, "-c", CAPTURE % ROOT], capture_output=True, text=True, timeout=300)
     assert r.returncode == 0 and "same" in r.stdout, r.stdout + r.stderr
+
+
+# Few samples under a map, or of one query row, are taken element by element: a table that fits beside them in shared memory, ones that are
+# too large or larger than what a CTA looks up, several rounds of a CTA, ragged ends.
+@pytest.mark.parametrize("batch,heads,tq,tk,n", [(1, 1, 1, 1, 1), (1, 2, 70, 71, 20), (2, 5, 33, 31, 2000), (4, 3, 65, 67, 5000), (2, 1, 97, 131, 12289),
+                                                 (1, 300, 130, 150, 12288), (3, 16, 1, 9001, 32), (4, 12, 197, 197, 732), (2, 7, 130, 257, 32768)])
+@pytest.mark.parametrize("dtype,weights", [("f32", "bf16"), ("bf16", "f32")])
+def test_bias_of_few_samples(batch, heads, tq, tk, n, dtype, weights):
+    for form in ("map", "distance") if tq == 1 else ("map",):
+        base._check_bias(batch, heads, tq, tk, n, dtype, weights, form, outside=n > 1)
+
+
+@pytest.mark.parametrize("tq,tk,n", [(50, 50, 172), (37, 129, 40), (1, 4097, 32)])
+def test_bias_of_a_sample_does_not_depend_on_the_others(tq, tk, n):
+    heads = 3
+    x = base._normal((9, heads, tq, tk), torch.bfloat16, "x")
+    x[:, :, :, 5::11] = float("-inf")
+    table = base._normal((n, heads), torch.float32, "t")
+    buckets = torch.randint(0, n, (tq, tk), generator=base._gen("b"), device="cuda").to(torch.int32)
+    whole = torch.empty_like(x)
+    s2a.s2a_relbias_fwd(x, table, buckets, whole, 9, heads, tq, tk)
+    for batch in range(1, 9):
+        part, y = x[:batch].contiguous(), torch.empty_like(x[:batch])
+        s2a.s2a_relbias_fwd(part, table, buckets, y, batch, heads, tq, tk)
+        base._done()
+        assert torch.equal(y, whole[:batch])
+
+
+@pytest.mark.parametrize("batch,n", [(1, 32), (2, 700), (4, 9000)])
+def test_bias_gradient_of_few_samples_and_real_numbers(batch, n):
+    heads, tq, tk = 4, 150, 151
+    buckets = torch.randint(-1, n, (tq, tk), generator=base._gen("b", n), device="cuda").to(torch.int32)
+    buckets[3] = 2                                  # runs of one bucket
+    buckets[5, ::2] = 4                             # and one bucket met again within a warp
+    for dt in (torch.float32, torch.bfloat16):
+        g = base._normal((batch, heads, tq, tk), dt, "g")
+        g[:, :, buckets == -1] = float("nan")       # what has no bucket leaves no trace
+        scratch = torch.empty(s2a.relbias_scratch_bytes(batch, heads, tq, tk, n), dtype=torch.uint8, device="cuda")
+        outs = []
+        for _ in range(3):
+            grad = torch.empty((n, heads), device="cuda")
+            scratch.fill_(0xFF)
+            s2a.s2a_relbias_bwd(g, buckets, grad, scratch, batch, heads, tq, tk)
+            outs.append(grad)
+        base._done()
+        assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2]), "repeated calls must give the same bits"
+        where = buckets.long().reshape(-1)
+        flat = g.double().sum(0).reshape(heads, -1).t()[where >= 0]
+        size = g.double().abs().sum(0).reshape(heads, -1).t()[where >= 0]
+        zero = torch.zeros((n, heads), dtype=torch.float64, device="cuda")
+        want, mass = zero.index_add(0, where[where >= 0], flat), zero.index_add(0, where[where >= 0], size)
+        # a sum of at most batch * count terms, in any order: (terms - 1) roundings each
+        terms = batch * int(torch.bincount(where[where >= 0]).max())
+        base._inside(outs[0], want, terms * U * mass, "grad_table")
