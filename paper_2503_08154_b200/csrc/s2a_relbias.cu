@@ -25,6 +25,8 @@
 // outweighs the add), eight rows ahead in forward (spills, 33 us), rows asked for in L2 before the forward kernel's look-up (no gain).
 #include <math.h>
 
+#include <numeric>
+
 #include "s2a_launch.h"
 #include "s2a_oct.cuh"
 
@@ -777,17 +779,54 @@ cudaError_t launch_relbias_bwd(int dt, int wdt, const void* g, const int32_t* bu
                            n_buckets, heads, grad_table, wdt);
 }
 
+// A product of at most kMaxBuckets / 2 whole numbers below 2^32, exactly: words, low ones first.
+struct WholeProduct {
+  uint32_t words = 1, w[kMaxBuckets / 2];
+  WholeProduct() { w[0] = 1; }
+  void times(uint32_t f) {
+    uint64_t carry = 0;
+    for (uint32_t i = 0; i < words; ++i) {
+      carry += (uint64_t)w[i] * f;
+      w[i] = (uint32_t)carry;
+      carry >>= 32;
+    }
+    if (carry) w[words++] = (uint32_t)carry;
+  }
+  bool at_least(const WholeProduct& o) const {
+    if (words != o.words) return words > o.words;
+    for (uint32_t i = words; i-- > 0;)
+      if (w[i] != o.w[i]) return w[i] > o.w[i];
+    return true;
+  }
+};
+
+// Whether n >= e (m / e)^(j / w) for 0 < j < w: n^w >= e^(w - j) m^j, the fraction in lowest terms.
+static bool reaches(uint32_t n, uint32_t e, uint32_t m, uint32_t j, uint32_t w) {
+  const uint32_t f = (uint32_t)std::gcd(j, w);
+  j /= f;
+  w /= f;
+  WholeProduct left, right;
+  for (uint32_t i = 0; i < w; ++i) {
+    left.times(n);
+    right.times(i < j ? m : e);
+  }
+  return left.at_least(right);
+}
+
 // The bucket of a distance, on the host.  Buckets of short distances hold one distance each; past max_exact (half of a
 // side's buckets) they widen geometrically up to max_distance: bucket max_exact + j starts at the smallest n with
-// n >= max_exact (max_distance / max_exact)^(j / (side - max_exact)).  The power is taken in long double, and a value that
-// lies within its rounding of a whole number counts as that number (8 * 16^(2/4) is 32, not the next double above it).
+// n >= max_exact (max_distance / max_exact)^(j / (side - max_exact)).  The power is taken in long double, off by less than 3e-18 of
+// itself (a few roundings of 2^-64, of which that of the exponent counts up to 21 times).  Where a whole number is within 1e-17, whole
+// numbers decide: borders that are whole themselves (8 * 16^(2/4) is 32), and those that lie just above one (with 256 buckets of
+// one distance, 256 wide ones and max_distance 1,073,822,369, border 223 is 6e-8 above 150,392,436).
 void log_buckets(int32_t* out, int64_t first, uint64_t count, uint32_t n_buckets, uint32_t max_distance, bool bidirectional) {
   const uint32_t side = bidirectional ? n_buckets / 2 : n_buckets, exact = side / 2, wide = side - exact;
   const auto start = [=](uint32_t u) -> int64_t {  // the smallest n of bucket u of a side; beyond the last, no end
     if (u <= exact) return u;
     if (u >= side) return INT64_MAX;
     const long double v = exact * powl((long double)max_distance / exact, (long double)(u - exact) / wide), near = roundl(v);
-    return (int64_t)(fabsl(v - near) <= 1e-15L * v ? near : ceill(v));
+    if (fabsl(v - near) > 1e-17L * v) return (int64_t)ceill(v);
+    return (int64_t)near + (reaches((uint32_t)near, exact, max_distance, u - exact, wide) ? 0 : 1);
   };
   const int64_t end = first + (int64_t)count;  // distances first .. end - 1, d = k - q
   for (uint32_t u = 0; u < side; ++u) {

@@ -2,6 +2,7 @@
 (all of them before any launch, so they are safe without a device), the dropout threshold, and the bucket of a distance
 against whole-number arithmetic."""
 import ctypes
+import math
 import os
 import re
 
@@ -166,6 +167,36 @@ def test_distance_buckets(lib, n_buckets, max_distance, bidirectional):
     for lo, m in ((-3, 7), (1, 5), (max_distance - 2, 4), (-max_distance, 1), (0, 1), (5, 0)):
         got = binding.log_buckets(lo, m, n_buckets, max_distance, bidirectional)
         assert got.tolist() == [_bucket(d, n_buckets, max_distance, bidirectional) for d in range(lo, lo + m)]
+
+
+@pytest.mark.parametrize("n_buckets,max_distance,j,n",
+                         [(512, 1073822369, 223, 150392436), (512, 1074060938, 222, 141722813), (32768, 2147483647, 16383, 2145937485)])
+def test_distance_buckets_where_a_border_is_almost_a_whole_number(lib, n_buckets, max_distance, j, n):
+    """Border j of the first two lies 5.8e-8 and 4.8e-8 above n, within 1e-15 of it: n is still in the bucket before.  The last is the
+    largest table's last border, the nearest distances to it."""
+    for k in range(-2, 3):
+        got = binding.log_buckets(-(n + k), 1, n_buckets, max_distance, False)
+        assert got.tolist() == [_bucket_at(n + k, n_buckets, max_distance, j)], k
+
+
+def _bucket_at(n, n_buckets, max_distance, j):
+    """`_bucket` for one side and an n known to lie by border j: which side of it n is on, in whole numbers."""
+    e = n_buckets // 2
+    w = n_buckets - e
+    f = math.gcd(j, w)          # n >= e (m / e)^(j / w), with the fraction in lowest terms
+    j, w = j // f, w // f
+    return e + j * f - (0 if n ** w >= e ** (w - j) * max_distance ** j else 1)
+
+
+@pytest.mark.parametrize("n_buckets,max_distance,bidirectional", [(128, 64 * 4 ** 12, False), (32, 8 * 3 ** 8, True), (96, 48 * 5 ** 6, False), (64, 18 * 32, False)])
+def test_distance_buckets_where_borders_are_whole_numbers(lib, n_buckets, max_distance, bidirectional):
+    side = n_buckets // 2 if bidirectional else n_buckets
+    e = side // 2
+    for j in range(1, side - e):
+        near = round(e * (max_distance / e) ** (j / (side - e)))
+        first = near - 3
+        got = binding.log_buckets(-(first + 6), 7, n_buckets, max_distance, bidirectional).tolist()
+        assert got == [_bucket(-n, n_buckets, max_distance, bidirectional) for n in range(first + 6, first - 1, -1)], j
 
 
 def test_distance_bucket_refusals(lib):
