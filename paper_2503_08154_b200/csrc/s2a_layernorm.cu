@@ -547,38 +547,44 @@ __global__ void __launch_bounds__(kReduceWarps * 32) norm_reduce_kernel(const fl
 }
 
 // ---------------------------------------------------------------- rows too long for registers
-// A CTA of 512 threads walks a row three times (sum; squared deviations; output), element by element.
+// A CTA of 512 threads walks a row three times (sum; squared deviations; output), element by element.  A thread may have four million
+// terms of a row: their sums are held in 64 bits, as terms that are alike would all be rounded the same way in 32 (30,000,001
+// bfloat16 elements about 1.1: the variance was off by 1.6e-4 of itself).  Four CTAs on an SM in forward: [2048, 20000] bfloat16 87 us
+// (1.9 TB/s) against 115 with three (40 registers a thread); backward is as fast with three where the rows are few
+// ([64, 65537] 39 us against 43), 130 us (1.9 TB/s) on [2048, 20000], 240 us with the weights' gradients.  The loads are single
+// elements, and a row comes from L2 in all passes but the first.
 constexpr int kLongThreads = 512;
 
-__device__ __forceinline__ float cta_sum(float v, float* buf) {
-  v = warp_sum(v);
+__device__ __forceinline__ double cta_sum(double v, double* buf) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
   __syncthreads();
   if (threadIdx.x % 32 == 0) buf[threadIdx.x / 32] = v;
   __syncthreads();
-  float t = 0.0f;
+  double t = 0.0;
 #pragma unroll
   for (int w = 0; w < kLongThreads / 32; ++w) t += buf[w];
   return t;
 }
 
 template <int DT>
-__global__ void __launch_bounds__(kLongThreads) norm_fwd_long_kernel(NormArgs a) {
+__global__ void __launch_bounds__(kLongThreads, 4) norm_fwd_long_kernel(NormArgs a) {
   using T = typename Io<DT>::T;
-  __shared__ float buf[kLongThreads / 32];
+  __shared__ double buf[kLongThreads / 32];
   enter_grid();
   const uint32_t L = a.row_len;
   for (uint64_t r = blockIdx.x; r < a.n_rows; r += gridDim.x) {
     const T* x = (const T*)a.x + r * a.x_stride;
     T* y = (T*)a.out + r * a.out_stride;
-    float s = 0.0f;
+    double s = 0.0;
     for (uint32_t c = threadIdx.x; c < L; c += kLongThreads) s += Io<DT>::widen(x[c]);
-    const float mean = cta_sum(s, buf) / (float)L;
-    s = 0.0f;
+    const float mean = (float)(cta_sum(s, buf) / L);
+    s = 0.0;
     for (uint32_t c = threadIdx.x; c < L; c += kLongThreads) {
       const float d = Io<DT>::widen(x[c]) - mean;
       s += d * d;
     }
-    const float rstd = __frsqrt_rn(cta_sum(s, buf) / (float)L + a.eps);
+    const float rstd = __frsqrt_rn((float)(cta_sum(s, buf) / L) + a.eps);
     if (a.stats_out && threadIdx.x == 0) ((float2*)a.stats_out)[r] = make_float2(mean, rstd);
     for (uint32_t c = threadIdx.x; c < L; c += kLongThreads) {
       const float gm = a.gamma ? load_param(a.gamma, c, a.wdt) : 1.0f, bt = a.beta ? load_param(a.beta, c, a.wdt) : 0.0f;
@@ -590,7 +596,7 @@ __global__ void __launch_bounds__(kLongThreads) norm_fwd_long_kernel(NormArgs a)
 template <int DT>
 __global__ void __launch_bounds__(kLongThreads) norm_bwd_long_kernel(NormArgs a) {
   using T = typename Io<DT>::T;
-  __shared__ float buf[kLongThreads / 32];
+  __shared__ double buf[kLongThreads / 32];
   enter_grid();
   const uint32_t L = a.row_len;
   for (uint64_t r = blockIdx.x; r < a.n_rows; r += gridDim.x) {
@@ -598,13 +604,13 @@ __global__ void __launch_bounds__(kLongThreads) norm_bwd_long_kernel(NormArgs a)
     const T* g = (const T*)a.g + r * a.g_stride;
     T* out = (T*)a.out + r * a.out_stride;
     const float2 st = ((const float2*)a.stats_in)[r];
-    float s1 = 0.0f, s2 = 0.0f;
+    double s1 = 0.0, s2 = 0.0;
     for (uint32_t c = threadIdx.x; c < L; c += kLongThreads) {
       const float w = Io<DT>::widen(g[c]) * (a.gamma ? load_param(a.gamma, c, a.wdt) : 1.0f);
       s1 += w;
-      s2 += w * ((Io<DT>::widen(x[c]) - st.x) * st.y);
+      s2 += w * (Io<DT>::widen(x[c]) - st.x);
     }
-    const float m1 = cta_sum(s1, buf) / (float)L, m2 = cta_sum(s2, buf) / (float)L;
+    const float m1 = (float)(cta_sum(s1, buf) / L), m2 = (float)(cta_sum(s2, buf) * st.y / L);
     for (uint32_t c = threadIdx.x; c < L; c += kLongThreads) {
       const float w = Io<DT>::widen(g[c]) * (a.gamma ? load_param(a.gamma, c, a.wdt) : 1.0f);
       const float xhat = (Io<DT>::widen(x[c]) - st.x) * st.y;

@@ -1,8 +1,8 @@
-"""Layer norm over many rows of every team width.
+"""Layer norm over many rows of every team width, and over rows of tens of millions of elements.
 
 Tolerances are those of test_block_layers_gpu.py, with the additions that a term passes through counted for the rows at hand:
 a column's sum over n rows by T teams of one CTA each at least has ceil(n / T) in a thread, T per CTA <= 32, at most 444 / 32 + 1
-partials and 5 shuffle steps."""
+partials and 5 shuffle steps; a long row's sums are held in 64 bits, and rounded to binary32 once."""
 import math
 
 import pytest
@@ -63,3 +63,16 @@ def test_norm_rings_are_refilled(lanes, L, dtype):
     s2a.s2a_layernorm_fwd(x, gamma, beta, x, again, L, 1e-6)
     base._done()
     assert torch.equal(x, y) and torch.equal(again, stats)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_norm_of_rows_of_tens_of_millions(dtype, monkeypatch):
+    """A thread has some sixty thousand terms of a row.  Of one sign and nearly alike, as here, they would all be rounded the same way
+    in a binary32 sum."""
+    rows, L, dt = 3, 30_000_001, base.DT[dtype]
+    x = (1.1 + base._normal((rows, L), torch.float32, "x", L) * 2.0 ** -6).to(dt)
+    x[2] = 1.1
+    g = (1.7 + base._normal((rows, L), torch.float32, "g", L) * 2.0 ** -6).to(dt)
+    monkeypatch.setattr(base, "_depth", lambda row_len: 4)   # a sum's rounding and those of its terms
+    _, stats = base._check_norm_fwd(x, None, None, L)
+    base._check_norm_bwd(g, x, None, stats, L)
