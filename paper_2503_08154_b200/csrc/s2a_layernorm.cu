@@ -11,7 +11,7 @@
 // thread copies its own pieces into a ring of STAGES rows in shared memory (cp.async), so the bytes in flight do not cost
 // registers, and since it reads back only what it copied itself the ring needs no barrier.  The variance is taken around
 // the mean (no difference of squares); the warps of a row merge (count, mean, squared deviations) with one exchange (Chan,
-// Golub and LeVeque's pairwise update).  All sums are binary32.
+// Golub and LeVeque's pairwise update).  All sums are binary32, but for those of rows beyond 16384 elements.
 //
 // Rows need not start on a 16-byte boundary.  A row's first element then sits s elements into a vector, pieces are the
 // vectors of the memory (piece v holds V columns from V v - s on), and the two at the row's ends are masked (EDGE).  A team keeps
@@ -249,6 +249,14 @@ __device__ __forceinline__ float lanes_sum(float v) {
   return v;
 }
 
+// sum / count, given 1 / count.  For bfloat16 rows what the product lacks of the sum is added, which makes the mean of a row of one
+// value that value (the sum of up to 16384 of 8 bits each is exact, and so is the quotient).  Binary32 rows have a rule of their own.
+template <int DT>
+__device__ __forceinline__ float mean_of(float sum, float count, float inv_count) {
+  const float q = sum * inv_count;
+  return DT == kBF16 ? fmaf(fmaf(-q, count, sum), inv_count, q) : q;
+}
+
 template <int LANES>
 __device__ __forceinline__ void team_barrier(uint32_t team) {
   if (LANES > 32) asm volatile("bar.sync %0, %1;" ::"r"(team + 1), "n"(LANES) : "memory");
@@ -336,30 +344,65 @@ __global__ void __launch_bounds__(threads_of(LANES), fwd_ctas(DT, EDGE, NO, LANE
       fetch<DT, EDGE, NO, LANES, THREADS>(slot, a.x, r + STAGES * step, a.x_stride, lane, L, s, false);
     copy_commit();
     stage = stage + 1 == STAGES ? 0 : stage + 1;
-    float mean = lanes_sum<GROUP>(f2_sum(sum)) * inv_count;
-    F2 sq = f2_both(0.0f);
+    float mean = mean_of<DT>(lanes_sum<GROUP>(f2_sum(sum)), WARPS > 1 ? count : (float)L, inv_count), dev;
+    // v - by, and the sum of its squares over the lanes of a warp
+    const auto centre = [&](float by) {
+      F2 sq = f2_both(0.0f);
 #pragma unroll
-    for (int j = 0; j < NP; ++j) {
-      const int c = piece_column<DT, LANES>(j, lane, s);
-      if (j >= kSure<DT, NO> && c >= L) continue;
+      for (int j = 0; j < NP; ++j) {
+        const int c = piece_column<DT, LANES>(j, lane, s);
+        if (j >= kSure<DT, NO> && c >= L) continue;
 #pragma unroll
-      for (int i = 0; i < PAIRS; ++i) v[j][i] = f2_sub(v[j][i], f2_both(mean));
-      if (EDGE && (j == 0 || j >= kSure<DT, NO>)) mask_ends<DT>(v[j], c, L);  // elements outside the row have no deviation
+        for (int i = 0; i < PAIRS; ++i) v[j][i] = f2_sub(v[j][i], f2_both(by));
+        if (EDGE && (j == 0 || j >= kSure<DT, NO>)) mask_ends<DT>(v[j], c, L);  // elements outside the row have no deviation
 #pragma unroll
-      for (int i = 0; i < PAIRS; ++i) sq = f2_fma(v[j][i], v[j][i], sq);
-    }
-    float dev = lanes_sum<GROUP>(f2_sum(sq)), shift = 0.0f;  // v holds x - mean, or x - mean of the warp: `shift` more
+        for (int i = 0; i < PAIRS; ++i) sq = f2_fma(v[j][i], v[j][i], sq);
+      }
+      return lanes_sum<GROUP>(f2_sum(sq));
+    };
+    dev = centre(mean);
     if (WARPS > 1) {
       if (lane % 32 == 0) merge[parity][team][lane / 32] = make_float4(mean, dev, count, 0.0f);
-      // the two buffers alternate: a warp writes one of them again only after the next row's barrier, which every
-      // warp of the team reaches after it has read this row's values
+      // the two buffers alternate: a warp writes one of them again only after the next barrier (of the next row, or below), which
+      // every warp of the team reaches after it has read this row's values
       team_barrier<LANES>(team);
       const float4 m = merge[parity][team][lane % WARPS];
-      shift = mean;
-      mean = lanes_sum<WARPS>(m.z * m.x) * inv_l;
+      float shift = mean;  // from x - mean of the warp to x - mean
+      mean = mean_of<DT>(lanes_sum<WARPS>(m.z * m.x), (float)L, inv_l);
       shift -= mean;
       dev = lanes_sum<WARPS>(m.y + m.z * (m.x - mean) * (m.x - mean));
       parity ^= 1;
+#pragma unroll
+      for (int j = 0; j < NP; ++j)
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) v[j][i] = f2_add(v[j][i], f2_both(shift));
+    }
+    // A binary32 row whose mean is large beside its spread, 64 times or more: the mean's rounding, no longer small beside the spread
+    // (and all there is, in a row of one value), is the mean of the deviations from it, and is taken out of them.  bfloat16 rows
+    // need it not (mean_of; and two neighbouring values are 2^-8 apart).  It costs the binary32 rows some 3 %.
+    const bool far = dev * inv_l + a.eps < mean * mean * 0x1p-12f;
+    if (DT == kF32 && __builtin_expect(LANES < 32 ? __any_sync(0xffffffffu, far) != 0 : far, 0)) {
+      const auto team_sum = [&](float t) {  // of the warps' sums
+        if (WARPS > 1) {
+          if (lane % 32 == 0) merge[parity][team][lane / 32].x = t;
+          team_barrier<LANES>(team);
+          t = lanes_sum<WARPS>(merge[parity][team][lane % WARPS].x);
+          parity ^= 1;
+        }
+        return t;
+      };
+      F2 rest = f2_both(0.0f);
+#pragma unroll
+      for (int j = 0; j < NP; ++j) {
+        const int c = piece_column<DT, LANES>(j, lane, s);
+        if (j >= kSure<DT, NO> && c >= L) continue;
+        if (EDGE && WARPS > 1 && (j == 0 || j >= kSure<DT, NO>)) mask_ends<DT>(v[j], c, L);
+#pragma unroll
+        for (int i = 0; i < PAIRS; ++i) rest = f2_add(rest, v[j][i]);
+      }
+      const float lean = team_sum(lanes_sum<GROUP>(f2_sum(rest))) * inv_l;
+      dev = team_sum(centre(lean));
+      mean += lean;
     }
     const float rstd = __frsqrt_rn(dev * inv_l + a.eps);
     if (LANES < 32 && r >= a.n_rows) continue;
@@ -371,7 +414,7 @@ __global__ void __launch_bounds__(threads_of(LANES), fwd_ctas(DT, EDGE, NO, LANE
       if (j >= kSure<DT, NO> && c >= L) continue;
 #pragma unroll
       for (int i = 0; i < PAIRS; ++i)
-        v[j][i] = f2_fma(f2_mul(WARPS > 1 ? f2_add(v[j][i], f2_both(shift)) : v[j][i], f2_both(rstd)), gamma[j][i], beta[j][i]);
+        v[j][i] = f2_fma(f2_mul(v[j][i], f2_both(rstd)), gamma[j][i], beta[j][i]);
       put_piece<DT, EDGE>(out, c, L, j > 0 && j < kSure<DT, NO>, EDGE && a.out_apart, v[j]);
     }
   }
@@ -578,17 +621,18 @@ __global__ void __launch_bounds__(kLongThreads, 4) norm_fwd_long_kernel(NormArgs
     T* y = (T*)a.out + r * a.out_stride;
     double s = 0.0;
     for (uint32_t c = threadIdx.x; c < L; c += kLongThreads) s += Io<DT>::widen(x[c]);
-    const float mean = (float)(cta_sum(s, buf) / L);
+    const double exact = cta_sum(s, buf) / L;
+    const float mean = (float)exact, lean = (float)(exact - mean);  // NaN where the mean is infinite, as x - mean is
     s = 0.0;
     for (uint32_t c = threadIdx.x; c < L; c += kLongThreads) {
       const float d = Io<DT>::widen(x[c]) - mean;
       s += d * d;
     }
-    const float rstd = __frsqrt_rn((float)(cta_sum(s, buf) / L) + a.eps);
+    const float rstd = __frsqrt_rn((float)(cta_sum(s, buf) / L - (double)lean * lean) + a.eps);
     if (a.stats_out && threadIdx.x == 0) ((float2*)a.stats_out)[r] = make_float2(mean, rstd);
     for (uint32_t c = threadIdx.x; c < L; c += kLongThreads) {
       const float gm = a.gamma ? load_param(a.gamma, c, a.wdt) : 1.0f, bt = a.beta ? load_param(a.beta, c, a.wdt) : 0.0f;
-      y[c] = Io<DT>::narrow(fmaf((Io<DT>::widen(x[c]) - mean) * rstd, gm, bt));
+      y[c] = Io<DT>::narrow(fmaf(((Io<DT>::widen(x[c]) - mean) - lean) * rstd, gm, bt));
     }
   }
 }

@@ -76,3 +76,59 @@ def test_norm_of_rows_of_tens_of_millions(dtype, monkeypatch):
     monkeypatch.setattr(base, "_depth", lambda row_len: 4)   # a sum's rounding and those of its terms
     _, stats = base._check_norm_fwd(x, None, None, L)
     base._check_norm_bwd(g, x, None, stats, L)
+
+
+def _centred_exact(x, gamma, beta, eps):
+    """The forward pass where a row's mean may be far larger than its spread.
+
+    Binary32: with m = D u max|x| the error of a first mean, s the mean and S the mean square of |x - mean|: the deviations from that first
+    mean are rounded once, and their own mean, which takes the error out again, is off by e = (D + 3) u (s + m).  That is done where the
+    mean is 64 times the spread or more (to be sure of that: 128 times as large as any deviation); elsewhere m stays as well.
+    bfloat16, rows of one sign and of values within a factor of two of each other: a sum of up to 2^15 of them has at most 8 + 15 + 1
+    bits and is exact, so that the first mean is off by its own two roundings, m = 2 u |mean|, and e = (D + 3) u s + m.
+    x - mean is off by e and three roundings; the variance by (D + 4) u (S + m^2) from its sum, and by 2 m e + e^2 + 4 u m^2 from the
+    square of what the mean is off."""
+    bf16 = x.dtype == torch.bfloat16
+    x, gm, bt = x.double(), gamma.double(), beta.double()
+    mean = x.mean(1, keepdim=True)
+    dev = x - mean
+    var = (dev ** 2).mean(1, keepdim=True)
+    rstd = (var + eps) ** -0.5
+    xhat = dev * rstd
+    y = xhat * gm + bt
+    D = 80 if x.shape[1] <= 16384 else 4
+    m = D * U * x.abs().amax(1, keepdim=True)
+    far = mean ** 2 > 2.0 ** 14 * (dev.abs().amax(1, keepdim=True) ** 2 + eps)
+    if bf16:
+        m = torch.where(far, 2 * U * mean.abs(), m)
+    e = (D + 3) * U * (dev.abs().mean(1, keepdim=True) + m)
+    e = torch.where(far & (not bf16), e, e + m)
+    spread = ((D + 4) * U * (var + m ** 2) + 2 * m * e + e ** 2 + 4 * U * m ** 2) / (var + eps)
+    tol = gm.abs() * rstd * (e + 3 * U * (dev.abs() + m)) + (gm * xhat).abs() * (spread / 2 + spread ** 2 + 4 * U) \
+        + U * ((gm * xhat).abs() + bt.abs() + y.abs())
+    if bf16:    # of one value: beta, exactly
+        tol = torch.where((dev == 0).all(1, keepdim=True), U * bt.abs(), tol)
+    return y, mean, rstd, tol, e + 2 * U * mean.abs(), rstd * (spread / 2 + spread ** 2 + 4 * U)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("L", [24, 63, 100, 197, 255, 500, 768, 1000, 1025, 2560, 3001, 5000, 10000, 12281, 20000])
+def test_norm_of_rows_far_from_zero(L, dtype):
+    """Rows of one value give beta, whatever the value: the mean's rounding must not become a deviation.  A small spread on a large mean
+    keeps the accuracy of the spread."""
+    dt = base.DT[dtype]
+    x = base._normal((10, L), torch.float32, "x", L)
+    for r, v in enumerate((1e4, 12345.678, -1e6 / 3, 0.1, 0.0)):
+        x[r] = v
+    x[5] += 1e4
+    x[6] = x[6] * 1e-2 + 1e4
+    x[7] += 1e6
+    x[8] = 3.0
+    x[8, L // 2] = 4.0
+    x = x.to(dt)
+    gamma, beta = base._normal((L,), torch.float32, "gamma", L), base._normal((L,), torch.float32, "beta", L)
+    y, stats = base._norm_fwd(x, gamma, beta, L)
+    want, mean, rstd, tol, tm, tr = _centred_exact(x, gamma, beta, 1e-6)
+    base._inside(y, want, tol + HALF[dt] * (want.abs() + tol), "y")
+    base._inside(stats[:, :1], mean, tm, "mean")
+    base._inside(stats[:, 1:], rstd, tr, "rstd")
