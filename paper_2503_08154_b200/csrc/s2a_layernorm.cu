@@ -400,7 +400,8 @@ __global__ void __launch_bounds__(threads_of(LANES), fwd_ctas(DT, EDGE, NO, LANE
 #pragma unroll
         for (int i = 0; i < PAIRS; ++i) rest = f2_add(rest, v[j][i]);
       }
-      const float lean = team_sum(lanes_sum<GROUP>(f2_sum(rest))) * inv_l;
+      float lean = team_sum(lanes_sum<GROUP>(f2_sum(rest))) * inv_l;
+      if (!far) lean = 0.0f;  // another row of the warp: this one keeps its bits
       dev = team_sum(centre(lean));
       mean += lean;
     }

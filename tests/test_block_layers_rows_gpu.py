@@ -132,3 +132,31 @@ def test_norm_of_rows_far_from_zero(L, dtype):
     base._inside(y, want, tol + HALF[dt] * (want.abs() + tol), "y")
     base._inside(stats[:, :1], mean, tm, "mean")
     base._inside(stats[:, 1:], rstd, tr, "rstd")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("lanes,L", [(lanes, L) for lanes, even, odd in TEAMS for L in (even, odd)] + [(512, 20000)])
+def test_norm_rows_far_from_zero_among_others(lanes, L, dtype):
+    """Every third row is far from zero.  The others must get the bits that they get without them, and the far rows theirs, in place too,
+    over several rows of every team."""
+    dt, rows = base.DT[dtype], _every_team_refills(lanes) if L < 16384 else 30
+    plain = base._normal((rows, L), torch.float32, "x", rows, L)
+    x = plain.clone()
+    x[1::3] = x[1::3] * 1e-2 + 1e4
+    x[4::9] = 12345.678
+    x, plain = x.to(dt), plain.to(dt)
+    gamma, beta = base._normal((L,), torch.float32, "gamma", L), base._normal((L,), torch.float32, "beta", L)
+    y, stats = base._norm_fwd(x, gamma, beta, L)
+    alone, alone_stats = base._norm_fwd(plain, gamma, beta, L)
+    other = torch.ones(rows, dtype=torch.bool, device="cuda")
+    other[1::3] = False
+    assert torch.equal(y[other], alone[other]) and torch.equal(stats[other], alone_stats[other])
+    far = x[~other]
+    want, mean, rstd, tol, tm, tr = _centred_exact(far, gamma, beta, 1e-6)
+    base._inside(y[~other], want, tol + HALF[dt] * (want.abs() + tol), "y")
+    base._inside(stats[~other][:, :1], mean, tm, "mean")
+    base._inside(stats[~other][:, 1:], rstd, tr, "rstd")
+    again = torch.empty_like(stats)
+    s2a.s2a_layernorm_fwd(x, gamma, beta, x, again, L, 1e-6)
+    base._done()
+    assert torch.equal(x, y) and torch.equal(again, stats)
