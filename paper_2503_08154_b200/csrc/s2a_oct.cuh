@@ -11,7 +11,6 @@ namespace s2a {
 template <int DT> struct Eight;
 template <> struct Eight<kBF16> {
   uint4 r;
-  __device__ __forceinline__ void zero() { r = make_uint4(0, 0, 0, 0); }
   __device__ __forceinline__ void load(const void* p) { r = *(const uint4*)p; }
   __device__ __forceinline__ void store(void* p) const { *(uint4*)p = r; }
   __device__ __forceinline__ void get(F2* v) const {
@@ -26,7 +25,6 @@ template <> struct Eight<kBF16> {
 };
 template <> struct Eight<kF32> {
   float4 a, b;
-  __device__ __forceinline__ void zero() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
   __device__ __forceinline__ void load(const void* p) { a = ((const float4*)p)[0]; b = ((const float4*)p)[1]; }
   __device__ __forceinline__ void store(void* p) const { ((float4*)p)[0] = a; ((float4*)p)[1] = b; }
   __device__ __forceinline__ void get(F2* v) const {
