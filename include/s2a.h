@@ -250,10 +250,10 @@ int s2a_lrp_fwd(const void* x, const float* A, const float* B, void* y, size_t b
 /* ---- The layers between the stash kernels of a transformer block --------------------------
  * Layer norm, dropout and the bucketed relative position bias, with their backward passes.
  * They belong to no equation of the paper; they are here because a block's remaining layers
- * would otherwise keep for backward what the stash saves: of these, layer norm keeps 8 bytes
- * a row and the other two keep nothing.  The conventions at the top hold, but for what is said
+ * would otherwise keep for backward what the stash saves: of these, layer norm keeps its input x and
+ * 8 bytes a row (no normalised copy), and the other two keep nothing (no mask, no bias map).  The conventions at the top hold, but for what is said
  * here.  `wdt` is the element type of learned parameters and of their gradients (S2A_F32 or
- * S2A_BF16, whatever dt is).  Sums are binary32 and in a fixed order: no atomics, so a call
+ * S2A_BF16, whatever dt is).  Sums are binary32 or wider and in a fixed order: no atomics, so a call
  * repeated on the same inputs writes the same bits.  Non-finite inputs are allowed and go where
  * the formulas take them.
  *
@@ -279,7 +279,8 @@ size_t s2a_layernorm_scratch_bytes(size_t n_rows, size_t row_len);
  * alike on the 16-byte grid are read in whole vectors, fastest where rows begin and end on it.
  * Rows of which one tensor's lie differently on the grid from x's are taken element by element in
  * that tensor.  y_stride must be at least row_len; the bytes between rows are not touched.
- * x_stride is free (0 repeats one row).  eps: finite, not negative.  An output whose rows
+ * x_stride is free (0 repeats one row).  A row whose mean is large beside its spread is centred to
+ * the spread's accuracy: rows of one value give beta to rounding, whatever the value.  eps: finite, not negative.  An output whose rows
  * overlap x's rows without being the same rows returns S2A_ERR_OVERLAP (rows of one stride may
  * interleave); gamma, beta and stats must not overlap an output (not checked).
  */
@@ -312,8 +313,8 @@ uint32_t s2a_dropout_threshold(double p);
  * Philox4x32-10 under key rng[0] (low word first) at counter (e / 8, rng[1] + site) (two 64-bit
  * numbers, low words first); of the four output words, word w holds element 2w of the eight in its
  * low half and element 2w + 1 in its high half.  The element is kept when its bits are at least
- * T = s2a_dropout_threshold(p) and then scaled by 65536 / (65536 - T) (binary32), which makes
- * the expectation x exactly; a dropped element counts as 0 whatever it holds.  T = 65536 drops
+ * T = s2a_dropout_threshold(p) and then scaled by 65536 / (65536 - T), which makes the expectation
+ * x, up to the rounding of the scale to binary32 and of the result; a dropped element counts as 0 whatever it holds.  T = 65536 drops
  * everything.
  *   x         in   n_elems elements of type dt
  *   residual  in   n_elems elements of type dt, or NULL

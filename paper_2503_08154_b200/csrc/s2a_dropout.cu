@@ -15,8 +15,9 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kAhead = 2;          // vectors of a thread in flight
 constexpr int kResident = 5;       // CTAs of an SM
-// Four times as many CTAs as fit: the last ones even out what the SMs have left.  [200,000,003] bfloat16: 126 us (6.34 TB/s),
-// against 132 with exactly as many as fit, and 154 with one vector in flight; [64, 12, 197, 197]: 21.4, 21.7, 25.1 us.
+// Four times as many CTAs as fit: the last ones even out what the SMs have left.  [200,000,003] bfloat16: 126 us (6.34 TB/s; in long
+// runs, at lower clocks, up to 138 us), against 132 with exactly as many as fit, and 154 with one vector in flight; [64, 12, 197, 197]:
+// 21.4, 21.7, 25.1 us.
 constexpr int kCtasPerSm = 20;
 
 struct PhiloxKey {

@@ -21,11 +21,13 @@
 // of its team, a CTA adds its teams' sums in order and writes one pair of rows to the caller's scratch, and a second kernel
 // adds those in order: no atomics, the same bits on every run.
 //
-// What it measures on a B200 (6.57 TB/s copy rate): [12608, 768] bfloat16 forward 8.0 us (4.9 TB/s), backward with weights
-// 14.7 us (4.0 TB/s), without 10.8 us (5.4 TB/s); of these about 2 us are the launch, 1.4 us the first rows' way from memory,
-// and 3 us the second kernel of the weights' gradients.  [65536, 4096] backward 262 us (6.1 TB/s).  The first kernels,
-// with rows loaded into registers one at a time, took 17.3 and 49.8 us.  Odd row lengths cost instructions, not bytes: [4616, 1025] binary32 backward
-// 16.9 us (3.4 TB/s), [20000, 1025] bfloat16 forward 31 us (2.7 TB/s), half of the issue slots at 16 warps an SM.
+// What it measures on a B200 (6.57 TB/s copy rate): [12608, 768] bfloat16 forward 8.0 us (4.8 TB/s), backward with weights
+// 14.6 us (4.0 TB/s), without 10.8 us (5.4 TB/s); of these about 2 us are the launch, 1.4 us the first rows' way from memory,
+// and 3 us the second kernel of the weights' gradients.  [65536, 4096] backward 263 us (6.1 TB/s) in short runs, 291 to 307 us (5.2 to 5.5 TB/s) in
+// long ones, where the clocks are lower.  The first kernels, with rows loaded into registers one at a time, took 17.3 us (forward) and 49.8 us
+// (backward) on [12608, 768].  Rows off the 16-byte grid cost instructions, not bytes (half of the issue slots at 16 warps an SM): the masks of their ends
+// are compared anew in every row, and one lane stores an end's elements one by one while its warp waits.  [4616, 1025] binary32 backward
+// 16.8 us (3.4 TB/s), [20000, 1025] bfloat16 forward 30.6 us (2.7 TB/s).
 #include "s2a_launch.h"
 #include "s2a_oct.cuh"
 
@@ -56,7 +58,8 @@ template <int DT, int NO> constexpr int kPieces = NO * 8 / kVec<DT>;  // pieces 
 __host__ __device__ constexpr int threads_of(int lanes) { return lanes > 256 ? lanes : 256; }
 // CTAs of the forward kernel on an SM.  Three of them hide the meeting of a row's warps better where their registers (80 a
 // thread) suffice without spills: [65536, 4096] bfloat16 193 us against 199 with two and 242 with four; in binary32, with half
-// the elements to a byte, two are ahead ([12608, 2048] 38.4 us against 39.7).
+// the elements to a byte, two are ahead ([12608, 2048] 38.4 us against 39.7).  The widest teams, of 12289 elements on, spill (up to 172 bytes a
+// thread off the grid, at the 128 registers that 512 threads leave): [8192, 16384] bfloat16 91 us (5.9 TB/s), [8192, 16383] 292 us (1.8 TB/s).
 __host__ __device__ constexpr int fwd_ctas(int dt, bool edge, int no, int lanes) {
   return lanes > 256 ? 1 : (no == 1 ? 4 : (no == 2 && dt == kBF16 && !edge ? 3 : 2));
 }

@@ -17,10 +17,11 @@
 //
 // What it measures on a B200 (6.57 TB/s copy rate), bfloat16: [64, 12, 197, 197] under a map of 732 buckets, forward 25.0 us (4.8 TB/s:
 // 18 us of walking, which is the copy rate, after the look-up of the chunk's biases, and the launch), one sample of [16, 1025, 1025] 25 us
-// (2.9 TB/s: bias_fwd_few_kernel, bound by its instructions per element), backward 19.3 us (3.1 TB/s:
-// about 13 of walking, the rest setup, tables and the second kernel), one sample of [16, 1025, 1025] 100 us (the tables' turns); by
-// distance [64, 12, 197, 197] 28 us; [2, 16, 2048, 2048] by distance,
-// forward 106 us (5.1 TB/s), backward 53 us (5.1 TB/s).  Looking the bucket of every element up where it is added costs 200 us
+// (2.9 TB/s: bias_fwd_few_kernel, element by element: 24 instructions a warp and 32 elements, 58 % of the issue slots, and the wait for
+// the bucket before the bias), backward 19.3 us (3.1 TB/s: about 13 of walking, the rest setup, tables and the second kernel), one
+// sample of [16, 1025, 1025] 100 us (bias_bwd_few_kernel says why); by distance [64, 12, 197, 197] forward 38 us (4.1 TB/s), backward 28 us, [16, 16,
+// 577, 577] 81 us (4.2 TB/s) and 41 us, [2, 16, 2048, 2048] 106 us (5.1 TB/s) and 53 us (5.1 TB/s): a row of an odd width is cut in two
+// vectors, and its classes are all eight.  Looking the bucket of every element up where it is added costs 200 us
 // there.  Measured and not kept: the rows through a ring of cp.async as in layer norm (92 us: the bookkeeping of a row's place
 // outweighs the add), eight rows ahead in forward (spills, 33 us), rows asked for in L2 before the forward kernel's look-up (no gain).
 #include <math.h>
@@ -41,7 +42,12 @@ constexpr int kStaged = 5;                   // slots that a thread looks up at 
 // bias_fwd_few_kernel and bias_bwd_few_kernel.  Up to so many samples they are faster than the diagonals, beyond that not always.
 // Forward, [B, 12, 401, 401] bfloat16: B = 2: 8.4 us against 14.4, 4: 12.3 against 15.6, 8: 20.2 against 18.7; [1, 16, 1025, 1025] 25 against
 // 75.  Backward, the same: 2: 18 against 34, 4: 21 against 35, 8: 26 against 37; [64, 12, 197, 197] 27.5 against 19.3; [1, 16, 1025, 1025] 100
-// against 243.
+// against 243.  Backward with larger tables, of which fewer warps have one (16 at 2,601 buckets, 8 at 5,329, 4 at 9,025 to 11,264), windows of
+// 12 heads, bfloat16, one and eight samples: 2,601 buckets 29 us against 82 and 61 against 93; 5,329: 175 against 438 and 407 against
+// 502; 6,561: 343 against 574 and 799 against 645; 7,225: 412 against 1314 and 967 against 1440; 9,025: 934 against 1361 and 2142 against 1456; 10,609:
+// 1282 against 3899 and 2940 against 4084.  With 3 heads they are ahead everywhere (9,025 buckets: 246 against 529, 540 against 559), in binary32 up to
+// six samples.  So from 6,000 buckets on the border lies anywhere between two samples and beyond eight, with how the
+// diagonals' tables happen to fit an SM; eight loses up to 1.5 times there and wins up to 2.5 times.
 constexpr uint32_t kFewSamplesFwd = 4, kFewSamplesBwd = 8;
 constexpr uint32_t kFewThreads = 512, kFewPerSm = 2;  // four keys and three or four CTAs an SM: 28 to 30 us
 constexpr int kFewKeys = 8;                           // keys of a thread in flight
@@ -552,8 +558,10 @@ __global__ void __launch_bounds__(kMostThreads, 3) bias_bwd_kernel(BiasArgs a) {
 }
 
 // As bias_fwd_few_kernel: a warp takes 32 neighbouring keys at a time, adds the samples up and the sums into its own table.  It is
-// bound by the turns at that table, so as many warps run as have room for one (asking for the next keys ahead of the turns: no
-// gain).
+// bound by the chain of that addition, eight times in a row: shuffles, tag, look whether it is still there, add, each waiting for the
+// one before ([1, 16, 1024, 1024], 3969 buckets: 29 % of the issue slots, a warp waits 2.9 cycles for fixed latencies and 4.5 for memory, global and
+// shared, to each instruction).  So as many warps run as have room for a table (asking for the next keys ahead of the additions:
+// no gain).
 template <int DT>
 __global__ void __launch_bounds__(kFewThreads, kFewPerSm) bias_bwd_few_kernel(BiasArgs a) {
   using T = typename Io<DT>::T;
