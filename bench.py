@@ -16,7 +16,6 @@ from __future__ import annotations
 
 import argparse
 import ctypes
-import hashlib
 import json
 import os
 import statistics
@@ -31,6 +30,7 @@ ROOT = os.path.dirname(os.path.abspath(__file__))
 sys.path.insert(0, ROOT)
 
 from paper_2503_08154_b200 import synth  # noqa: E402
+from paper_2503_08154_b200.ncu_summary import kernel_source_digest  # noqa: E402
 
 KERNELS = ("softmax_fwd", "gelu_fwd", "gelu_bwd", "softmax_bwd")
 L2_BYTES = 126 * 1024 * 1024
@@ -168,14 +168,6 @@ def measured_peak():
         return float(json.load(open(path))["hbm_gbs"]), "measured"
     except Exception:
         return 6650.0, "fallback"
-
-
-def kernel_source_digest():
-    h = hashlib.sha256()
-    csrc = os.path.join(ROOT, "paper_2503_08154_b200", "csrc")
-    for name in sorted(os.listdir(csrc)):
-        h.update(open(os.path.join(csrc, name), "rb").read())
-    return h.hexdigest()[:16]
 
 
 def stored_traffic(kernel, workload):

@@ -54,3 +54,21 @@ def test_code_flip_count_accepts_flips_at_a_bin_edge_only():
     assert flips == 1
     if dist[near] <= 1e-5:       # within the slack every flip is granted, whatever the row's scale
         assert outside == 0
+
+
+def test_captured_traffic_outlives_changes_of_other_kernels(tmp_path):
+    """The DRAM bytes of a capture hold as long as the benchmarked kernels are those of the capture, and no longer."""
+    src = os.path.join(os.path.dirname(bench.__file__), "paper_2503_08154_b200", "csrc")
+    for name in os.listdir(src):
+        (tmp_path / name).write_bytes(open(os.path.join(src, name), "rb").read())
+    digest = bench.kernel_source_digest(str(tmp_path))
+    assert digest == bench.kernel_source_digest()
+    for name in ("s2a_layernorm.cu", "s2a_side.cu", "s2a_launch.h", "s2a_another.cu"):
+        with open(tmp_path / name, "a") as f:
+            f.write("// another operator\n")
+    assert bench.kernel_source_digest(str(tmp_path)) == digest
+    for name in ("s2a_common.cuh", "s2a_tile.cuh", "s2a_tile.cu", "s2a_tile_gelu_fwd.cu"):
+        before = bench.kernel_source_digest(str(tmp_path))
+        with open(tmp_path / name, "a") as f:
+            f.write("// changed\n")
+        assert bench.kernel_source_digest(str(tmp_path)) != before
