@@ -257,7 +257,9 @@ __device__ __forceinline__ float lanes_sum(float v) {
 template <int DT>
 __device__ __forceinline__ float mean_of(float sum, float count, float inv_count) {
   const float q = sum * inv_count;
-  return DT == kBF16 ? fmaf(fmaf(-q, count, sum), inv_count, q) : q;
+  if (DT == kF32) return q;
+  const float whole = fmaf(fmaf(-q, count, sum), inv_count, q);
+  return whole == whole ? whole : q;  // an infinite sum leaves no remainder
 }
 
 template <int LANES>

@@ -160,3 +160,22 @@ def test_norm_rows_far_from_zero_among_others(lanes, L, dtype):
     s2a.s2a_layernorm_fwd(x, gamma, beta, x, again, L, 1e-6)
     base._done()
     assert torch.equal(x, y) and torch.equal(again, stats)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("L", [5, 24, 63, 197, 768, 1000, 1025, 3001, 10000, 20000])
+def test_norm_statistics_of_infinite_rows(L, dtype):
+    """The mean of a row with an infinity is that infinity, of both it is NaN; the rows around it keep their bits."""
+    dt = base.DT[dtype]
+    plain = base._normal((6, L), dt, "x", L)
+    x = plain.clone()
+    x[1, L // 2] = float("inf")
+    x[2, L - 1] = float("-inf")
+    x[3, 0], x[3, L - 1] = float("inf"), float("-inf")
+    x[4, L // 3] = float("nan")
+    y, stats = base._norm_fwd(x, None, None, L)
+    alone, alone_stats = base._norm_fwd(plain, None, None, L)
+    assert float(stats[1, 0]) == float("inf") and float(stats[2, 0]) == float("-inf")
+    assert bool(torch.isnan(stats[3:5, 0]).all()) and bool(torch.isnan(stats[1:5, 1]).all()) and bool(torch.isnan(y[1:5]).all())
+    for r in (0, 5):
+        assert torch.equal(y[r], alone[r]) and torch.equal(stats[r], alone_stats[r])
