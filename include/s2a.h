@@ -66,7 +66,8 @@ typedef enum {
   S2A_ERR_DEVICE = 6, /* a kernel gave up on a bounded wait (see s2a_device_error) */
   S2A_ERR_TOO_LARGE = 7, /* beyond the built-in scratch of s2a_gelu_fwd_tensor_range_static */
   S2A_ERR_OVERLAP = 8, /* the output overlaps the input without being the same tensor  */
-  S2A_ERR_VALUE = 9   /* a scalar argument (eps, p, a distance) is outside its range   */
+  S2A_ERR_VALUE = 9,  /* a scalar argument (eps, p, a distance) is outside its range   */
+  S2A_ERR_MEMORY = 10 /* the host has no memory for a plan's checks                    */
 } s2a_status;
 
 /* Bytes of packed codes for n_elems elements: (n_elems + 1) / 2. */
@@ -376,6 +377,155 @@ int s2a_relbias_bwd(const void* grad_out, const int32_t* buckets, int by_distanc
  */
 int s2a_relbias_log_buckets(int32_t* buckets, int64_t first_distance, size_t count, size_t n_buckets, size_t max_distance,
                             int bidirectional);
+
+/* ---- Around the scores: rotary positions, and the norms of queries and keys -----------------
+ * Queries q and keys k (and what belongs to them) are tensors [batch, tokens, heads, head_dim] given by
+ * their strides, so that every order of the first three dimensions and slices of a packed buffer are
+ * taken as they are; the elements of a row of head_dim are contiguous.  One call serves both; heads_k = 0
+ * with NULL for the keys' tensors serves one alone.
+ *   strides  HOST memory: three numbers for each tensor, in the order of the call's tensors (queries and
+ *            keys alternate): elements from batch to batch, token to token, head to head.  Inputs may have
+ *            any, 0 included (then each row has its own output, or gradient); the rows of an output must
+ *            not overlap.  An output may be the input it belongs to (for the backward call of the norm:
+ *            the gradient or x), with the same strides; tensors inside one buffer may interleave.  Any
+ *            other overlap returns S2A_ERR_OVERLAP.  Pointers need the alignment of their element type
+ *            only; rows on the 16-byte grid, whose rot_dim / 2 and head_dim are whole 16-byte vectors too,
+ *            are the fastest.
+ *   table    (turn, axis) of each of the rot_dim / 2 pairs, two 64-bit words in DEVICE memory, 16-byte aligned:
+ *            turn = the pair's radians per position / (2 pi), as a binary fraction times 2^64, so that
+ *            the angle of any position is exact; axis: which of a token's positions it goes by (an axis
+ *            beyond the last counts as the last).  s2a_rope_table fills one.
+ *   positions  int32 in DEVICE memory, read when the kernel runs: that of (axis, batch, token) lies at
+ *            axis * pos_axis_stride + batch * pos_batch_stride + token (a stride of 0 shares them).  NULL,
+ *            with one axis: first + token.
+ *   rot_dim  the first rot_dim elements of a row turn, the rest stays: even, 2 .. head_dim; 0 (with table
+ *            NULL) for a norm without rotation.  Pairs are (i, i + rot_dim / 2), or (2 i, 2 i + 1) where `interleaved`.
+ *   scale    multiplies the cosines and sines (1 but for some scaled contexts): finite
+ * head_dim: 1 .. 512; heads: at most 65535 each; batch * tokens at most 2^31-1.
+ */
+
+/* Forward: with the angle w = position * frequency of its pair, (a, b) -> (a cos w - b sin w, a sin w + b cos w).
+ * Tensors, and strides[12] in this order: q, k, out_q, out_k. */
+int s2a_rope_fwd(const void* q, const void* k, void* out_q, void* out_k, const size_t* strides, const int32_t* positions,
+                 int64_t first, size_t pos_batch_stride, size_t pos_axis_stride, size_t axes, const uint64_t* table,
+                 size_t batch, size_t tokens, size_t heads_q, size_t heads_k, size_t head_dim, size_t rot_dim, int interleaved,
+                 float scale, int dt, void* cuda_stream);
+
+/* Backward: the gradients turn by the opposite angles (and are multiplied by the same scale).  Keeps nothing of the forward
+ * pass but the positions.  Tensors, and strides[12]: grad_q, grad_k, grad_in_q, grad_in_k. */
+int s2a_rope_bwd(const void* grad_q, const void* grad_k, void* grad_in_q, void* grad_in_k, const size_t* strides,
+                 const int32_t* positions, int64_t first, size_t pos_batch_stride, size_t pos_axis_stride, size_t axes,
+                 const uint64_t* table, size_t batch, size_t tokens, size_t heads_q, size_t heads_k, size_t head_dim,
+                 size_t rot_dim, int interleaved, float scale, int dt, void* cuda_stream);
+
+/* The norm of each head's row, and the rotation, in one pass: rstd = 1 / sqrt(sum(x^2) / head_dim + eps),
+ * out = rotation(x * rstd * gamma).  gamma_q, gamma_k: head_dim elements of type wdt, or NULL (ones).  Rows whose sum of squares
+ * is beyond binary32 become zeros.  Tensors, and strides[12]: q, k, out_q, out_k. */
+int s2a_qknorm_rope_fwd(const void* q, const void* k, const void* gamma_q, const void* gamma_k, void* out_q, void* out_k,
+                        const size_t* strides, const int32_t* positions, int64_t first, size_t pos_batch_stride,
+                        size_t pos_axis_stride, size_t axes, const uint64_t* table, size_t batch, size_t tokens, size_t heads_q,
+                        size_t heads_k, size_t head_dim, size_t rot_dim, int interleaved, float scale, float eps, int dt, int wdt,
+                        void* cuda_stream);
+
+/* Bytes of scratch for the weights' gradients of s2a_qknorm_rope_bwd (0 where head_dim is 0 or above 512): the same
+ * for every batch and number of tokens, at most 889 * head_dim * 4. */
+size_t s2a_qknorm_rope_scratch_bytes(size_t batch, size_t tokens, size_t heads_q, size_t heads_k, size_t head_dim);
+
+/* Its backward pass, from x alone (the inputs q and k of the forward call; rstd is computed again).  With u = the gradient turned
+ * back, a = u * gamma and xhat = x * rstd:
+ *   grad_in = rstd * (a - xhat * sum(a * xhat) / head_dim),  grad_gamma = sum over all rows of u * xhat
+ *   grad_gamma_q, grad_gamma_k  out  head_dim elements of type wdt, or NULL each; overwritten, zeros where there are no rows
+ *   scratch                     s2a_qknorm_rope_scratch_bytes(...) bytes; may be NULL where both are
+ * Tensors, and strides[18]: grad_q, grad_k, q, k, grad_in_q, grad_in_k. */
+int s2a_qknorm_rope_bwd(const void* grad_q, const void* grad_k, const void* q, const void* k, const void* gamma_q,
+                        const void* gamma_k, void* grad_in_q, void* grad_in_k, void* grad_gamma_q, void* grad_gamma_k,
+                        void* scratch, const size_t* strides, const int32_t* positions, int64_t first, size_t pos_batch_stride,
+                        size_t pos_axis_stride, size_t axes, const uint64_t* table, size_t batch, size_t tokens, size_t heads_q,
+                        size_t heads_k, size_t head_dim, size_t rot_dim, int interleaved, float scale, float eps, int dt, int wdt,
+                        void* cuda_stream);
+
+/* A table of turns, written to HOST memory: 2 words for each of the rot_dim / 2 pairs.  The pairs are split evenly
+ * among the axes, in order (axes must divide rot_dim / 2), each with the frequencies base^(-j / n), j = 0 .. n - 1, of its n
+ * pairs.  scaling, for contexts `factor` times as long:
+ *   0  none
+ *   1  linear: every frequency / factor
+ *   2  base: base * factor^(n / (n - 1)) in the place of base, so that the last frequency is divided by factor and the first stays
+ *   3  by parts: a pair that turns r times over original_length positions keeps its frequency for r >= fast, has it
+ *      divided by factor for r <= slow, and in between a mixture linear in r
+ * base: at least 1, finite; factor (scaling > 0): above 0, finite; original_length above 0 and 0 <= slow < fast, finite (scaling 3).
+ */
+int s2a_rope_table(uint64_t* table, size_t rot_dim, double base, int scaling, double factor, double original_length,
+                   double slow, double fast, size_t axes);
+
+/* ---- After the backward pass: the gradients' norm and the AdamW step over many tensors ------------------
+ * Both go by a plan: the list of tensors, checked and laid out once in HOST memory (s2a_step_plan_fill), copied by the
+ * caller to 16-byte aligned device memory, and good for any number of calls as long as the tensors stay where
+ * they are.
+ */
+typedef struct {
+  void* param;              /* n elements of type pdt                                                   */
+  const void* grad;         /* n elements of type gdt                                                   */
+  void* exp_avg;            /* n binary32 numbers (state_bits 32) or e4m3 codes (state_bits 8)          */
+  void* exp_avg_sq;         /* likewise                                                                 */
+  float* exp_avg_scale;     /* state_bits 8: the largest magnitude of every 256 elements, (n + 255) / 256 floats */
+  float* exp_avg_sq_scale;  /* likewise, of sqrt(v)                                                     */
+  void* copy;               /* NULL, or with binary32 parameters n bfloat16 elements: a rounded copy    */
+  size_t n;
+  float weight_decay;
+  float lr_scale;           /* multiplies the learning rate                                             */
+} s2a_step_tensor;
+
+typedef struct {
+  size_t bytes;             /* of the image */
+  size_t n_tensors, n_chunks;
+  int pdt, gdt, state_bits, grads_only;
+} s2a_step_plan;
+
+/* Bytes of the plan's image (0 where it would be too large). */
+size_t s2a_step_plan_bytes(const s2a_step_tensor* tensors, size_t n_tensors);
+
+/* Checks the tensors and writes the image, s2a_step_plan_bytes(...) bytes of HOST memory, 16-byte aligned, and *plan.  All pointers
+ * but copy are needed where n > 0 (the scales with state_bits 8 only); with param NULL in every tensor the plan serves s2a_grad_norm only, and the
+ * rest but grad and n is ignored.  Pointers need the alignment of their element type; what is written may not overlap anything
+ * else (S2A_ERR_OVERLAP: the same tensor twice, a gradient inside a parameter); gradients may be shared.  Weight decay and lr_scale: finite, not negative.
+ * Fastest where all of a tensor lies on the 16-byte grid (with 32-bit states: from some common element among the first
+ * eight on).
+ */
+int s2a_step_plan_fill(const s2a_step_tensor* tensors, size_t n_tensors, int pdt, int gdt, int state_bits, void* image,
+                       s2a_step_plan* plan);
+
+/* One step, for each element, with lr and wd as scaled for its tensor and g' = grad * control[2] (* clip[1]):
+ *   m = m + (1 - beta1)(g' - m),  v = beta2 v + (1 - beta2) g'^2
+ *   p = p - lr wd p - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
+ *   plan     HOST, image DEVICE: as filled and copied
+ *   control  DEVICE, three floats: learning rate, t (the step's number, from 1), scale of the gradients (1, or 1 / the
+ *            loss scale): read when the kernel runs, so that a captured graph follows them
+ *   clip     DEVICE, two floats as written by s2a_grad_norm, or NULL.  Where clip[0] is not finite nothing is changed.
+ *   rng      DEVICE, (seed, offset) as for s2a_dropout_fwd, or NULL: round to nearest
+ *   site     as for s2a_dropout_fwd
+ * 8-bit states hold m and sqrt(v) as e4m3 codes, 448 standing for the largest magnitude of each 256 elements, counted from the tensor's first; the
+ * step itself uses the unrounded m and v.  A sqrt(v) above zero never gets the code zero.  A block of which the largest magnitude is below
+ * 2^-110 is stored as zeros.  With rng, 8-bit states and bfloat16 parameters are rounded at random, up with the probability of
+ * what lies above the lower neighbour (binary32 ones need no rounding, copies are rounded to nearest): element e of a tensor that starts at block b of 256 in the
+ * plan (each tensor takes whole blocks) owns 16 bits of Philox4x32-10 under key rng[0] at counter (32 b + e / 8, rng[1] + site),
+ * laid out as for s2a_dropout_fwd, for m; their two bytes exchanged for sqrt(v); and those with the first counter's top bit set for
+ * the parameter.  With nearest, a state that moves by less than half a code's step stays where it is: use rng for long runs with 8-bit
+ * states.
+ * beta1, beta2: in [0, 1); eps: finite, not negative.
+ */
+int s2a_adamw_step(const s2a_step_plan* plan, const void* image, const float* control, const float* clip, const uint64_t* rng,
+                   uint64_t site, double beta1, double beta2, double eps, void* cuda_stream);
+
+/* Bytes of scratch for s2a_grad_norm. */
+size_t s2a_grad_norm_scratch_bytes(const s2a_step_plan* plan);
+
+/* The norm of all gradients of a plan and the factor that limits it: clip[0] = control[2] * sqrt(sum of grad^2), clip[1] =
+ * min(1, max_norm / (clip[0] + 1e-6)).  The sum does not overflow where the norm fits binary32.
+ *   clip     DEVICE  out  two floats
+ *   max_norm  not negative (an infinity: no limit)
+ */
+int s2a_grad_norm(const s2a_step_plan* plan, const void* image, const float* control, double max_norm, float* clip, void* scratch,
+                  void* cuda_stream);
 
 /* The pipelined kernels wait on shared-memory barriers with an iteration limit; a
  * wait that runs out records a bit in a per-device word and the kernel returns early.

@@ -32,6 +32,9 @@ EXPORTS = (
     "s2a_layernorm_scratch_bytes", "s2a_layernorm_fwd", "s2a_layernorm_bwd",
     "s2a_dropout_threshold", "s2a_dropout_fwd", "s2a_dropout_bwd",
     "s2a_relbias_scratch_bytes", "s2a_relbias_fwd", "s2a_relbias_bwd", "s2a_relbias_log_buckets",
+    "s2a_rope_fwd", "s2a_rope_bwd", "s2a_qknorm_rope_fwd", "s2a_qknorm_rope_scratch_bytes", "s2a_qknorm_rope_bwd",
+    "s2a_rope_table", "s2a_step_plan_bytes", "s2a_step_plan_fill", "s2a_adamw_step", "s2a_grad_norm_scratch_bytes",
+    "s2a_grad_norm",
 )
 
 _lib = None
@@ -39,6 +42,17 @@ _lib = None
 
 class S2AError(RuntimeError):
     pass
+
+
+class _StepTensor(ctypes.Structure):    # s2a_step_tensor
+    _fields_ = [(name, ctypes.c_void_p) for name in ("param", "grad", "exp_avg", "exp_avg_sq", "exp_avg_scale",
+                                                     "exp_avg_sq_scale", "copy")]
+    _fields_ += [("n", ctypes.c_size_t), ("weight_decay", ctypes.c_float), ("lr_scale", ctypes.c_float)]
+
+
+class _StepPlan(ctypes.Structure):      # s2a_step_plan
+    _fields_ = [(name, ctypes.c_size_t) for name in ("bytes", "n_tensors", "n_chunks")]
+    _fields_ += [(name, ctypes.c_int) for name in ("pdt", "gdt", "state_bits", "grads_only")]
 
 
 def use_library(path: str) -> None:
@@ -106,6 +120,9 @@ def lib() -> ctypes.CDLL:
             f.argtypes = [c.c_void_p, c.c_void_p, c.c_void_p, c.c_size_t, c.c_int, c.c_void_p]
             f.restype = c.c_int
         ptr, size = c.c_void_p, c.c_size_t
+        # positions .. interleaved of the calls that turn
+        turn = [ptr, c.c_int64, size, size, size, ptr] + [size] * 6 + [c.c_int]
+        rope = [ptr] * 5 + turn + [c.c_float, c.c_int, ptr]
         for name, res, args in (
                 ("s2a_layernorm_scratch_bytes", size, [size, size]),
                 ("s2a_layernorm_fwd", c.c_int, [ptr] * 5 + [size] * 4 + [c.c_float, c.c_int, c.c_int, ptr]),
@@ -116,7 +133,18 @@ def lib() -> ctypes.CDLL:
                 ("s2a_relbias_scratch_bytes", size, [size] * 5),
                 ("s2a_relbias_fwd", c.c_int, [ptr, ptr, ptr, c.c_int, ptr] + [size] * 5 + [c.c_int, c.c_int, ptr]),
                 ("s2a_relbias_bwd", c.c_int, [ptr, ptr, c.c_int, ptr, ptr] + [size] * 5 + [c.c_int, c.c_int, ptr]),
-                ("s2a_relbias_log_buckets", c.c_int, [ptr, c.c_int64, size, size, size, c.c_int])):
+                ("s2a_relbias_log_buckets", c.c_int, [ptr, c.c_int64, size, size, size, c.c_int]),
+                ("s2a_rope_fwd", c.c_int, rope),
+                ("s2a_rope_bwd", c.c_int, rope),
+                ("s2a_qknorm_rope_fwd", c.c_int, [ptr] * 7 + turn + [c.c_float, c.c_float, c.c_int, c.c_int, ptr]),
+                ("s2a_qknorm_rope_scratch_bytes", size, [size] * 5),
+                ("s2a_qknorm_rope_bwd", c.c_int, [ptr] * 12 + turn + [c.c_float, c.c_float, c.c_int, c.c_int, ptr]),
+                ("s2a_rope_table", c.c_int, [ptr, size, c.c_double, c.c_int] + [c.c_double] * 4 + [size]),
+                ("s2a_step_plan_bytes", size, [ptr, size]),
+                ("s2a_step_plan_fill", c.c_int, [ptr, size, c.c_int, c.c_int, c.c_int, ptr, ptr]),
+                ("s2a_adamw_step", c.c_int, [ptr] * 5 + [c.c_uint64] + [c.c_double] * 3 + [ptr]),
+                ("s2a_grad_norm_scratch_bytes", size, [ptr]),
+                ("s2a_grad_norm", c.c_int, [ptr] * 3 + [c.c_double] + [ptr] * 3)):
             f = getattr(L, name)
             f.argtypes, f.restype = args, res
         L.s2a_device_error.argtypes = [c.POINTER(c.c_uint), c.c_int]
@@ -571,6 +599,260 @@ def log_buckets(first_distance: int, count: int, n_buckets: int, max_distance: i
     out = torch.empty(count, dtype=torch.int32)
     check(lib().s2a_relbias_log_buckets(out.data_ptr(), first_distance, count, n_buckets, max_distance, int(bidirectional)))
     return out
+
+
+# ------------------------------------------- rotary positions, norms of queries and keys with them
+_SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
+_Strides4, _Strides6 = ctypes.c_size_t * 12, ctypes.c_size_t * 18
+
+
+def rope_table(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_length: float = 0.0,
+               slow: float = 1.0, fast: float = 32.0, axes: int = 1) -> torch.Tensor:
+    """The turns of each pair as a CPU int64 tensor [rot_dim / 2, 2] (s2a_rope_table), to be moved to the GPU once.
+    scaling: 'none', 'linear', 'base' or 'parts'."""
+    if scaling not in _SCALINGS:
+        raise S2AError("scaling must be one of %s" % ", ".join(_SCALINGS))
+    out = torch.empty((max(rot_dim, 0) // 2, 2), dtype=torch.int64)
+    check(lib().s2a_rope_table(out.data_ptr(), rot_dim, base, _SCALINGS[scaling], factor, original_length, slow, fast, axes))
+    return out
+
+
+def _heads_like(t, like, what: str):
+    """The strides of a tensor of heads [batch, tokens, heads, head_dim] of the shape and dtype of `like`."""
+    if t is None or t.shape != like.shape or t.dtype is not like.dtype:
+        raise S2AError("%s must match in shape and dtype" % what)
+    stride = t.stride()
+    if stride[3] != 1 and like.shape[3] != 1:
+        raise S2AError("%s: the elements of a head's row must be contiguous" % what)
+    return stride
+
+
+def _rope_args(q, k, table, positions):
+    """(batch, tokens, heads_q, heads_k, head_dim, rot_dim), and what belongs to the positions."""
+    shape = q.shape
+    if len(shape) != 4:
+        raise S2AError("queries and keys must be [batch, tokens, heads, head_dim]")
+    batch, tokens, heads_q, dim = shape
+    heads_k = 0
+    if k is not None:
+        other = k.shape
+        if len(other) != 4 or other[0] != batch or other[1] != tokens or other[3] != dim or k.dtype is not q.dtype:
+            raise S2AError("the keys must match the queries but for the number of heads")
+        heads_k = other[2]
+    rot, where = 0, None
+    if table is not None:
+        if table.dtype is not torch.int64 or table.dim() != 2 or table.shape[1] != 2 or not table.is_contiguous():
+            raise S2AError("the table must be contiguous int64 [rot_dim / 2, 2]")
+        rot, where = 2 * table.shape[0], table.data_ptr()
+    if positions is None:
+        return (batch, tokens, heads_q, heads_k, dim, rot), (None, 0, 0, 1, where)
+    shape, stride = positions.shape, positions.stride()
+    n = len(shape)
+    if positions.dtype is not torch.int32 or n < 1 or n > 3 or shape[-1] != tokens or (n > 1 and shape[-2] != batch):
+        raise S2AError("positions must be int32 [tokens], [batch, tokens] or [axes, batch, tokens]")
+    if tokens > 1 and stride[-1] != 1:
+        raise S2AError("the positions of a sequence's tokens must be contiguous")
+    return (batch, tokens, heads_q, heads_k, dim, rot), (
+        positions.data_ptr(), stride[-2] if n > 1 else 0, stride[0] if n > 2 else 0, shape[0] if n > 2 else 1, where)
+
+
+def _address(t):
+    return None if t is None else t.data_ptr()
+
+
+def _rope(call, q, k, out_q, out_k, positions, table, scale, interleaved, first):
+    if table is None:
+        raise S2AError("a table of turns is needed")
+    dev = _on_device(q, k, out_q, out_k, positions, table)
+    size, (pos, per_batch, per_axis, axes, where) = _rope_args(q, k, table, positions)
+    a, c = _heads_like(q, q, "the queries"), _heads_like(out_q, q, "the queries' output")
+    b, d = (_heads_like(k, k, "the keys"), _heads_like(out_k, k, "the keys' output")) if k is not None else (a, a)
+    strides = _Strides4(a[0], a[1], a[2], b[0], b[1], b[2], c[0], c[1], c[2], d[0], d[1], d[2])
+    status = call(q.data_ptr(), _address(k), out_q.data_ptr(), _address(out_k), strides, pos, first, per_batch, per_axis, axes,
+                  where, *size, interleaved, scale, _code(q), _stream_on(dev))
+    if status:
+        check(status)
+
+
+def s2a_rope_fwd(q, k, out_q, out_k, positions, table, scale: float = 1.0, interleaved: bool = False, first: int = 0) -> None:
+    """Rotary positions of queries and keys [batch, tokens, heads, head_dim] (any strides; k and out_k may be None; an
+    output may be its input).  positions: int32 [tokens], [batch, tokens] or [axes, batch, tokens], or None for first +
+    token; table: rope_table(...) on the GPU, or one of the caller's own."""
+    _rope((_lib or lib()).s2a_rope_fwd, q, k, out_q, out_k, positions, table, scale, interleaved, first)
+
+
+def s2a_rope_bwd(grad_q, grad_k, grad_in_q, grad_in_k, positions, table, scale: float = 1.0, interleaved: bool = False,
+                 first: int = 0) -> None:
+    """The gradients of s2a_rope_fwd: turned back."""
+    _rope((_lib or lib()).s2a_rope_bwd, grad_q, grad_k, grad_in_q, grad_in_k, positions, table, scale, interleaved, first)
+
+
+def s2a_qknorm_rope_fwd(q, k, gamma_q, gamma_k, out_q, out_k, positions, table, eps: float, scale: float = 1.0,
+                        interleaved: bool = False, first: int = 0) -> None:
+    """The norm of each head's row (by its root mean square; gamma_q, gamma_k [head_dim] or None) and the rotation in one pass.
+    table None: the norm alone.  The rest as for s2a_rope_fwd."""
+    dev = _on_device(q, k, gamma_q, gamma_k, out_q, out_k, positions, table)
+    size, (pos, per_batch, per_axis, axes, where) = _rope_args(q, k, table, positions)
+    a, c = _heads_like(q, q, "the queries"), _heads_like(out_q, q, "the queries' output")
+    b, d = (_heads_like(k, k, "the keys"), _heads_like(out_k, k, "the keys' output")) if k is not None else (a, a)
+    strides = _Strides4(a[0], a[1], a[2], b[0], b[1], b[2], c[0], c[1], c[2], d[0], d[1], d[2])
+    dim = size[4]
+    status = (_lib or lib()).s2a_qknorm_rope_fwd(
+        q.data_ptr(), _address(k), _param(gamma_q, dim, "gamma_q"), _param(gamma_k, dim, "gamma_k"), out_q.data_ptr(),
+        _address(out_k), strides, pos, first, per_batch, per_axis, axes, where, *size, interleaved, scale, eps, _code(q),
+        _param_dtype(gamma_q, gamma_k), _stream_on(dev))
+    if status:
+        check(status)
+
+
+def qknorm_rope_scratch_bytes(batch: int, tokens: int, heads_q: int, heads_k: int, head_dim: int) -> int:
+    return int(lib().s2a_qknorm_rope_scratch_bytes(batch, tokens, heads_q, heads_k, head_dim))
+
+
+def s2a_qknorm_rope_bwd(grad_q, grad_k, q, k, gamma_q, gamma_k, grad_in_q, grad_in_k, grad_gamma_q, grad_gamma_k, scratch,
+                        positions, table, eps: float, scale: float = 1.0, interleaved: bool = False, first: int = 0) -> None:
+    """The backward pass of s2a_qknorm_rope_fwd from its inputs q and k.  grad_gamma_q and grad_gamma_k may be None (frozen
+    weights; without both, scratch may be None too); scratch holds qknorm_rope_scratch_bytes(...) bytes.  grad_in_q may be
+    grad_q or q, grad_in_k grad_k or k."""
+    dev = _on_device(q, grad_q, grad_k, k, gamma_q, gamma_k, grad_in_q, grad_in_k, grad_gamma_q, grad_gamma_k, scratch, positions,
+                     table)
+    size, (pos, per_batch, per_axis, axes, where) = _rope_args(q, k, table, positions)
+    g, a, c = _heads_like(grad_q, q, "grad_q"), _heads_like(q, q, "the queries"), _heads_like(grad_in_q, q, "grad_in_q")
+    h, b, d = (_heads_like(grad_k, k, "grad_k"), _heads_like(k, k, "the keys"), _heads_like(grad_in_k, k, "grad_in_k")) \
+        if k is not None else (a, a, a)
+    strides = _Strides6(g[0], g[1], g[2], h[0], h[1], h[2], a[0], a[1], a[2], b[0], b[1], b[2], c[0], c[1], c[2], d[0], d[1], d[2])
+    dim = size[4]
+    sums = grad_gamma_q is not None or grad_gamma_k is not None
+    status = (_lib or lib()).s2a_qknorm_rope_bwd(
+        grad_q.data_ptr(), _address(grad_k), q.data_ptr(), _address(k), _param(gamma_q, dim, "gamma_q"),
+        _param(gamma_k, dim, "gamma_k"), grad_in_q.data_ptr(), _address(grad_in_k), _param(grad_gamma_q, dim, "grad_gamma_q"),
+        _param(grad_gamma_k, dim, "grad_gamma_k"), _scratch(scratch, qknorm_rope_scratch_bytes(*size[:5])) if sums else None,
+        strides, pos, first, per_batch, per_axis, axes, where, *size, interleaved, scale, eps, _code(q),
+        _param_dtype(gamma_q, gamma_k, grad_gamma_q, grad_gamma_k), _stream_on(dev))
+    if status:
+        check(status)
+
+
+# --------------------------------------------------- the AdamW step over many tensors, the gradients' norm
+class AdamWPlan:
+    """The tensors of a step, checked and laid out once (adamw_plan); it keeps them alive and is good as long as they stay
+    where they are: with other gradient tensors, make another plan."""
+
+    __slots__ = ("plan", "address", "image", "device", "tensors")
+
+
+def _state_bits(m, v) -> int:
+    if m.dtype is torch.float32 and v.dtype is torch.float32:
+        return 32
+    if m.dtype is torch.float8_e4m3fn and v.dtype is torch.float8_e4m3fn:
+        return 8
+    raise S2AError("exp_avg and exp_avg_sq must both be float32 or both float8_e4m3fn")
+
+
+def adamw_plan(params, grads, exp_avgs, exp_avg_sqs, exp_avg_scales=None, exp_avg_sq_scales=None, copies=None,
+               weight_decay=0.0, lr_scale=1.0) -> AdamWPlan:
+    """A plan for s2a_adamw_step and s2a_grad_norm over lists of contiguous CUDA tensors, one entry of each list per
+    parameter.  Parameters have one dtype, gradients one, states are float32, or float8_e4m3fn codes with float32 scales of (n +
+    255) // 256 elements; copies: None, or bfloat16 tensors (None in the list: no copy).  weight_decay and lr_scale: a
+    number, or one for each tensor.  params None (with exp_avgs and exp_avg_sqs None): gradients alone, for s2a_grad_norm."""
+    count = len(grads)
+    lists = {"params": params, "exp_avgs": exp_avgs, "exp_avg_sqs": exp_avg_sqs, "exp_avg_scales": exp_avg_scales,
+             "exp_avg_sq_scales": exp_avg_sq_scales, "copies": copies}
+    for what, ts in lists.items():
+        if ts is not None and len(ts) != count:
+            raise S2AError("%s must have one entry for each gradient" % what)
+    if params is None and any(ts is not None for ts in lists.values()):
+        raise S2AError("a plan without parameters has gradients alone")
+    if params is not None and (exp_avgs is None or exp_avg_sqs is None):
+        raise S2AError("exp_avgs and exp_avg_sqs are needed")
+    decays = [float(w) for w in weight_decay] if isinstance(weight_decay, (list, tuple)) else [float(weight_decay)] * count
+    rates = [float(w) for w in lr_scale] if isinstance(lr_scale, (list, tuple)) else [float(lr_scale)] * count
+    if len(decays) != count or len(rates) != count:
+        raise S2AError("weight_decay and lr_scale must have one entry for each gradient")
+    records = (_StepTensor * max(count, 1))()
+    pdt, gdt, bits, dev = F32, F32, 32, None
+
+    def same(found, new, i, what):
+        if i and found != new:
+            raise S2AError("%s must have one dtype" % what)
+        return new
+
+    def address(t, n, what, dtype=None):
+        nonlocal dev
+        if not t.is_cuda or (dev is not None and t.get_device() != dev):
+            raise S2AError("%s must be CUDA tensors of one device" % what)
+        if not t.is_contiguous() or t.numel() != n or (dtype is not None and t.dtype is not dtype):
+            raise S2AError("%s must be contiguous, of the right size%s" % (what, "" if dtype is None else " and %s" % dtype))
+        dev = t.get_device()
+        return t.data_ptr()
+
+    for i in range(count):
+        r, n = records[i], grads[i].numel()
+        r.n, r.weight_decay, r.lr_scale = n, decays[i], rates[i]
+        r.grad = address(grads[i], n, "gradients")
+        gdt = same(gdt, _code(grads[i]), i, "gradients")
+        if params is None:
+            continue
+        r.param = address(params[i], n, "parameters")
+        pdt = same(pdt, _code(params[i]), i, "parameters")
+        bits = same(bits, _state_bits(exp_avgs[i], exp_avg_sqs[i]), i, "states")
+        r.exp_avg = address(exp_avgs[i], n, "exp_avgs")
+        r.exp_avg_sq = address(exp_avg_sqs[i], n, "exp_avg_sqs")
+        if bits == 8:
+            if exp_avg_scales is None or exp_avg_sq_scales is None:
+                raise S2AError("states in 8 bits need their scales")
+            blocks = (n + 255) // 256
+            r.exp_avg_scale = address(exp_avg_scales[i], blocks, "exp_avg_scales", torch.float32)
+            r.exp_avg_sq_scale = address(exp_avg_sq_scales[i], blocks, "exp_avg_sq_scales", torch.float32)
+        if copies is not None and copies[i] is not None:
+            r.copy = address(copies[i], n, "copies", torch.bfloat16)
+    self = AdamWPlan()
+    need = int(lib().s2a_step_plan_bytes(records, count))
+    host = torch.zeros(max(need, 16) // 8 + 2, dtype=torch.int64)
+    start = -host.data_ptr() % 16 // 8      # 16-byte aligned
+    self.plan = _StepPlan()
+    check(lib().s2a_step_plan_fill(records, count, pdt, gdt, bits, host.data_ptr() + 8 * start, ctypes.byref(self.plan)))
+    self.device = torch.cuda.current_device() if dev is None else dev
+    self.image = host[start:start + max(need, 16) // 8 + 1].to(torch.device("cuda", self.device))
+    self.address = ctypes.addressof(self.plan)
+    self.tensors = (list(grads),) + tuple(None if ts is None else list(ts) for ts in lists.values())
+    return self
+
+
+def _float_words(t, n: int, what: str):
+    if t.dtype is not torch.float32 or t.numel() < n or not t.is_contiguous():
+        raise S2AError("%s must be contiguous float32 with %d elements" % (what, n))
+    return t.data_ptr()
+
+
+def s2a_adamw_step(plan: AdamWPlan, control, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, clip=None, rng=None,
+                   site: int = 0) -> None:
+    """One AdamW step over the plan's tensors, in place.  control: float32 (learning rate, number of the step from 1, scale of
+    the gradients) on the device; clip: what s2a_grad_norm wrote, or None; rng: int64 (seed, offset) on the device for
+    rounding at random, or None."""
+    dev = _on_device(plan.image, control, clip, rng)
+    if rng is not None and (rng.dtype is not torch.int64 or rng.numel() != 2 or not rng.is_contiguous()):
+        raise S2AError("rng must be contiguous int64 (seed, offset)")
+    status = (_lib or lib()).s2a_adamw_step(plan.address, plan.image.data_ptr(), _float_words(control, 3, "control"),
+                                            None if clip is None else _float_words(clip, 2, "clip"), _address(rng), site, beta1,
+                                            beta2, eps, _stream_on(dev))
+    if status:
+        check(status)
+
+
+def grad_norm_scratch_bytes(plan: AdamWPlan) -> int:
+    return int(lib().s2a_grad_norm_scratch_bytes(plan.address))
+
+
+def s2a_grad_norm(plan: AdamWPlan, control, max_norm: float, clip, scratch) -> None:
+    """The norm of all the plan's gradients, times control[2], and the factor that limits it to max_norm: written to clip
+    (float32, two elements).  scratch holds grad_norm_scratch_bytes(plan) bytes."""
+    dev = _on_device(plan.image, control, clip, scratch)
+    status = (_lib or lib()).s2a_grad_norm(plan.address, plan.image.data_ptr(), _float_words(control, 3, "control"), max_norm,
+                                           _float_words(clip, 2, "clip"), _scratch(scratch, grad_norm_scratch_bytes(plan)),
+                                           _stream_on(dev))
+    if status:
+        check(status)
 
 
 def s2a_device_error(clear: bool = False) -> int:

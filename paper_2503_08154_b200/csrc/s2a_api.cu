@@ -77,6 +77,7 @@ const char* s2a_status_string(int status) {
              "(536,870,912 elements); use s2a_gelu_fwd_tensor_range with your own scratch";
     case S2A_ERR_OVERLAP: return "S2A_ERR_OVERLAP: the output overlaps the input without being the same tensor";
     case S2A_ERR_VALUE: return "S2A_ERR_VALUE: a scalar argument is outside its range";
+    case S2A_ERR_MEMORY: return "S2A_ERR_MEMORY: the host has no memory for a plan's checks";
     default: return "unknown s2a status";
   }
 }

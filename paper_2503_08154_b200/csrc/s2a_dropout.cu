@@ -8,6 +8,7 @@
 // elements take 176 us instead of 126.
 #include "s2a_launch.h"
 #include "s2a_oct.cuh"
+#include "s2a_philox.cuh"
 
 namespace s2a {
 namespace {
@@ -19,33 +20,6 @@ constexpr int kResident = 5;       // CTAs of an SM
 // runs, at lower clocks, up to 138 us), against 132 with exactly as many as fit, and 154 with one vector in flight; [64, 12, 197, 197]:
 // 21.4, 21.7, 25.1 us.
 constexpr int kCtasPerSm = 20;
-
-struct PhiloxKey {
-  uint32_t k0[10], k1[10];
-  __device__ __forceinline__ explicit PhiloxKey(uint64_t seed) {
-    uint32_t a = (uint32_t)seed, b = (uint32_t)(seed >> 32);
-#pragma unroll
-    for (int i = 0; i < 10; ++i) {
-      k0[i] = a;
-      k1[i] = b;
-      a += 0x9E3779B9u;
-      b += 0xBB67AE85u;
-    }
-  }
-};
-
-__device__ __forceinline__ uint4 philox(const PhiloxKey& key, uint64_t block, uint64_t count) {
-  uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = (uint32_t)count, c3 = (uint32_t)(count >> 32);
-#pragma unroll
-  for (int i = 0; i < 10; ++i) {
-    const uint64_t p0 = (uint64_t)c0 * 0xD2511F53u, p1 = (uint64_t)c2 * 0xCD9E8D57u;
-    c0 = (uint32_t)(p1 >> 32) ^ c1 ^ key.k0[i];
-    c1 = (uint32_t)p1;
-    c2 = (uint32_t)(p0 >> 32) ^ c3 ^ key.k1[i];
-    c3 = (uint32_t)p0;
-  }
-  return make_uint4(c0, c1, c2, c3);
-}
 
 // An element is kept when its 16 bits are at least T; `limit` is T << 16, so that each field is compared in the
 // top half of a word, and what lies below it does not matter.

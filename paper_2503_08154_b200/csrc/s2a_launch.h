@@ -88,6 +88,71 @@ cudaError_t launch_relbias_bwd(int dt, int wdt, const void* g, const int32_t* bu
                                cudaStream_t st);
 void log_buckets(int32_t* out, int64_t first, uint64_t count, uint32_t n_buckets, uint32_t max_distance, bool bidirectional);
 
+// Rotary positions and the norms of queries and keys.  A tensor of heads [batch, tokens, heads, head_dim] by its strides in
+// elements; index 0 stands for queries and 1 for keys, and heads[1] may be 0.
+constexpr uint32_t kMaxHeadDim = 512;
+constexpr uint32_t kMaxRopePartials = 148 * 6 + 1;  // rows of scratch at most
+enum { kRopePlain = 0, kRopeFwdNorm = 1, kRopeBwdNorm = 2 };
+enum { kRopeScaleNone = 0, kRopeScaleLinear = 1, kRopeScaleBase = 2, kRopeScaleParts = 3 };
+struct HeadsArg {
+  const void* data;
+  uint64_t batch, token, head;
+};
+struct RopeArgs {
+  HeadsArg in[2], grad[2], out[2];  // grad: of the norm's backward pass, whose `in` is x
+  const void* gamma[2];             // NULL: ones
+  const int32_t* positions;         // NULL: first + token
+  const void* table;                // (turn, axis) of each pair
+  float* partials;
+  int64_t first;
+  uint64_t pos_axis, pos_batch, units;
+  uint32_t heads[2];
+  uint32_t batch, tokens, head_dim, pairs, axes, parts, ctas0;
+  uint32_t lanes, rows_per_warp, slots, turn_slots;  // lanes and slots of a row (slots: see the kernels), turning slots
+  int interleaved, back, wdt;
+  float scale, eps, inv_dim;
+};
+uint64_t qknorm_scratch_bytes(uint32_t head_dim);
+cudaError_t launch_rope(int mode, int dt, RopeArgs a, void* grad_gamma_q, void* grad_gamma_k, float* scratch, cudaStream_t st);
+void rope_table(uint64_t* out, uint32_t pairs, double base, int scaling, double factor, double original, double slow, double fast,
+                uint32_t axes);
+
+// The AdamW step and the norm of all gradients, over the tensors of a plan: an image in device memory of `n_tensors`
+// StepTensor and, after them, the tensor of each chunk (uint32_t).
+constexpr uint32_t kStepBlock = 256;                 // elements under one scale of 8-bit states
+constexpr uint32_t kStepChunk = 4 * kStepBlock;      // what a warp takes at a time
+constexpr int kMaxNormCtas = 148 * 4;
+struct StepTensor {
+  void* p;
+  const void* g;
+  void* m;
+  void* v;
+  float* m_scale;
+  float* v_scale;
+  void* copy;         // bfloat16, or NULL
+  uint64_t n;
+  uint64_t block0;    // 256-element blocks of the plan before this tensor's: what random bits go by
+  uint32_t chunk0;    // chunks of the plan before this tensor's
+  uint32_t head;      // elements before the first that lies on the 16-byte grid in all tensors; kStepScalar: none does
+  float decay, lr;
+  uint64_t unused;    // a multiple of 16 bytes
+};
+static_assert(sizeof(StepTensor) == 96, "whole 16-byte pieces");
+constexpr uint32_t kStepScalar = 8;
+struct StepArgs {
+  const StepTensor* tensors;
+  const uint32_t* owner;
+  uint32_t n_tensors, n_chunks;
+  const float* control;   // learning rate, number of the step, scale of the gradients
+  const float* clip;      // norm and factor, or NULL
+  const uint64_t* rng;    // seed and offset, or NULL: round to nearest
+  uint64_t site;
+  float one_beta1, beta2, one_beta2, log_beta1, log_beta2, eps;
+};
+cudaError_t launch_adamw(int pdt, int gdt, int state_bits, const StepArgs& a, cudaStream_t st);
+uint64_t grad_norm_scratch_bytes(uint32_t n_chunks);
+cudaError_t launch_grad_norm(int gdt, const StepArgs& a, float max_norm, float* out, double* scratch, cudaStream_t st);
+
 // ---------------------------------------------------------------- pipelined tiles
 // A tile is `tile_rows` consecutive rows whose flat element span starts and ends on a
 // multiple of 32 elements (128 / bits in general), so that its data and its code bytes can
