@@ -401,7 +401,7 @@ int s2a_relbias_log_buckets(int32_t* buckets, int64_t first_distance, size_t cou
  *   rot_dim  the first rot_dim elements of a row turn, the rest stays: even, 2 .. head_dim; 0 (with table
  *            NULL) for a norm without rotation.  Pairs are (i, i + rot_dim / 2), or (2 i, 2 i + 1) where `interleaved`.
  *   scale    multiplies the cosines and sines (1 but for some scaled contexts): finite
- * head_dim: 1 .. 512; heads: at most 65535 each; batch * tokens at most 2^31-1.
+ * head_dim: 1 .. 512; axes: 1 .. 4; heads: at most 65535 each; batch * tokens at most 2^31-1.
  */
 
 /* Forward: with the angle w = position * frequency of its pair, (a, b) -> (a cos w - b sin w, a sin w + b cos w).
@@ -445,7 +445,7 @@ int s2a_qknorm_rope_bwd(const void* grad_q, const void* grad_k, const void* q, c
                         void* cuda_stream);
 
 /* A table of turns, written to HOST memory: 2 words for each of the rot_dim / 2 pairs.  The pairs are split evenly
- * among the axes, in order (axes must divide rot_dim / 2), each with the frequencies base^(-j / n), j = 0 .. n - 1, of its n
+ * among the axes, in order (1 .. 4, dividing rot_dim / 2), each with the frequencies base^(-j / n), j = 0 .. n - 1, of its n
  * pairs.  scaling, for contexts `factor` times as long:
  *   0  none
  *   1  linear: every frequency / factor

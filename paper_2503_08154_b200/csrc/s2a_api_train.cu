@@ -115,7 +115,7 @@ int run_rope(const RopeCall& c) {
   if (bad_dtype(c.dt) || (norm && bad_dtype(c.wdt))) return S2A_ERR_DTYPE;
   if (c.head_dim == 0 || c.head_dim > kMaxHeadDim || c.rot_dim % 2 != 0 || c.rot_dim > c.head_dim || (!norm && c.rot_dim == 0) ||
       c.heads[0] > 65535u || c.heads[1] > 65535u || c.batch > 0x7fffffffull || c.tokens > 0x7fffffffull ||
-      c.batch * c.tokens > 0x7fffffffull || (c.rot_dim && (c.axes == 0 || c.axes > c.rot_dim / 2)))
+      c.batch * c.tokens > 0x7fffffffull || (c.rot_dim && (c.axes == 0 || c.axes > kMaxAxes)))
     return S2A_ERR_SHAPE;
   if (!(fabsf(c.scale) <= 3.4028234e38f) || (norm && !(c.eps >= 0.0f && c.eps <= 3.4028234e38f))) return S2A_ERR_VALUE;
   const bool sums = c.grad_gamma[0] || c.grad_gamma[1];
@@ -283,7 +283,7 @@ int s2a_qknorm_rope_bwd(const void* grad_q, const void* grad_k, const void* q, c
 int s2a_rope_table(uint64_t* table, size_t rot_dim, double base, int scaling, double factor, double original_length, double slow,
                    double fast, size_t axes) {
   const size_t pairs = rot_dim / 2;
-  if (rot_dim % 2 != 0 || rot_dim > kMaxHeadDim || axes == 0 || (pairs && (axes > pairs || pairs % axes != 0))) return S2A_ERR_SHAPE;
+  if (rot_dim % 2 != 0 || rot_dim > kMaxHeadDim || axes == 0 || axes > kMaxAxes || pairs % axes != 0) return S2A_ERR_SHAPE;
   if (!(base >= 1.0) || isinf(base) || scaling < kRopeScaleNone || scaling > kRopeScaleParts) return S2A_ERR_VALUE;
   if (scaling != kRopeScaleNone && (!(factor > 0.0) || isinf(factor))) return S2A_ERR_VALUE;
   if (scaling == kRopeScaleParts &&

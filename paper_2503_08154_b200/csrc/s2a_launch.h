@@ -91,6 +91,7 @@ void log_buckets(int32_t* out, int64_t first, uint64_t count, uint32_t n_buckets
 // Rotary positions and the norms of queries and keys.  A tensor of heads [batch, tokens, heads, head_dim] by its strides in
 // elements; index 0 stands for queries and 1 for keys, and heads[1] may be 0.
 constexpr uint32_t kMaxHeadDim = 512;
+constexpr uint32_t kMaxAxes = 4;                    // a token's positions fit 16 bytes
 constexpr uint32_t kMaxRopePartials = 148 * 6 + 1;  // rows of scratch at most
 enum { kRopePlain = 0, kRopeFwdNorm = 1, kRopeBwdNorm = 2 };
 enum { kRopeScaleNone = 0, kRopeScaleLinear = 1, kRopeScaleBase = 2, kRopeScaleParts = 3 };
@@ -105,7 +106,7 @@ struct RopeArgs {
   const void* table;                // (turn, axis) of each pair
   float* partials;
   int64_t first;
-  uint64_t pos_axis, pos_batch, units;
+  uint64_t pos_axis, pos_batch;
   uint32_t heads[2];
   uint32_t batch, tokens, head_dim, pairs, axes, parts, ctas0;
   uint32_t lanes, rows_per_warp, slots, turn_slots;  // lanes and slots of a row (slots: see the kernels), turning slots

@@ -1,0 +1,750 @@
+// Rotary positions, and the norms of queries and keys with the rotation in the same pass, forward and backward.
+//
+// A head's row of D elements turns in pairs: (a, b) -> (a cos - b sin, a sin + b cos), pair i of a token at position p by the
+// angle p * w_i; backward turns by the opposite angle.  The phase is exact at any position: the table holds w_i / (2 pi) as a
+// 64-bit binary fraction of a turn, so that turn * p modulo 2^64 is the angle's fraction of a turn (the error of the
+// table's last bit times p: below 2^-33 of a turn for |p| < 2^31).  One integer product takes the place of a table of cosines over all positions
+// or of products in 64 bits.
+//
+// With the norm: y = R(x * rstd * gamma), rstd = 1 / sqrt(mean(x^2) + eps).  Backward keeps nothing but x: with u = R^-1(g),
+// a = u * gamma, xhat = x * rstd:  grad_x = rstd * (a - xhat * mean(a * xhat)),  grad_gamma = sum of u * xhat; the row is in
+// registers anyway, so rstd costs one more sum and no memory.
+//
+// All of it is bound by memory: each row is read once (backward: g and x) and written once.  A lane owns 16 elements of a row
+// as K slots of two vectors of V; a slot holds V pairs, or 2 V of the elements that do not turn.  The two vectors of a turning
+// slot are rot / 2 elements apart in both layouts, so that pairs never cross lanes and a warp's accesses are alike.  A warp
+// takes 32 / L rows (L lanes a row) of one token at a time, all heads of queries and keys in turn, so that a token's
+// cosines and sines are computed once, one or a few a lane, and shared through the warp's own shared memory.  Rows come through a ring
+// of asynchronous copies of each warp's own, four groups of rows deep, and the walk over tokens adds to its addresses instead of
+// computing them: with plain loads, addresses from scratch and the weights read per token, the norm of [64, 197, 12 + 12, 64] bfloat16
+// took 581 instructions a group and 39.5 us.
+//
+// Rows that turn as a whole and fill 4, 8 or 16 lanes (heads of 64, 128, 256 on the 16-byte grid) have kernels of their own (L > 0), in which
+// every slot exists; the others (L = 0) ask for each slot.
+#pragma once
+
+#include "s2a_launch.h"
+#include "s2a_oct.cuh"
+
+namespace s2a {
+namespace {
+
+constexpr int kWarps = 8;
+constexpr int kThreads = kWarps * 32;
+constexpr int kLaneElems = 16;
+constexpr int kStages = 4;  // groups of rows of a warp in flight or in work
+
+// Where a warp's lanes stand in the rows they take together.
+template <int L>
+struct Lane {
+  uint32_t slot, row, per;  // slot of k = 0 in the row, row of the group, rows of a group
+  bool on;
+  __device__ __forceinline__ explicit Lane(const RopeArgs& a) {
+    const uint32_t lane = threadIdx.x & 31u;
+    row = lane / lanes(a);
+    slot = lane - row * lanes(a);
+    per = L ? 32 / (L ? L : 1) : a.rows_per_warp;
+    on = L ? true : row < per;
+  }
+  static __device__ __forceinline__ uint32_t lanes(const RopeArgs& a) { return L ? L : a.lanes; }
+};
+
+// (cos, sin) of turn * pos, times `scale`; `sign` turns back.  The fraction's top 32 bits: a quarter turn to the nearest, and what
+// is left of it, at most an eighth of a turn, for which Taylor's polynomials to x^9 and x^10 are off by 2e-9 and 1e-10.
+__device__ __forceinline__ float2 phase(uint64_t turn, int64_t pos, float scale, float sign) {
+  const uint32_t top = (uint32_t)((turn * (uint64_t)pos) >> 32);
+  const uint32_t quarter = (top + 0x20000000u) >> 30;
+  const float x = (float)(int32_t)(top - (quarter << 30)) * 1.4629180792671596e-09f;  // radians: 2 pi / 2^32
+  const float z = x * x;
+  float s = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 2.7557319e-6f, -1.9841270e-4f), 8.3333333e-3f), -1.6666667e-1f) * x, x);
+  float c = fmaf(z, fmaf(z, fmaf(z, fmaf(z, fmaf(z, -2.7557319e-7f, 2.4801587e-5f), -1.3888889e-3f), 4.1666667e-2f), -0.5f), 1.0f);
+  // a quarter more: (c, s) becomes (-s, c); a half more: both signs
+  const float u = (quarter & 1u) ? -s : c, v = (quarter & 1u) ? c : s;
+  const float turned = (quarter & 2u) ? -scale : scale;
+  return make_float2(u * turned, v * (turned * sign));
+}
+
+template <int BYTES> struct RawOf;
+template <> struct RawOf<16> { using T = uint4; };
+template <> struct RawOf<8> { using T = uint2; };
+template <> struct RawOf<4> { using T = uint32_t; };
+template <> struct RawOf<2> { using T = uint16_t; };
+
+// A vector of V elements as F2s: V / 2, or one with nothing in its upper half.
+template <int V> constexpr int kHalf = V > 1 ? V / 2 : 1;
+
+template <int DT, int V>
+__device__ __forceinline__ void read_vector(const void* p, F2 (&f)[kHalf<V>]) {
+  if constexpr (DT == kF32) {
+    if constexpr (V == 4) {
+      const ulonglong2 r = *(const ulonglong2*)p;
+      f[0].v = r.x;
+      f[1].v = r.y;
+    } else if constexpr (V == 2) {
+      f[0].v = *(const unsigned long long*)p;
+    } else {
+      f[0] = f2_pack(*(const float*)p, 0.0f);
+    }
+  } else if constexpr (V == 8) {
+    const uint4 r = *(const uint4*)p;
+    f[0] = f2_from_bf16x2(r.x);
+    f[1] = f2_from_bf16x2(r.y);
+    f[2] = f2_from_bf16x2(r.z);
+    f[3] = f2_from_bf16x2(r.w);
+  } else if constexpr (V == 4) {
+    const uint2 r = *(const uint2*)p;
+    f[0] = f2_from_bf16x2(r.x);
+    f[1] = f2_from_bf16x2(r.y);
+  } else if constexpr (V == 2) {
+    f[0] = f2_from_bf16x2(*(const uint32_t*)p);
+  } else {
+    f[0] = f2_pack(__uint_as_float((uint32_t) * (const uint16_t*)p << 16), 0.0f);
+  }
+}
+
+template <int DT, int V>
+__device__ __forceinline__ void write_vector(void* p, const F2 (&f)[kHalf<V>]) {
+  if constexpr (DT == kF32) {
+    if constexpr (V == 4) {
+      *(ulonglong2*)p = make_ulonglong2(f[0].v, f[1].v);
+    } else if constexpr (V == 2) {
+      *(unsigned long long*)p = f[0].v;
+    } else {
+      float a, b;
+      f2_unpack(f[0], a, b);
+      *(float*)p = a;
+    }
+  } else if constexpr (V == 8) {
+    *(uint4*)p = make_uint4(f2_to_bf16x2(f[0]), f2_to_bf16x2(f[1]), f2_to_bf16x2(f[2]), f2_to_bf16x2(f[3]));
+  } else if constexpr (V == 4) {
+    *(uint2*)p = make_uint2(f2_to_bf16x2(f[0]), f2_to_bf16x2(f[1]));
+  } else if constexpr (V == 2) {
+    *(uint32_t*)p = f2_to_bf16x2(f[0]);
+  } else {
+    float a, b;
+    f2_unpack(f[0], a, b);
+    *(__nv_bfloat16*)p = __float2bfloat16_rn(a);
+  }
+}
+
+// V binary32 numbers of shared memory, on a boundary of V of them (16 bytes at most).
+template <int V>
+__device__ __forceinline__ void read_floats(const float* p, F2 (&f)[kHalf<V>]) {
+  if constexpr (V >= 4) {
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) {
+      const ulonglong2 r = ((const ulonglong2*)p)[i];
+      f[2 * i].v = r.x;
+      f[2 * i + 1].v = r.y;
+    }
+  } else if constexpr (V == 2) {
+    f[0].v = *(const unsigned long long*)p;
+  } else {
+    f[0] = f2_pack(*p, 0.0f);
+  }
+}
+
+// A lane's places in a row, the same in every row of a launch: the two vectors of each slot, and which of them exist.
+template <int V, int K, bool INTER, int L>
+struct Places {
+  uint32_t at[K], to[K];  // elements of the first and the second vector
+  uint32_t pair[K], pair2[K];  // first pair of the first and, interleaved, of the second vector
+  uint32_t first, second, turns;  // bits: which of them exist, and which slots turn
+  __device__ __forceinline__ bool has_first(int k) const { return L || ((first >> k) & 1u); }
+  __device__ __forceinline__ bool has_second(int k) const { return L || ((second >> k) & 1u); }
+  __device__ __forceinline__ bool turning(int k) const { return L || ((turns >> k) & 1u); }
+  __device__ __forceinline__ Places(const RopeArgs& a, const Lane<L>& l) {
+    first = second = turns = 0u;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      const uint32_t s = l.slot + k * Lane<L>::lanes(a);
+      const uint32_t pairs = L ? L * kLaneElems / 2 : a.pairs;
+      at[k] = to[k] = pair[k] = pair2[k] = 0u;
+      if (!L && (!l.on || s >= a.slots)) continue;
+      first |= 1u << k;
+      if (L || s < a.turn_slots) {
+        turns |= 1u << k;
+        second |= 1u << k;
+        if (V == 1) {  // single pairs: adjacent, or half apart
+          at[k] = a.interleaved ? 2 * s : s;
+          to[k] = a.interleaved ? 2 * s + 1 : s + pairs;
+          pair[k] = s;
+        } else {
+          at[k] = V * s;
+          to[k] = V * s + pairs;
+          pair[k] = INTER ? at[k] / 2 : at[k];
+          pair2[k] = INTER ? to[k] / 2 : 0u;
+        }
+      } else {
+        at[k] = 2 * pairs + 2 * V * (s - a.turn_slots);
+        to[k] = at[k] + V;
+        if (to[k] < a.head_dim) second |= 1u << k;
+        else to[k] = at[k];
+      }
+    }
+  }
+};
+
+// A lane's cosines and sines, of the slots that turn.
+template <int V, int K, bool INTER, int L>
+struct Angles {
+  F2 c[K][kHalf<V>], s[K][kHalf<V>];  // of the pairs in order
+  __device__ __forceinline__ void read(const Places<V, K, INTER, L>& p, const float* cs, const float* sn) {
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (!p.turning(k)) continue;
+      if constexpr (INTER) {
+        read_part(cs + p.pair[k], cs + p.pair2[k], c[k]);
+        read_part(sn + p.pair[k], sn + p.pair2[k], s[k]);
+      } else {
+        read_floats<V>(cs + p.pair[k], c[k]);
+        read_floats<V>(sn + p.pair[k], s[k]);
+      }
+    }
+  }
+  // V / 2 numbers from each of two places
+  static __device__ __forceinline__ void read_part(const float* p, const float* q, F2 (&f)[kHalf<V>]) {
+    if constexpr (V == 2) {
+      f[0] = f2_pack(*p, *q);
+    } else {
+      F2 x[kHalf<V / 2>], y[kHalf<V / 2>];
+      read_floats<V / 2>(p, x);
+      read_floats<V / 2>(q, y);
+#pragma unroll
+      for (int i = 0; i < V / 4; ++i) {
+        f[i] = x[i];
+        f[V / 4 + i] = y[i];
+      }
+    }
+  }
+  static __device__ __forceinline__ F2 turn_pair(F2 x, float c, float s) {
+    float a, b;
+    f2_unpack(x, a, b);
+    return f2_pack(fmaf(a, c, -(b * s)), fmaf(a, s, b * c));
+  }
+  __device__ __forceinline__ void turn(int k, F2 (&a)[kHalf<V>], F2 (&b)[kHalf<V>]) const {
+    if constexpr (INTER) {
+#pragma unroll
+      for (int j = 0; j < V / 2; ++j) {
+        float c0, c1, s0, s1;
+        f2_unpack(c[k][j / 2], c0, c1);
+        f2_unpack(s[k][j / 2], s0, s1);
+        a[j] = turn_pair(a[j], j % 2 ? c1 : c0, j % 2 ? s1 : s0);
+        const int i = V / 2 + j;
+        f2_unpack(c[k][i / 2], c0, c1);
+        f2_unpack(s[k][i / 2], s0, s1);
+        b[j] = turn_pair(b[j], i % 2 ? c1 : c0, i % 2 ? s1 : s0);
+      }
+    } else {  // two pairs an instruction
+#pragma unroll
+      for (int j = 0; j < kHalf<V>; ++j) {
+        const F2 u = f2_sub(f2_mul(a[j], c[k][j]), f2_mul(b[j], s[k][j]));
+        b[j] = f2_fma(a[j], s[k][j], f2_mul(b[j], c[k][j]));
+        a[j] = u;
+      }
+    }
+  }
+};
+
+// A copy of BYTES at constant offsets from both addresses, or zeros where there is nothing.
+template <int BYTES, int TO, int FROM>
+__device__ __forceinline__ void copy_or_zero(uint32_t to, uint64_t from, bool there) {
+  if constexpr (BYTES == 16)
+    asm volatile("cp.async.cg.shared.global [%0+%3], [%1+%4], 16, %2;" ::"r"(to), "l"(from), "r"(there ? 16 : 0), "n"(TO), "n"(FROM) : "memory");
+  else
+    asm volatile("cp.async.ca.shared.global [%0+%4], [%1+%5], %2, %3;" ::"r"(to), "l"(from), "n"(BYTES), "r"(there ? BYTES : 0), "n"(TO), "n"(FROM)
+                 : "memory");
+}
+
+// A warp's group of rows in a stage of its ring.  Rows with kernels of their own (L > 0): each lane copies what it will read, to a place
+// of its own, and writes from registers.  Others: their rows lie one behind the other, copied by vectors in order, so that neighbouring lanes have
+// neighbouring vectors whatever the row's length, read by each lane at its places, and written back the same way ([3, 16 + 16, 2001,
+// 80] binary32, half turning: 36.9 us with each lane's own copies, most of which cut 32-byte sectors).
+template <int DT, int V, int K, int L>
+struct Group {
+  static constexpr int kBytes = V * Io<DT>::kBytes;
+  static constexpr int kGroupBytes = 2 * K * 32 * kBytes;  // of a warp
+  static constexpr int kApart = L * (kLaneElems / 2) * Io<DT>::kBytes;  // bytes from the first half of a row to the second
+  uint32_t vectors, inverse;  // L = 0: vectors of a row, and 2^20 / that, rounded up: j / vectors is exact for j < 512
+  __device__ __forceinline__ explicit Group(const RopeArgs& a) : vectors(a.head_dim / V), inverse((1048576u + a.head_dim / V - 1) / (a.head_dim / V)) {}
+
+  // rows first .. of a token: row r of the queries lies at q + r * q_head, of the keys (r >= heads0) at k + r * k_head
+  struct Source {
+    uint64_t q, k, q_head, k_head;
+    uint32_t heads0, heads;
+    __device__ __forceinline__ uint64_t row(uint32_t r) const {
+      const bool keys = r >= heads0;
+      // (the kernels for L > 0 are taken where a head's stride fits 32 bits)
+      if constexpr (L > 0) return (keys ? k : q) + (uint64_t)r * (uint32_t)(keys ? k_head : q_head);
+      else return (keys ? k : q) + r * (keys ? k_head : q_head);
+    }
+  };
+
+  __device__ __forceinline__ void fetch(char* stage, const Source& from, uint32_t first, const Lane<L>& l) const {
+    const uint32_t lane = threadIdx.x & 31u;
+    const uint32_t to = (uint32_t)__cvta_generic_to_shared(stage) + lane * kBytes;
+    if constexpr (L > 0) {
+      const uint32_t r = first + l.row;
+      const uint64_t row = from.row(r) + l.slot * kBytes;
+      const bool there = r < from.heads;
+      copy_or_zero<kBytes, 0, 0>(to, row, there);
+      copy_or_zero<kBytes, 32 * kBytes, kApart>(to, row, there);
+      if constexpr (K == 2) {
+        copy_or_zero<kBytes, 64 * kBytes, L * kBytes>(to, row, there);
+        copy_or_zero<kBytes, 96 * kBytes, L * kBytes + kApart>(to, row, there);
+      }
+    } else {
+#pragma unroll
+      for (int m = 0; m < 2 * K; ++m) {
+        const uint32_t j = m * 32 + lane, r = (j * inverse) >> 20, c = j - r * vectors;
+        const bool there = r < l.per && first + r < from.heads;
+        const uint64_t at = from.row(first + r) + c * kBytes;
+        if constexpr (kBytes >= 4) {
+          if (r < l.per) copy_or_zero<kBytes, 0, 0>(to + m * 32 * kBytes, at, there);
+        } else if (r < l.per) {
+          *(uint16_t*)(stage + j * kBytes) = there ? *(const uint16_t*)at : (uint16_t)0;
+        }
+      }
+    }
+  }
+  template <typename P>
+  __device__ __forceinline__ void read(const char* stage, const P& p, int k, const Lane<L>& l, F2 (&a)[kHalf<V>], F2 (&b)[kHalf<V>]) const {
+    if constexpr (L > 0) {
+      const char* own = stage + (2 * k * 32 + (threadIdx.x & 31u)) * kBytes;
+      read_vector<DT, V>(own, a);
+      read_vector<DT, V>(own + 32 * kBytes, b);
+    } else {
+      const char* row = stage + l.row * vectors * kBytes;
+#pragma unroll
+      for (int j = 0; j < kHalf<V>; ++j) a[j] = b[j] = f2_both(0.0f);
+      if (p.has_first(k)) read_vector<DT, V>(row + p.at[k] * Io<DT>::kBytes, a);
+      if (p.has_second(k)) read_vector<DT, V>(row + p.to[k] * Io<DT>::kBytes, b);
+    }
+  }
+  // L > 0: to memory.  L = 0: back to the stage, from where `flush` takes it.
+  template <typename P>
+  __device__ __forceinline__ void write(char* stage, uint64_t out, const P& p, int k, const Lane<L>& l, bool on, const F2 (&a)[kHalf<V>],
+                                        const F2 (&b)[kHalf<V>]) const {
+    if constexpr (L > 0) {
+      if (!on) return;
+      write_vector<DT, V>((void*)(out + k * L * kBytes), a);
+      write_vector<DT, V>((void*)(out + k * L * kBytes + kApart), b);
+    } else {
+      char* row = stage + l.row * vectors * kBytes;
+      if (p.has_first(k)) write_vector<DT, V>(row + p.at[k] * Io<DT>::kBytes, a);
+      if (p.has_second(k)) write_vector<DT, V>(row + p.to[k] * Io<DT>::kBytes, b);
+    }
+  }
+  __device__ __forceinline__ void flush(const char* stage, const Source& to, uint32_t first, const Lane<L>& l) const {
+    if constexpr (L == 0) {
+      using Raw = typename RawOf<kBytes>::T;
+      const uint32_t lane = threadIdx.x & 31u;
+      __syncwarp();
+#pragma unroll
+      for (int m = 0; m < 2 * K; ++m) {
+        const uint32_t j = m * 32 + lane, r = (j * inverse) >> 20, c = j - r * vectors;
+        if (r < l.per && first + r < to.heads) *(Raw*)(to.row(first + r) + c * kBytes) = *(const Raw*)(stage + j * kBytes);
+      }
+      __syncwarp();  // before the stage is filled again
+    }
+  }
+};
+
+// Sum over the `lanes` neighbouring lanes of a row, at every one of them.  L = 0: any number of lanes up to 32.
+template <int L>
+__device__ __forceinline__ float row_sum(F2 two, uint32_t in_row, uint32_t lanes) {
+  float v, w;
+  f2_unpack(two, v, w);
+  v += w;
+  if constexpr (L > 0) {
+#pragma unroll
+    for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+  } else {
+    for (uint32_t o = 1; o < lanes; o <<= 1) {
+      w = __shfl_down_sync(0xffffffffu, v, o);
+      if (in_row + o < lanes) v += w;
+    }
+    return __shfl_sync(0xffffffffu, v, (threadIdx.x & 31u) - in_row);
+  }
+}
+
+// The shared memory of a CTA: the table, the weights in binary32, and for each warp cosines, sines, positions and the ring.
+struct Layout {
+  uint32_t gamma, warps, warp_bytes, positions, ring;  // byte offsets; the last two within a warp's part
+  __host__ __device__ Layout(uint32_t pairs, uint32_t head_dim, int weights, uint32_t group_bytes) {
+    const uint32_t row = (head_dim * 4 + 15) / 16 * 16, half = (pairs * 4 + 15) / 16 * 16;
+    gamma = pairs * 16;
+    warps = gamma + weights * row;
+    positions = 2 * half;
+    ring = positions + kStages * 16;
+    warp_bytes = ring + kStages * group_bytes;
+  }
+  __host__ __device__ uint32_t bytes() const { return warps + kWarps * warp_bytes; }
+};
+
+// A walk over units: the tokens of all sequences, times the parts that each token's groups of rows are cut into (part by part).  A
+// warp's units are a stride apart, taken apart into sequences and tokens once, so that going on needs no division.
+struct Walk {
+  uint32_t b, t, part, i;  // sequence, token, part, group of rows
+  bool on;
+  uint32_t sequences, tokens;  // the stride
+  __device__ __forceinline__ Walk(const RopeArgs& a, uint32_t unit, uint32_t stride, uint32_t parts) {
+    const uint32_t all = a.batch * a.tokens;
+    part = unit / all;
+    const uint32_t n = unit - part * all;
+    b = n / a.tokens;
+    t = n - b * a.tokens;
+    i = part;
+    on = part < parts;
+    sequences = stride / a.tokens;
+    tokens = stride - sequences * a.tokens;
+  }
+  // true where a new unit begins
+  __device__ __forceinline__ bool next(const RopeArgs& a, uint32_t parts, uint32_t groups) {
+    i += parts;
+    if (i < groups) return false;
+    b += sequences;
+    t += tokens;
+    if (t >= a.tokens) {
+      t -= a.tokens;
+      ++b;
+    }
+    if (b >= a.batch) {  // the next part, or the end
+      part += b / a.batch;
+      b %= a.batch;
+      on = part < parts;
+    }
+    i = part;
+    return true;
+  }
+  __device__ __forceinline__ uint64_t row0(const HeadsArg& h) const { return (uint64_t)h.data + b * h.batch + t * h.token; }
+};
+
+// The table and the weights into shared memory, by the whole CTA.
+__device__ __forceinline__ void stage_table(const RopeArgs& a, char* shared, const Layout& l, const void* g0, const void* g1, int weights) {
+  for (uint32_t i = threadIdx.x; i < a.pairs; i += kThreads) ((ulonglong2*)shared)[i] = ((const ulonglong2*)a.table)[i];
+  const uint32_t row = (a.head_dim + 3) / 4 * 4;
+  float* gamma = (float*)(shared + l.gamma);
+  for (int w = 0; w < weights; ++w) {
+    const void* g = w ? g1 : g0;
+    for (uint32_t i = threadIdx.x; i < a.head_dim; i += kThreads) gamma[w * row + i] = g ? load_param(g, i, a.wdt) : 1.0f;
+  }
+}
+
+// The positions of a unit's token on the way to its stage.
+__device__ __forceinline__ void copy_positions(const RopeArgs& a, int32_t* to, const Walk& w) {
+  const uint32_t lane = threadIdx.x & 31u;
+  if (a.positions && lane < a.axes) copy_async<4>(to + lane, a.positions + lane * a.pos_axis + w.b * a.pos_batch + w.t);
+}
+
+// The warp's cosines and sines of one token, from the positions in its stage.
+__device__ __forceinline__ void warp_phases(const RopeArgs& a, const char* table, const int32_t* at, uint32_t t, float sign, float* cs, float* sn) {
+  for (uint32_t i = threadIdx.x & 31u; i < a.pairs; i += 32) {
+    const ulonglong2 e = ((const ulonglong2*)table)[i];
+    const int64_t pos = a.positions ? (int64_t)at[e.y < a.axes ? (uint32_t)e.y : a.axes - 1] : a.first + t;
+    const float2 v = phase(e.x, pos, a.scale, sign);
+    cs[i] = v.x;
+    sn[i] = v.y;
+  }
+}
+
+enum { kPlain = 0, kNorm = 1 };
+
+// Forward of both operators, and the rotation's backward.  The rows of a token are those of its queries' heads, then those of its
+// keys'.
+template <int DT, int V, bool INTER, int L, int NORM>
+__global__ void __launch_bounds__(kThreads, V == 1 ? 2 : 3) rope_kernel(const __grid_constant__ RopeArgs a) {
+  constexpr int K = kLaneElems / (2 * V);
+  using Rows = Group<DT, V, K, L>;
+  extern __shared__ __align__(16) char shared[];
+  const Layout lay(a.pairs, a.head_dim, NORM == kNorm ? 2 : 0, Rows::kGroupBytes);
+  const uint32_t warp = threadIdx.x >> 5;
+  const Lane<L> l(a);
+  const Places<V, K, INTER, L> p(a, l);
+  const Rows rows(a);
+  char* mine = shared + lay.warps + warp * lay.warp_bytes;
+  float* cs = (float*)mine;
+  float* sn = cs + (a.pairs + 3) / 4 * 4;
+  int32_t* positions = (int32_t*)(mine + lay.positions);
+  char* ring = mine + lay.ring;
+  const uint32_t heads0 = a.heads[0], heads = heads0 + a.heads[1];
+  const uint32_t groups = (heads + l.per - 1) / l.per;
+  enter_grid();
+
+  Walk ahead(a, blockIdx.x * kWarps + warp, gridDim.x * kWarps, a.parts);
+  Walk now = ahead;
+  bool fresh = true;
+  typename Rows::Source from{0, 0, a.in[0].head, a.in[1].head, heads0, heads}, to{0, 0, a.out[0].head, a.out[1].head, heads0, heads};
+  const auto fetch = [&](uint32_t stage) {
+    if (ahead.on) {
+      if (fresh) {
+        from.q = ahead.row0(a.in[0]);
+        from.k = ahead.row0(a.in[1]) - heads0 * a.in[1].head;
+        copy_positions(a, positions + 4 * stage, ahead);
+      }
+      rows.fetch(ring + stage * Rows::kGroupBytes, from, ahead.i * l.per, l);
+      fresh = ahead.next(a, a.parts, groups);
+    }
+    copy_commit();
+  };
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) fetch(s);
+  stage_table(a, shared, lay, a.gamma[0], a.gamma[1], NORM == kNorm ? 2 : 0);
+  __syncthreads();
+
+  Angles<V, K, INTER, L> angles;
+  bool begins = true;
+  const float sign = a.back ? -1.0f : 1.0f;
+  const float* gamma = (const float*)(shared + lay.gamma);
+  const uint32_t gamma_row = (a.head_dim + 3) / 4 * 4;
+  for (uint32_t stage = 0; now.on; stage = (stage + 1) % kStages) {
+    copy_wait<kStages - 2>();
+    if (L == 0 || begins) __syncwarp();  // what other lanes copied is here, and the last token's cosines have been read
+    if (begins) {
+      warp_phases(a, shared, positions + 4 * stage, now.t, sign, cs, sn);
+      __syncwarp();
+      angles.read(p, cs, sn);
+      to.q = now.row0(a.out[0]);
+      to.k = now.row0(a.out[1]) - heads0 * a.out[1].head;
+    }
+    const uint32_t row = now.i * l.per + l.row;
+    char* at = ring + stage * Rows::kGroupBytes;
+    F2 fa[K][kHalf<V>], fb[K][kHalf<V>];
+#pragma unroll
+    for (int k = 0; k < K; ++k) rows.read(at, p, k, l, fa[k], fb[k]);
+    fetch((stage + kStages - 1) % kStages);
+    if (NORM == kNorm) {
+      F2 sa = f2_both(0.0f), sb = f2_both(0.0f);
+#pragma unroll
+      for (int k = 0; k < K; ++k)
+#pragma unroll
+        for (int j = 0; j < kHalf<V>; ++j) {
+          sa = f2_fma(fa[k][j], fa[k][j], sa);
+          sb = f2_fma(fb[k][j], fb[k][j], sb);
+        }
+      const F2 rstd = f2_both(rsqrtf(row_sum<L>(f2_add(sa, sb), l.slot, a.lanes) * a.inv_dim + a.eps));
+      const float* weights = gamma + (row >= heads0 ? gamma_row : 0u);
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        F2 g[kHalf<V>];
+        read_floats<V>(weights + p.at[k], g);
+#pragma unroll
+        for (int j = 0; j < kHalf<V>; ++j) fa[k][j] = f2_mul(f2_mul(fa[k][j], rstd), g[j]);
+        read_floats<V>(weights + p.to[k], g);
+#pragma unroll
+        for (int j = 0; j < kHalf<V>; ++j) fb[k][j] = f2_mul(f2_mul(fb[k][j], rstd), g[j]);
+      }
+    }
+    const uint64_t out = L ? to.row(row) + l.slot * Rows::kBytes : 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (p.turning(k)) angles.turn(k, fa[k], fb[k]);
+      // without a norm, what does not turn stays in its stage as it came, bit for bit
+      if (NORM == kNorm || p.turning(k)) rows.write(at, out, p, k, l, row < heads, fa[k], fb[k]);
+    }
+    rows.flush(at, to, now.i * l.per, l);
+    begins = now.next(a, a.parts, groups);
+  }
+}
+
+// The norm's backward.  A CTA takes rows of queries or of keys only (the first ctas0 CTAs those of queries), so that a lane
+// keeps one set of sums for grad_gamma; they are added up over the CTA's rows and left in the scratch, one row of head_dim a CTA.
+template <int DT, int V, bool INTER, int L>
+__global__ void __launch_bounds__(kThreads, V == 1 ? 1 : 2) qknorm_bwd_kernel(const __grid_constant__ RopeArgs a) {
+  constexpr int K = kLaneElems / (2 * V);
+  using Rows = Group<DT, V, K, L>;
+  extern __shared__ __align__(16) char shared[];
+  const Layout lay(a.pairs, a.head_dim, 1, 2 * Rows::kGroupBytes);
+  const uint32_t warp = threadIdx.x >> 5;
+  const Lane<L> l(a);
+  const Places<V, K, INTER, L> p(a, l);
+  const Rows rows(a);
+  char* mine = shared + lay.warps + warp * lay.warp_bytes;
+  float* cs = (float*)mine;
+  float* sn = cs + (a.pairs + 3) / 4 * 4;
+  int32_t* positions = (int32_t*)(mine + lay.positions);
+  char* ring = mine + lay.ring;
+  const int which = blockIdx.x >= a.ctas0;
+  const HeadsArg& x = a.in[which];
+  const HeadsArg& g = a.grad[which];
+  const HeadsArg& o = a.out[which];
+  const uint32_t cta = which ? blockIdx.x - a.ctas0 : blockIdx.x, ctas = which ? gridDim.x - a.ctas0 : a.ctas0;
+  const uint32_t heads = a.heads[which], groups = (heads + l.per - 1) / l.per;
+  const uint32_t parts = a.parts < groups ? a.parts : groups;
+  enter_grid();
+
+  Walk ahead(a, cta * kWarps + warp, ctas * kWarps, parts);
+  Walk now = ahead;
+  bool fresh = true;
+  // all rows count as queries' here
+  typename Rows::Source from_x{0, 0, x.head, 0, heads, heads}, from_g{0, 0, g.head, 0, heads, heads}, to{0, 0, o.head, 0, heads, heads};
+  const auto fetch = [&](uint32_t stage) {
+    if (ahead.on) {
+      if (fresh) {
+        from_x.q = ahead.row0(x);
+        from_g.q = ahead.row0(g);
+        copy_positions(a, positions + 4 * stage, ahead);
+      }
+      char* at = ring + stage * 2 * Rows::kGroupBytes;
+      rows.fetch(at, from_x, ahead.i * l.per, l);
+      rows.fetch(at + Rows::kGroupBytes, from_g, ahead.i * l.per, l);
+      fresh = ahead.next(a, parts, groups);
+    }
+    copy_commit();
+  };
+#pragma unroll
+  for (int s = 0; s < kStages - 1; ++s) fetch(s);
+  stage_table(a, shared, lay, a.gamma[which], nullptr, 1);
+  __syncthreads();
+
+  Angles<V, K, INTER, L> angles;
+  F2 sa[K][kHalf<V>], sb[K][kHalf<V>];
+#pragma unroll
+  for (int k = 0; k < K; ++k)
+#pragma unroll
+    for (int j = 0; j < kHalf<V>; ++j) sa[k][j] = sb[k][j] = f2_both(0.0f);
+  bool begins = true;
+  const float* gamma = (const float*)(shared + lay.gamma);
+  for (uint32_t stage = 0; now.on; stage = (stage + 1) % kStages) {
+    copy_wait<kStages - 2>();
+    if (L == 0 || begins) __syncwarp();
+    if (begins) {
+      warp_phases(a, shared, positions + 4 * stage, now.t, -1.0f, cs, sn);
+      __syncwarp();
+      angles.read(p, cs, sn);
+      to.q = now.row0(o);
+    }
+    const uint32_t row = now.i * l.per + l.row;
+    const bool on = l.on && row < heads;
+    F2 xa[K][kHalf<V>], xb[K][kHalf<V>], ua[K][kHalf<V>], ub[K][kHalf<V>];
+    char* at = ring + stage * 2 * Rows::kGroupBytes;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      rows.read(at, p, k, l, xa[k], xb[k]);
+      rows.read(at + Rows::kGroupBytes, p, k, l, ua[k], ub[k]);
+    }
+    fetch((stage + kStages - 1) % kStages);
+    F2 sum = f2_both(0.0f), other = f2_both(0.0f);
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int j = 0; j < kHalf<V>; ++j) {
+        sum = f2_fma(xa[k][j], xa[k][j], sum);
+        other = f2_fma(xb[k][j], xb[k][j], other);
+      }
+    // a row that does not exist is zeros in x and in the gradient: with this rstd it adds nothing to any sum
+    float root = rsqrtf(row_sum<L>(f2_add(sum, other), l.slot, a.lanes) * a.inv_dim + a.eps);
+    if (!on) root = 0.0f;
+    const F2 rstd = f2_both(root);
+    sum = other = f2_both(0.0f);
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+      if (p.turning(k)) angles.turn(k, ua[k], ub[k]);
+      F2 w[kHalf<V>];
+      read_floats<V>(gamma + p.at[k], w);
+#pragma unroll
+      for (int j = 0; j < kHalf<V>; ++j) {
+        xa[k][j] = f2_mul(xa[k][j], rstd);  // xhat
+        sa[k][j] = f2_fma(ua[k][j], xa[k][j], sa[k][j]);
+        ua[k][j] = f2_mul(ua[k][j], w[j]);
+        sum = f2_fma(ua[k][j], xa[k][j], sum);
+      }
+      read_floats<V>(gamma + p.to[k], w);
+#pragma unroll
+      for (int j = 0; j < kHalf<V>; ++j) {
+        xb[k][j] = f2_mul(xb[k][j], rstd);
+        sb[k][j] = f2_fma(ub[k][j], xb[k][j], sb[k][j]);
+        ub[k][j] = f2_mul(ub[k][j], w[j]);
+        other = f2_fma(ub[k][j], xb[k][j], other);
+      }
+    }
+    const F2 mean = f2_both(-row_sum<L>(f2_add(sum, other), l.slot, a.lanes) * a.inv_dim);
+    const uint64_t out = L ? to.row(row) + l.slot * Rows::kBytes : 0;
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+#pragma unroll
+      for (int j = 0; j < kHalf<V>; ++j) {
+        ua[k][j] = f2_mul(f2_fma(mean, xa[k][j], ua[k][j]), rstd);
+        ub[k][j] = f2_mul(f2_fma(mean, xb[k][j], ub[k][j]), rstd);
+      }
+      rows.write(at, out, p, k, l, on, ua[k], ub[k]);
+    }
+    rows.flush(at, to, now.i * l.per, l);
+    begins = now.next(a, parts, groups);
+  }
+  if (!a.partials) return;
+  copy_wait<0>();
+  __syncthreads();  // the rings' place becomes the sums'
+  const uint32_t D = a.head_dim, all = kWarps * l.per;
+  float* sums = (float*)(shared + lay.warps);
+  if (l.on) {
+    float* own = sums + (warp * l.per + l.row) * D;
+#pragma unroll
+    for (int k = 0; k < K; ++k)
+#pragma unroll
+      for (int j = 0; j < kHalf<V>; ++j) {
+        float u, v;
+        f2_unpack(sa[k][j], u, v);
+        if (p.has_first(k)) {
+          own[p.at[k] + 2 * j] = u;
+          if (V > 1) own[p.at[k] + 2 * j + 1] = v;
+        }
+        f2_unpack(sb[k][j], u, v);
+        if (p.has_second(k)) {
+          own[p.to[k] + 2 * j] = u;
+          if (V > 1) own[p.to[k] + 2 * j + 1] = v;
+        }
+      }
+  }
+  __syncthreads();
+  for (uint32_t d = threadIdx.x; d < D; d += kThreads) {
+    float s = 0.0f;
+    for (uint32_t r = 0; r < all; ++r) s += sums[r * D + d];
+    a.partials[(uint64_t)blockIdx.x * D + d] = s;
+  }
+}
+
+template <int DT, int V, bool INTER, int L>
+cudaError_t launch_one(int mode, const RopeArgs& a, unsigned grid, cudaStream_t st) {
+  static std::atomic<uint64_t> ready[3] = {};
+  constexpr uint32_t group = Group<DT, V, kLaneElems / (2 * V), L>::kGroupBytes;
+  // the sums of the backward pass take the rings' place: 16 floats a lane
+  static_assert(kStages * 2 * group >= 32 * kLaneElems * sizeof(float), "the sums fit in the rings");
+  const int weights = mode == kRopeFwdNorm ? 2 : (mode == kRopeBwdNorm ? 1 : 0);
+  const uint32_t ring = mode == kRopeBwdNorm ? 2 * group : group;
+  const size_t smem = Layout(a.pairs, a.head_dim, weights, ring).bytes();
+  const size_t most = Layout(kMaxHeadDim / 2, kMaxHeadDim, weights, ring).bytes();  // the leave is asked for once, for any shape
+  const auto go = [&](void (*kernel)(const RopeArgs)) {
+    const cudaError_t e = allow_shared(kernel, most, ready[mode]);
+    return e != cudaSuccess ? e : launch_overlapped(kernel, dim3(grid), kThreads, smem, st, a);
+  };
+  if (mode == kRopeBwdNorm) return go(qknorm_bwd_kernel<DT, V, INTER, L>);
+  return mode == kRopeFwdNorm ? go(rope_kernel<DT, V, INTER, L, kNorm>) : go(rope_kernel<DT, V, INTER, L, kPlain>);
+}
+
+template <int DT, int V, int L>
+cudaError_t launch_layout(int mode, const RopeArgs& a, unsigned grid, cudaStream_t st) {
+  if constexpr (V > 1)
+    if (a.interleaved) return launch_one<DT, V, true, L>(mode, a, grid, st);
+  return launch_one<DT, V, false, L>(mode, a, grid, st);
+}
+
+}  // namespace
+
+template <int DT>
+cudaError_t launch_rope_kernel(int mode, uint32_t V, const RopeArgs& a, unsigned grid, cudaStream_t st) {
+  constexpr int W = 16 / Io<DT>::kBytes;  // the widest vector
+  bool near = true;  // heads less than 4 GB apart
+  for (const HeadsArg* h : {&a.in[0], &a.in[1], &a.grad[0], &a.grad[1], &a.out[0], &a.out[1]}) near = near && h->head >> 32 == 0;
+  if (V == W && near && 2 * a.pairs == a.head_dim) {
+    if (a.head_dim == 64) return launch_layout<DT, W, 4>(mode, a, grid, st);
+    if (a.head_dim == 128) return launch_layout<DT, W, 8>(mode, a, grid, st);
+    if (a.head_dim == 256) return launch_layout<DT, W, 16>(mode, a, grid, st);
+  }
+  if (V == W) return launch_layout<DT, W, 0>(mode, a, grid, st);
+  if (DT == kBF16 && V == 4) return launch_layout<DT, 4, 0>(mode, a, grid, st);
+  return V == 2 ? launch_layout<DT, 2, 0>(mode, a, grid, st) : launch_layout<DT, 1, 0>(mode, a, grid, st);
+}
+
+}  // namespace s2a

@@ -320,6 +320,29 @@ def test_rows_do_not_leak_into_their_neighbours(D):
             assert not got[0][bad].any()       # a sum of squares beyond binary32
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("D,rot", [(40, 16), (128, 64), (11, 4), (24, 2)])
+def test_what_does_not_turn_is_copied_bit_for_bit(D, rot, dtype):
+    """Infinities, NaN and negative zeros behind the turning part stay what and where they are; so do those of a pair in their pair."""
+    dt = DT[dtype]
+    x = _normal((2, 3, 5, D), dt, "x", D)
+    x[..., rot::2] = float("inf")
+    x[..., rot + 1::3] = -0.0
+    x[..., D - 1] = float("nan")
+    x[0, :, :, 0] = float("inf")
+    table = s2a.rope_table(rot).cuda()
+    for inter in (False, True):
+        y = torch.empty_like(x)
+        s2a.s2a_rope_fwd(x, None, y, None, None, table, interleaved=inter)
+        _done()
+        kind = {2: torch.int16, 4: torch.int32}[dt.itemsize]
+        assert torch.equal(y[..., rot:].contiguous().view(kind), x[..., rot:].contiguous().view(kind))
+        pair = [0, 1] if inter else [0, rot // 2]
+        others = [i for i in range(rot) if i not in pair]
+        assert bool(torch.isfinite(y[..., others]).all()) and bool(torch.isfinite(y[1, ..., :rot]).all())
+        assert not bool(torch.isfinite(y[0, ..., pair[0]]).any())
+
+
 def test_broadcast_keys_and_shared_positions():
     """One key row expanded over heads and batch is read as it is; each copy has its own gradient."""
     one = _normal((1, 6, 1, 32), torch.bfloat16, "k")
