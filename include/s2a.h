@@ -382,15 +382,14 @@ int s2a_relbias_log_buckets(int32_t* buckets, int64_t first_distance, size_t cou
  * Queries q and keys k (and what belongs to them) are tensors [batch, tokens, heads, head_dim] given by
  * their strides, so that every order of the first three dimensions and slices of a packed buffer are
  * taken as they are; the elements of a row of head_dim are contiguous.  One call serves both; heads_k = 0
- * with NULL for the keys' tensors serves one alone.
- *   strides  HOST memory: three numbers for each tensor, in the order of the call's tensors (queries and
- *            keys alternate): elements from batch to batch, token to token, head to head.  Inputs may have
- *            any, 0 included (then each row has its own output, or gradient); the rows of an output must
- *            not overlap.  An output may be the input it belongs to (for the backward call of the norm:
- *            the gradient or x), with the same strides; tensors inside one buffer may interleave.  Any
- *            other overlap returns S2A_ERR_OVERLAP.  Pointers need the alignment of their element type
- *            only; rows on the 16-byte grid, whose rot_dim / 2 and head_dim are whole 16-byte vectors too,
- *            are the fastest.
+ * (its pointers are ignored then) serves queries alone.  These calls take their arguments in a struct, of which
+ * a call ignores the members that are not its own.
+ *   *_stride  elements from batch to batch, token to token, head to head.  Inputs may have any, 0 included (then each row
+ *            has its own output, or gradient); the rows of an output must not overlap.  An output may be the
+ *            input it belongs to (for the backward call of the norm: the gradient or x), with the same
+ *            strides; tensors inside one buffer may interleave.  Any other overlap returns S2A_ERR_OVERLAP.
+ *            Pointers need the alignment of their element type only; rows on the 16-byte grid, whose
+ *            rot_dim / 2 and head_dim are whole 16-byte vectors too, are the fastest.
  *   table    (turn, axis) of each of the rot_dim / 2 pairs, two 64-bit words in DEVICE memory, 16-byte aligned:
  *            turn = the pair's radians per position / (2 pi), as a binary fraction times 2^64, so that
  *            the angle of any position is exact; axis: which of a token's positions it goes by (an axis
@@ -398,34 +397,39 @@ int s2a_relbias_log_buckets(int32_t* buckets, int64_t first_distance, size_t cou
  *   positions  int32 in DEVICE memory, read when the kernel runs: that of (axis, batch, token) lies at
  *            axis * pos_axis_stride + batch * pos_batch_stride + token (a stride of 0 shares them).  NULL,
  *            with one axis: first + token.
- *   rot_dim  the first rot_dim elements of a row turn, the rest stays: even, 2 .. head_dim; 0 (with table
- *            NULL) for a norm without rotation.  Pairs are (i, i + rot_dim / 2), or (2 i, 2 i + 1) where `interleaved`.
+ *   rot_dim  the first rot_dim elements of a row turn, the rest stays: even, 2 .. head_dim; 0 (table and positions are
+ *            ignored) for a norm without rotation.  Pairs are (i, i + rot_dim / 2), or (2 i, 2 i + 1) where `interleaved`.
  *   scale    multiplies the cosines and sines (1 but for some scaled contexts): finite
- * head_dim: 1 .. 512; axes: 1 .. 4; heads: at most 65535 each; batch * tokens at most 2^31-1.
+ *   gamma_*  head_dim elements of type wdt, or NULL (ones)
+ * head_dim: 1 .. 512; axes: 1 .. 4; heads: at most 65535 each, less than 2^32 elements from head to head; batch * tokens at
+ * most 2^31-1.
  */
+typedef struct {
+  const void *q, *k;               /* inputs; for s2a_rope_bwd the gradients                    */
+  void *out_q, *out_k;             /* outputs; for the backward calls the inputs' gradients     */
+  const int32_t* positions;
+  const uint64_t* table;
+  const void *gamma_q, *gamma_k;   /* norms only, from here to scratch                          */
+  const void *grad_q, *grad_k;     /* backward of the norm: the outputs' gradients              */
+  void *grad_gamma_q, *grad_gamma_k, *scratch;
+  int64_t first;
+  size_t pos_batch_stride, pos_axis_stride, axes;
+  size_t batch, tokens, heads_q, heads_k, head_dim, rot_dim;
+  size_t q_stride[3], k_stride[3], out_q_stride[3], out_k_stride[3], grad_q_stride[3], grad_k_stride[3];
+  float scale, eps;
+  int interleaved, dt, wdt;
+} s2a_rope_args;
 
-/* Forward: with the angle w = position * frequency of its pair, (a, b) -> (a cos w - b sin w, a sin w + b cos w).
- * Tensors, and strides[12] in this order: q, k, out_q, out_k. */
-int s2a_rope_fwd(const void* q, const void* k, void* out_q, void* out_k, const size_t* strides, const int32_t* positions,
-                 int64_t first, size_t pos_batch_stride, size_t pos_axis_stride, size_t axes, const uint64_t* table,
-                 size_t batch, size_t tokens, size_t heads_q, size_t heads_k, size_t head_dim, size_t rot_dim, int interleaved,
-                 float scale, int dt, void* cuda_stream);
+/* Forward: with the angle w = position * frequency of its pair, (a, b) -> (a cos w - b sin w, a sin w + b cos w). */
+int s2a_rope_fwd(const s2a_rope_args* args, void* cuda_stream);
 
-/* Backward: the gradients turn by the opposite angles (and are multiplied by the same scale).  Keeps nothing of the forward
- * pass but the positions.  Tensors, and strides[12]: grad_q, grad_k, grad_in_q, grad_in_k. */
-int s2a_rope_bwd(const void* grad_q, const void* grad_k, void* grad_in_q, void* grad_in_k, const size_t* strides,
-                 const int32_t* positions, int64_t first, size_t pos_batch_stride, size_t pos_axis_stride, size_t axes,
-                 const uint64_t* table, size_t batch, size_t tokens, size_t heads_q, size_t heads_k, size_t head_dim,
-                 size_t rot_dim, int interleaved, float scale, int dt, void* cuda_stream);
+/* Backward: the gradients (q, k) turn by the opposite angles, and are multiplied by the same scale.  Keeps nothing of the forward
+ * pass but the positions. */
+int s2a_rope_bwd(const s2a_rope_args* args, void* cuda_stream);
 
 /* The norm of each head's row, and the rotation, in one pass: rstd = 1 / sqrt(sum(x^2) / head_dim + eps),
- * out = rotation(x * rstd * gamma).  gamma_q, gamma_k: head_dim elements of type wdt, or NULL (ones).  Rows whose sum of squares
- * is beyond binary32 become zeros.  Tensors, and strides[12]: q, k, out_q, out_k. */
-int s2a_qknorm_rope_fwd(const void* q, const void* k, const void* gamma_q, const void* gamma_k, void* out_q, void* out_k,
-                        const size_t* strides, const int32_t* positions, int64_t first, size_t pos_batch_stride,
-                        size_t pos_axis_stride, size_t axes, const uint64_t* table, size_t batch, size_t tokens, size_t heads_q,
-                        size_t heads_k, size_t head_dim, size_t rot_dim, int interleaved, float scale, float eps, int dt, int wdt,
-                        void* cuda_stream);
+ * out = rotation(x * rstd * gamma).  eps: finite, not negative.  Rows whose sum of squares is beyond binary32 become zeros. */
+int s2a_qknorm_rope_fwd(const s2a_rope_args* args, void* cuda_stream);
 
 /* Bytes of scratch for the weights' gradients of s2a_qknorm_rope_bwd (0 where head_dim is 0 or above 512): the same
  * for every batch and number of tokens, at most 889 * head_dim * 4. */
@@ -433,16 +437,11 @@ size_t s2a_qknorm_rope_scratch_bytes(size_t batch, size_t tokens, size_t heads_q
 
 /* Its backward pass, from x alone (the inputs q and k of the forward call; rstd is computed again).  With u = the gradient turned
  * back, a = u * gamma and xhat = x * rstd:
- *   grad_in = rstd * (a - xhat * sum(a * xhat) / head_dim),  grad_gamma = sum over all rows of u * xhat
+ *   out = rstd * (a - xhat * sum(a * xhat) / head_dim),  grad_gamma = sum over all rows of u * xhat
  *   grad_gamma_q, grad_gamma_k  out  head_dim elements of type wdt, or NULL each; overwritten, zeros where there are no rows
  *   scratch                     s2a_qknorm_rope_scratch_bytes(...) bytes; may be NULL where both are
- * Tensors, and strides[18]: grad_q, grad_k, q, k, grad_in_q, grad_in_k. */
-int s2a_qknorm_rope_bwd(const void* grad_q, const void* grad_k, const void* q, const void* k, const void* gamma_q,
-                        const void* gamma_k, void* grad_in_q, void* grad_in_k, void* grad_gamma_q, void* grad_gamma_k,
-                        void* scratch, const size_t* strides, const int32_t* positions, int64_t first, size_t pos_batch_stride,
-                        size_t pos_axis_stride, size_t axes, const uint64_t* table, size_t batch, size_t tokens, size_t heads_q,
-                        size_t heads_k, size_t head_dim, size_t rot_dim, int interleaved, float scale, float eps, int dt, int wdt,
-                        void* cuda_stream);
+ */
+int s2a_qknorm_rope_bwd(const s2a_rope_args* args, void* cuda_stream);
 
 /* A table of turns, written to HOST memory: 2 words for each of the rot_dim / 2 pairs.  The pairs are split evenly
  * among the axes, in order (1 .. 4, dividing rot_dim / 2), each with the frequencies base^(-j / n), j = 0 .. n - 1, of its n

@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -120,9 +121,6 @@ def lib() -> ctypes.CDLL:
             f.argtypes = [c.c_void_p, c.c_void_p, c.c_void_p, c.c_size_t, c.c_int, c.c_void_p]
             f.restype = c.c_int
         ptr, size = c.c_void_p, c.c_size_t
-        # positions .. interleaved of the calls that turn
-        turn = [ptr, c.c_int64, size, size, size, ptr] + [size] * 6 + [c.c_int]
-        rope = [ptr] * 5 + turn + [c.c_float, c.c_int, ptr]
         for name, res, args in (
                 ("s2a_layernorm_scratch_bytes", size, [size, size]),
                 ("s2a_layernorm_fwd", c.c_int, [ptr] * 5 + [size] * 4 + [c.c_float, c.c_int, c.c_int, ptr]),
@@ -134,11 +132,11 @@ def lib() -> ctypes.CDLL:
                 ("s2a_relbias_fwd", c.c_int, [ptr, ptr, ptr, c.c_int, ptr] + [size] * 5 + [c.c_int, c.c_int, ptr]),
                 ("s2a_relbias_bwd", c.c_int, [ptr, ptr, c.c_int, ptr, ptr] + [size] * 5 + [c.c_int, c.c_int, ptr]),
                 ("s2a_relbias_log_buckets", c.c_int, [ptr, c.c_int64, size, size, size, c.c_int]),
-                ("s2a_rope_fwd", c.c_int, rope),
-                ("s2a_rope_bwd", c.c_int, rope),
-                ("s2a_qknorm_rope_fwd", c.c_int, [ptr] * 7 + turn + [c.c_float, c.c_float, c.c_int, c.c_int, ptr]),
+                ("s2a_rope_fwd", c.c_int, [c.c_char_p, ptr]),           # s2a_rope_args as packed bytes
+                ("s2a_rope_bwd", c.c_int, [c.c_char_p, ptr]),
+                ("s2a_qknorm_rope_fwd", c.c_int, [c.c_char_p, ptr]),
                 ("s2a_qknorm_rope_scratch_bytes", size, [size] * 5),
-                ("s2a_qknorm_rope_bwd", c.c_int, [ptr] * 12 + turn + [c.c_float, c.c_float, c.c_int, c.c_int, ptr]),
+                ("s2a_qknorm_rope_bwd", c.c_int, [c.c_char_p, ptr]),
                 ("s2a_rope_table", c.c_int, [ptr, size, c.c_double, c.c_int] + [c.c_double] * 4 + [size]),
                 ("s2a_step_plan_bytes", size, [ptr, size]),
                 ("s2a_step_plan_fill", c.c_int, [ptr, size, c.c_int, c.c_int, c.c_int, ptr, ptr]),
@@ -603,7 +601,7 @@ def log_buckets(first_distance: int, count: int, n_buckets: int, max_distance: i
 
 # ------------------------------------------- rotary positions, norms of queries and keys with them
 _SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
-_Strides4, _Strides6 = ctypes.c_size_t * 12, ctypes.c_size_t * 18
+_rope_args = struct.Struct("@13Pq27Q2f3i0q").pack   # s2a_rope_args
 
 
 def rope_table(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_length: float = 0.0,
@@ -617,59 +615,71 @@ def rope_table(rot_dim: int, base: float = 10000.0, scaling: str = "none", facto
     return out
 
 
-def _heads_like(t, like, what: str):
-    """The strides of a tensor of heads [batch, tokens, heads, head_dim] of the shape and dtype of `like`."""
-    if t is None or t.shape != like.shape or t.dtype is not like.dtype:
-        raise S2AError("%s must match in shape and dtype" % what)
+def _heads(t, shape, dtype, what: str):
+    """The strides of a tensor of heads of this shape and dtype."""
+    if t.shape != shape or t.dtype is not dtype:
+        raise S2AError("%s must be [batch, tokens, heads, head_dim] like what it belongs to, and of its dtype" % what)
     stride = t.stride()
-    if stride[3] != 1 and like.shape[3] != 1:
+    if stride[3] != 1 and shape[3] != 1:
         raise S2AError("%s: the elements of a head's row must be contiguous" % what)
     return stride
 
 
-def _rope_args(q, k, table, positions):
-    """(batch, tokens, heads_q, heads_k, head_dim, rot_dim), and what belongs to the positions."""
-    shape = q.shape
+def _address(t):
+    return 0 if t is None else t.data_ptr()
+
+
+_NONE = (0, 0, 0, 0)
+
+
+def _rope(call, q, k, out_q, out_k, positions, table, scale, interleaved, first, dev, eps=0.0, wdt=F32, gamma_q=0, gamma_k=0,
+          grad_q=None, grad_k=None, sum_q=0, sum_k=0, scratch=0):
+    shape, dtype = q.shape, q.dtype
     if len(shape) != 4:
         raise S2AError("queries and keys must be [batch, tokens, heads, head_dim]")
     batch, tokens, heads_q, dim = shape
-    heads_k = 0
+    a, b = _heads(q, shape, dtype, "q"), _heads(out_q, shape, dtype, "the queries' output")
+    e = _heads(grad_q, shape, dtype, "grad_q") if grad_q is not None else _NONE
+    c, d, f, heads_k = _NONE, _NONE, _NONE, 0
     if k is not None:
         other = k.shape
-        if len(other) != 4 or other[0] != batch or other[1] != tokens or other[3] != dim or k.dtype is not q.dtype:
+        if len(other) != 4 or other[0] != batch or other[1] != tokens or other[3] != dim:
             raise S2AError("the keys must match the queries but for the number of heads")
+        if out_k is None or (grad_q is not None and grad_k is None):
+            raise S2AError("the keys' tensors are needed")
         heads_k = other[2]
-    rot, where = 0, None
+        c, d = _heads(k, other, dtype, "k"), _heads(out_k, other, dtype, "the keys' output")
+        if grad_k is not None:
+            f = _heads(grad_k, other, dtype, "grad_k")
+    rot = where = pos = per_batch = per_axis = 0
+    axes = 1
     if table is not None:
-        if table.dtype is not torch.int64 or table.dim() != 2 or table.shape[1] != 2 or not table.is_contiguous():
+        size = table.shape
+        if table.dtype is not torch.int64 or len(size) != 2 or size[1] != 2 or not table.is_contiguous():
             raise S2AError("the table must be contiguous int64 [rot_dim / 2, 2]")
-        rot, where = 2 * table.shape[0], table.data_ptr()
-    if positions is None:
-        return (batch, tokens, heads_q, heads_k, dim, rot), (None, 0, 0, 1, where)
-    shape, stride = positions.shape, positions.stride()
-    n = len(shape)
-    if positions.dtype is not torch.int32 or n < 1 or n > 3 or shape[-1] != tokens or (n > 1 and shape[-2] != batch):
-        raise S2AError("positions must be int32 [tokens], [batch, tokens] or [axes, batch, tokens]")
-    if tokens > 1 and stride[-1] != 1:
-        raise S2AError("the positions of a sequence's tokens must be contiguous")
-    return (batch, tokens, heads_q, heads_k, dim, rot), (
-        positions.data_ptr(), stride[-2] if n > 1 else 0, stride[0] if n > 2 else 0, shape[0] if n > 2 else 1, where)
-
-
-def _address(t):
-    return None if t is None else t.data_ptr()
-
-
-def _rope(call, q, k, out_q, out_k, positions, table, scale, interleaved, first):
-    if table is None:
-        raise S2AError("a table of turns is needed")
-    dev = _on_device(q, k, out_q, out_k, positions, table)
-    size, (pos, per_batch, per_axis, axes, where) = _rope_args(q, k, table, positions)
-    a, c = _heads_like(q, q, "the queries"), _heads_like(out_q, q, "the queries' output")
-    b, d = (_heads_like(k, k, "the keys"), _heads_like(out_k, k, "the keys' output")) if k is not None else (a, a)
-    strides = _Strides4(a[0], a[1], a[2], b[0], b[1], b[2], c[0], c[1], c[2], d[0], d[1], d[2])
-    status = call(q.data_ptr(), _address(k), out_q.data_ptr(), _address(out_k), strides, pos, first, per_batch, per_axis, axes,
-                  where, *size, interleaved, scale, _code(q), _stream_on(dev))
+        rot, where = 2 * size[0], table.data_ptr()
+        if positions is not None:
+            size, stride = positions.shape, positions.stride()
+            n = len(size)
+            if positions.dtype is not torch.int32 or n < 1 or n > 3 or size[-1] != tokens or (n > 1 and size[-2] != batch):
+                raise S2AError("positions must be int32 [tokens], [batch, tokens] or [axes, batch, tokens]")
+            if tokens > 1 and stride[-1] != 1:
+                raise S2AError("the positions of a sequence's tokens must be contiguous")
+            pos = positions.data_ptr()
+            if n > 1:
+                per_batch = stride[-2]
+                if n > 2:
+                    per_axis, axes = stride[0], size[0]
+    code = _CODES.get(dtype)
+    try:
+        packed = _rope_args(
+            q.data_ptr(), _address(k), out_q.data_ptr(), _address(out_k), pos, where, gamma_q, gamma_k, _address(grad_q),
+            _address(grad_k), sum_q, sum_k, scratch, first, per_batch, per_axis, axes, batch, tokens, heads_q, heads_k, dim, rot, a[0],
+            a[1], a[2], c[0], c[1], c[2], b[0], b[1], b[2], d[0], d[1], d[2], e[0], e[1], e[2], f[0], f[1], f[2], scale, eps, interleaved,
+            dtype_code(q) if code is None else code, wdt)
+    except (struct.error, OverflowError) as error:
+        raise S2AError("scale, eps, interleaved and first must be plain numbers: %s" % error)
+    status = call(packed, _stream_on(dev))
     if status:
         check(status)
 
@@ -678,13 +688,19 @@ def s2a_rope_fwd(q, k, out_q, out_k, positions, table, scale: float = 1.0, inter
     """Rotary positions of queries and keys [batch, tokens, heads, head_dim] (any strides; k and out_k may be None; an
     output may be its input).  positions: int32 [tokens], [batch, tokens] or [axes, batch, tokens], or None for first +
     token; table: rope_table(...) on the GPU, or one of the caller's own."""
-    _rope((_lib or lib()).s2a_rope_fwd, q, k, out_q, out_k, positions, table, scale, interleaved, first)
+    if table is None:
+        raise S2AError("a table of turns is needed")
+    _rope((_lib or lib()).s2a_rope_fwd, q, k, out_q, out_k, positions, table, scale, interleaved, first,
+          _on_device(q, k, out_q, out_k, positions, table))
 
 
 def s2a_rope_bwd(grad_q, grad_k, grad_in_q, grad_in_k, positions, table, scale: float = 1.0, interleaved: bool = False,
                  first: int = 0) -> None:
     """The gradients of s2a_rope_fwd: turned back."""
-    _rope((_lib or lib()).s2a_rope_bwd, grad_q, grad_k, grad_in_q, grad_in_k, positions, table, scale, interleaved, first)
+    if table is None:
+        raise S2AError("a table of turns is needed")
+    _rope((_lib or lib()).s2a_rope_bwd, grad_q, grad_k, grad_in_q, grad_in_k, positions, table, scale, interleaved, first,
+          _on_device(grad_q, grad_k, grad_in_q, grad_in_k, positions, table))
 
 
 def s2a_qknorm_rope_fwd(q, k, gamma_q, gamma_k, out_q, out_k, positions, table, eps: float, scale: float = 1.0,
@@ -692,17 +708,9 @@ def s2a_qknorm_rope_fwd(q, k, gamma_q, gamma_k, out_q, out_k, positions, table, 
     """The norm of each head's row (by its root mean square; gamma_q, gamma_k [head_dim] or None) and the rotation in one pass.
     table None: the norm alone.  The rest as for s2a_rope_fwd."""
     dev = _on_device(q, k, gamma_q, gamma_k, out_q, out_k, positions, table)
-    size, (pos, per_batch, per_axis, axes, where) = _rope_args(q, k, table, positions)
-    a, c = _heads_like(q, q, "the queries"), _heads_like(out_q, q, "the queries' output")
-    b, d = (_heads_like(k, k, "the keys"), _heads_like(out_k, k, "the keys' output")) if k is not None else (a, a)
-    strides = _Strides4(a[0], a[1], a[2], b[0], b[1], b[2], c[0], c[1], c[2], d[0], d[1], d[2])
-    dim = size[4]
-    status = (_lib or lib()).s2a_qknorm_rope_fwd(
-        q.data_ptr(), _address(k), _param(gamma_q, dim, "gamma_q"), _param(gamma_k, dim, "gamma_k"), out_q.data_ptr(),
-        _address(out_k), strides, pos, first, per_batch, per_axis, axes, where, *size, interleaved, scale, eps, _code(q),
-        _param_dtype(gamma_q, gamma_k), _stream_on(dev))
-    if status:
-        check(status)
+    dim = q.shape[-1]
+    _rope((_lib or lib()).s2a_qknorm_rope_fwd, q, k, out_q, out_k, positions, table, scale, interleaved, first, dev, eps,
+          _param_dtype(gamma_q, gamma_k), _param(gamma_q, dim, "gamma_q") or 0, _param(gamma_k, dim, "gamma_k") or 0)
 
 
 def qknorm_rope_scratch_bytes(batch: int, tokens: int, heads_q: int, heads_k: int, head_dim: int) -> int:
@@ -716,21 +724,15 @@ def s2a_qknorm_rope_bwd(grad_q, grad_k, q, k, gamma_q, gamma_k, grad_in_q, grad_
     grad_q or q, grad_in_k grad_k or k."""
     dev = _on_device(q, grad_q, grad_k, k, gamma_q, gamma_k, grad_in_q, grad_in_k, grad_gamma_q, grad_gamma_k, scratch, positions,
                      table)
-    size, (pos, per_batch, per_axis, axes, where) = _rope_args(q, k, table, positions)
-    g, a, c = _heads_like(grad_q, q, "grad_q"), _heads_like(q, q, "the queries"), _heads_like(grad_in_q, q, "grad_in_q")
-    h, b, d = (_heads_like(grad_k, k, "grad_k"), _heads_like(k, k, "the keys"), _heads_like(grad_in_k, k, "grad_in_k")) \
-        if k is not None else (a, a, a)
-    strides = _Strides6(g[0], g[1], g[2], h[0], h[1], h[2], a[0], a[1], a[2], b[0], b[1], b[2], c[0], c[1], c[2], d[0], d[1], d[2])
-    dim = size[4]
-    sums = grad_gamma_q is not None or grad_gamma_k is not None
-    status = (_lib or lib()).s2a_qknorm_rope_bwd(
-        grad_q.data_ptr(), _address(grad_k), q.data_ptr(), _address(k), _param(gamma_q, dim, "gamma_q"),
-        _param(gamma_k, dim, "gamma_k"), grad_in_q.data_ptr(), _address(grad_in_k), _param(grad_gamma_q, dim, "grad_gamma_q"),
-        _param(grad_gamma_k, dim, "grad_gamma_k"), _scratch(scratch, qknorm_rope_scratch_bytes(*size[:5])) if sums else None,
-        strides, pos, first, per_batch, per_axis, axes, where, *size, interleaved, scale, eps, _code(q),
-        _param_dtype(gamma_q, gamma_k, grad_gamma_q, grad_gamma_k), _stream_on(dev))
-    if status:
-        check(status)
+    dim, room = q.shape[-1], 0
+    if grad_gamma_q is not None or grad_gamma_k is not None:
+        room = _scratch(scratch, qknorm_rope_scratch_bytes(0, 0, 0, 0, dim))
+    if grad_q is None:
+        raise S2AError("grad_q is needed")
+    _rope((_lib or lib()).s2a_qknorm_rope_bwd, q, k, grad_in_q, grad_in_k, positions, table, scale, interleaved, first, dev, eps,
+          _param_dtype(gamma_q, gamma_k, grad_gamma_q, grad_gamma_k), _param(gamma_q, dim, "gamma_q") or 0,
+          _param(gamma_k, dim, "gamma_k") or 0, grad_q, grad_k, _param(grad_gamma_q, dim, "grad_gamma_q") or 0,
+          _param(grad_gamma_k, dim, "grad_gamma_k") or 0, room)
 
 
 # --------------------------------------------------- the AdamW step over many tensors, the gradients' norm
@@ -834,7 +836,7 @@ def s2a_adamw_step(plan: AdamWPlan, control, beta1: float = 0.9, beta2: float = 
     if rng is not None and (rng.dtype is not torch.int64 or rng.numel() != 2 or not rng.is_contiguous()):
         raise S2AError("rng must be contiguous int64 (seed, offset)")
     status = (_lib or lib()).s2a_adamw_step(plan.address, plan.image.data_ptr(), _float_words(control, 3, "control"),
-                                            None if clip is None else _float_words(clip, 2, "clip"), _address(rng), site, beta1,
+                                            None if clip is None else _float_words(clip, 2, "clip"), _address(rng) or None, site, beta1,
                                             beta2, eps, _stream_on(dev))
     if status:
         check(status)

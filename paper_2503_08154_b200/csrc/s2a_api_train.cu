@@ -40,6 +40,7 @@ bool make_rows(const size_t* strides, size_t batch, size_t tokens, size_t heads,
   size_t extent = r.row;
   for (int i = 0; i < 3; ++i) {
     if (n[i] <= 1) continue;
+    if (i == 2 && strides[i] >> 32) return false;  // the kernels hold a head's stride in 32 bits
     if (strides[i] != 0 && n[i] - 1 > (kMaxExtent - extent) / es / strides[i]) return false;
     extent += (n[i] - 1) * strides[i] * es;
     int at = r.dims++;
@@ -92,102 +93,84 @@ bool tensors_meet(const void* pa, const Rows& a, const void* pb, const Rows& b) 
   return rows_meet(a, 0, b, 0, (long long)((uintptr_t)pb - (uintptr_t)pa));
 }
 
-struct RopeCall {
-  int mode, back;
-  const void *in[2], *grad[2], *gamma[2];  // grad: NULL but for the norm's backward pass
-  void* out[2];
-  void* grad_gamma[2];
-  void* scratch;
-  const size_t* strides;  // of in and out; with gradients of grad, in and out
-  const int32_t* positions;
-  int64_t first;
-  size_t pos_batch, pos_axis, axes;
-  const uint64_t* table;
-  size_t batch, tokens, heads[2], head_dim, rot_dim;
-  int interleaved;
-  float scale, eps;
-  int dt, wdt;
-  void* stream;
-};
-
-int run_rope(const RopeCall& c) {
-  const bool norm = c.mode != kRopePlain, bwd = c.mode == kRopeBwdNorm;
+int run_rope(const s2a_rope_args* args, int mode, int back, void* stream) {
+  if (!args) return S2A_ERR_NULL;
+  const s2a_rope_args& c = *args;
+  const bool norm = mode != kRopePlain, bwd = mode == kRopeBwdNorm;
+  const size_t heads[2] = {c.heads_q, c.heads_k};
   if (bad_dtype(c.dt) || (norm && bad_dtype(c.wdt))) return S2A_ERR_DTYPE;
   if (c.head_dim == 0 || c.head_dim > kMaxHeadDim || c.rot_dim % 2 != 0 || c.rot_dim > c.head_dim || (!norm && c.rot_dim == 0) ||
-      c.heads[0] > 65535u || c.heads[1] > 65535u || c.batch > 0x7fffffffull || c.tokens > 0x7fffffffull ||
+      heads[0] > 65535u || heads[1] > 65535u || c.batch > 0x7fffffffull || c.tokens > 0x7fffffffull ||
       c.batch * c.tokens > 0x7fffffffull || (c.rot_dim && (c.axes == 0 || c.axes > kMaxAxes)))
     return S2A_ERR_SHAPE;
   if (!(fabsf(c.scale) <= 3.4028234e38f) || (norm && !(c.eps >= 0.0f && c.eps <= 3.4028234e38f))) return S2A_ERR_VALUE;
-  const bool sums = c.grad_gamma[0] || c.grad_gamma[1];
-  const size_t es = elem_bytes(c.dt), ws = elem_bytes(c.wdt);
-  const bool empty = c.batch * c.tokens == 0 || c.heads[0] + c.heads[1] == 0;
-  if (misaligned(c.gamma[0], ws) || misaligned(c.gamma[1], ws) || misaligned(c.grad_gamma[0], ws) || misaligned(c.grad_gamma[1], ws))
-    return S2A_ERR_ALIGN;
+  const void* const in[2] = {c.q, c.k};
+  const void* const grad[2] = {c.grad_q, c.grad_k};
+  void* const out[2] = {c.out_q, c.out_k};
+  const void* const gamma[2] = {norm ? c.gamma_q : nullptr, norm ? c.gamma_k : nullptr};
+  void* const sums[2] = {bwd ? c.grad_gamma_q : nullptr, bwd ? c.grad_gamma_k : nullptr};
+  const size_t* const in_stride[2] = {c.q_stride, c.k_stride};
+  const size_t* const grad_stride[2] = {c.grad_q_stride, c.grad_k_stride};
+  const size_t* const out_stride[2] = {c.out_q_stride, c.out_k_stride};
+  const size_t es = elem_bytes(c.dt), ws = norm ? elem_bytes(c.wdt) : 1;
+  const bool empty = c.batch * c.tokens == 0 || heads[0] + heads[1] == 0;
+  for (int i = 0; i < 2; ++i)
+    if (misaligned(gamma[i], ws) || misaligned(sums[i], ws)) return S2A_ERR_ALIGN;
   if (!empty) {
-    if (!c.strides || (c.rot_dim && !c.table) || (c.rot_dim && !c.positions && c.axes > 1) || (sums && !c.scratch)) return S2A_ERR_NULL;
-    if (misaligned(c.table, 16) || misaligned(c.positions, 4) || misaligned(c.scratch, 16)) return S2A_ERR_ALIGN;
-    if (c.positions && (c.pos_batch > kMaxExtent / 0x7fffffffull || c.pos_axis > kMaxExtent / 512)) return S2A_ERR_SHAPE;
+    if ((c.rot_dim && (!c.table || (!c.positions && c.axes > 1))) || ((sums[0] || sums[1]) && !c.scratch)) return S2A_ERR_NULL;
+    if ((c.rot_dim && (misaligned(c.table, 16) || misaligned(c.positions, 4))) || (bwd && misaligned(c.scratch, 16))) return S2A_ERR_ALIGN;
+    if (c.rot_dim && c.positions && (c.pos_batch_stride > kMaxExtent / 0x7fffffffull || c.pos_axis_stride > kMaxExtent / kMaxAxes))
+      return S2A_ERR_SHAPE;
   }
   RopeArgs a = {};
-  Rows out[2], in[4];
-  const void* in_data[4];
-  int n_in = 0;
+  Rows wrote[2], had[4];
+  const void* had_at[4];
+  int n = 0;
   for (int i = 0; i < 2 && !empty; ++i) {
-    if (c.heads[i] == 0) continue;
-    if (!c.in[i] || !c.out[i] || (bwd && !c.grad[i])) return S2A_ERR_NULL;
-    if (misaligned(c.in[i], es) || misaligned(c.out[i], es) || misaligned(c.grad[i], es)) return S2A_ERR_ALIGN;
-    const size_t* s = c.strides + 3 * i;
+    if (heads[i] == 0) continue;
+    if (!in[i] || !out[i] || (bwd && !grad[i])) return S2A_ERR_NULL;
+    if (misaligned(in[i], es) || misaligned(out[i], es) || (bwd && misaligned(grad[i], es))) return S2A_ERR_ALIGN;
+    const auto take = [&](const void* p, const size_t* s, HeadsArg& h, Rows& r) {
+      // a dimension of one has no stride
+      h = HeadsArg{p, c.batch > 1 ? s[0] : 0, c.tokens > 1 ? s[1] : 0, heads[i] > 1 ? s[2] : 0};
+      return make_rows(s, c.batch, c.tokens, heads[i], c.head_dim, es, r);
+    };
+    had_at[n] = in[i];
+    if (!take(in[i], in_stride[i], a.in[i], had[n++])) return S2A_ERR_SHAPE;
     if (bwd) {
-      a.grad[i] = HeadsArg{c.grad[i], s[0], s[1], s[2]};
-      if (!make_rows(s, c.batch, c.tokens, c.heads[i], c.head_dim, es, in[n_in])) return S2A_ERR_SHAPE;
-      in_data[n_in++] = c.grad[i];
-      s += 6;
+      had_at[n] = grad[i];
+      if (!take(grad[i], grad_stride[i], a.grad[i], had[n++])) return S2A_ERR_SHAPE;
     }
-    a.in[i] = HeadsArg{c.in[i], s[0], s[1], s[2]};
-    if (!make_rows(s, c.batch, c.tokens, c.heads[i], c.head_dim, es, in[n_in])) return S2A_ERR_SHAPE;
-    in_data[n_in++] = c.in[i];
-    s += 6;
-    a.out[i] = HeadsArg{c.out[i], s[0], s[1], s[2]};
-    if (!make_rows(s, c.batch, c.tokens, c.heads[i], c.head_dim, es, out[i]) || folds(out[i])) return S2A_ERR_SHAPE;
-    a.heads[i] = (uint32_t)c.heads[i];
+    if (!take(out[i], out_stride[i], a.out[i], wrote[i]) || folds(wrote[i])) return S2A_ERR_SHAPE;
+    a.heads[i] = (uint32_t)heads[i];
   }
   for (int i = 0; i < 2 && !empty; ++i) {
-    if (c.heads[i] == 0) continue;
-    for (int j = 0; j < n_in; ++j) {
-      const bool own = in_data[j] == c.in[i] || in_data[j] == c.grad[i];
-      if (own && in_data[j] == c.out[i] && same_rows(in[j], out[i])) continue;  // in place
-      if (tensors_meet(in_data[j], in[j], c.out[i], out[i])) return S2A_ERR_OVERLAP;
+    if (heads[i] == 0) continue;
+    for (int j = 0; j < n; ++j) {
+      const bool own = had_at[j] == in[i] || (bwd && had_at[j] == grad[i]);
+      if (own && had_at[j] == out[i] && same_rows(had[j], wrote[i])) continue;  // in place
+      if (tensors_meet(had_at[j], had[j], out[i], wrote[i])) return S2A_ERR_OVERLAP;
     }
-    if (i == 1 && c.heads[0] && tensors_meet(c.out[0], out[0], c.out[1], out[1])) return S2A_ERR_OVERLAP;
+    if (i == 1 && heads[0] && tensors_meet(out[0], wrote[0], out[1], wrote[1])) return S2A_ERR_OVERLAP;
   }
-  for (int i = 0; i < 2; ++i) {
-    // a dimension of one has no stride
-    HeadsArg* h[3] = {&a.in[i], &a.grad[i], &a.out[i]};
-    for (HeadsArg* t : h) {
-      if (c.batch <= 1) t->batch = 0;
-      if (c.tokens <= 1) t->token = 0;
-      if (c.heads[i] <= 1) t->head = 0;
-    }
-    a.gamma[i] = c.gamma[i];
-  }
-  a.positions = c.positions;
+  a.gamma[0] = gamma[0];
+  a.gamma[1] = gamma[1];
+  a.positions = c.rot_dim ? c.positions : nullptr;
   a.table = c.table;
   a.first = c.first;
-  a.pos_axis = c.pos_axis;
-  a.pos_batch = c.pos_batch;
+  a.pos_axis = c.pos_axis_stride;
+  a.pos_batch = c.pos_batch_stride;
   a.batch = (uint32_t)c.batch;
   a.tokens = (uint32_t)c.tokens;
   a.head_dim = (uint32_t)c.head_dim;
   a.pairs = (uint32_t)(c.rot_dim / 2);
-  a.axes = (uint32_t)c.axes;
+  a.axes = c.rot_dim ? (uint32_t)c.axes : 1u;
   a.interleaved = c.interleaved != 0;
-  a.back = c.back;
+  a.back = back;
   a.wdt = c.wdt;
   a.scale = c.scale;
   a.eps = c.eps;
-  if (empty) a.heads[0] = a.heads[1] = 0;
-  return launch_rope(c.mode, c.dt, a, c.grad_gamma[0], c.grad_gamma[1], (float*)c.scratch, (cudaStream_t)c.stream) == cudaSuccess
-             ? S2A_OK : S2A_ERR_CUDA;
+  return launch_rope(mode, c.dt, a, sums[0], sums[1], (float*)c.scratch, (cudaStream_t)stream) == cudaSuccess ? S2A_OK : S2A_ERR_CUDA;
 }
 
 // ---- the plan of a step
@@ -233,51 +216,13 @@ StepArgs step_args(const s2a_step_plan* plan, const void* image, const float* co
 
 extern "C" {
 
-int s2a_rope_fwd(const void* q, const void* k, void* out_q, void* out_k, const size_t* strides, const int32_t* positions,
-                 int64_t first, size_t pos_batch_stride, size_t pos_axis_stride, size_t axes, const uint64_t* table,
-                 size_t batch, size_t tokens, size_t heads_q, size_t heads_k, size_t head_dim, size_t rot_dim, int interleaved,
-                 float scale, int dt, void* cuda_stream) {
-  const RopeCall c = {kRopePlain, 0, {q, k}, {nullptr, nullptr}, {nullptr, nullptr}, {out_q, out_k}, {nullptr, nullptr}, nullptr,
-                      strides, positions, first, pos_batch_stride, pos_axis_stride, axes, table, batch, tokens,
-                      {heads_q, heads_k}, head_dim, rot_dim, interleaved, scale, 0.0f, dt, S2A_F32, cuda_stream};
-  return run_rope(c);
-}
-
-int s2a_rope_bwd(const void* grad_q, const void* grad_k, void* grad_in_q, void* grad_in_k, const size_t* strides,
-                 const int32_t* positions, int64_t first, size_t pos_batch_stride, size_t pos_axis_stride, size_t axes,
-                 const uint64_t* table, size_t batch, size_t tokens, size_t heads_q, size_t heads_k, size_t head_dim,
-                 size_t rot_dim, int interleaved, float scale, int dt, void* cuda_stream) {
-  const RopeCall c = {kRopePlain, 1, {grad_q, grad_k}, {nullptr, nullptr}, {nullptr, nullptr}, {grad_in_q, grad_in_k},
-                      {nullptr, nullptr}, nullptr, strides, positions, first, pos_batch_stride, pos_axis_stride, axes, table, batch,
-                      tokens, {heads_q, heads_k}, head_dim, rot_dim, interleaved, scale, 0.0f, dt, S2A_F32, cuda_stream};
-  return run_rope(c);
-}
-
-int s2a_qknorm_rope_fwd(const void* q, const void* k, const void* gamma_q, const void* gamma_k, void* out_q, void* out_k,
-                        const size_t* strides, const int32_t* positions, int64_t first, size_t pos_batch_stride,
-                        size_t pos_axis_stride, size_t axes, const uint64_t* table, size_t batch, size_t tokens, size_t heads_q,
-                        size_t heads_k, size_t head_dim, size_t rot_dim, int interleaved, float scale, float eps, int dt, int wdt,
-                        void* cuda_stream) {
-  const RopeCall c = {kRopeFwdNorm, 0, {q, k}, {nullptr, nullptr}, {gamma_q, gamma_k}, {out_q, out_k}, {nullptr, nullptr}, nullptr,
-                      strides, positions, first, pos_batch_stride, pos_axis_stride, axes, table, batch, tokens,
-                      {heads_q, heads_k}, head_dim, rot_dim, interleaved, scale, eps, dt, wdt, cuda_stream};
-  return run_rope(c);
-}
+int s2a_rope_fwd(const s2a_rope_args* args, void* cuda_stream) { return run_rope(args, kRopePlain, 0, cuda_stream); }
+int s2a_rope_bwd(const s2a_rope_args* args, void* cuda_stream) { return run_rope(args, kRopePlain, 1, cuda_stream); }
+int s2a_qknorm_rope_fwd(const s2a_rope_args* args, void* cuda_stream) { return run_rope(args, kRopeFwdNorm, 0, cuda_stream); }
+int s2a_qknorm_rope_bwd(const s2a_rope_args* args, void* cuda_stream) { return run_rope(args, kRopeBwdNorm, 1, cuda_stream); }
 
 size_t s2a_qknorm_rope_scratch_bytes(size_t, size_t, size_t, size_t, size_t head_dim) {
   return head_dim == 0 || head_dim > kMaxHeadDim ? 0 : (size_t)qknorm_scratch_bytes((uint32_t)head_dim);
-}
-
-int s2a_qknorm_rope_bwd(const void* grad_q, const void* grad_k, const void* q, const void* k, const void* gamma_q,
-                        const void* gamma_k, void* grad_in_q, void* grad_in_k, void* grad_gamma_q, void* grad_gamma_k,
-                        void* scratch, const size_t* strides, const int32_t* positions, int64_t first, size_t pos_batch_stride,
-                        size_t pos_axis_stride, size_t axes, const uint64_t* table, size_t batch, size_t tokens, size_t heads_q,
-                        size_t heads_k, size_t head_dim, size_t rot_dim, int interleaved, float scale, float eps, int dt, int wdt,
-                        void* cuda_stream) {
-  const RopeCall c = {kRopeBwdNorm, 1, {q, k}, {grad_q, grad_k}, {gamma_q, gamma_k}, {grad_in_q, grad_in_k},
-                      {grad_gamma_q, grad_gamma_k}, scratch, strides, positions, first, pos_batch_stride, pos_axis_stride, axes,
-                      table, batch, tokens, {heads_q, heads_k}, head_dim, rot_dim, interleaved, scale, eps, dt, wdt, cuda_stream};
-  return run_rope(c);
 }
 
 int s2a_rope_table(uint64_t* table, size_t rot_dim, double base, int scaling, double factor, double original_length, double slow,

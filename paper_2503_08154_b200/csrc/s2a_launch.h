@@ -108,7 +108,8 @@ struct RopeArgs {
   int64_t first;
   uint64_t pos_axis, pos_batch;
   uint32_t heads[2];
-  uint32_t batch, tokens, head_dim, pairs, axes, parts, ctas0;
+  uint32_t batch, tokens, head_dim, pairs, axes;
+  uint32_t ctas0, share[2], more[2];                 // CTAs of queries; groups of rows a warp, and how many warps have one more
   uint32_t lanes, rows_per_warp, slots, turn_slots;  // lanes and slots of a row (slots: see the kernels), turning slots
   int interleaved, back, wdt;
   float scale, eps, inv_dim;

@@ -2,6 +2,8 @@
 // gradients; the kernels are in s2a_rope.cuh.
 #include <math.h>
 
+#include <algorithm>
+
 #include "s2a_launch.h"
 #include "s2a_oct.cuh"
 
@@ -73,26 +75,28 @@ cudaError_t launch_rope(int mode, int dt, RopeArgs a, void* grad_gamma_q, void* 
   a.lanes = (a.slots + K - 1) / K;
   a.rows_per_warp = 32 / a.lanes;
   a.inv_dim = 1.0f / (float)a.head_dim;
-  const uint32_t sms = (uint32_t)sm_count();
-  const uint32_t groups = (heads + a.rows_per_warp - 1) / a.rows_per_warp;
-  // few tokens: a token's groups are shared by several warps, until every SM has its warps
-  const uint64_t want = (uint64_t)sms * kWarps * 3;
-  const uint64_t shares = (want + tokens - 1) / tokens;
-  a.parts = (uint32_t)(shares < groups ? shares : groups);
-  const uint64_t units = tokens * a.parts;
+  // A warp each for the groups of rows of all tokens, until the GPU is full; then shares.
+  const auto groups_of = [&](uint32_t rows) { return (rows + a.rows_per_warp - 1) / a.rows_per_warp; };
+  const auto cut = [&](uint32_t rows, uint32_t ctas, int which) {
+    const uint64_t items = tokens * groups_of(rows), warps = (uint64_t)ctas * kWarps;
+    a.share[which] = (uint32_t)(items / warps);
+    a.more[which] = (uint32_t)(items % warps);
+  };
+  const auto ctas_for = [&](uint64_t items, uint64_t cap) { return (uint32_t)std::min<uint64_t>((items + kWarps - 1) / kWarps, cap); };
+  if (tokens * (groups_of(a.heads[0]) + groups_of(a.heads[1])) >> 32) return cudaErrorInvalidValue;  // more than any memory holds
   unsigned grid;
   if (mode == kRopeBwdNorm) {
-    const uint64_t need = (units + kWarps - 1) / kWarps;
-    uint32_t cap = 148 * 2;
-    if (need < cap) cap = (uint32_t)need;
-    a.ctas0 = a.heads[1] == 0 ? cap : (a.heads[0] == 0 ? 0 : (uint32_t)((uint64_t)cap * a.heads[0] / heads));
-    if (a.heads[0] && a.ctas0 == 0) a.ctas0 = 1;
-    grid = cap;
-    if (a.heads[1] && a.ctas0 >= cap) grid = a.ctas0 + 1;
+    const uint64_t items0 = tokens * groups_of(a.heads[0]), items1 = tokens * groups_of(a.heads[1]);
+    const uint64_t cap = 148 * 2, share0 = cap * items0 / (items0 + items1);
+    a.ctas0 = items0 ? ctas_for(items0, items1 ? std::min(std::max<uint64_t>(share0, 1), cap - 1) : cap) : 0;
+    const uint32_t ctas1 = items1 ? ctas_for(items1, cap - a.ctas0) : 0;
+    grid = a.ctas0 + ctas1;
+    if (items0) cut(a.heads[0], a.ctas0, 0);
+    if (items1) cut(a.heads[1], ctas1, 1);
     a.partials = sums ? scratch : nullptr;
   } else {
-    const uint64_t need = (units + kWarps - 1) / kWarps, cap = (uint64_t)sms * 3;
-    grid = (unsigned)(need < cap ? need : cap);
+    grid = ctas_for(tokens * groups_of(heads), (uint64_t)sm_count() * 3);
+    cut(heads, grid, 0);
   }
   // from here on strides are in bytes
   for (HeadsArg* h : {&a.in[0], &a.in[1], &a.grad[0], &a.grad[1], &a.out[0], &a.out[1]}) {

@@ -246,6 +246,33 @@ struct Angles {
   }
 };
 
+// A warp's part of all groups of rows, `groups` for each token: an even share of neighbouring ones.  The tokens are counted through the
+// sequences first, so that neighbours have the same place in their sequences and, as a rule, the same position, whose cosines then stay.
+struct Walk {
+  uint32_t b, t, i, left;  // sequence, token, group of rows, groups left
+  __device__ __forceinline__ Walk(const RopeArgs& a, uint32_t warp, uint32_t share, uint32_t more, uint32_t groups) {
+    // the first `more` warps have one more
+    const uint32_t start = warp * share + (warp < more ? warp : more);
+    left = share + (warp < more ? 1u : 0u);
+    const uint32_t n = start / groups;
+    i = start - n * groups;
+    t = n / a.batch;
+    b = n - t * a.batch;
+  }
+  // true where a new token begins
+  __device__ __forceinline__ bool next(const RopeArgs& a, uint32_t groups) {
+    --left;
+    if (++i < groups) return false;
+    i = 0;
+    if (++b == a.batch) {
+      b = 0;
+      ++t;
+    }
+    return true;
+  }
+  __device__ __forceinline__ uint64_t row0(const HeadsArg& h) const { return (uint64_t)h.data + b * h.batch + t * h.token; }
+};
+
 // A copy of BYTES at constant offsets from both addresses, or zeros where there is nothing.
 template <int BYTES, int TO, int FROM>
 __device__ __forceinline__ void copy_or_zero(uint32_t to, uint64_t from, bool there) {
@@ -259,25 +286,68 @@ __device__ __forceinline__ void copy_or_zero(uint32_t to, uint64_t from, bool th
 // A warp's group of rows in a stage of its ring.  Rows with kernels of their own (L > 0): each lane copies what it will read, to a place
 // of its own, and writes from registers.  Others: their rows lie one behind the other, copied by vectors in order, so that neighbouring lanes have
 // neighbouring vectors whatever the row's length, read by each lane at its places, and written back the same way ([3, 16 + 16, 2001,
-// 80] binary32, half turning: 36.9 us with each lane's own copies, most of which cut 32-byte sectors).
+// 80] binary32, half turning: 36.9 us with each lane's own copies, most of which cut 32-byte sectors).  Behind the rows of a stage stand 16
+// bytes of zeros, which a lane reads in the place of a vector that does not exist.
 template <int DT, int V, int K, int L>
 struct Group {
   static constexpr int kBytes = V * Io<DT>::kBytes;
-  static constexpr int kGroupBytes = 2 * K * 32 * kBytes;  // of a warp
+  static constexpr int kRowsBytes = 2 * K * 32 * kBytes;
+  static constexpr int kGroupBytes = kRowsBytes + (L ? 0 : 16);  // of a warp
   static constexpr int kApart = L * (kLaneElems / 2) * Io<DT>::kBytes;  // bytes from the first half of a row to the second
-  uint32_t vectors, inverse;  // L = 0: vectors of a row, and 2^20 / that, rounded up: j / vectors is exact for j < 512
-  __device__ __forceinline__ explicit Group(const RopeArgs& a) : vectors(a.head_dim / V), inverse((1048576u + a.head_dim / V - 1) / (a.head_dim / V)) {}
+  static constexpr int kKept = 2 * K <= 4 ? 2 * K : 1;
+  uint32_t vectors, inverse;          // L = 0: vectors of a row, and 2^20 / that, rounded up: j / vectors is exact for j < 512
+  uint32_t row_of[kKept], byte_of[kKept];  // row and place in it of the lane's vectors, where they are few
+  uint32_t off_a[L ? 1 : K], off_b[L ? 1 : K];  // where the lane's two vectors of a slot lie in a stage
+  template <typename P>
+  __device__ __forceinline__ Group(const RopeArgs& a, const Lane<L>& l, const P& p) {
+    if constexpr (L == 0) {
+      vectors = a.head_dim / V;
+      inverse = (1048576u + vectors - 1) / vectors;
+      if constexpr (2 * K <= 4)
+#pragma unroll
+        for (int m = 0; m < 2 * K; ++m) split(m, l, row_of[m], byte_of[m]);
+#pragma unroll
+      for (int k = 0; k < K; ++k) {
+        const uint32_t row = l.row * vectors * kBytes;
+        off_a[k] = p.has_first(k) ? row + p.at[k] * Io<DT>::kBytes : kRowsBytes;
+        off_b[k] = p.has_second(k) ? row + p.to[k] * Io<DT>::kBytes : kRowsBytes;
+      }
+    }
+  }
+  __device__ __forceinline__ void split(int m, const Lane<L>& l, uint32_t& r, uint32_t& byte) const {
+    const uint32_t j = m * 32 + (threadIdx.x & 31u);
+    r = (j * inverse) >> 20;
+    byte = (j - r * vectors) * kBytes;
+    if (r >= l.per) r = 0x40000000u;  // beyond the rows of any token
+  }
+  __device__ __forceinline__ void vector(int m, const Lane<L>& l, uint32_t& r, uint32_t& byte) const {
+    if constexpr (2 * K <= 4) {
+      r = row_of[m];
+      byte = byte_of[m];
+    } else {
+      split(m, l, r, byte);
+    }
+  }
+  __device__ __forceinline__ void clear(char* ring, uint32_t groups) const {
+    if (L == 0 && (threadIdx.x & 31u) < groups) *(uint4*)(ring + (threadIdx.x & 31u) * kGroupBytes + kRowsBytes) = make_uint4(0u, 0u, 0u, 0u);
+  }
 
-  // rows first .. of a token: row r of the queries lies at q + r * q_head, of the keys (r >= heads0) at k + r * k_head
+  // Rows of a token: row r of the queries lies at q + r * q_head vectors, of the keys (r >= heads0) at k + r * k_head vectors.
   struct Source {
-    uint64_t q, k, q_head, k_head;
-    uint32_t heads0, heads;
+    uint64_t q, k;
+    uint32_t q_head, k_head, heads0, heads;
+    __device__ __forceinline__ Source(const HeadsArg& hq, const HeadsArg& hk, uint32_t h0, uint32_t h)
+        : q(0), k(0), q_head((uint32_t)(hq.head / kBytes)), k_head((uint32_t)(hk.head / kBytes)), heads0(h0), heads(h) {}
     __device__ __forceinline__ uint64_t row(uint32_t r) const {
       const bool keys = r >= heads0;
-      // (the kernels for L > 0 are taken where a head's stride fits 32 bits)
-      if constexpr (L > 0) return (keys ? k : q) + (uint64_t)r * (uint32_t)(keys ? k_head : q_head);
-      else return (keys ? k : q) + r * (keys ? k_head : q_head);
+      return (keys ? k : q) + (uint64_t)(r * kBytes) * (keys ? k_head : q_head);
     }
+    // on to the walk's token: one sequence further, or anew
+    __device__ __forceinline__ void enter(const Walk& w, const HeadsArg& hq, const HeadsArg& hk) {
+      q = w.row0(hq);
+      k = w.row0(hk) - heads0 * hk.head;
+    }
+    __device__ __forceinline__ void enter(const Walk& w, const HeadsArg& hq) { q = w.row0(hq); }
   };
 
   __device__ __forceinline__ void fetch(char* stage, const Source& from, uint32_t first, const Lane<L>& l) const {
@@ -296,54 +366,48 @@ struct Group {
     } else {
 #pragma unroll
       for (int m = 0; m < 2 * K; ++m) {
-        const uint32_t j = m * 32 + lane, r = (j * inverse) >> 20, c = j - r * vectors;
-        const bool there = r < l.per && first + r < from.heads;
-        const uint64_t at = from.row(first + r) + c * kBytes;
-        if constexpr (kBytes >= 4) {
-          if (r < l.per) copy_or_zero<kBytes, 0, 0>(to + m * 32 * kBytes, at, there);
-        } else if (r < l.per) {
-          *(uint16_t*)(stage + j * kBytes) = there ? *(const uint16_t*)at : (uint16_t)0;
-        }
+        uint32_t r, byte;
+        vector(m, l, r, byte);
+        r += first;
+        const bool there = r < from.heads;
+        const uint64_t at = from.row(r) + byte;
+        if constexpr (kBytes >= 4) copy_or_zero<kBytes, 0, 0>(to + m * 32 * kBytes, at, there);
+        else *(uint16_t*)(stage + (m * 32 + lane) * kBytes) = there ? *(const uint16_t*)at : (uint16_t)0;
       }
     }
   }
-  template <typename P>
-  __device__ __forceinline__ void read(const char* stage, const P& p, int k, const Lane<L>& l, F2 (&a)[kHalf<V>], F2 (&b)[kHalf<V>]) const {
+  __device__ __forceinline__ void read(const char* stage, int k, F2 (&a)[kHalf<V>], F2 (&b)[kHalf<V>]) const {
     if constexpr (L > 0) {
       const char* own = stage + (2 * k * 32 + (threadIdx.x & 31u)) * kBytes;
       read_vector<DT, V>(own, a);
       read_vector<DT, V>(own + 32 * kBytes, b);
     } else {
-      const char* row = stage + l.row * vectors * kBytes;
-#pragma unroll
-      for (int j = 0; j < kHalf<V>; ++j) a[j] = b[j] = f2_both(0.0f);
-      if (p.has_first(k)) read_vector<DT, V>(row + p.at[k] * Io<DT>::kBytes, a);
-      if (p.has_second(k)) read_vector<DT, V>(row + p.to[k] * Io<DT>::kBytes, b);
+      read_vector<DT, V>(stage + off_a[k], a);
+      read_vector<DT, V>(stage + off_b[k], b);
     }
   }
   // L > 0: to memory.  L = 0: back to the stage, from where `flush` takes it.
-  template <typename P>
-  __device__ __forceinline__ void write(char* stage, uint64_t out, const P& p, int k, const Lane<L>& l, bool on, const F2 (&a)[kHalf<V>],
-                                        const F2 (&b)[kHalf<V>]) const {
+  __device__ __forceinline__ void write(char* stage, uint64_t out, int k, bool on, const F2 (&a)[kHalf<V>], const F2 (&b)[kHalf<V>]) const {
     if constexpr (L > 0) {
       if (!on) return;
       write_vector<DT, V>((void*)(out + k * L * kBytes), a);
       write_vector<DT, V>((void*)(out + k * L * kBytes + kApart), b);
     } else {
-      char* row = stage + l.row * vectors * kBytes;
-      if (p.has_first(k)) write_vector<DT, V>(row + p.at[k] * Io<DT>::kBytes, a);
-      if (p.has_second(k)) write_vector<DT, V>(row + p.to[k] * Io<DT>::kBytes, b);
+      if (off_a[k] < kRowsBytes) write_vector<DT, V>(stage + off_a[k], a);
+      if (off_b[k] < kRowsBytes) write_vector<DT, V>(stage + off_b[k], b);
     }
   }
   __device__ __forceinline__ void flush(const char* stage, const Source& to, uint32_t first, const Lane<L>& l) const {
     if constexpr (L == 0) {
       using Raw = typename RawOf<kBytes>::T;
-      const uint32_t lane = threadIdx.x & 31u;
+      const char* own = stage + (threadIdx.x & 31u) * kBytes;
       __syncwarp();
 #pragma unroll
       for (int m = 0; m < 2 * K; ++m) {
-        const uint32_t j = m * 32 + lane, r = (j * inverse) >> 20, c = j - r * vectors;
-        if (r < l.per && first + r < to.heads) *(Raw*)(to.row(first + r) + c * kBytes) = *(const Raw*)(stage + j * kBytes);
+        uint32_t r, byte;
+        vector(m, l, r, byte);
+        r += first;
+        if (r < to.heads) *(Raw*)(to.row(r) + byte) = *(const Raw*)(own + m * 32 * kBytes);
       }
       __syncwarp();  // before the stage is filled again
     }
@@ -383,44 +447,6 @@ struct Layout {
   __host__ __device__ uint32_t bytes() const { return warps + kWarps * warp_bytes; }
 };
 
-// A walk over units: the tokens of all sequences, times the parts that each token's groups of rows are cut into (part by part).  A
-// warp's units are a stride apart, taken apart into sequences and tokens once, so that going on needs no division.
-struct Walk {
-  uint32_t b, t, part, i;  // sequence, token, part, group of rows
-  bool on;
-  uint32_t sequences, tokens;  // the stride
-  __device__ __forceinline__ Walk(const RopeArgs& a, uint32_t unit, uint32_t stride, uint32_t parts) {
-    const uint32_t all = a.batch * a.tokens;
-    part = unit / all;
-    const uint32_t n = unit - part * all;
-    b = n / a.tokens;
-    t = n - b * a.tokens;
-    i = part;
-    on = part < parts;
-    sequences = stride / a.tokens;
-    tokens = stride - sequences * a.tokens;
-  }
-  // true where a new unit begins
-  __device__ __forceinline__ bool next(const RopeArgs& a, uint32_t parts, uint32_t groups) {
-    i += parts;
-    if (i < groups) return false;
-    b += sequences;
-    t += tokens;
-    if (t >= a.tokens) {
-      t -= a.tokens;
-      ++b;
-    }
-    if (b >= a.batch) {  // the next part, or the end
-      part += b / a.batch;
-      b %= a.batch;
-      on = part < parts;
-    }
-    i = part;
-    return true;
-  }
-  __device__ __forceinline__ uint64_t row0(const HeadsArg& h) const { return (uint64_t)h.data + b * h.batch + t * h.token; }
-};
-
 // The table and the weights into shared memory, by the whole CTA.
 __device__ __forceinline__ void stage_table(const RopeArgs& a, char* shared, const Layout& l, const void* g0, const void* g1, int weights) {
   for (uint32_t i = threadIdx.x; i < a.pairs; i += kThreads) ((ulonglong2*)shared)[i] = ((const ulonglong2*)a.table)[i];
@@ -438,15 +464,25 @@ __device__ __forceinline__ void copy_positions(const RopeArgs& a, int32_t* to, c
   if (a.positions && lane < a.axes) copy_async<4>(to + lane, a.positions + lane * a.pos_axis + w.b * a.pos_batch + w.t);
 }
 
-// The warp's cosines and sines of one token, from the positions in its stage.
-__device__ __forceinline__ void warp_phases(const RopeArgs& a, const char* table, const int32_t* at, uint32_t t, float sign, float* cs, float* sn) {
-  for (uint32_t i = threadIdx.x & 31u; i < a.pairs; i += 32) {
+// The warp's cosines and sines of a token, from the positions in its stage, unless they are those of the last token.  True where they
+// are new.
+__device__ __forceinline__ bool warp_phases(const RopeArgs& a, const char* table, const int32_t* at, uint32_t t, bool start, int32_t& last, float* cs,
+                                            float* sn) {
+  const uint32_t lane = threadIdx.x & 31u;
+  const int32_t key = a.positions ? at[lane < a.axes ? lane : 0] : (int32_t)t;
+  const bool same = key == last;
+  last = key;
+  if (__all_sync(0xffffffffu, same) && !start) return false;
+  const float sign = a.back ? -1.0f : 1.0f;
+  for (uint32_t i = lane; i < a.pairs; i += 32) {
     const ulonglong2 e = ((const ulonglong2*)table)[i];
     const int64_t pos = a.positions ? (int64_t)at[e.y < a.axes ? (uint32_t)e.y : a.axes - 1] : a.first + t;
     const float2 v = phase(e.x, pos, a.scale, sign);
     cs[i] = v.x;
     sn[i] = v.y;
   }
+  __syncwarp();
+  return true;
 }
 
 enum { kPlain = 0, kNorm = 1 };
@@ -462,7 +498,7 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 2 : 3) rope_kernel(const __
   const uint32_t warp = threadIdx.x >> 5;
   const Lane<L> l(a);
   const Places<V, K, INTER, L> p(a, l);
-  const Rows rows(a);
+  const Rows rows(a, l, p);
   char* mine = shared + lay.warps + warp * lay.warp_bytes;
   float* cs = (float*)mine;
   float* sn = cs + (a.pairs + 3) / 4 * 4;
@@ -472,47 +508,45 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 2 : 3) rope_kernel(const __
   const uint32_t groups = (heads + l.per - 1) / l.per;
   enter_grid();
 
-  Walk ahead(a, blockIdx.x * kWarps + warp, gridDim.x * kWarps, a.parts);
+  Walk ahead(a, blockIdx.x * kWarps + warp, a.share[0], a.more[0], groups);
   Walk now = ahead;
   bool fresh = true;
-  typename Rows::Source from{0, 0, a.in[0].head, a.in[1].head, heads0, heads}, to{0, 0, a.out[0].head, a.out[1].head, heads0, heads};
+  typename Rows::Source from(a.in[0], a.in[1], heads0, heads), to(a.out[0], a.out[1], heads0, heads);
   const auto fetch = [&](uint32_t stage) {
-    if (ahead.on) {
+    if (ahead.left) {
       if (fresh) {
-        from.q = ahead.row0(a.in[0]);
-        from.k = ahead.row0(a.in[1]) - heads0 * a.in[1].head;
+        from.enter(ahead, a.in[0], a.in[1]);
         copy_positions(a, positions + 4 * stage, ahead);
       }
       rows.fetch(ring + stage * Rows::kGroupBytes, from, ahead.i * l.per, l);
-      fresh = ahead.next(a, a.parts, groups);
+      fresh = ahead.next(a, groups);
     }
     copy_commit();
   };
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s) fetch(s);
+  rows.clear(ring, kStages);
   stage_table(a, shared, lay, a.gamma[0], a.gamma[1], NORM == kNorm ? 2 : 0);
   __syncthreads();
 
   Angles<V, K, INTER, L> angles;
-  bool begins = true;
-  const float sign = a.back ? -1.0f : 1.0f;
+  bool begins = true, start = true;
+  int32_t last = 0;
   const float* gamma = (const float*)(shared + lay.gamma);
   const uint32_t gamma_row = (a.head_dim + 3) / 4 * 4;
-  for (uint32_t stage = 0; now.on; stage = (stage + 1) % kStages) {
+  for (uint32_t stage = 0; now.left; stage = (stage + 1) % kStages) {
     copy_wait<kStages - 2>();
     if (L == 0 || begins) __syncwarp();  // what other lanes copied is here, and the last token's cosines have been read
     if (begins) {
-      warp_phases(a, shared, positions + 4 * stage, now.t, sign, cs, sn);
-      __syncwarp();
-      angles.read(p, cs, sn);
-      to.q = now.row0(a.out[0]);
-      to.k = now.row0(a.out[1]) - heads0 * a.out[1].head;
+      if (warp_phases(a, shared, positions + 4 * stage, now.t, start, last, cs, sn)) angles.read(p, cs, sn);
+      start = false;
+      to.enter(now, a.out[0], a.out[1]);
     }
     const uint32_t row = now.i * l.per + l.row;
     char* at = ring + stage * Rows::kGroupBytes;
     F2 fa[K][kHalf<V>], fb[K][kHalf<V>];
 #pragma unroll
-    for (int k = 0; k < K; ++k) rows.read(at, p, k, l, fa[k], fb[k]);
+    for (int k = 0; k < K; ++k) rows.read(at, k, fa[k], fb[k]);
     fetch((stage + kStages - 1) % kStages);
     if (NORM == kNorm) {
       F2 sa = f2_both(0.0f), sb = f2_both(0.0f);
@@ -541,10 +575,10 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 2 : 3) rope_kernel(const __
     for (int k = 0; k < K; ++k) {
       if (p.turning(k)) angles.turn(k, fa[k], fb[k]);
       // without a norm, what does not turn stays in its stage as it came, bit for bit
-      if (NORM == kNorm || p.turning(k)) rows.write(at, out, p, k, l, row < heads, fa[k], fb[k]);
+      if (NORM == kNorm || p.turning(k)) rows.write(at, out, k, row < heads, fa[k], fb[k]);
     }
     rows.flush(at, to, now.i * l.per, l);
-    begins = now.next(a, a.parts, groups);
+    begins = now.next(a, groups);
   }
 }
 
@@ -559,7 +593,7 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 1 : 2) qknorm_bwd_kernel(co
   const uint32_t warp = threadIdx.x >> 5;
   const Lane<L> l(a);
   const Places<V, K, INTER, L> p(a, l);
-  const Rows rows(a);
+  const Rows rows(a, l, p);
   char* mine = shared + lay.warps + warp * lay.warp_bytes;
   float* cs = (float*)mine;
   float* sn = cs + (a.pairs + 3) / 4 * 4;
@@ -569,32 +603,32 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 1 : 2) qknorm_bwd_kernel(co
   const HeadsArg& x = a.in[which];
   const HeadsArg& g = a.grad[which];
   const HeadsArg& o = a.out[which];
-  const uint32_t cta = which ? blockIdx.x - a.ctas0 : blockIdx.x, ctas = which ? gridDim.x - a.ctas0 : a.ctas0;
+  const uint32_t cta = which ? blockIdx.x - a.ctas0 : blockIdx.x;
   const uint32_t heads = a.heads[which], groups = (heads + l.per - 1) / l.per;
-  const uint32_t parts = a.parts < groups ? a.parts : groups;
   enter_grid();
 
-  Walk ahead(a, cta * kWarps + warp, ctas * kWarps, parts);
+  Walk ahead(a, cta * kWarps + warp, a.share[which], a.more[which], groups);
   Walk now = ahead;
   bool fresh = true;
   // all rows count as queries' here
-  typename Rows::Source from_x{0, 0, x.head, 0, heads, heads}, from_g{0, 0, g.head, 0, heads, heads}, to{0, 0, o.head, 0, heads, heads};
+  typename Rows::Source from_x(x, x, heads, heads), from_g(g, g, heads, heads), to(o, o, heads, heads);
   const auto fetch = [&](uint32_t stage) {
-    if (ahead.on) {
+    if (ahead.left) {
       if (fresh) {
-        from_x.q = ahead.row0(x);
-        from_g.q = ahead.row0(g);
+        from_x.enter(ahead, x);
+        from_g.enter(ahead, g);
         copy_positions(a, positions + 4 * stage, ahead);
       }
       char* at = ring + stage * 2 * Rows::kGroupBytes;
       rows.fetch(at, from_x, ahead.i * l.per, l);
       rows.fetch(at + Rows::kGroupBytes, from_g, ahead.i * l.per, l);
-      fresh = ahead.next(a, parts, groups);
+      fresh = ahead.next(a, groups);
     }
     copy_commit();
   };
 #pragma unroll
   for (int s = 0; s < kStages - 1; ++s) fetch(s);
+  rows.clear(ring, 2 * kStages);
   stage_table(a, shared, lay, a.gamma[which], nullptr, 1);
   __syncthreads();
 
@@ -604,16 +638,16 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 1 : 2) qknorm_bwd_kernel(co
   for (int k = 0; k < K; ++k)
 #pragma unroll
     for (int j = 0; j < kHalf<V>; ++j) sa[k][j] = sb[k][j] = f2_both(0.0f);
-  bool begins = true;
+  bool begins = true, start = true;
+  int32_t last = 0;
   const float* gamma = (const float*)(shared + lay.gamma);
-  for (uint32_t stage = 0; now.on; stage = (stage + 1) % kStages) {
+  for (uint32_t stage = 0; now.left; stage = (stage + 1) % kStages) {
     copy_wait<kStages - 2>();
     if (L == 0 || begins) __syncwarp();
     if (begins) {
-      warp_phases(a, shared, positions + 4 * stage, now.t, -1.0f, cs, sn);
-      __syncwarp();
-      angles.read(p, cs, sn);
-      to.q = now.row0(o);
+      if (warp_phases(a, shared, positions + 4 * stage, now.t, start, last, cs, sn)) angles.read(p, cs, sn);
+      start = false;
+      to.enter(now, o);
     }
     const uint32_t row = now.i * l.per + l.row;
     const bool on = l.on && row < heads;
@@ -621,8 +655,8 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 1 : 2) qknorm_bwd_kernel(co
     char* at = ring + stage * 2 * Rows::kGroupBytes;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
-      rows.read(at, p, k, l, xa[k], xb[k]);
-      rows.read(at + Rows::kGroupBytes, p, k, l, ua[k], ub[k]);
+      rows.read(at, k, xa[k], xb[k]);
+      rows.read(at + Rows::kGroupBytes, k, ua[k], ub[k]);
     }
     fetch((stage + kStages - 1) % kStages);
     F2 sum = f2_both(0.0f), other = f2_both(0.0f);
@@ -668,10 +702,10 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 1 : 2) qknorm_bwd_kernel(co
         ua[k][j] = f2_mul(f2_fma(mean, xa[k][j], ua[k][j]), rstd);
         ub[k][j] = f2_mul(f2_fma(mean, xb[k][j], ub[k][j]), rstd);
       }
-      rows.write(at, out, p, k, l, on, ua[k], ub[k]);
+      rows.write(at, out, k, on, ua[k], ub[k]);
     }
     rows.flush(at, to, now.i * l.per, l);
-    begins = now.next(a, parts, groups);
+    begins = now.next(a, groups);
   }
   if (!a.partials) return;
   copy_wait<0>();
@@ -735,9 +769,7 @@ cudaError_t launch_layout(int mode, const RopeArgs& a, unsigned grid, cudaStream
 template <int DT>
 cudaError_t launch_rope_kernel(int mode, uint32_t V, const RopeArgs& a, unsigned grid, cudaStream_t st) {
   constexpr int W = 16 / Io<DT>::kBytes;  // the widest vector
-  bool near = true;  // heads less than 4 GB apart
-  for (const HeadsArg* h : {&a.in[0], &a.in[1], &a.grad[0], &a.grad[1], &a.out[0], &a.out[1]}) near = near && h->head >> 32 == 0;
-  if (V == W && near && 2 * a.pairs == a.head_dim) {
+  if (V == W && 2 * a.pairs == a.head_dim) {
     if (a.head_dim == 64) return launch_layout<DT, W, 4>(mode, a, grid, st);
     if (a.head_dim == 128) return launch_layout<DT, W, 8>(mode, a, grid, st);
     if (a.head_dim == 256) return launch_layout<DT, W, 16>(mode, a, grid, st);
