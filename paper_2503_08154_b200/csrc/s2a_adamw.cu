@@ -21,89 +21,116 @@ namespace {
 
 constexpr int kStepWarps = 8;
 constexpr int kStepThreads = kStepWarps * 32;
-constexpr float kTopCode = 448.0f;          // the largest e4m3 value
-constexpr uint32_t kTopBits = 0x7Eu;        // and its code
-constexpr float kTwoM120 = 7.52316384526264e-37f, kTwo120 = 1.329227995784916e+36f;
+constexpr uint32_t kChunkBlocks = kStepChunk / kStepBlock;
+constexpr float kTopCode = 448.0f;                // the largest e4m3 value
+constexpr float kSmallest = 7.703719777548943e-34f;  // 2^-110: a block of which the largest magnitude is below is stored as zeros
 
-// Eight neighbouring elements: `count` of them exist.  `vec`: they lie on the 16-byte grid.
-template <int DT>
-__device__ __forceinline__ void load8(const void* base, uint64_t at, uint32_t count, bool vec, float (&f)[8]) {
-  const typename Io<DT>::T* p = (const typename Io<DT>::T*)base + at;
-  if (vec && count == 8) {
-    if constexpr (DT == kF32) {
-      const float4 a = ((const float4*)p)[0], b = ((const float4*)p)[1];
-      f[0] = a.x, f[1] = a.y, f[2] = a.z, f[3] = a.w, f[4] = b.x, f[5] = b.y, f[6] = b.z, f[7] = b.w;
+// A lane's eight elements of a block.  QUAD: elements 4 lane .. 4 lane + 3 and 128 more, so that a warp's accesses of binary32 have no gaps;
+// otherwise 8 lane .. 8 lane + 7, which share 128 random bits.  `first` and `left`: where its elements begin and how many of the
+// tensor's there are from there on.
+template <bool QUAD>
+struct Spot {
+  uint64_t first;
+  int32_t left;  // from `first`, at most 256
+  __device__ __forceinline__ int32_t count(int half) const {  // of the four elements of a half
+    const int32_t n = left - (QUAD ? 128 : 4) * half;
+    return n < 0 ? 0 : (n < 4 ? n : 4);
+  }
+  __device__ __forceinline__ uint64_t at(int half) const { return first + (QUAD ? 128 : 4) * half; }
+};
+
+// Eight elements as they lie in memory: binary32 in eight words, bfloat16 in four, codes in two.
+template <int ES>
+struct Raw {
+  uint32_t w[2 * ES];
+  template <bool QUAD>
+  __device__ __forceinline__ void load(const void* base, const Spot<QUAD>& s, bool vec) {
+    const char* p = (const char*)base;
+    if (vec && s.count(1) == 4) {  // all eight
+      if constexpr (ES == 4) {
+        const uint4 a = *(const uint4*)(p + s.at(0) * 4), b = *(const uint4*)(p + s.at(1) * 4);
+        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
+      } else if constexpr (ES == 2 && !QUAD) {
+        const uint4 a = *(const uint4*)(p + s.at(0) * 2);
+        w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+      } else if constexpr (ES == 2) {
+        const uint2 a = *(const uint2*)(p + s.at(0) * 2), b = *(const uint2*)(p + s.at(1) * 2);
+        w[0] = a.x, w[1] = a.y, w[2] = b.x, w[3] = b.y;
+      } else {
+        const uint2 a = *(const uint2*)(p + s.at(0));
+        w[0] = a.x, w[1] = a.y;
+      }
     } else {
-      const uint4 r = *(const uint4*)p;
-      const uint32_t w[4] = {r.x, r.y, r.z, r.w};
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        f[2 * i] = __uint_as_float(w[i] << 16);
-        f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+      for (int i = 0; i < 2 * ES; ++i) w[i] = 0u;
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i % 4 < s.count(i / 4)) {
+          const uint64_t at = s.at(i / 4) + i % 4;
+          if constexpr (ES == 4) w[i] = ((const uint32_t*)base)[at];
+          else if constexpr (ES == 2) w[i / 2] |= (uint32_t)((const uint16_t*)base)[at] << (16 * (i % 2));
+          else w[i / 4] |= (uint32_t)((const uint8_t*)base)[at] << (8 * (i % 4));
+        }
+    }
+  }
+  template <bool QUAD>
+  __device__ __forceinline__ void store(void* base, const Spot<QUAD>& s, bool vec) const {
+    char* p = (char*)base;
+    if (vec && s.count(1) == 4) {
+      if constexpr (ES == 4) {
+        *(uint4*)(p + s.at(0) * 4) = make_uint4(w[0], w[1], w[2], w[3]);
+        *(uint4*)(p + s.at(1) * 4) = make_uint4(w[4], w[5], w[6], w[7]);
+      } else if constexpr (ES == 2 && !QUAD) {
+        *(uint4*)(p + s.at(0) * 2) = make_uint4(w[0], w[1], w[2], w[3]);
+      } else if constexpr (ES == 2) {
+        *(uint2*)(p + s.at(0) * 2) = make_uint2(w[0], w[1]);
+        *(uint2*)(p + s.at(1) * 2) = make_uint2(w[2], w[3]);
+      } else {
+        *(uint2*)(p + s.at(0)) = make_uint2(w[0], w[1]);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i % 4 < s.count(i / 4)) {
+          const uint64_t at = s.at(i / 4) + i % 4;
+          if constexpr (ES == 4) ((uint32_t*)base)[at] = w[i];
+          else if constexpr (ES == 2) ((uint16_t*)base)[at] = (uint16_t)(w[i / 2] >> (16 * (i % 2)));
+          else ((uint8_t*)base)[at] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
+        }
+    }
+  }
+  // as binary32, two by two (elements; codes: their values)
+  __device__ __forceinline__ void get(F2 (&f)[4]) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (ES == 4) f[i] = f2_pack(__uint_as_float(w[2 * i]), __uint_as_float(w[2 * i + 1]));
+      else if constexpr (ES == 2) f[i] = f2_from_bf16x2(w[i]);
+      else f[i] = code_values((uint16_t)(w[i / 2] >> (16 * (i % 2))));
+    }
+  }
+  __device__ __forceinline__ void set(const F2 (&f)[4]) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if constexpr (ES == 4) {
+        float a, b;
+        f2_unpack(f[i], a, b);
+        w[2 * i] = __float_as_uint(a);
+        w[2 * i + 1] = __float_as_uint(b);
+      } else {
+        static_assert(ES == 2, "codes are put together elsewhere");
+        w[i] = f2_to_bf16x2(f[i]);
       }
     }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) f[i] = (uint32_t)i < count ? Io<DT>::widen(p[i]) : 0.0f;
   }
-}
-
-template <int DT>
-__device__ __forceinline__ void store8(void* base, uint64_t at, uint32_t count, bool vec, const float (&f)[8]) {
-  typename Io<DT>::T* p = (typename Io<DT>::T*)base + at;
-  if (vec && count == 8) {
-    if constexpr (DT == kF32) {
-      ((float4*)p)[0] = make_float4(f[0], f[1], f[2], f[3]);
-      ((float4*)p)[1] = make_float4(f[4], f[5], f[6], f[7]);
-    } else {
-      uint32_t w[4];
-#pragma unroll
-      for (int i = 0; i < 4; ++i) w[i] = f2_to_bf16x2(f2_pack(f[2 * i], f[2 * i + 1]));
-      *(uint4*)p = make_uint4(w[0], w[1], w[2], w[3]);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if ((uint32_t)i < count) p[i] = Io<DT>::narrow(f[i]);
+  // two e4m3 codes, each exactly a binary16 number
+  static __device__ __forceinline__ F2 code_values(uint16_t codes) {
+    uint32_t h;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(h) : "h"(codes));
+    float lo, hi;
+    asm("{.reg .b16 a, b; mov.b32 {a, b}, %2; cvt.f32.f16 %0, a; cvt.f32.f16 %1, b;}" : "=f"(lo), "=f"(hi) : "r"(h));
+    return f2_pack(lo, hi);
   }
-}
-
-__device__ __forceinline__ void load_codes(const void* base, uint64_t at, uint32_t count, bool vec, uint32_t (&w)[2]) {
-  const uint8_t* p = (const uint8_t*)base + at;
-  if (vec && count == 8) {
-    const uint2 r = *(const uint2*)p;
-    w[0] = r.x;
-    w[1] = r.y;
-  } else {
-    w[0] = w[1] = 0u;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if ((uint32_t)i < count) w[i / 4] |= (uint32_t)p[i] << (8 * (i % 4));
-  }
-}
-__device__ __forceinline__ void store_codes(void* base, uint64_t at, uint32_t count, bool vec, const uint32_t (&w)[2]) {
-  uint8_t* p = (uint8_t*)base + at;
-  if (vec && count == 8) {
-    *(uint2*)p = make_uint2(w[0], w[1]);
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if ((uint32_t)i < count) p[i] = (uint8_t)(w[i / 4] >> (8 * (i % 4)));
-  }
-}
-
-// The value of an e4m3 code: times 2^-120 the type's exponents are those of binary32, its subnormals too.  (The codes 0x7F and
-// 0xFF, which nothing here writes, come out as 480.)
-__device__ __forceinline__ float code_value(uint32_t code) {
-  return __uint_as_float(((code & 0x7Fu) << 20) | ((code & 0x80u) << 24)) * kTwo120;
-}
-// The code of a magnitude x of at most 448: to nearest (ties to even), or with 16 random bits, and half of one, below the last kept bit.
-__device__ __forceinline__ uint32_t code_of(float x, bool random, uint32_t bits) {
-  const uint32_t w = __float_as_uint(x * kTwoM120);
-  const uint32_t add = random ? (bits << 4) | 8u : 0x7FFFFu + ((w >> 20) & 1u);
-  const uint32_t code = (w + add) >> 20;
-  return code < kTopBits ? code : kTopBits;
-}
+};
 
 __device__ __forceinline__ float approx_sqrt(float x) {
   float y;
@@ -113,135 +140,289 @@ __device__ __forceinline__ float approx_sqrt(float x) {
 
 // What is the same for every element of a step.
 struct Rates {
-  float scale, lr, first, root;  // lr / (1 - b1^t) and 1 / sqrt(1 - b2^t)
-  uint64_t count;                // the generator's second counter word
+  float lr, first, root;   // lr / (1 - b1^t) and 1 / sqrt(1 - b2^t)
+  float grad1, grad2;      // what a gradient is multiplied with for m, and for sqrt(v): scale (1 - b1), scale sqrt(1 - b2)
+  uint64_t count;          // the generator's second counter word
 };
 
-// bfloat16 at random: 16 random bits below the last kept one.  An infinity stays one; a NaN too.
-__device__ __forceinline__ float random_bf16(float x, uint32_t bits) {
-  const uint32_t w = __float_as_uint(x);
-  if ((w & 0x7F800000u) == 0x7F800000u) return x;
-  return __uint_as_float((w + bits) & 0xFFFF0000u);
+// m' and sqrt(v') from the gradients, m and sqrt(v): keep1 and keep2 are b1 and sqrt(b2), times the scales of 8-bit states.
+//   m' = keep1 m + (1 - b1) g,  v' = (keep2 sqrt(v))^2 + (sqrt(1 - b2) g)^2
+__device__ __forceinline__ void moments(const F2 (&g)[4], F2 (&m)[4], F2 (&r)[4], const Rates& k, float keep1, float keep2) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    m[i] = f2_fma(m[i], f2_both(keep1), f2_mul(g[i], f2_both(k.grad1)));
+    const F2 a = f2_mul(r[i], f2_both(keep2)), b = f2_mul(g[i], f2_both(k.grad2));
+    float x, y;
+    f2_unpack(f2_fma(a, a, f2_mul(b, b)), x, y);
+    r[i] = f2_pack(approx_sqrt(x), approx_sqrt(y));
+  }
 }
 
-// One block of 256 elements (or the `count` elements of a lane that exist).
-template <int PDT, int GDT, int BITS, bool RANDOM>
-__device__ __forceinline__ void step_block(const StepArgs& a, const StepTensor& t, const Rates& r, const PhiloxKey& key, uint64_t draw,
-                                           uint64_t at, uint32_t count, bool vec, uint64_t block) {
-  const uint32_t lane = threadIdx.x & 31u;
-  float p[8], g[8], m[8], v[8], root[8];
-  load8<GDT>(t.g, at, count, vec, g);
-  load8<PDT>(t.p, at, count, vec, p);
-  if constexpr (BITS == 32) {
-    load8<kF32>(t.m, at, count, vec, m);
-    load8<kF32>(t.v, at, count, vec, v);
-  } else {
-    uint32_t mw[2], vw[2];
-    load_codes(t.m, at, count, vec, mw);
-    load_codes(t.v, at, count, vec, vw);
-    const float ms = t.m_scale[block] * (1.0f / kTopCode), vs = t.v_scale[block] * (1.0f / kTopCode);
+// p' = p - shrink p - step m / (root sqrt(v) + eps)
+__device__ __forceinline__ void update(F2 (&p)[4], const F2 (&m)[4], const F2 (&r)[4], float shrink, float step, float root, float eps) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      m[i] = code_value((mw[i / 4] >> (8 * (i % 4))) & 0xFFu) * ms;
-      const float x = code_value((vw[i / 4] >> (8 * (i % 4))) & 0x7Fu) * vs;
-      v[i] = x * x;
+  for (int i = 0; i < 4; ++i) {
+    float x, y;
+    f2_unpack(f2_fma(r[i], f2_both(root), f2_both(eps)), x, y);
+    const F2 q = f2_mul(m[i], f2_pack(__fdividef(1.0f, x), __fdividef(1.0f, y)));
+    p[i] = f2_fma(q, f2_both(-step), f2_fma(p[i], f2_both(-shrink), p[i]));
+  }
+}
+
+// bfloat16 at random: 16 random bits below the last kept one; an infinity or a NaN stays what it is.
+__device__ __forceinline__ void random_bf16(const F2 (&p)[4], const uint4& bits, Raw<2>& out) {
+  const uint32_t b[4] = {bits.x, bits.y, bits.z, bits.w};
+  F2 zero = f2_both(0.0f);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    zero = f2_fma(p[i], f2_both(0.0f), zero);  // NaN once one is not finite
+    float x, y;
+    f2_unpack(p[i], x, y);
+    out.w[i] = __byte_perm(__float_as_uint(x) + (b[i] & 0xFFFFu), __float_as_uint(y) + (b[i] >> 16), 0x7632);
+  }
+  float x, y;
+  f2_unpack(zero, x, y);
+  if (!(x + y == 0.0f)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f2_unpack(p[i], x, y);
+      if (!(fabsf(x) <= 3.4028235e38f)) out.w[i] = (out.w[i] & 0xFFFF0000u) | (f2_to_bf16x2(f2_pack(x, 0.0f)) & 0xFFFFu);
+      if (!(fabsf(y) <= 3.4028235e38f)) out.w[i] = (out.w[i] & 0x0000FFFFu) | (f2_to_bf16x2(f2_pack(0.0f, y)) & 0xFFFF0000u);
     }
   }
-  const float shrink = r.lr * t.decay * t.lr, step = r.first * t.lr;
+}
+
+// The e4m3 codes of eight values x / scale * 448, |x| at most the scale, with 16 random bits and half of one below the last kept bit.
+// Times 2^-120 the type's exponents are those of binary32, its subnormals too: a code is what stands from bit 20 on, moved to bit 24 here,
+// so that a code is a byte and each field of random bits lies where one byte permutation puts it.  (The largest is at most two roundings
+// above 448, and with the bits below the code at most 0xFFFF80 cannot carry.)  SIGNED: m; otherwise sqrt(v), whose fields have their bytes exchanged
+// and which is never rounded from above zero to zero.
+template <bool SIGNED>
+__device__ __forceinline__ void random_codes(const F2 (&x)[4], float inverse, const uint4& bits, Raw<1>& out) {
+  const uint32_t b[4] = {bits.x, bits.y, bits.z, bits.w};
+  uint32_t c[8], least = 0xFFFFFFFFu;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float x = g[i] * r.scale;
-    m[i] = fmaf(a.one_beta1, x - m[i], m[i]);
-    v[i] = fmaf(a.one_beta2 * x, x, a.beta2 * v[i]);
-    root[i] = approx_sqrt(v[i]);
-    p[i] = fmaf(-shrink, p[i], p[i]) - __fdividef(step * m[i], fmaf(root[i], r.root, a.eps));
+  for (int i = 0; i < 4; ++i) {
+    float lo, hi;
+    f2_unpack(f2_mul(f2_mul(x[i], f2_both(inverse)), f2_both(7.52316384526264e-37f)), lo, hi);
+    c[2 * i] = (__float_as_uint(lo) << 4) + __byte_perm(b[i], 0x80u, SIGNED ? 0x5104 : 0x5014);
+    c[2 * i + 1] = (__float_as_uint(hi) << 4) + __byte_perm(b[i], 0x80u, SIGNED ? 0x5324 : 0x5234);
+    if (SIGNED) {
+      f2_unpack(x[i], lo, hi);
+      c[2 * i] = (c[2 * i] & 0x7FFFFFFFu) | (__float_as_uint(lo) & 0x80000000u);
+      c[2 * i + 1] = (c[2 * i + 1] & 0x7FFFFFFFu) | (__float_as_uint(hi) & 0x80000000u);
+    } else {
+      least = min(least, min(c[2 * i], c[2 * i + 1]));
+    }
   }
-  if (PDT == kBF16 && RANDOM) {
-    float q[8];
-    const uint4 bits = philox(key, (draw + lane) | (1ull << 63), r.count);
-    const uint32_t w[4] = {bits.x, bits.y, bits.z, bits.w};
-#pragma unroll
-    for (int i = 0; i < 8; ++i) q[i] = random_bf16(p[i], i % 2 ? w[i / 2] >> 16 : w[i / 2] & 0xFFFFu);
-    store8<PDT>(t.p, at, count, vec, q);
-  } else {
-    store8<PDT>(t.p, at, count, vec, p);
-  }
-  if (PDT == kF32 && t.copy) store8<kBF16>(t.copy, at, count, vec, p);
-  if constexpr (BITS == 32) {
-    store8<kF32>(t.m, at, count, vec, m);
-    store8<kF32>(t.v, at, count, vec, v);
-  } else {
-    // magnitudes as whole numbers: a NaN is above everything and makes the block's scale one
-    uint32_t tm = 0u, tv = 0u;
+  if (!SIGNED && least < 0x01000000u) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      if ((uint32_t)i >= count) m[i] = root[i] = 0.0f;
-      tm = max(tm, __float_as_uint(m[i]) & 0x7FFFFFFFu);
-      tv = max(tv, __float_as_uint(root[i]) & 0x7FFFFFFFu);
+      float lo, hi;
+      f2_unpack(f2_mul(x[i / 2], f2_both(inverse)), lo, hi);
+      if (c[i] < 0x01000000u && (i % 2 ? hi : lo) > 0.0f) c[i] = 0x01000000u;
     }
-    const float top_m = __uint_as_float(__reduce_max_sync(0xffffffffu, tm)), top_v = __uint_as_float(__reduce_max_sync(0xffffffffu, tv));
-    // a block whose largest magnitude is below 2^-110 is stored as zeros
-    const float im = top_m >= 7.703719777548943e-34f ? __fdiv_rn(kTopCode, top_m) : 0.0f;
-    const float iv = top_v >= 7.703719777548943e-34f ? __fdiv_rn(kTopCode, top_v) : 0.0f;
-    uint32_t w[4] = {0u, 0u, 0u, 0u};
-    if (RANDOM) {
-      const uint4 bits = philox(key, draw + lane, r.count);
-      w[0] = bits.x, w[1] = bits.y, w[2] = bits.z, w[3] = bits.w;
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+    out.w[i] = __byte_perm(__byte_perm(c[4 * i], c[4 * i + 1], 0x0073), __byte_perm(c[4 * i + 2], c[4 * i + 3], 0x0073), 0x5410);
+}
+
+// The same to nearest (ties to even).
+template <bool SIGNED>
+__device__ __forceinline__ void nearest_codes(const F2 (&x)[4], float inverse, Raw<1>& out) {
+  uint32_t least = 0xFFu;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    uint32_t half[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      float lo, hi;
+      f2_unpack(f2_mul(x[2 * i + j], f2_both(inverse)), lo, hi);
+      uint16_t pair;
+      asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(pair) : "f"(hi), "f"(lo));
+      half[j] = pair;
+      if (!SIGNED) least = min(least, min(half[j] & 0xFFu, half[j] >> 8));
     }
-    uint32_t mw[2] = {0u, 0u}, vw[2] = {0u, 0u};
+    out.w[i] = half[0] | (half[1] << 16);
+  }
+  if (!SIGNED && least == 0u) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const uint32_t bits = i % 2 ? w[i / 2] >> 16 : w[i / 2] & 0xFFFFu;
-      const uint32_t other = __byte_perm(bits, 0u, 0x4401);  // the root's: the two bytes the other way round
-      uint32_t c = code_of(fabsf(m[i]) * im, RANDOM, bits) | (m[i] < 0.0f ? 0x80u : 0u);
-      mw[i / 4] |= c << (8 * (i % 4));
-      c = code_of(root[i] * iv, RANDOM, other);
-      if (c == 0u && root[i] * iv > 0.0f) c = 1u;
-      vw[i / 4] |= c << (8 * (i % 4));
+      float lo, hi;
+      f2_unpack(f2_mul(x[i / 2], f2_both(inverse)), lo, hi);
+      if (((out.w[i / 4] >> (8 * (i % 4))) & 0xFFu) == 0u && (i % 2 ? hi : lo) > 0.0f) out.w[i / 4] |= 1u << (8 * (i % 4));
     }
-    store_codes(t.m, at, count, vec, mw);
-    store_codes(t.v, at, count, vec, vw);
-    if (lane == 0) {
+  }
+}
+
+// The largest magnitude of a block, as a whole number (a NaN is above everything, and the scale becomes one), and 448 / that.
+__device__ __forceinline__ float largest(const F2 (&x)[4], float& inverse) {
+  uint32_t top = 0u;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float lo, hi;
+    f2_unpack(x[i], lo, hi);
+    top = max(top, max(__float_as_uint(lo) & 0x7FFFFFFFu, __float_as_uint(hi) & 0x7FFFFFFFu));
+  }
+  const float t = __uint_as_float(__reduce_max_sync(0xffffffffu, top));
+  // the approximate reciprocal (of a quarter: it is normal for every t) and one correction on the remainder: right to a rounding
+  const float r = rcp_approx(0.25f * t), q = 0.25f * kTopCode * r;
+  inverse = t >= kSmallest && t <= 3.4028235e38f ? fmaf(fmaf(-t, q, kTopCode), 0.25f * r, q) : 0.0f;
+  return t;
+}
+
+// Everything of a lane's eight elements before the step, on its way from memory.
+template <int PDT, int GDT, int BITS>
+struct Loaded {
+  Raw<Io<PDT>::kBytes> p;
+  Raw<Io<GDT>::kBytes> g;
+  Raw<BITS / 8> m, v;
+  float ms, vs;
+  template <bool QUAD>
+  __device__ __forceinline__ void load(const StepTensor& t, const Spot<QUAD>& s, bool vec, uint64_t block) {
+    g.load(t.g, s, vec);
+    p.load(t.p, s, vec);
+    m.load(t.m, s, vec);
+    v.load(t.v, s, vec);
+    if (BITS == 8) {
+      ms = t.m_scale[block];
+      vs = t.v_scale[block];
+    }
+  }
+};
+
+template <int PDT, int GDT, int BITS, bool RANDOM, bool QUAD>
+__device__ __forceinline__ void step_block(const StepArgs& a, const StepTensor& t, const Rates& k, const PhiloxKey& key, uint64_t draw,
+                                           const Loaded<PDT, GDT, BITS>& x, const Spot<QUAD>& s, bool vec, uint64_t block) {
+  F2 p[4], g[4], m[4], r[4];
+  x.g.get(g);
+  x.p.get(p);
+  x.m.get(m);
+  x.v.get(r);
+  float keep1 = a.beta1, keep2 = a.root_beta2;
+  if constexpr (BITS == 8) {
+    keep1 *= x.ms * (1.0f / kTopCode);
+    keep2 *= x.vs * (1.0f / kTopCode);
+    moments(g, m, r, k, keep1, keep2);
+  } else {  // v itself: v' = b2 v + (sqrt(1 - b2) g)^2
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      m[i] = f2_fma(m[i], f2_both(keep1), f2_mul(g[i], f2_both(k.grad1)));
+      const F2 b = f2_mul(g[i], f2_both(k.grad2));
+      r[i] = f2_fma(b, b, f2_mul(r[i], f2_both(a.beta2)));
+    }
+    Raw<4> out;
+    out.set(m);
+    out.store(t.m, s, vec);
+    out.set(r);
+    out.store(t.v, s, vec);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float lo, hi;
+      f2_unpack(r[i], lo, hi);
+      r[i] = f2_pack(approx_sqrt(lo), approx_sqrt(hi));
+    }
+  }
+  update(p, m, r, k.lr * t.decay * t.lr, k.first * t.lr, k.root, a.eps);
+  if constexpr (PDT == kBF16 && RANDOM) {
+    Raw<2> out;
+    random_bf16(p, philox(key, draw | (1ull << 63), k.count), out);
+    out.store(t.p, s, vec);
+  } else {
+    Raw<Io<PDT>::kBytes> out;
+    out.set(p);
+    out.store(t.p, s, vec);
+  }
+  if (PDT == kF32 && t.copy) {
+    Raw<2> out;
+    out.set(p);
+    out.store(t.copy, s, vec);
+  }
+  if constexpr (BITS == 8) {
+    float im, iv;
+    if (s.left < 8) {  // what does not exist has no part in the block's largest magnitude (m, v and g are zeros there, and so are these)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float lo, hi;
+        f2_unpack(m[i], lo, hi);
+        m[i] = f2_pack(2 * i < s.left ? lo : 0.0f, 2 * i + 1 < s.left ? hi : 0.0f);
+        f2_unpack(r[i], lo, hi);
+        r[i] = f2_pack(2 * i < s.left ? lo : 0.0f, 2 * i + 1 < s.left ? hi : 0.0f);
+      }
+    }
+    const float top_m = largest(m, im), top_v = largest(r, iv);
+    Raw<1> cm, cv;
+    if constexpr (RANDOM) {
+      const uint4 bits = philox(key, draw, k.count);
+      random_codes<true>(m, im, bits, cm);
+      random_codes<false>(r, iv, bits, cv);
+    } else {
+      nearest_codes<true>(m, im, cm);
+      nearest_codes<false>(r, iv, cv);
+    }
+    cm.store(t.m, s, vec);
+    cv.store(t.v, s, vec);
+    if ((threadIdx.x & 31u) == 0) {
       t.m_scale[block] = top_m;
       t.v_scale[block] = top_v;
     }
   }
 }
 
+// A unit is a chunk of four blocks, or (few chunks: more warps at work) one block of it.
 template <int PDT, int GDT, int BITS, bool RANDOM>
-__global__ void __launch_bounds__(kStepThreads) adamw_kernel(StepArgs a) {
+__global__ void __launch_bounds__(kStepThreads, BITS == 8 ? 3 : 2) adamw_kernel(const __grid_constant__ StepArgs a) {
+  // random bits and 8-bit blocks are counted from the tensor's first element, and its vectors with them
+  constexpr bool COUNTED = RANDOM || BITS == 8, QUAD = !COUNTED;
   enter_grid();
   const uint32_t lane = threadIdx.x & 31u;
-  Rates r;
-  r.scale = a.control[2];
-  r.lr = a.control[0];
+  float scale = a.control[2];
+  Rates k;
+  k.lr = a.control[0];
   if (a.clip) {
     const float norm = a.clip[0];
     if (!(fabsf(norm) <= 3.4028235e38f)) return;  // gradients that overflowed: nothing is changed
-    r.scale *= a.clip[1];
+    scale *= a.clip[1];
   }
   const float number = a.control[1];
-  r.first = __fdiv_rn(r.lr, -expm1f(number * a.log_beta1));
-  r.root = __frsqrt_rn(-expm1f(number * a.log_beta2));
+  k.first = __fdiv_rn(k.lr, -expm1f(number * a.log_beta1));
+  k.root = __frsqrt_rn(-expm1f(number * a.log_beta2));
+  k.grad1 = scale * a.one_beta1;
+  k.grad2 = scale * a.root_one_beta2;
   const PhiloxKey key(RANDOM ? a.rng[0] : 0ull);
-  r.count = RANDOM ? a.rng[1] + a.site : 0ull;
-  for (uint64_t c = (uint64_t)blockIdx.x * kStepWarps + (threadIdx.x >> 5); c < a.n_chunks; c += (uint64_t)gridDim.x * kStepWarps) {
+  k.count = RANDOM ? a.rng[1] + a.site : 0ull;
+  const uint32_t each = kChunkBlocks / a.split;
+  const uint64_t units = (uint64_t)a.n_chunks * a.split;
+  for (uint64_t u = (uint64_t)blockIdx.x * kStepWarps + (threadIdx.x >> 5); u < units; u += (uint64_t)gridDim.x * kStepWarps) {
+    const uint32_t c = (uint32_t)(u / a.split), begin = (uint32_t)(u % a.split) * each;
     const StepTensor t = a.tensors[a.owner[c]];
-    const uint64_t from = (c - t.chunk0) * kStepChunk;
-    // random bits and blocks are counted from the tensor's first element, and its vectors with them
-    constexpr bool COUNTED = RANDOM || BITS == 8;
+    const uint64_t from = (uint64_t)(c - t.chunk0) * kStepChunk;
     const bool vec = COUNTED ? t.head == 0u : t.head != kStepScalar;
     const uint32_t head = vec ? t.head : 0u;
-    // the elements before the grid, as a block of one lane's
-    if (!COUNTED && head && from == 0)
-      step_block<PDT, GDT, BITS, RANDOM>(a, t, r, key, t.block0 * 32, 0, lane == 0 ? (t.n < head ? (uint32_t)t.n : head) : 0u, false, 0);
+    if (QUAD && head && from == 0 && begin == 0) {  // the elements before the grid, as a block of two lanes'
+      const uint64_t n = t.n < head ? t.n : head;
+      const Spot<QUAD> s{4 * lane, (int32_t)(n > 4 * lane ? (n - 4 * lane < 4 ? n - 4 * lane : 4) : 0)};
+      Loaded<PDT, GDT, BITS> x;
+      x.load(t, s, false, 0);
+      step_block<PDT, GDT, BITS, RANDOM, QUAD>(a, t, k, key, 0, x, s, false, 0);
+    }
+    const auto spot = [&](uint32_t i) {
+      const uint64_t first = head + from + (uint64_t)i * kStepBlock + (QUAD ? 4 : 8) * lane;
+      return Spot<QUAD>{first, first >= t.n ? 0 : (t.n - first < 256 ? (int32_t)(t.n - first) : 256)};
+    };
+    const uint64_t block = from / kStepBlock;
+    const uint64_t rest = t.n > head + from ? t.n - head - from : 0;  // of the tensor from this chunk on
+    const uint32_t blocks = rest >= kStepChunk ? kChunkBlocks : (uint32_t)((rest + kStepBlock - 1) / kStepBlock);
+    const uint32_t end = begin + each < blocks ? begin + each : blocks;
+    if (begin >= end) continue;
+    Loaded<PDT, GDT, BITS> x;
+    x.load(t, spot(begin), vec, block + begin);
 #pragma unroll 1
-    for (uint32_t k = 0; k < kStepChunk / kStepBlock; ++k) {
-      const uint64_t base = head + from + k * kStepBlock;
-      if (base >= t.n) break;
-      const uint64_t at = base + 8 * lane, block = (from + k * kStepBlock) / kStepBlock;
-      const uint32_t count = at >= t.n ? 0u : (t.n - at < 8 ? (uint32_t)(t.n - at) : 8u);
-      step_block<PDT, GDT, BITS, RANDOM>(a, t, r, key, (t.block0 + block) * 32, at, count, vec, block);
+    for (uint32_t i = begin; i < end; ++i) {
+      const Loaded<PDT, GDT, BITS> now = x;
+      if (i + 1 < end) x.load(t, spot(i + 1), vec, block + i + 1);
+      step_block<PDT, GDT, BITS, RANDOM, QUAD>(a, t, k, key, (t.block0 + block + i) * 32 + lane, now, spot(i), vec, block + i);
     }
   }
 }
@@ -250,43 +431,56 @@ __global__ void __launch_bounds__(kStepThreads) adamw_kernel(StepArgs a) {
 // Squares of eight elements: in 32 bits where the largest magnitude is from 2^-40 to 2^50, whose squares neither overflow nor, beside
 // it, vanish; else in 64.  Sums of eights are added in 64 bits.
 template <int GDT>
-__device__ __forceinline__ double square_sum(const float (&g)[8]) {
-  float top = 0.0f, s = 0.0f;
+__device__ __forceinline__ double square_sum(const Raw<Io<GDT>::kBytes>& raw) {
+  F2 g[4], two = f2_both(0.0f);
+  raw.get(g);
+  float top = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    top = fmaxf(top, fabsf(g[i]));
-    s = fmaf(g[i], g[i], s);
+  for (int i = 0; i < 4; ++i) {
+    two = f2_fma(g[i], g[i], two);
+    float lo, hi;
+    f2_unpack(g[i], lo, hi);
+    top = fmaxf(top, fmaxf(fabsf(lo), fabsf(hi)));
   }
-  if (top == 0.0f || (top >= 9.094947e-13f && top <= 1.1258999e15f)) return (double)s;
+  float x, y;
+  f2_unpack(two, x, y);
+  if (top == 0.0f || (top >= 9.094947e-13f && top <= 1.1258999e15f)) return (double)(x + y);
   double d = 0.0;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) d = fma((double)g[i], (double)g[i], d);
+  for (int i = 0; i < 4; ++i) {
+    f2_unpack(g[i], x, y);
+    d = fma((double)x, (double)x, fma((double)y, (double)y, d));
+  }
   return d;
 }
 
 template <int GDT>
-__global__ void __launch_bounds__(kStepThreads) grad_norm_kernel(StepArgs a, double* partials) {
+__global__ void __launch_bounds__(kStepThreads, 4) grad_norm_kernel(const __grid_constant__ StepArgs a, double* partials) {
   __shared__ double buf[kStepWarps];
+  constexpr int ES = Io<GDT>::kBytes;
   enter_grid();
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
   double sum = 0.0;
   for (uint64_t c = (uint64_t)blockIdx.x * kStepWarps + warp; c < a.n_chunks; c += (uint64_t)gridDim.x * kStepWarps) {
-    const StepTensor t = a.tensors[a.owner[c]];
-    const uint64_t from = (c - t.chunk0) * kStepChunk;
-    const bool vec = t.head != kStepScalar;
-    const uint32_t head = vec ? t.head : 0u;
-    float g[8];
+    const StepTensor& tensor = a.tensors[a.owner[c]];
+    const void* const grad = tensor.g;
+    const uint64_t n = tensor.n, from = (c - tensor.chunk0) * kStepChunk;
+    const bool vec = tensor.head != kStepScalar;
+    const uint32_t head = vec ? tensor.head : 0u;
+    Raw<ES> raw[kChunkBlocks];
+#pragma unroll
+    for (uint32_t i = 0; i < kChunkBlocks; ++i) {
+      const uint64_t first = head + from + (uint64_t)i * kStepBlock + 4 * lane;
+      raw[i].load(grad, Spot<true>{first, first >= n ? 0 : (n - first < 256 ? (int32_t)(n - first) : 256)}, vec);
+    }
     if (head && from == 0) {
-      load8<GDT>(t.g, 0, lane == 0 ? (t.n < head ? (uint32_t)t.n : head) : 0u, false, g);
-      sum += square_sum<GDT>(g);
+      const uint64_t before = n < head ? n : head;
+      Raw<ES> front;
+      front.load(grad, Spot<true>{4 * lane, (int32_t)(before > 4 * lane ? (before - 4 * lane < 4 ? before - 4 * lane : 4) : 0)}, false);
+      sum += square_sum<GDT>(front);
     }
 #pragma unroll
-    for (uint32_t k = 0; k < kStepChunk / kStepBlock; ++k) {
-      const uint64_t at = head + from + k * kStepBlock + 8 * lane;
-      const uint32_t count = at >= t.n ? 0u : (t.n - at < 8 ? (uint32_t)(t.n - at) : 8u);
-      load8<GDT>(t.g, at, count, vec, g);
-      sum += square_sum<GDT>(g);
-    }
+    for (uint32_t i = 0; i < kChunkBlocks; ++i) sum += square_sum<GDT>(raw[i]);
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -330,9 +524,11 @@ cudaError_t launch_adamw_types(int bits, const StepArgs& a, unsigned grid, cudaS
 
 }  // namespace
 
-cudaError_t launch_adamw(int pdt, int gdt, int state_bits, const StepArgs& a, cudaStream_t st) {
+cudaError_t launch_adamw(int pdt, int gdt, int state_bits, StepArgs a, cudaStream_t st) {
   if (a.n_chunks == 0) return cudaSuccess;
-  const uint64_t want = ((uint64_t)a.n_chunks + kStepWarps - 1) / kStepWarps, cap = (uint64_t)sm_count() * 16;
+  const uint64_t resident = (uint64_t)sm_count() * (state_bits == 8 ? 3 : 2);  // CTAs at once
+  a.split = (uint64_t)a.n_chunks * kChunkBlocks <= resident * kStepWarps ? kChunkBlocks : 1;
+  const uint64_t want = ((uint64_t)a.n_chunks * a.split + kStepWarps - 1) / kStepWarps, cap = resident * 4;
   const unsigned grid = (unsigned)(want < cap ? want : cap);
   if (pdt == kF32)
     return gdt == kF32 ? launch_adamw_types<kF32, kF32>(state_bits, a, grid, st) : launch_adamw_types<kF32, kBF16>(state_bits, a, grid, st);

@@ -149,9 +149,10 @@ struct StepArgs {
   const float* clip;      // norm and factor, or NULL
   const uint64_t* rng;    // seed and offset, or NULL: round to nearest
   uint64_t site;
-  float one_beta1, beta2, one_beta2, log_beta1, log_beta2, eps;
+  float beta1, one_beta1, beta2, root_beta2, root_one_beta2, log_beta1, log_beta2, eps;  // root: sqrt(beta2), sqrt(1 - beta2)
+  uint32_t split;         // parts of a chunk, set by launch_adamw
 };
-cudaError_t launch_adamw(int pdt, int gdt, int state_bits, const StepArgs& a, cudaStream_t st);
+cudaError_t launch_adamw(int pdt, int gdt, int state_bits, StepArgs a, cudaStream_t st);
 uint64_t grad_norm_scratch_bytes(uint32_t n_chunks);
 cudaError_t launch_grad_norm(int gdt, const StepArgs& a, float max_norm, float* out, double* scratch, cudaStream_t st);
 
