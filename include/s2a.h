@@ -476,11 +476,11 @@ typedef struct {
 
 typedef struct {
   size_t bytes;             /* of the image */
-  size_t n_tensors, n_chunks;
+  size_t n_tensors, n_chunks, chunk_blocks;
   int pdt, gdt, state_bits, grads_only;
 } s2a_step_plan;
 
-/* Bytes of the plan's image (0 where it would be too large). */
+/* Bytes of the plan's image. */
 size_t s2a_step_plan_bytes(const s2a_step_tensor* tensors, size_t n_tensors);
 
 /* Checks the tensors and writes the image, s2a_step_plan_bytes(...) bytes of HOST memory, 16-byte aligned, and *plan.  All pointers

@@ -52,7 +52,7 @@ class _StepTensor(ctypes.Structure):    # s2a_step_tensor
 
 
 class _StepPlan(ctypes.Structure):      # s2a_step_plan
-    _fields_ = [(name, ctypes.c_size_t) for name in ("bytes", "n_tensors", "n_chunks")]
+    _fields_ = [(name, ctypes.c_size_t) for name in ("bytes", "n_tensors", "n_chunks", "chunk_blocks")]
     _fields_ += [(name, ctypes.c_int) for name in ("pdt", "gdt", "state_bits", "grads_only")]
 
 

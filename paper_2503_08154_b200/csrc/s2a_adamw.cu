@@ -10,8 +10,8 @@
 // rounded at random, by the 16 bits of a counter-based generator, it moves as it should on average.
 //
 // Bound by memory: a warp takes 256 elements at a time, eight neighbouring ones a lane, everything of them in registers between
-// one load and one store, the block's largest magnitudes by two warp reductions.  A chunk of four such blocks is what a warp takes from the
-// plan at a time; the plan has the tensor of each chunk, so that no warp searches.
+// one load and one store, the block's largest magnitudes by two warp reductions.  What a warp takes from the plan
+// at a time is a chunk of such blocks; the plan has the tensor of each chunk, so that no warp searches.
 #include "s2a_launch.h"
 #include "s2a_oct.cuh"
 #include "s2a_philox.cuh"
@@ -19,20 +19,24 @@
 namespace s2a {
 namespace {
 
-constexpr int kStepWarps = 8;
+constexpr int kStepWarps = 4;
 constexpr int kStepThreads = kStepWarps * 32;
-constexpr uint32_t kChunkBlocks = kStepChunk / kStepBlock;
+constexpr int kNormWarps = 8;
+constexpr int kNormThreads = kNormWarps * 32;
 constexpr float kTopCode = 448.0f;                // the largest e4m3 value
+constexpr float kTwoM120 = 7.52316384526264e-37f;
 constexpr float kSmallest = 7.703719777548943e-34f;  // 2^-110: a block of which the largest magnitude is below is stored as zeros
 
 // A lane's eight elements of a block.  QUAD: elements 4 lane .. 4 lane + 3 and 128 more, so that a warp's accesses of binary32 have no gaps;
 // otherwise 8 lane .. 8 lane + 7, which share 128 random bits.  `first` and `left`: where its elements begin and how many of the
 // tensor's there are from there on.
-template <bool QUAD>
+// WHOLE: the block is, and on the 16-byte grid.
+template <bool QUAD, bool WHOLE = false>
 struct Spot {
   uint64_t first;
   int32_t left;  // from `first`, at most 256
   __device__ __forceinline__ int32_t count(int half) const {  // of the four elements of a half
+    if (WHOLE) return 4;
     const int32_t n = left - (QUAD ? 128 : 4) * half;
     return n < 0 ? 0 : (n < 4 ? n : 4);
   }
@@ -43,10 +47,10 @@ struct Spot {
 template <int ES>
 struct Raw {
   uint32_t w[2 * ES];
-  template <bool QUAD>
-  __device__ __forceinline__ void load(const void* base, const Spot<QUAD>& s, bool vec) {
+  template <bool QUAD, bool WHOLE>
+  __device__ __forceinline__ void load(const void* base, const Spot<QUAD, WHOLE>& s, bool vec) {
     const char* p = (const char*)base;
-    if (vec && s.count(1) == 4) {  // all eight
+    if (WHOLE || (vec && s.count(1) == 4)) {  // all eight
       if constexpr (ES == 4) {
         const uint4 a = *(const uint4*)(p + s.at(0) * 4), b = *(const uint4*)(p + s.at(1) * 4);
         w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w, w[4] = b.x, w[5] = b.y, w[6] = b.z, w[7] = b.w;
@@ -73,10 +77,10 @@ struct Raw {
         }
     }
   }
-  template <bool QUAD>
-  __device__ __forceinline__ void store(void* base, const Spot<QUAD>& s, bool vec) const {
+  template <bool QUAD, bool WHOLE>
+  __device__ __forceinline__ void store(void* base, const Spot<QUAD, WHOLE>& s, bool vec) const {
     char* p = (char*)base;
-    if (vec && s.count(1) == 4) {
+    if (WHOLE || (vec && s.count(1) == 4)) {
       if constexpr (ES == 4) {
         *(uint4*)(p + s.at(0) * 4) = make_uint4(w[0], w[1], w[2], w[3]);
         *(uint4*)(p + s.at(1) * 4) = make_uint4(w[4], w[5], w[6], w[7]);
@@ -138,6 +142,21 @@ __device__ __forceinline__ float approx_sqrt(float x) {
   return y;
 }
 
+// The round keys of the generator, from shared memory: in registers all twenty would cost the kernel a CTA of each SM.
+struct SharedKey {
+  const uint4* keys;  // of two rounds each
+  __device__ __forceinline__ uint4 draw(uint64_t block, uint64_t count) const {
+    uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = (uint32_t)count, c3 = (uint32_t)(count >> 32);
+#pragma unroll
+    for (int i = 0; i < 5; ++i) {
+      const uint4 k = keys[i];
+      philox_round(c0, c1, c2, c3, k.x, k.y);
+      philox_round(c0, c1, c2, c3, k.z, k.w);
+    }
+    return make_uint4(c0, c1, c2, c3);
+  }
+};
+
 // What is the same for every element of a step.
 struct Rates {
   float lr, first, root;   // lr / (1 - b1^t) and 1 / sqrt(1 - b2^t)
@@ -193,34 +212,35 @@ __device__ __forceinline__ void random_bf16(const F2 (&p)[4], const uint4& bits,
 }
 
 // The e4m3 codes of eight values x / scale * 448, |x| at most the scale, with 16 random bits and half of one below the last kept bit.
-// Times 2^-120 the type's exponents are those of binary32, its subnormals too: a code is what stands from bit 20 on, moved to bit 24 here,
-// so that a code is a byte and each field of random bits lies where one byte permutation puts it.  (The largest is at most two roundings
-// above 448, and with the bits below the code at most 0xFFFF80 cannot carry.)  SIGNED: m; otherwise sqrt(v), whose fields have their bytes exchanged
-// and which is never rounded from above zero to zero.
-template <bool SIGNED>
+// Times 2^-120 (LARGE: apart from `inverse`, which would leave the normal range) the type's exponents are those of binary32, its subnormals too: a code is what stands from
+// bit 20 on, moved to bit 24 here, so that a code is a byte and each field of random bits lies where one byte permutation puts it.  (The
+// largest is at most two roundings above 448, and with the bits below the code at most 0xFFFF80 cannot carry.)  SIGNED: m; otherwise sqrt(v),
+// whose fields have their bytes exchanged and which is never rounded from above zero to zero.
+template <bool SIGNED, bool LARGE>
 __device__ __forceinline__ void random_codes(const F2 (&x)[4], float inverse, const uint4& bits, Raw<1>& out) {
   const uint32_t b[4] = {bits.x, bits.y, bits.z, bits.w};
-  uint32_t c[8], least = 0xFFFFFFFFu;
+  uint32_t c[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     float lo, hi;
-    f2_unpack(f2_mul(f2_mul(x[i], f2_both(inverse)), f2_both(7.52316384526264e-37f)), lo, hi);
+    f2_unpack(LARGE ? f2_mul(f2_mul(x[i], f2_both(inverse)), f2_both(kTwoM120)) : f2_mul(x[i], f2_both(inverse)), lo, hi);
     c[2 * i] = (__float_as_uint(lo) << 4) + __byte_perm(b[i], 0x80u, SIGNED ? 0x5104 : 0x5014);
     c[2 * i + 1] = (__float_as_uint(hi) << 4) + __byte_perm(b[i], 0x80u, SIGNED ? 0x5324 : 0x5234);
     if (SIGNED) {
       f2_unpack(x[i], lo, hi);
       c[2 * i] = (c[2 * i] & 0x7FFFFFFFu) | (__float_as_uint(lo) & 0x80000000u);
       c[2 * i + 1] = (c[2 * i + 1] & 0x7FFFFFFFu) | (__float_as_uint(hi) & 0x80000000u);
-    } else {
-      least = min(least, min(c[2 * i], c[2 * i + 1]));
     }
   }
-  if (!SIGNED && least < 0x01000000u) {
+  if (!SIGNED) {
+    const uint32_t least = __vimin3_u32(__vimin3_u32(c[0], c[1], c[2]), __vimin3_u32(c[3], c[4], c[5]), min(c[6], c[7]));
+    if (least < 0x01000000u) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float lo, hi;
-      f2_unpack(f2_mul(x[i / 2], f2_both(inverse)), lo, hi);
-      if (c[i] < 0x01000000u && (i % 2 ? hi : lo) > 0.0f) c[i] = 0x01000000u;
+      for (int i = 0; i < 8; ++i) {
+        float lo, hi;
+        f2_unpack(x[i / 2], lo, hi);
+        if (c[i] < 0x01000000u && (i % 2 ? hi : lo) > 0.0f && inverse > 0.0f) c[i] = 0x01000000u;
+      }
     }
   }
 #pragma unroll
@@ -250,26 +270,37 @@ __device__ __forceinline__ void nearest_codes(const F2 (&x)[4], float inverse, R
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       float lo, hi;
-      f2_unpack(f2_mul(x[i / 2], f2_both(inverse)), lo, hi);
-      if (((out.w[i / 4] >> (8 * (i % 4))) & 0xFFu) == 0u && (i % 2 ? hi : lo) > 0.0f) out.w[i / 4] |= 1u << (8 * (i % 4));
+      f2_unpack(x[i / 2], lo, hi);
+      if (((out.w[i / 4] >> (8 * (i % 4))) & 0xFFu) == 0u && (i % 2 ? hi : lo) > 0.0f && inverse > 0.0f) out.w[i / 4] |= 1u << (8 * (i % 4));
     }
   }
 }
 
-// The largest magnitude of a block, as a whole number (a NaN is above everything, and the scale becomes one), and 448 / that.
+// The largest magnitude of three, or a NaN if there is one.
+__device__ __forceinline__ float largest3(float a, float b, float c) {
+  float d;
+  asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+
+// The largest magnitude of a block (a NaN, as a whole number, is above everything, and the scale becomes one), and what its elements are multiplied
+// with for their codes: 448 / that.
 __device__ __forceinline__ float largest(const F2 (&x)[4], float& inverse) {
-  uint32_t top = 0u;
+  float f[8];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    float lo, hi;
-    f2_unpack(x[i], lo, hi);
-    top = max(top, max(__float_as_uint(lo) & 0x7FFFFFFFu, __float_as_uint(hi) & 0x7FFFFFFFu));
-  }
-  const float t = __uint_as_float(__reduce_max_sync(0xffffffffu, top));
+  for (int i = 0; i < 4; ++i) f2_unpack(x[i], f[2 * i], f[2 * i + 1]);
+  const float mine = largest3(largest3(f[0], f[1], f[2]), largest3(f[3], f[4], f[5]), largest3(f[6], f[7], 0.0f));
+  const float t = __uint_as_float(__reduce_max_sync(0xffffffffu, __float_as_uint(mine)));
   // the approximate reciprocal (of a quarter: it is normal for every t) and one correction on the remainder: right to a rounding
   const float r = rcp_approx(0.25f * t), q = 0.25f * kTopCode * r;
   inverse = t >= kSmallest && t <= 3.4028235e38f ? fmaf(fmaf(-t, q, kTopCode), 0.25f * r, q) : 0.0f;
   return t;
+}
+
+template <bool SIGNED>
+__device__ __forceinline__ void random_codes(const F2 (&x)[4], float top, float inverse, const uint4& bits, Raw<1>& out) {
+  if (top <= 16384.0f) random_codes<SIGNED, false>(x, inverse * kTwoM120, bits, out);
+  else random_codes<SIGNED, true>(x, inverse, bits, out);
 }
 
 // Everything of a lane's eight elements before the step, on its way from memory.
@@ -279,8 +310,8 @@ struct Loaded {
   Raw<Io<GDT>::kBytes> g;
   Raw<BITS / 8> m, v;
   float ms, vs;
-  template <bool QUAD>
-  __device__ __forceinline__ void load(const StepTensor& t, const Spot<QUAD>& s, bool vec, uint64_t block) {
+  template <bool QUAD, bool WHOLE>
+  __device__ __forceinline__ void load(const StepTensor& t, const Spot<QUAD, WHOLE>& s, bool vec, uint64_t block) {
     g.load(t.g, s, vec);
     p.load(t.p, s, vec);
     m.load(t.m, s, vec);
@@ -292,9 +323,9 @@ struct Loaded {
   }
 };
 
-template <int PDT, int GDT, int BITS, bool RANDOM, bool QUAD>
-__device__ __forceinline__ void step_block(const StepArgs& a, const StepTensor& t, const Rates& k, const PhiloxKey& key, uint64_t draw,
-                                           const Loaded<PDT, GDT, BITS>& x, const Spot<QUAD>& s, bool vec, uint64_t block) {
+template <bool RANDOM, int PDT, int GDT, int BITS, bool QUAD, bool WHOLE>
+__device__ __forceinline__ void step_block(const StepArgs& a, const StepTensor& t, const Rates& k, const SharedKey& key, uint64_t draw,
+                                           const Loaded<PDT, GDT, BITS>& x, const Spot<QUAD, WHOLE>& s, bool vec, uint64_t block) {
   F2 p[4], g[4], m[4], r[4];
   x.g.get(g);
   x.p.get(p);
@@ -327,7 +358,7 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const StepTensor& 
   update(p, m, r, k.lr * t.decay * t.lr, k.first * t.lr, k.root, a.eps);
   if constexpr (PDT == kBF16 && RANDOM) {
     Raw<2> out;
-    random_bf16(p, philox(key, draw | (1ull << 63), k.count), out);
+    random_bf16(p, key.draw(draw | (1ull << 63), k.count), out);
     out.store(t.p, s, vec);
   } else {
     Raw<Io<PDT>::kBytes> out;
@@ -341,7 +372,7 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const StepTensor& 
   }
   if constexpr (BITS == 8) {
     float im, iv;
-    if (s.left < 8) {  // what does not exist has no part in the block's largest magnitude (m, v and g are zeros there, and so are these)
+    if (!WHOLE && s.left < 8) {  // what does not exist has no part in the block's largest magnitude (m, v and g are zeros there, and so are these)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float lo, hi;
@@ -354,9 +385,9 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const StepTensor& 
     const float top_m = largest(m, im), top_v = largest(r, iv);
     Raw<1> cm, cv;
     if constexpr (RANDOM) {
-      const uint4 bits = philox(key, draw, k.count);
-      random_codes<true>(m, im, bits, cm);
-      random_codes<false>(r, iv, bits, cv);
+      const uint4 bits = key.draw(draw, k.count);
+      random_codes<true>(m, top_m, im, bits, cm);
+      random_codes<false>(r, top_v, iv, bits, cv);
     } else {
       nearest_codes<true>(m, im, cm);
       nearest_codes<false>(r, iv, cv);
@@ -370,13 +401,26 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const StepTensor& 
   }
 }
 
-// A unit is a chunk of four blocks, or (few chunks: more warps at work) one block of it.
+// CTAs of an SM.
+template <int BITS> constexpr int kStepCtas = BITS == 8 ? 5 : 4;
+
 template <int PDT, int GDT, int BITS, bool RANDOM>
-__global__ void __launch_bounds__(kStepThreads, BITS == 8 ? 3 : 2) adamw_kernel(const __grid_constant__ StepArgs a) {
+__global__ void __launch_bounds__(kStepThreads, kStepCtas<BITS>) adamw_kernel(const __grid_constant__ StepArgs a) {
   // random bits and 8-bit blocks are counted from the tensor's first element, and its vectors with them
   constexpr bool COUNTED = RANDOM || BITS == 8, QUAD = !COUNTED;
+  __shared__ uint4 keys[5];
   enter_grid();
   const uint32_t lane = threadIdx.x & 31u;
+  if constexpr (RANDOM) {
+    if (threadIdx.x < 5) {
+      const PhiloxKey key(a.rng[0]);
+#pragma unroll
+      for (int i = 0; i < 5; ++i)
+        if (threadIdx.x == i) keys[i] = make_uint4(key.k0[2 * i], key.k1[2 * i], key.k0[2 * i + 1], key.k1[2 * i + 1]);
+    }
+    __syncthreads();
+  }
+  const SharedKey key{keys};
   float scale = a.control[2];
   Rates k;
   k.lr = a.control[0];
@@ -390,97 +434,112 @@ __global__ void __launch_bounds__(kStepThreads, BITS == 8 ? 3 : 2) adamw_kernel(
   k.root = __frsqrt_rn(-expm1f(number * a.log_beta2));
   k.grad1 = scale * a.one_beta1;
   k.grad2 = scale * a.root_one_beta2;
-  const PhiloxKey key(RANDOM ? a.rng[0] : 0ull);
   k.count = RANDOM ? a.rng[1] + a.site : 0ull;
-  const uint32_t each = kChunkBlocks / a.split;
-  const uint64_t units = (uint64_t)a.n_chunks * a.split;
-  for (uint64_t u = (uint64_t)blockIdx.x * kStepWarps + (threadIdx.x >> 5); u < units; u += (uint64_t)gridDim.x * kStepWarps) {
-    const uint32_t c = (uint32_t)(u / a.split), begin = (uint32_t)(u % a.split) * each;
+  const uint32_t blocks = a.chunk_blocks;
+  for (uint64_t c = (uint64_t)blockIdx.x * kStepWarps + (threadIdx.x >> 5); c < a.n_chunks; c += (uint64_t)gridDim.x * kStepWarps) {
     const StepTensor t = a.tensors[a.owner[c]];
-    const uint64_t from = (uint64_t)(c - t.chunk0) * kStepChunk;
+    const uint64_t block = (c - t.chunk0) * blocks, from = block * kStepBlock;
     const bool vec = COUNTED ? t.head == 0u : t.head != kStepScalar;
     const uint32_t head = vec ? t.head : 0u;
-    if (QUAD && head && from == 0 && begin == 0) {  // the elements before the grid, as a block of two lanes'
+    if (QUAD && head && from == 0) {  // the elements before the grid, as a block of two lanes'
       const uint64_t n = t.n < head ? t.n : head;
       const Spot<QUAD> s{4 * lane, (int32_t)(n > 4 * lane ? (n - 4 * lane < 4 ? n - 4 * lane : 4) : 0)};
       Loaded<PDT, GDT, BITS> x;
       x.load(t, s, false, 0);
-      step_block<PDT, GDT, BITS, RANDOM, QUAD>(a, t, k, key, 0, x, s, false, 0);
+      step_block<RANDOM>(a, t, k, key, 0, x, s, false, 0);
     }
-    const auto spot = [&](uint32_t i) {
-      const uint64_t first = head + from + (uint64_t)i * kStepBlock + (QUAD ? 4 : 8) * lane;
-      return Spot<QUAD>{first, first >= t.n ? 0 : (t.n - first < 256 ? (int32_t)(t.n - first) : 256)};
-    };
-    const uint64_t block = from / kStepBlock;
+    const uint64_t draw = (t.block0 + block) * 32 + lane;
+    const uint64_t base = head + from + (QUAD ? 4 : 8) * lane;  // the lane's first element in block 0 of the chunk
     const uint64_t rest = t.n > head + from ? t.n - head - from : 0;  // of the tensor from this chunk on
-    const uint32_t blocks = rest >= kStepChunk ? kChunkBlocks : (uint32_t)((rest + kStepBlock - 1) / kStepBlock);
-    const uint32_t end = begin + each < blocks ? begin + each : blocks;
-    if (begin >= end) continue;
-    Loaded<PDT, GDT, BITS> x;
-    x.load(t, spot(begin), vec, block + begin);
+    if (vec && blocks > 1 && rest >= (uint64_t)blocks * kStepBlock) {
+      // whole blocks: the next one is on its way while one is in work
+      const auto spot = [&](uint32_t i) { return Spot<QUAD, true>{base + i * kStepBlock, 256}; };
+      Loaded<PDT, GDT, BITS> x, y;
+      x.load(t, spot(0), true, block);
 #pragma unroll 1
-    for (uint32_t i = begin; i < end; ++i) {
-      const Loaded<PDT, GDT, BITS> now = x;
-      if (i + 1 < end) x.load(t, spot(i + 1), vec, block + i + 1);
-      step_block<PDT, GDT, BITS, RANDOM, QUAD>(a, t, k, key, (t.block0 + block + i) * 32 + lane, now, spot(i), vec, block + i);
+      for (uint32_t i = 0; i < blocks; i += 2) {
+        y.load(t, spot(i + 1), true, block + i + 1);
+        step_block<RANDOM>(a, t, k, key, draw + 32 * i, x, spot(i), true, block + i);
+        if (i + 2 < blocks) x.load(t, spot(i + 2), true, block + i + 2);
+        step_block<RANDOM>(a, t, k, key, draw + 32 * (i + 1), y, spot(i + 1), true, block + i + 1);
+      }
+      continue;
+    }
+#pragma unroll 1
+    for (uint32_t i = 0; i < blocks && (uint64_t)i * kStepBlock < rest; ++i) {
+      const uint64_t first = base + i * kStepBlock;
+      const Spot<QUAD> s{first, first >= t.n ? 0 : (t.n - first < 256 ? (int32_t)(t.n - first) : 256)};
+      Loaded<PDT, GDT, BITS> x;
+      x.load(t, s, vec, block + i);
+      step_block<RANDOM>(a, t, k, key, draw + 32 * i, x, s, vec, block + i);
     }
   }
 }
 
 // ---------------------------------------------------------------- the gradients' norm
-// Squares of eight elements: in 32 bits where the largest magnitude is from 2^-40 to 2^50, whose squares neither overflow nor, beside
-// it, vanish; else in 64.  Sums of eights are added in 64 bits.
+// The sum of eight squares: in 32 bits where it comes out far from both ends of their range (no square overflowed, and none that vanished
+// matters beside 2^-80), else in 64.
 template <int GDT>
-__device__ __forceinline__ double square_sum(const Raw<Io<GDT>::kBytes>& raw) {
-  F2 g[4], two = f2_both(0.0f);
+__device__ __forceinline__ float square_sum(const Raw<Io<GDT>::kBytes>& raw, double& wide) {
+  F2 g[4];
   raw.get(g);
-  float top = 0.0f;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    two = f2_fma(g[i], g[i], two);
-    float lo, hi;
-    f2_unpack(g[i], lo, hi);
-    top = fmaxf(top, fmaxf(fabsf(lo), fabsf(hi)));
-  }
   float x, y;
-  f2_unpack(two, x, y);
-  if (top == 0.0f || (top >= 9.094947e-13f && top <= 1.1258999e15f)) return (double)(x + y);
-  double d = 0.0;
+  f2_unpack(f2_add(f2_fma(g[0], g[0], f2_mul(g[1], g[1])), f2_fma(g[2], g[2], f2_mul(g[3], g[3]))), x, y);
+  const float s = x + y;
+  if (s >= 8.271806e-25f && s <= 1.2676506e30f) return s;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     f2_unpack(g[i], x, y);
-    d = fma((double)x, (double)x, fma((double)y, (double)y, d));
+    wide = fma((double)x, (double)x, fma((double)y, (double)y, wide));
   }
-  return d;
+  return 0.0f;
 }
 
+constexpr uint32_t kAhead = 4;  // blocks in flight
+
 template <int GDT>
-__global__ void __launch_bounds__(kStepThreads, 4) grad_norm_kernel(const __grid_constant__ StepArgs a, double* partials) {
-  __shared__ double buf[kStepWarps];
+__global__ void __launch_bounds__(kNormThreads, 4) grad_norm_kernel(const __grid_constant__ StepArgs a, double* partials) {
+  __shared__ double buf[kNormWarps];
   constexpr int ES = Io<GDT>::kBytes;
+  constexpr bool QUAD = ES == 4;
   enter_grid();
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
   double sum = 0.0;
-  for (uint64_t c = (uint64_t)blockIdx.x * kStepWarps + warp; c < a.n_chunks; c += (uint64_t)gridDim.x * kStepWarps) {
+  const uint32_t blocks = a.chunk_blocks;
+  for (uint64_t c = (uint64_t)blockIdx.x * kNormWarps + warp; c < a.n_chunks; c += (uint64_t)gridDim.x * kNormWarps) {
     const StepTensor& tensor = a.tensors[a.owner[c]];
     const void* const grad = tensor.g;
-    const uint64_t n = tensor.n, from = (c - tensor.chunk0) * kStepChunk;
+    const uint64_t from = (c - tensor.chunk0) * blocks * kStepBlock;
     const bool vec = tensor.head != kStepScalar;
     const uint32_t head = vec ? tensor.head : 0u;
-    Raw<ES> raw[kChunkBlocks];
-#pragma unroll
-    for (uint32_t i = 0; i < kChunkBlocks; ++i) {
-      const uint64_t first = head + from + (uint64_t)i * kStepBlock + 4 * lane;
-      raw[i].load(grad, Spot<true>{first, first >= n ? 0 : (n - first < 256 ? (int32_t)(n - first) : 256)}, vec);
-    }
-    if (head && from == 0) {
+    const uint64_t base = head + from + (QUAD ? 4 : 8) * lane, end = head + from + (uint64_t)blocks * kStepBlock;
+    const uint64_t n = tensor.n < end ? tensor.n : end;  // where the chunk ends
+    if (head && from == 0) {  // the elements before the grid
       const uint64_t before = n < head ? n : head;
       Raw<ES> front;
       front.load(grad, Spot<true>{4 * lane, (int32_t)(before > 4 * lane ? (before - 4 * lane < 4 ? before - 4 * lane : 4) : 0)}, false);
-      sum += square_sum<GDT>(front);
+      const float s = square_sum<GDT>(front, sum);
+      sum += (double)s;
     }
+#pragma unroll 1
+    for (uint32_t k = 0; k < blocks; k += kAhead) {
+      if (head + from + k * kStepBlock >= n) break;
+      Raw<ES> raw[kAhead];
+      if (vec && head + from + (k + kAhead) * kStepBlock <= n) {
 #pragma unroll
-    for (uint32_t i = 0; i < kChunkBlocks; ++i) sum += square_sum<GDT>(raw[i]);
+        for (uint32_t i = 0; i < kAhead; ++i) raw[i].load(grad, Spot<QUAD, true>{base + (k + i) * kStepBlock, 256}, true);
+      } else {
+#pragma unroll
+        for (uint32_t i = 0; i < kAhead; ++i) {
+          const uint64_t first = base + (k + i) * kStepBlock;
+          raw[i].load(grad, Spot<QUAD>{first, first >= n ? 0 : (n - first < 256 ? (int32_t)(n - first) : 256)}, vec);
+        }
+      }
+      float s = 0.0f;
+#pragma unroll
+      for (uint32_t i = 0; i < kAhead; ++i) s += square_sum<GDT>(raw[i], sum);
+      sum += (double)s;  // of 32 elements, each eight from 2^-80 to 2^100
+    }
   }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
@@ -488,24 +547,30 @@ __global__ void __launch_bounds__(kStepThreads, 4) grad_norm_kernel(const __grid
   __syncthreads();
   if (threadIdx.x == 0) {
 #pragma unroll
-    for (int w = 1; w < kStepWarps; ++w) sum += buf[w];
+    for (int w = 1; w < kNormWarps; ++w) sum += buf[w];
     partials[blockIdx.x] = sum;
   }
 }
 
-__global__ void __launch_bounds__(1024) grad_norm_finish_kernel(const double* partials, uint32_t n, const float* control, float max_norm,
+constexpr int kFinishThreads = 256;
+
+__global__ void __launch_bounds__(kFinishThreads) grad_norm_finish_kernel(const double* partials, uint32_t n, const float* control, float max_norm,
                                                                 float* out) {
-  __shared__ double buf[32];
+  __shared__ double buf[kFinishThreads / 32];
   enter_grid();
   double sum = 0.0;
-  for (uint32_t i = threadIdx.x; i < n; i += 1024) sum += partials[i];
+#pragma unroll
+  for (int i = 0; i < (kMaxNormCtas + kFinishThreads - 1) / kFinishThreads; ++i) {
+    const uint32_t at = threadIdx.x + i * kFinishThreads;
+    if (at < n) sum += partials[at];
+  }
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (threadIdx.x % 32 == 0) buf[threadIdx.x / 32] = sum;
   __syncthreads();
   if (threadIdx.x == 0) {
 #pragma unroll
-    for (int w = 1; w < 32; ++w) sum += buf[w];
+    for (int w = 1; w < kFinishThreads / 32; ++w) sum += buf[w];
     const double norm = sqrt(sum) * fabs((double)control[2]);
     const double factor = (double)max_norm / (norm + 1e-6);
     out[0] = (float)norm;
@@ -524,28 +589,29 @@ cudaError_t launch_adamw_types(int bits, const StepArgs& a, unsigned grid, cudaS
 
 }  // namespace
 
-cudaError_t launch_adamw(int pdt, int gdt, int state_bits, StepArgs a, cudaStream_t st) {
+cudaError_t launch_adamw(int pdt, int gdt, int state_bits, const StepArgs& a, cudaStream_t st) {
   if (a.n_chunks == 0) return cudaSuccess;
-  const uint64_t resident = (uint64_t)sm_count() * (state_bits == 8 ? 3 : 2);  // CTAs at once
-  a.split = (uint64_t)a.n_chunks * kChunkBlocks <= resident * kStepWarps ? kChunkBlocks : 1;
-  const uint64_t want = ((uint64_t)a.n_chunks * a.split + kStepWarps - 1) / kStepWarps, cap = resident * 4;
+  const uint64_t resident = (uint64_t)sm_count() * (state_bits == 8 ? kStepCtas<8> : kStepCtas<32>);  // CTAs at once
+  // four times as many CTAs as fit: the last ones even out what the SMs have left
+  const uint64_t want = ((uint64_t)a.n_chunks + kStepWarps - 1) / kStepWarps, cap = resident * 4;
   const unsigned grid = (unsigned)(want < cap ? want : cap);
   if (pdt == kF32)
     return gdt == kF32 ? launch_adamw_types<kF32, kF32>(state_bits, a, grid, st) : launch_adamw_types<kF32, kBF16>(state_bits, a, grid, st);
   return gdt == kF32 ? launch_adamw_types<kBF16, kF32>(state_bits, a, grid, st) : launch_adamw_types<kBF16, kBF16>(state_bits, a, grid, st);
 }
 
+// As many CTAs as fit a B200 at most, whatever the device: the scratch is sized by them.
 uint64_t grad_norm_scratch_bytes(uint32_t n_chunks) {
-  const uint64_t want = ((uint64_t)n_chunks + kStepWarps - 1) / kStepWarps;
+  const uint64_t want = ((uint64_t)n_chunks + kNormWarps - 1) / kNormWarps;
   return (want < 1 ? 1 : (want < kMaxNormCtas ? want : kMaxNormCtas)) * sizeof(double);
 }
 
 cudaError_t launch_grad_norm(int gdt, const StepArgs& a, float max_norm, float* out, double* scratch, cudaStream_t st) {
   const unsigned grid = (unsigned)(grad_norm_scratch_bytes(a.n_chunks) / sizeof(double));
-  const cudaError_t e = gdt == kF32 ? launch_overlapped(grad_norm_kernel<kF32>, dim3(grid), kStepThreads, 0, st, a, scratch)
-                                    : launch_overlapped(grad_norm_kernel<kBF16>, dim3(grid), kStepThreads, 0, st, a, scratch);
+  const cudaError_t e = gdt == kF32 ? launch_overlapped(grad_norm_kernel<kF32>, dim3(grid), kNormThreads, 0, st, a, scratch)
+                                    : launch_overlapped(grad_norm_kernel<kBF16>, dim3(grid), kNormThreads, 0, st, a, scratch);
   if (e != cudaSuccess) return e;
-  return launch_overlapped(grad_norm_finish_kernel, dim3(1), 1024, 0, st, (const double*)scratch, grid, a.control, max_norm, out);
+  return launch_overlapped(grad_norm_finish_kernel, dim3(1), kFinishThreads, 0, st, (const double*)scratch, grid, a.control, max_norm, out);
 }
 
 }  // namespace s2a

@@ -179,7 +179,27 @@ struct Span {
   bool written;
 };
 
-size_t chunks_of(size_t n) { return (n + kStepChunk - 1) / kStepChunk; }
+size_t blocks_of(size_t n) { return (n + kStepBlock - 1) / kStepBlock; }
+
+// Blocks of a chunk: few where the plan is small, so that every warp gets one; many where every warp gets sixteen all the same, as
+// each chunk costs a look at the plan and a wait for its first block (302 M weights with 8-bit states: 680 us with 16 blocks, 771 with 4).
+size_t chunk_blocks_of(size_t blocks) {
+  const size_t warps = 148 * 20;
+  return blocks >= 256 * warps ? 16 : (blocks >= 16 * warps ? 4 : 1);
+}
+
+// The plan's chunks, and blocks of a chunk; 0 where there are too many.
+size_t count_chunks(const s2a_step_tensor* tensors, size_t n_tensors, size_t& chunk_blocks) {
+  size_t blocks = 0, chunks = 0;
+  for (size_t i = 0; i < n_tensors; ++i) {
+    if (tensors[i].n > kMaxExtent) return 0;
+    blocks += blocks_of(tensors[i].n);
+    if (blocks > ((size_t)1 << 40)) return 0;
+  }
+  chunk_blocks = chunk_blocks_of(blocks);
+  for (size_t i = 0; i < n_tensors; ++i) chunks += (blocks_of(tensors[i].n) + chunk_blocks - 1) / chunk_blocks;
+  return chunks > 0x7fffffffull ? 0 : chunks;
+}
 
 // Elements before the first that lies on the 16-byte grid in all of a tensor's parts, or kStepScalar.  Eight elements are whole
 // vectors in every type.
@@ -198,7 +218,7 @@ int bad_plan(const s2a_step_plan* plan, const void* image) {
   if (!plan) return S2A_ERR_NULL;
   if (plan->n_chunks && !image) return S2A_ERR_NULL;
   if (misaligned(image, 16)) return S2A_ERR_ALIGN;
-  if (plan->n_chunks > 0x7fffffffull || plan->n_tensors > 0x7fffffffull) return S2A_ERR_SHAPE;
+  if (plan->n_chunks > 0x7fffffffull || plan->n_tensors > 0x7fffffffull || plan->chunk_blocks > 16) return S2A_ERR_SHAPE;
   return S2A_OK;
 }
 
@@ -208,6 +228,7 @@ StepArgs step_args(const s2a_step_plan* plan, const void* image, const float* co
   a.owner = (const uint32_t*)((const char*)image + plan->n_tensors * sizeof(StepTensor));
   a.n_tensors = (uint32_t)plan->n_tensors;
   a.n_chunks = (uint32_t)plan->n_chunks;
+  a.chunk_blocks = (uint32_t)plan->chunk_blocks;
   a.control = control;
   return a;
 }
@@ -243,13 +264,8 @@ int s2a_rope_table(uint64_t* table, size_t rot_dim, double base, int scaling, do
 
 size_t s2a_step_plan_bytes(const s2a_step_tensor* tensors, size_t n_tensors) {
   if (!tensors || n_tensors > 0x7fffffffull) return 0;
-  size_t chunks = 0;
-  for (size_t i = 0; i < n_tensors; ++i) {
-    if (tensors[i].n > kMaxExtent) return 0;
-    chunks += chunks_of(tensors[i].n);
-    if (chunks > 0x7fffffffull) return 0;
-  }
-  return n_tensors * sizeof(StepTensor) + chunks * sizeof(uint32_t);
+  size_t chunk_blocks;
+  return n_tensors * sizeof(StepTensor) + count_chunks(tensors, n_tensors, chunk_blocks) * sizeof(uint32_t);
 }
 
 int s2a_step_plan_fill(const s2a_step_tensor* tensors, size_t n_tensors, int pdt, int gdt, int state_bits, void* image,
@@ -260,7 +276,9 @@ int s2a_step_plan_fill(const s2a_step_tensor* tensors, size_t n_tensors, int pdt
   for (size_t i = 0; i < n_tensors; ++i) grads_only = grads_only && !tensors[i].param;
   if (bad_dtype(gdt) || (!grads_only && bad_dtype(pdt))) return S2A_ERR_DTYPE;
   if (!grads_only && state_bits != 8 && state_bits != 32) return S2A_ERR_VALUE;
-  if (n_tensors && s2a_step_plan_bytes(tensors, n_tensors) == 0) return S2A_ERR_SHAPE;
+  size_t chunk_blocks = 1, elems = 0;
+  for (size_t i = 0; i < n_tensors; ++i) elems |= tensors[i].n;
+  if (count_chunks(tensors, n_tensors, chunk_blocks) == 0 && elems) return S2A_ERR_SHAPE;
   if (misaligned(image, 16)) return S2A_ERR_ALIGN;
   const size_t ps = elem_bytes(pdt), gs = elem_bytes(gdt), ss = state_bits == 8 ? 1 : 4;
   for (size_t i = 0; i < n_tensors; ++i) {
@@ -285,7 +303,7 @@ int s2a_step_plan_fill(const s2a_step_tensor* tensors, size_t n_tensors, int pdt
     };
     for (size_t i = 0; i < n_tensors; ++i) {
       const s2a_step_tensor& t = tensors[i];
-      const size_t blocks = (t.n + kStepBlock - 1) / kStepBlock;
+      const size_t blocks = blocks_of(t.n);
       add(t.param, t.n * ps, true);
       add(t.grad, t.n * gs, false);
       add(t.exp_avg, t.n * ss, true);
@@ -334,12 +352,13 @@ int s2a_step_plan_fill(const s2a_step_tensor* tensors, size_t n_tensors, int pdt
         o.v_scale = t.exp_avg_sq_scale;
       }
     }
-    block += (t.n + kStepBlock - 1) / kStepBlock;
-    for (size_t c = chunks_of(t.n); c > 0; --c) owner[chunk++] = (uint32_t)i;
+    block += blocks_of(t.n);
+    for (size_t c = (blocks_of(t.n) + chunk_blocks - 1) / chunk_blocks; c > 0; --c) owner[chunk++] = (uint32_t)i;
   }
   plan->bytes = n_tensors * sizeof(StepTensor) + (size_t)chunk * sizeof(uint32_t);
   plan->n_tensors = n_tensors;
   plan->n_chunks = chunk;
+  plan->chunk_blocks = chunk_blocks;
   plan->pdt = pdt;
   plan->gdt = gdt;
   plan->state_bits = state_bits;

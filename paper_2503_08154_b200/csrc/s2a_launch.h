@@ -122,7 +122,6 @@ void rope_table(uint64_t* out, uint32_t pairs, double base, int scaling, double 
 // The AdamW step and the norm of all gradients, over the tensors of a plan: an image in device memory of `n_tensors`
 // StepTensor and, after them, the tensor of each chunk (uint32_t).
 constexpr uint32_t kStepBlock = 256;                 // elements under one scale of 8-bit states
-constexpr uint32_t kStepChunk = 4 * kStepBlock;      // what a warp takes at a time
 constexpr int kMaxNormCtas = 148 * 4;
 struct StepTensor {
   void* p;
@@ -150,9 +149,9 @@ struct StepArgs {
   const uint64_t* rng;    // seed and offset, or NULL: round to nearest
   uint64_t site;
   float beta1, one_beta1, beta2, root_beta2, root_one_beta2, log_beta1, log_beta2, eps;  // root: sqrt(beta2), sqrt(1 - beta2)
-  uint32_t split;         // parts of a chunk, set by launch_adamw
+  uint32_t chunk_blocks;  // blocks of a chunk, which a warp takes at a time: 1, 4 or 16
 };
-cudaError_t launch_adamw(int pdt, int gdt, int state_bits, StepArgs a, cudaStream_t st);
+cudaError_t launch_adamw(int pdt, int gdt, int state_bits, const StepArgs& a, cudaStream_t st);
 uint64_t grad_norm_scratch_bytes(uint32_t n_chunks);
 cudaError_t launch_grad_norm(int gdt, const StepArgs& a, float max_norm, float* out, double* scratch, cudaStream_t st);
 

@@ -21,16 +21,18 @@ struct PhiloxKey {
   }
 };
 
+__device__ __forceinline__ void philox_round(uint32_t& c0, uint32_t& c1, uint32_t& c2, uint32_t& c3, uint32_t k0, uint32_t k1) {
+  const uint64_t p0 = (uint64_t)c0 * 0xD2511F53u, p1 = (uint64_t)c2 * 0xCD9E8D57u;
+  c0 = (uint32_t)(p1 >> 32) ^ c1 ^ k0;
+  c1 = (uint32_t)p1;
+  c2 = (uint32_t)(p0 >> 32) ^ c3 ^ k1;
+  c3 = (uint32_t)p0;
+}
+
 __device__ __forceinline__ uint4 philox(const PhiloxKey& key, uint64_t block, uint64_t count) {
   uint32_t c0 = (uint32_t)block, c1 = (uint32_t)(block >> 32), c2 = (uint32_t)count, c3 = (uint32_t)(count >> 32);
 #pragma unroll
-  for (int i = 0; i < 10; ++i) {
-    const uint64_t p0 = (uint64_t)c0 * 0xD2511F53u, p1 = (uint64_t)c2 * 0xCD9E8D57u;
-    c0 = (uint32_t)(p1 >> 32) ^ c1 ^ key.k0[i];
-    c1 = (uint32_t)p1;
-    c2 = (uint32_t)(p0 >> 32) ^ c3 ^ key.k1[i];
-    c3 = (uint32_t)p0;
-  }
+  for (int i = 0; i < 10; ++i) philox_round(c0, c1, c2, c3, key.k0[i], key.k1[i]);
   return make_uint4(c0, c1, c2, c3);
 }
 
