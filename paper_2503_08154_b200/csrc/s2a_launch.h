@@ -110,6 +110,8 @@ struct RopeArgs {
   uint32_t heads[2];
   uint32_t batch, tokens, head_dim, pairs, axes;
   uint32_t ctas0, share[2], more[2];                 // CTAs of queries; groups of rows a warp, and how many warps have one more
+  uint32_t group_tokens[2], step_b[2], step_t[2];    // tokens of a group, and what they are in sequences and places
+  uint32_t pairs_inverse;                            // 2^20 / pairs, rounded up
   uint32_t lanes, rows_per_warp, slots, turn_slots;  // lanes and slots of a row (slots: see the kernels), turning slots
   int interleaved, back, wdt;
   float scale, eps, inv_dim;

@@ -9,8 +9,12 @@
 
 namespace s2a {
 
+// s2a_rope.cuh: rows of 64, 128 or 256 elements that turn as a whole, on the 16-byte grid; and any others (MULTI: tokens with fewer rows than
+// a group has)
 template <int DT>
-cudaError_t launch_rope_kernel(int mode, uint32_t V, const RopeArgs& a, unsigned grid, cudaStream_t st);  // s2a_rope.cuh
+cudaError_t launch_rope_whole(int mode, const RopeArgs& a, unsigned grid, cudaStream_t st);
+template <int DT, bool MULTI>
+cudaError_t launch_rope_any(int mode, uint32_t V, uint32_t W, const RopeArgs& a, unsigned grid, cudaStream_t st);
 
 namespace {
 
@@ -61,50 +65,72 @@ cudaError_t launch_rope(int mode, int dt, RopeArgs a, void* grad_gamma_q, void* 
     return sums && grad_gamma_k ? cudaMemsetAsync(grad_gamma_k, 0, bytes, st) : cudaSuccess;
   }
   const uint32_t es = dt == kF32 ? 4u : 2u;
-  // the widest vector that divides the turning half, the rest of the row, and every address
-  uint32_t V = 16 / es;
-  for (; V > 1; V /= 2) {
-    bool ok = a.pairs % V == 0 && (a.head_dim - 2 * a.pairs) % V == 0;
+  // W: the widest vector that divides a row and every address.  V: the widest within it that divides what turns and what does not: in the
+  // layout of halves the half that turns and the rest, interleaved (where pairs lie within vectors) all that turns.
+  const uint32_t widest = 16 / es;
+  uint32_t W = widest;
+  for (; W > 1; W /= 2) {
+    bool ok = a.head_dim % W == 0;
     for (int i = 0; i < 2 && ok; ++i)
-      ok = fits(a.in[i], a.heads[i], es, V * es) && fits(a.grad[i], a.heads[i], es, V * es) && fits(a.out[i], a.heads[i], es, V * es);
+      ok = fits(a.in[i], a.heads[i], es, W * es) && fits(a.grad[i], a.heads[i], es, W * es) && fits(a.out[i], a.heads[i], es, W * es);
     if (ok) break;
   }
+  uint32_t V = W;
+  while (V > 1 && (a.interleaved ? (2 * a.pairs) % V : a.pairs % V || (a.head_dim - 2 * a.pairs) % V)) V /= 2;
+  if (W != widest) W = V = V > 2 ? 2 : V;
   const uint32_t K = kLaneElems / (2 * V);
+  const bool inside = a.interleaved && V > 1;  // pairs within vectors
   a.turn_slots = a.pairs / V;
-  a.slots = a.turn_slots + (a.head_dim - 2 * a.pairs + 2 * V - 1) / (2 * V);
+  a.slots = inside ? (a.head_dim / V + 1) / 2 : a.turn_slots + (a.head_dim - 2 * a.pairs + 2 * V - 1) / (2 * V);
   a.lanes = (a.slots + K - 1) / K;
   a.rows_per_warp = 32 / a.lanes;
   a.inv_dim = 1.0f / (float)a.head_dim;
-  // A warp each for the groups of rows of all tokens, until the GPU is full; then shares.
-  const auto groups_of = [&](uint32_t rows) { return (rows + a.rows_per_warp - 1) / a.rows_per_warp; };
-  const auto cut = [&](uint32_t rows, uint32_t ctas, int which) {
-    const uint64_t items = tokens * groups_of(rows), warps = (uint64_t)ctas * kWarps;
-    a.share[which] = (uint32_t)(items / warps);
-    a.more[which] = (uint32_t)(items % warps);
+  a.pairs_inverse = a.pairs ? (1048576u + a.pairs - 1) / a.pairs : 0u;
+  // A group is rows of one token; or, where the tokens of some kind have fewer than a group's rows, those of several tokens.
+  const auto few = [&](uint32_t rows) { return rows != 0 && 2 * rows <= a.rows_per_warp; };
+  const bool multi = mode == kRopeBwdNorm ? few(a.heads[0]) || few(a.heads[1]) : few(heads);
+  // A warp each for the groups, until the GPU is full; then shares.  `which`: the forward kernels (and queries), keys.
+  uint64_t items[2] = {0, 0};
+  const auto group = [&](uint32_t rows, int which) {
+    a.group_tokens[which] = multi && few(rows) ? a.rows_per_warp / rows : 1;
+    a.step_b[which] = a.group_tokens[which] % a.batch;
+    a.step_t[which] = a.group_tokens[which] / a.batch;
+    items[which] = a.group_tokens[which] > 1 ? (tokens + a.group_tokens[which] - 1) / a.group_tokens[which]
+                                             : tokens * ((rows + a.rows_per_warp - 1) / a.rows_per_warp);
   };
-  const auto ctas_for = [&](uint64_t items, uint64_t cap) { return (uint32_t)std::min<uint64_t>((items + kWarps - 1) / kWarps, cap); };
-  if (tokens * (groups_of(a.heads[0]) + groups_of(a.heads[1])) >> 32) return cudaErrorInvalidValue;  // more than any memory holds
+  const auto cut = [&](uint32_t ctas, int which) {
+    const uint64_t warps = (uint64_t)ctas * kWarps;
+    a.share[which] = (uint32_t)(items[which] / warps);
+    a.more[which] = (uint32_t)(items[which] % warps);
+  };
+  const auto ctas_for = [&](uint64_t n, uint64_t cap) { return (uint32_t)std::min<uint64_t>((n + kWarps - 1) / kWarps, cap); };
   unsigned grid;
   if (mode == kRopeBwdNorm) {
-    const uint64_t items0 = tokens * groups_of(a.heads[0]), items1 = tokens * groups_of(a.heads[1]);
-    const uint64_t cap = 148 * 2, share0 = cap * items0 / (items0 + items1);
-    a.ctas0 = items0 ? ctas_for(items0, items1 ? std::min(std::max<uint64_t>(share0, 1), cap - 1) : cap) : 0;
-    const uint32_t ctas1 = items1 ? ctas_for(items1, cap - a.ctas0) : 0;
+    group(a.heads[0], 0);
+    group(a.heads[1], 1);
+    const uint64_t cap = 148 * 2, share0 = cap * items[0] / (items[0] + items[1]);
+    a.ctas0 = items[0] ? ctas_for(items[0], items[1] ? std::min(std::max<uint64_t>(share0, 1), cap - 1) : cap) : 0;
+    const uint32_t ctas1 = items[1] ? ctas_for(items[1], cap - a.ctas0) : 0;
     grid = a.ctas0 + ctas1;
-    if (items0) cut(a.heads[0], a.ctas0, 0);
-    if (items1) cut(a.heads[1], ctas1, 1);
+    if (items[0]) cut(a.ctas0, 0);
+    if (items[1]) cut(ctas1, 1);
     a.partials = sums ? scratch : nullptr;
   } else {
-    grid = ctas_for(tokens * groups_of(heads), (uint64_t)sm_count() * 3);
-    cut(heads, grid, 0);
+    group(heads, 0);
+    grid = ctas_for(items[0], (uint64_t)sm_count() * (multi ? 2 : 3));
+    cut(grid, 0);
   }
+  if ((items[0] | items[1]) >> 32) return cudaErrorInvalidValue;  // more rows than any memory holds
   // from here on strides are in bytes
   for (HeadsArg* h : {&a.in[0], &a.in[1], &a.grad[0], &a.grad[1], &a.out[0], &a.out[1]}) {
     h->batch *= es;
     h->token *= es;
     h->head *= es;
   }
-  const cudaError_t e = dt == kF32 ? launch_rope_kernel<kF32>(mode, V, a, grid, st) : launch_rope_kernel<kBF16>(mode, V, a, grid, st);
+  const bool whole = !multi && V == widest && 2 * a.pairs == a.head_dim && (a.head_dim == 64 || a.head_dim == 128 || a.head_dim == 256);
+  const cudaError_t e = whole ? (dt == kF32 ? launch_rope_whole<kF32>(mode, a, grid, st) : launch_rope_whole<kBF16>(mode, a, grid, st))
+                        : multi ? (dt == kF32 ? launch_rope_any<kF32, true>(mode, V, W, a, grid, st) : launch_rope_any<kBF16, true>(mode, V, W, a, grid, st))
+                                : (dt == kF32 ? launch_rope_any<kF32, false>(mode, V, W, a, grid, st) : launch_rope_any<kBF16, false>(mode, V, W, a, grid, st));
   if (e != cudaSuccess || !sums) return e;
   return launch_overlapped(qknorm_reduce_kernel, dim3((a.head_dim + 31) / 32, 2), 1024, 0, st, scratch, a.ctas0, grid, a.head_dim,
                            grad_gamma_q, grad_gamma_k, a.wdt);
