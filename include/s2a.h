@@ -401,6 +401,7 @@ int s2a_relbias_log_buckets(int32_t* buckets, int64_t first_distance, size_t cou
  *            ignored) for a norm without rotation.  Pairs are (i, i + rot_dim / 2), or (2 i, 2 i + 1) where `interleaved`.
  *   scale    multiplies the cosines and sines (1 but for some scaled contexts): finite
  *   gamma_*  head_dim elements of type wdt, or NULL (ones)
+ * No other argument may overlap an output (not checked).
  * head_dim: 1 .. 512; axes: 1 .. 4; heads: at most 65535 each, less than 2^32 elements from head to head; batch * tokens at
  * most 2^31-1.
  */
@@ -432,7 +433,7 @@ int s2a_rope_bwd(const s2a_rope_args* args, void* cuda_stream);
 int s2a_qknorm_rope_fwd(const s2a_rope_args* args, void* cuda_stream);
 
 /* Bytes of scratch for the weights' gradients of s2a_qknorm_rope_bwd (0 where head_dim is 0 or above 512): the same
- * for every batch and number of tokens, at most 889 * head_dim * 4. */
+ * for every batch and number of tokens, 296 * head_dim * 4. */
 size_t s2a_qknorm_rope_scratch_bytes(size_t batch, size_t tokens, size_t heads_q, size_t heads_k, size_t head_dim);
 
 /* Its backward pass, from x alone (the inputs q and k of the forward call; rstd is computed again).  With u = the gradient turned

@@ -781,7 +781,7 @@ def adamw_plan(params, grads, exp_avgs, exp_avg_sqs, exp_avg_scales=None, exp_av
 
     def address(t, n, what, dtype=None):
         nonlocal dev
-        if not t.is_cuda or (dev is not None and t.get_device() != dev):
+        if not isinstance(t, torch.Tensor) or not t.is_cuda or (dev is not None and t.get_device() != dev):
             raise S2AError("%s must be CUDA tensors of one device" % what)
         if not t.is_contiguous() or t.numel() != n or (dtype is not None and t.dtype is not dtype):
             raise S2AError("%s must be contiguous, of the right size%s" % (what, "" if dtype is None else " and %s" % dtype))
@@ -789,6 +789,8 @@ def adamw_plan(params, grads, exp_avgs, exp_avg_sqs, exp_avg_scales=None, exp_av
         return t.data_ptr()
 
     for i in range(count):
+        if not isinstance(grads[i], torch.Tensor):
+            raise S2AError("gradients must be CUDA tensors of one device")
         r, n = records[i], grads[i].numel()
         r.n, r.weight_decay, r.lr_scale = n, decays[i], rates[i]
         r.grad = address(grads[i], n, "gradients")

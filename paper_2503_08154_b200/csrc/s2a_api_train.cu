@@ -181,11 +181,12 @@ struct Span {
 
 size_t blocks_of(size_t n) { return (n + kStepBlock - 1) / kStepBlock; }
 
-// Blocks of a chunk: few where the plan is small, so that every warp gets one; many where every warp gets sixteen all the same, as
-// each chunk costs a look at the plan and a wait for its first block (302 M weights with 8-bit states: 680 us with 16 blocks, 771 with 4).
+// Blocks of a chunk: one where the plan is small, so that every warp gets one; four where every warp gets a chunk all the same, and sixteen where it
+// gets sixteen, as each chunk costs a look at the plan and a wait for its first block (302 M weights with 8-bit states: 680 us with 16 blocks,
+// 771 with 4).
 size_t chunk_blocks_of(size_t blocks) {
   const size_t warps = 148 * 20;
-  return blocks >= 256 * warps ? 16 : (blocks >= 16 * warps ? 4 : 1);
+  return blocks >= 256 * warps ? 16 : (blocks >= 4 * warps ? 4 : 1);
 }
 
 // The plan's chunks, and blocks of a chunk; 0 where there are too many.

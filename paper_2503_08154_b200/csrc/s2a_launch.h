@@ -92,7 +92,7 @@ void log_buckets(int32_t* out, int64_t first, uint64_t count, uint32_t n_buckets
 // elements; index 0 stands for queries and 1 for keys, and heads[1] may be 0.
 constexpr uint32_t kMaxHeadDim = 512;
 constexpr uint32_t kMaxAxes = 4;                    // a token's positions fit 16 bytes
-constexpr uint32_t kMaxRopePartials = 148 * 6 + 1;  // rows of scratch at most
+constexpr uint32_t kMaxRopePartials = 148 * 2;      // CTAs of the norm's backward pass at most: rows of scratch
 enum { kRopePlain = 0, kRopeFwdNorm = 1, kRopeBwdNorm = 2 };
 enum { kRopeScaleNone = 0, kRopeScaleLinear = 1, kRopeScaleBase = 2, kRopeScaleParts = 3 };
 struct HeadsArg {

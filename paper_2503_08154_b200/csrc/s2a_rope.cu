@@ -21,23 +21,30 @@ namespace {
 constexpr int kWarps = 8;         // as in the kernels
 constexpr int kLaneElems = 16;
 
-// grad_gamma of queries (blockIdx.y = 0) and keys: the CTAs' partial rows added in a fixed order, a column a lane.
-__global__ void __launch_bounds__(1024) qknorm_reduce_kernel(const float* partials, uint32_t ctas0, uint32_t ctas, uint32_t D,
-                                                             void* gq, void* gk, int wdt) {
-  __shared__ float buf[32][33];
+// grad_gamma of queries (blockIdx.y = 0) and keys: the CTAs' partial rows added in a fixed order, a column a lane, a warp's share of the rows
+// in flight at once.
+constexpr int kReduceWarps = 16;
+constexpr int kReduceRows = (kMaxRopePartials + kReduceWarps - 1) / kReduceWarps;  // of a warp
+
+__global__ void __launch_bounds__(kReduceWarps * 32) qknorm_reduce_kernel(const float* partials, uint32_t ctas0, uint32_t ctas, uint32_t D,
+                                                                         void* gq, void* gk, int wdt) {
+  __shared__ float buf[kReduceWarps][33];
   enter_grid();
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, d = blockIdx.x * 32 + lane;
   const uint32_t from = blockIdx.y ? ctas0 : 0, to = blockIdx.y ? ctas : ctas0;
   void* out = blockIdx.y ? gk : gq;
   float s = 0.0f;
-  if (d < D)
-    for (uint32_t r = from + warp; r < to; r += 32) s += partials[(uint64_t)r * D + d];
+#pragma unroll
+  for (int i = 0; i < kReduceRows; ++i) {
+    const uint32_t r = from + warp + i * kReduceWarps;
+    if (d < D && r < to) s += partials[(uint64_t)r * D + d];
+  }
   buf[warp][lane] = s;
   __syncthreads();
   if (warp == 0 && d < D && out) {
     s = 0.0f;
 #pragma unroll
-    for (int w = 0; w < 32; ++w) s += buf[w][lane];
+    for (int w = 0; w < kReduceWarps; ++w) s += buf[w][lane];
     store_param(out, d, wdt, s);
   }
 }
@@ -108,7 +115,7 @@ cudaError_t launch_rope(int mode, int dt, RopeArgs a, void* grad_gamma_q, void* 
   if (mode == kRopeBwdNorm) {
     group(a.heads[0], 0);
     group(a.heads[1], 1);
-    const uint64_t cap = 148 * 2, share0 = cap * items[0] / (items[0] + items[1]);
+    const uint64_t cap = kMaxRopePartials, share0 = cap * items[0] / (items[0] + items[1]);
     a.ctas0 = items[0] ? ctas_for(items[0], items[1] ? std::min(std::max<uint64_t>(share0, 1), cap - 1) : cap) : 0;
     const uint32_t ctas1 = items[1] ? ctas_for(items[1], cap - a.ctas0) : 0;
     grid = a.ctas0 + ctas1;
@@ -132,7 +139,7 @@ cudaError_t launch_rope(int mode, int dt, RopeArgs a, void* grad_gamma_q, void* 
                         : multi ? (dt == kF32 ? launch_rope_any<kF32, true>(mode, V, W, a, grid, st) : launch_rope_any<kBF16, true>(mode, V, W, a, grid, st))
                                 : (dt == kF32 ? launch_rope_any<kF32, false>(mode, V, W, a, grid, st) : launch_rope_any<kBF16, false>(mode, V, W, a, grid, st));
   if (e != cudaSuccess || !sums) return e;
-  return launch_overlapped(qknorm_reduce_kernel, dim3((a.head_dim + 31) / 32, 2), 1024, 0, st, scratch, a.ctas0, grid, a.head_dim,
+  return launch_overlapped(qknorm_reduce_kernel, dim3((a.head_dim + 31) / 32, 2), kReduceWarps * 32, 0, st, scratch, a.ctas0, grid, a.head_dim,
                            grad_gamma_q, grad_gamma_k, a.wdt);
 }
 

@@ -10,7 +10,7 @@ Tolerances, with u = 2^-24 (half a step of binary32) and h the half step of the 
 * backward: u' = the gradient turned back (d), a = u' gamma: d |gamma| + u |a|; the mean of a xhat: (sum |da| |x| + 23 u
   sum |a x|) rstd / D + 15 u of itself; grad = (a - xhat mean) rstd with 14 u of it for rstd and 18 u of xhat mean.
 * grad_gamma: terms u' xhat are off by d |xhat| + 17 u |u' xhat|; a term passes through at most as many additions as a
-  lane has rows, at most the rows over 32 / lanes, then 256 and 889 partials over 32, and 32.
+  lane has rows, fewer than the rows over 32 / lanes at these sizes, then 256 in a CTA, 19 of the CTAs and 16 warps.
 Results below the normal range may be flushed: + 2^-126.
 """
 import math
