@@ -639,8 +639,10 @@ def _rope(call, q, k, out_q, out_k, positions, table, scale, interleaved, first,
         raise S2AError("queries and keys must be [batch, tokens, heads, head_dim]")
     batch, tokens, heads_q, dim = shape
     a, b = _heads(q, shape, dtype, "q"), _heads(out_q, shape, dtype, "the queries' output")
-    e = _heads(grad_q, shape, dtype, "grad_q") if grad_q is not None else _NONE
-    c, d, f, heads_k = _NONE, _NONE, _NONE, 0
+    c, d, e, f, heads_k = _NONE, _NONE, _NONE, _NONE, 0
+    k_at = out_k_at = grad_q_at = grad_k_at = 0
+    if grad_q is not None:
+        e, grad_q_at = _heads(grad_q, shape, dtype, "grad_q"), grad_q.data_ptr()
     if k is not None:
         other = k.shape
         if len(other) != 4 or other[0] != batch or other[1] != tokens or other[3] != dim:
@@ -648,9 +650,9 @@ def _rope(call, q, k, out_q, out_k, positions, table, scale, interleaved, first,
         if out_k is None or (grad_q is not None and grad_k is None):
             raise S2AError("the keys' tensors are needed")
         heads_k = other[2]
-        c, d = _heads(k, other, dtype, "k"), _heads(out_k, other, dtype, "the keys' output")
+        c, d, k_at, out_k_at = _heads(k, other, dtype, "k"), _heads(out_k, other, dtype, "the keys' output"), k.data_ptr(), out_k.data_ptr()
         if grad_k is not None:
-            f = _heads(grad_k, other, dtype, "grad_k")
+            f, grad_k_at = _heads(grad_k, other, dtype, "grad_k"), grad_k.data_ptr()
     rot = where = pos = per_batch = per_axis = 0
     axes = 1
     if table is not None:
@@ -673,8 +675,7 @@ def _rope(call, q, k, out_q, out_k, positions, table, scale, interleaved, first,
     code = _CODES.get(dtype)
     try:
         packed = _rope_args(
-            q.data_ptr(), _address(k), out_q.data_ptr(), _address(out_k), pos, where, gamma_q, gamma_k, _address(grad_q),
-            _address(grad_k), sum_q, sum_k, scratch, first, per_batch, per_axis, axes, batch, tokens, heads_q, heads_k, dim, rot, a[0],
+            q.data_ptr(), k_at, out_q.data_ptr(), out_k_at, pos, where, gamma_q, gamma_k, grad_q_at, grad_k_at, sum_q, sum_k, scratch, first, per_batch, per_axis, axes, batch, tokens, heads_q, heads_k, dim, rot, a[0],
             a[1], a[2], c[0], c[1], c[2], b[0], b[1], b[2], d[0], d[1], d[2], e[0], e[1], e[2], f[0], f[1], f[2], scale, eps, interleaved,
             dtype_code(q) if code is None else code, wdt)
     except (struct.error, OverflowError) as error:

@@ -9,7 +9,7 @@
 
 namespace s2a {
 
-// s2a_rope.cuh: rows of 64, 128 or 256 elements that turn as a whole, on the 16-byte grid; and any others (MULTI: tokens with fewer rows than
+// s2a_rope.cuh: rows of 32, 64, 96, 128, 160, 192 or 256 elements that turn as a whole, on the 16-byte grid; and any others (MULTI: tokens with fewer rows than
 // a group has)
 template <int DT>
 cudaError_t launch_rope_whole(int mode, const RopeArgs& a, unsigned grid, cudaStream_t st);
@@ -134,7 +134,7 @@ cudaError_t launch_rope(int mode, int dt, RopeArgs a, void* grad_gamma_q, void* 
     h->token *= es;
     h->head *= es;
   }
-  const bool whole = !multi && V == widest && 2 * a.pairs == a.head_dim && (a.head_dim == 64 || a.head_dim == 128 || a.head_dim == 256);
+  const bool whole = !multi && V == widest && 2 * a.pairs == a.head_dim && a.head_dim % 32 == 0 && a.head_dim <= 256 && a.head_dim != 224;
   const cudaError_t e = whole ? (dt == kF32 ? launch_rope_whole<kF32>(mode, a, grid, st) : launch_rope_whole<kBF16>(mode, a, grid, st))
                         : multi ? (dt == kF32 ? launch_rope_any<kF32, true>(mode, V, W, a, grid, st) : launch_rope_any<kBF16, true>(mode, V, W, a, grid, st))
                                 : (dt == kF32 ? launch_rope_any<kF32, false>(mode, V, W, a, grid, st) : launch_rope_any<kBF16, false>(mode, V, W, a, grid, st));

@@ -18,8 +18,8 @@
 // asynchronous copies of each warp's own, four groups deep.  With plain loads, addresses from scratch and the weights read per token, the norm
 // of [64, 197, 12 + 12, 64] bfloat16 took 581 instructions a group and 39.5 us.
 //
-// Rows that turn as a whole and fill 4, 8 or 16 lanes (heads of 64, 128, 256 on the 16-byte grid) have kernels of their own (L > 0), in which
-// every slot exists and each lane copies for itself; the others (L = 0) ask for each slot and copy by vectors of W elements in order.
+// Rows that turn as a whole and are 2, 4, 6, 8, 10, 12 or 16 lanes (heads of 32 to 256, whose halves are whole 32-byte sectors) have kernels of their
+// own (L > 0), in which every slot exists and each lane copies for itself; the others (L = 0) ask for each slot and copy by vectors of W elements in order.
 #pragma once
 
 #include <algorithm>
@@ -46,7 +46,7 @@ struct Lane {
     const uint32_t lane = threadIdx.x & 31u, n = lanes(a), rows = L ? 32 / (L ? L : 1) : a.rows_per_warp;
     row = lane / n;
     slot = lane - row * n;
-    on = row < rows;
+    on = row < rows;  // (always, where L divides 32)
     if (MULTI && group_tokens > 1) {  // all rows of several tokens
       token = row / heads;
       head = row - token * heads;
@@ -479,10 +479,17 @@ __device__ __forceinline__ float row_sum(F2 two, uint32_t in_row, uint32_t lanes
   float v, w;
   f2_unpack(two, v, w);
   v += w;
-  if constexpr (L > 0) {
+  if constexpr (L > 0 && (L & (L - 1)) == 0) {
 #pragma unroll
     for (int o = L / 2; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
+  } else if constexpr (L > 0) {
+#pragma unroll
+    for (uint32_t o = 1; o < L; o <<= 1) {
+      w = __shfl_down_sync(0xffffffffu, v, o);
+      if (in_row + o < L) v += w;
+    }
+    return __shfl_sync(0xffffffffu, v, (threadIdx.x & 31u) - in_row);
   } else {
     for (uint32_t o = 1; o < lanes; o <<= 1) {
       w = __shfl_down_sync(0xffffffffu, v, o);
@@ -638,7 +645,7 @@ __global__ void __launch_bounds__(kThreads, V == 1 || MULTI ? 2 : 3) rope_kernel
       if (!MULTI) to.enter(now, a.out[0], a.out[1]);
     }
     const uint32_t row = now.i * l.per + l.head;
-    const uint64_t out = MULTI ? mine.outs[32 * stage] : (L && row < heads ? to.row(row) : 0);
+    const uint64_t out = MULTI ? mine.outs[32 * stage] : (L && l.on && row < heads ? to.row(row) : 0);
     char* at = mine.ring + stage * Rows::kGroupBytes;
     F2 fa[K][kHalf<V>], fb[K][kHalf<V>];
 #pragma unroll
@@ -749,7 +756,7 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 1 : 2) qknorm_bwd_kernel(co
       if (!MULTI) to.enter(now, o);
     }
     const uint32_t row = now.i * l.per + l.head;
-    const uint64_t out = MULTI ? mine.outs[32 * stage] : (L && row < heads ? to.row(row) : 0);
+    const uint64_t out = MULTI ? mine.outs[32 * stage] : (L && l.on && row < heads ? to.row(row) : 0);
     const bool there = MULTI ? out != 0 : l.on && row < heads;
     F2 xa[K][kHalf<V>], xb[K][kHalf<V>], ua[K][kHalf<V>], ub[K][kHalf<V>];
     char* at = mine.ring + stage * 2 * Rows::kGroupBytes;
@@ -872,9 +879,15 @@ cudaError_t launch_layout(int mode, const RopeArgs& a, unsigned grid, cudaStream
 template <int DT>
 cudaError_t launch_rope_whole(int mode, const RopeArgs& a, unsigned grid, cudaStream_t st) {
   constexpr int W = 16 / Io<DT>::kBytes;  // the widest vector
-  if (a.head_dim == 64) return launch_layout<DT, W, W, 4, false>(mode, a, grid, st);
-  if (a.head_dim == 128) return launch_layout<DT, W, W, 8, false>(mode, a, grid, st);
-  return launch_layout<DT, W, W, 16, false>(mode, a, grid, st);
+  switch (a.head_dim) {
+    case 32: return launch_layout<DT, W, W, 2, false>(mode, a, grid, st);
+    case 64: return launch_layout<DT, W, W, 4, false>(mode, a, grid, st);
+    case 96: return launch_layout<DT, W, W, 6, false>(mode, a, grid, st);
+    case 128: return launch_layout<DT, W, W, 8, false>(mode, a, grid, st);
+    case 160: return launch_layout<DT, W, W, 10, false>(mode, a, grid, st);
+    case 192: return launch_layout<DT, W, W, 12, false>(mode, a, grid, st);
+    default: return launch_layout<DT, W, W, 16, false>(mode, a, grid, st);
+  }
 }
 #else
 // (V, W) is one of these: W the widest vector, or both 2 or 1.
