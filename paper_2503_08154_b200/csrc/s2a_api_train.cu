@@ -157,7 +157,7 @@ int run_rope(const s2a_rope_args* args, int mode, int back, void* stream) {
   a.gamma[1] = gamma[1];
   a.positions = c.rot_dim ? c.positions : nullptr;
   a.table = c.table;
-  a.first = c.first;
+  a.first = a.positions ? 0 : c.first;
   a.pos_axis = c.pos_axis_stride;
   a.pos_batch = c.pos_batch_stride;
   a.batch = (uint32_t)c.batch;

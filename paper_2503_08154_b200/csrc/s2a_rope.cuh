@@ -33,8 +33,9 @@ namespace {
 constexpr int kWarps = 8;
 constexpr int kThreads = kWarps * 32;
 constexpr int kLaneElems = 16;
-// Stages of a warp's ring: groups of rows in flight or in work.  Two tensors of binary32 have three, so that two CTAs fit an SM.
-template <int DT> constexpr int kBwdStages = DT == kF32 ? 3 : 4;
+// Stages of a warp's ring: groups of rows in flight or in work.  Two tensors have five in bfloat16 ([4, 4097, 32 + 8, 128]
+// backward 94 us, 100 with four) and three in binary32, so that two CTAs fit an SM.
+template <int DT> constexpr int kBwdStages = DT == kF32 ? 3 : 5;
 
 // Where a warp's lanes stand in a group of rows: `row` of the group, and what that is: row `head` (plus groups already done) of token `token`
 // of the group's.
@@ -394,26 +395,28 @@ struct Group {
     if (L == 0 && (threadIdx.x & 31u) < groups) *(uint4*)(ring + (threadIdx.x & 31u) * kGroupBytes + kRowsBytes) = make_uint4(0u, 0u, 0u, 0u);
   }
 
-  // Rows of a token: row r of the queries lies at q + r * q_head vectors, of the keys (r >= heads0) at k + r * k_head vectors.
+  // Rows of a token: row r of the queries lies at q + r * q_head vectors; with KEYS those from heads0 on are the keys', at k + r * k_head vectors.
+  template <bool KEYS>
   struct Source {
     uint64_t q, k;
     uint32_t q_head, k_head, heads0, heads;
     __device__ __forceinline__ Source(const HeadsArg& hq, const HeadsArg& hk, uint32_t h0, uint32_t h)
         : q(0), k(0), q_head((uint32_t)(hq.head / kBytes)), k_head((uint32_t)(hk.head / kBytes)), heads0(h0), heads(h) {}
     __device__ __forceinline__ uint64_t row(uint32_t r) const {
+      if (!KEYS) return q + (uint64_t)(r * kBytes) * q_head;
       const bool keys = r >= heads0;
       return (keys ? k : q) + (uint64_t)(r * kBytes) * (keys ? k_head : q_head);
     }
     // on to the walk's token
     __device__ __forceinline__ void enter(const Walk<MULTI>& w, const HeadsArg& hq, const HeadsArg& hk) {
       q = w.row0(hq);
-      k = w.row0(hk) - heads0 * hk.head;
+      if (KEYS) k = w.row0(hk) - heads0 * hk.head;
     }
-    __device__ __forceinline__ void enter(const Walk<MULTI>& w, const HeadsArg& hq) { q = w.row0(hq); }
   };
 
   // first: the group's first row of the token; r: the lane's; there: whether it exists
-  __device__ __forceinline__ void fetch(char* stage, const RopeArgs& a, const Source& from, uint32_t first, uint32_t r, bool there,
+  template <typename S>
+  __device__ __forceinline__ void fetch(char* stage, const RopeArgs& a, const S& from, uint32_t first, uint32_t r, bool there,
                                         const Lane<L, MULTI>& l) const {
     const uint32_t lane = threadIdx.x & 31u;
     const uint32_t to = (uint32_t)__cvta_generic_to_shared(stage) + lane * kBytes;
@@ -458,7 +461,8 @@ struct Group {
     }
   }
   // row: the address of the lane's row, 0 for none
-  __device__ __forceinline__ void flush(const char* stage, const RopeArgs& a, uint64_t row, const Source& to, uint32_t first) const {
+  template <typename S>
+  __device__ __forceinline__ void flush(const char* stage, const RopeArgs& a, uint64_t row, const S& to, uint32_t first) const {
     if constexpr (L == 0) {
       using Raw = typename RawOf<kBytes>::T;
       const char* own = stage + (threadIdx.x & 31u) * kBytes;
@@ -607,7 +611,7 @@ __global__ void __launch_bounds__(kThreads, V == 1 || MULTI ? 2 : 3) rope_kernel
   Walk<MULTI> ahead(a, blockIdx.x * kWarps + (threadIdx.x >> 5), 0, groups, l.token);
   Walk<MULTI> now = ahead;  // (several tokens: the addresses to write to come through the ring, and this one only counts)
   bool fresh = true;
-  typename Rows::Source from(a.in[0], a.in[1], heads0, heads), to(a.out[0], a.out[1], heads0, heads);
+  typename Rows::template Source<true> from(a.in[0], a.in[1], heads0, heads), to(a.out[0], a.out[1], heads0, heads);
   const auto fetch = [&](uint32_t stage) {
     if (ahead.left) {
       if (fresh) {
@@ -710,14 +714,13 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 1 : 2) qknorm_bwd_kernel(co
   Walk<MULTI> ahead(a, cta * kWarps + warp, which, groups, l.token);
   Walk<MULTI> now = ahead;
   bool fresh = true;
-  // all rows count as queries' here
-  typename Rows::Source from_x(x, x, heads, heads), from_g(g, g, heads, heads), to(o, o, heads, heads);
+  typename Rows::template Source<false> from_x(x, x, heads, heads), from_g(g, g, heads, heads), to(o, o, heads, heads);
   const auto fetch = [&](uint32_t stage) {
     if (ahead.left) {
       if (fresh) {
-        from_x.enter(ahead, x);
-        from_g.enter(ahead, g);
-        if (MULTI) to.enter(ahead, o);
+        from_x.enter(ahead, x, x);
+        from_g.enter(ahead, g, g);
+        if (MULTI) to.enter(ahead, o, o);
         copy_positions(a, mine.positions + 4 * stage * group_tokens, ahead, l);
       }
       char* at = mine.ring + stage * 2 * Rows::kGroupBytes;
@@ -753,7 +756,7 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 1 : 2) qknorm_bwd_kernel(co
                       mine.cs, mine.sn))
         angles.read(p, mine.cs + phases, mine.sn + phases);
       start = false;
-      if (!MULTI) to.enter(now, o);
+      if (!MULTI) to.enter(now, o, o);
     }
     const uint32_t row = now.i * l.per + l.head;
     const uint64_t out = MULTI ? mine.outs[32 * stage] : (L && l.on && row < heads ? to.row(row) : 0);

@@ -276,6 +276,22 @@ def test_turning_back_and_lengths():
         assert torch.allclose(y.square().sum(-1), x.square().sum(-1), rtol=1e-5)
 
 
+def test_positions_come_before_first():
+    """With positions, `first` is not looked at; without rotation nothing of them is."""
+    x = _normal((2, 9, 3, 32), torch.float32, "x")
+    pos = torch.randint(0, 500, (2, 9), generator=_gen("p"), device="cuda", dtype=torch.int32)
+    table = s2a.rope_table(32).cuda()
+    y, z = torch.empty_like(x), torch.empty_like(x)
+    s2a.s2a_rope_fwd(x, None, y, None, pos, table)
+    s2a.s2a_rope_fwd(x, None, z, None, pos, table, first=77)
+    _done()
+    assert torch.equal(y, z)
+    s2a.s2a_qknorm_rope_fwd(x, None, None, None, y, None, None, None, 1e-6)
+    s2a.s2a_qknorm_rope_fwd(x, None, None, None, z, None, pos[:, :3], None, 1e-6, first=5)
+    _done()
+    assert torch.equal(y, z)
+
+
 def test_a_table_of_the_callers_own_and_an_axis_beyond_the_last():
     x = _normal((1, 9, 2, 16), torch.float32, "x")
     pos = torch.randint(0, 50, (2, 1, 9), generator=_gen("p"), device="cuda", dtype=torch.int32)
