@@ -401,8 +401,10 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const StepTensor& 
   }
 }
 
-// CTAs of an SM.
-template <int BITS> constexpr int kStepCtas = BITS == 8 ? 5 : 4;
+// CTAs of an SM.  8-bit states: five, and two blocks of a warp's in registers at once (302 M weights: 664 us; 778 with four CTAs, 736 with six, 778 with
+// seven and one block).  32-bit states: a block is 128 bytes a lane already, and six CTAs with one block each take 10.6 M weights at odd places
+// in 49.6 us, four with two 56.
+template <int BITS> constexpr int kStepCtas = BITS == 8 ? 5 : 6;
 
 template <int PDT, int GDT, int BITS, bool RANDOM>
 __global__ void __launch_bounds__(kStepThreads, kStepCtas<BITS>) adamw_kernel(const __grid_constant__ StepArgs a) {
@@ -452,16 +454,24 @@ __global__ void __launch_bounds__(kStepThreads, kStepCtas<BITS>) adamw_kernel(co
     const uint64_t base = head + from + (QUAD ? 4 : 8) * lane;  // the lane's first element in block 0 of the chunk
     const uint64_t rest = t.n > head + from ? t.n - head - from : 0;  // of the tensor from this chunk on
     if (vec && blocks > 1 && rest >= (uint64_t)blocks * kStepBlock) {
-      // whole blocks: the next one is on its way while one is in work
       const auto spot = [&](uint32_t i) { return Spot<QUAD, true>{base + i * kStepBlock, 256}; };
-      Loaded<PDT, GDT, BITS> x, y;
-      x.load(t, spot(0), true, block);
+      Loaded<PDT, GDT, BITS> x;
+      if constexpr (BITS == 8) {  // the next block is on its way while one is in work
+        Loaded<PDT, GDT, BITS> y;
+        x.load(t, spot(0), true, block);
 #pragma unroll 1
-      for (uint32_t i = 0; i < blocks; i += 2) {
-        y.load(t, spot(i + 1), true, block + i + 1);
-        step_block<RANDOM>(a, t, k, key, draw + 32 * i, x, spot(i), true, block + i);
-        if (i + 2 < blocks) x.load(t, spot(i + 2), true, block + i + 2);
-        step_block<RANDOM>(a, t, k, key, draw + 32 * (i + 1), y, spot(i + 1), true, block + i + 1);
+        for (uint32_t i = 0; i < blocks; i += 2) {
+          y.load(t, spot(i + 1), true, block + i + 1);
+          step_block<RANDOM>(a, t, k, key, draw + 32 * i, x, spot(i), true, block + i);
+          if (i + 2 < blocks) x.load(t, spot(i + 2), true, block + i + 2);
+          step_block<RANDOM>(a, t, k, key, draw + 32 * (i + 1), y, spot(i + 1), true, block + i + 1);
+        }
+      } else {
+#pragma unroll 1
+        for (uint32_t i = 0; i < blocks; ++i) {
+          x.load(t, spot(i), true, block + i);
+          step_block<RANDOM>(a, t, k, key, draw + 32 * i, x, spot(i), true, block + i);
+        }
       }
       continue;
     }
@@ -580,9 +590,11 @@ __global__ void __launch_bounds__(kFinishThreads) grad_norm_finish_kernel(const 
 
 template <int PDT, int GDT>
 cudaError_t launch_adamw_types(int bits, const StepArgs& a, unsigned grid, cudaStream_t st) {
-  if (bits == 32)
-    return a.rng ? launch_overlapped(adamw_kernel<PDT, GDT, 32, true>, dim3(grid), kStepThreads, 0, st, a)
-                 : launch_overlapped(adamw_kernel<PDT, GDT, 32, false>, dim3(grid), kStepThreads, 0, st, a);
+  if (bits == 32) {
+    if constexpr (PDT == kBF16)  // binary32 weights and states need no rounding
+      if (a.rng) return launch_overlapped(adamw_kernel<PDT, GDT, 32, true>, dim3(grid), kStepThreads, 0, st, a);
+    return launch_overlapped(adamw_kernel<PDT, GDT, 32, false>, dim3(grid), kStepThreads, 0, st, a);
+  }
   return a.rng ? launch_overlapped(adamw_kernel<PDT, GDT, 8, true>, dim3(grid), kStepThreads, 0, st, a)
                : launch_overlapped(adamw_kernel<PDT, GDT, 8, false>, dim3(grid), kStepThreads, 0, st, a);
 }
