@@ -511,6 +511,7 @@ int s2a_step_plan_fill(const s2a_step_tensor* tensors, size_t n_tensors, int pdt
  * laid out as for s2a_dropout_fwd, for m; their two bytes exchanged for sqrt(v); and those with the first counter's top bit set for
  * the parameter.  With nearest, a state that moves by less than half a code's step stays where it is: use rng for long runs with 8-bit
  * states.
+ * A v below 2^-126 counts as zero in the step, and so does, with eps 0, a sqrt(v / (1 - beta2^t)).
  * beta1, beta2: in [0, 1); eps: finite, not negative.
  */
 int s2a_adamw_step(const s2a_step_plan* plan, const void* image, const float* control, const float* clip, const uint64_t* rng,

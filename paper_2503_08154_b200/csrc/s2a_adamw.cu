@@ -136,9 +136,10 @@ struct Raw {
   }
 };
 
+// One step of binary32 at most; what is below the normal range counts as zero, which saves the instructions of its scaling.
 __device__ __forceinline__ float approx_sqrt(float x) {
   float y;
-  asm("sqrt.approx.f32 %0, %1;" : "=f"(y) : "f"(x));
+  asm("sqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
 
@@ -183,7 +184,7 @@ __device__ __forceinline__ void update(F2 (&p)[4], const F2 (&m)[4], const F2 (&
   for (int i = 0; i < 4; ++i) {
     float x, y;
     f2_unpack(f2_fma(r[i], f2_both(root), f2_both(eps)), x, y);
-    const F2 q = f2_mul(m[i], f2_pack(__fdividef(1.0f, x), __fdividef(1.0f, y)));
+    const F2 q = f2_mul(m[i], f2_pack(rcp_approx(x), rcp_approx(y)));
     p[i] = f2_fma(q, f2_both(-step), f2_fma(p[i], f2_both(-shrink), p[i]));
   }
 }

@@ -477,6 +477,12 @@ struct Group {
   }
 };
 
+__device__ __forceinline__ float rsqrt_approx(float x) {  // 2^-22.9 of itself
+  float y;
+  asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+
 // Sum over the `lanes` neighbouring lanes of a row, at every one of them.  L = 0: any number of lanes up to 32.
 template <int L>
 __device__ __forceinline__ float row_sum(F2 two, uint32_t in_row, uint32_t lanes) {
@@ -664,7 +670,7 @@ __global__ void __launch_bounds__(kThreads, V == 1 || MULTI ? 2 : 3) rope_kernel
           sa = f2_fma(fa[k][j], fa[k][j], sa);
           sb = f2_fma(fb[k][j], fb[k][j], sb);
         }
-      const F2 rstd = f2_both(rsqrtf(row_sum<L>(f2_add(sa, sb), l.slot, a.lanes) * a.inv_dim + a.eps));
+      const F2 rstd = f2_both(rsqrt_approx(row_sum<L>(f2_add(sa, sb), l.slot, a.lanes) * a.inv_dim + a.eps));
       const float* weights = gamma + (row >= heads0 ? gamma_row : 0u);
 #pragma unroll
       for (int k = 0; k < K; ++k) {
@@ -778,7 +784,7 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 1 : 2) qknorm_bwd_kernel(co
         other = f2_fma(xb[k][j], xb[k][j], other);
       }
     // a row that does not exist is zeros in x and in the gradient: with this rstd it adds nothing to any sum
-    float root = rsqrtf(row_sum<L>(f2_add(sum, other), l.slot, a.lanes) * a.inv_dim + a.eps);
+    float root = rsqrt_approx(row_sum<L>(f2_add(sum, other), l.slot, a.lanes) * a.inv_dim + a.eps);
     if (!there) root = 0.0f;
     const F2 rstd = f2_both(root);
     sum = other = f2_both(0.0f);
