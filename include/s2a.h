@@ -429,7 +429,8 @@ int s2a_rope_fwd(const s2a_rope_args* args, void* cuda_stream);
 int s2a_rope_bwd(const s2a_rope_args* args, void* cuda_stream);
 
 /* The norm of each head's row, and the rotation, in one pass: rstd = 1 / sqrt(sum(x^2) / head_dim + eps),
- * out = rotation(x * rstd * gamma).  eps: finite, not negative.  Rows whose sum of squares is beyond binary32 become zeros. */
+ * out = rotation(x * rstd * gamma).  eps: finite, not negative.  Rows whose sum of squares is beyond binary32 become
+ * zeros; with eps 0, a mean square below 2^-126 counts as zero. */
 int s2a_qknorm_rope_fwd(const s2a_rope_args* args, void* cuda_stream);
 
 /* Bytes of scratch for the weights' gradients of s2a_qknorm_rope_bwd (0 where head_dim is 0 or above 512): the same

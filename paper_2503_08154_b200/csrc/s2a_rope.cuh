@@ -745,7 +745,6 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 1 : 2) qknorm_bwd_kernel(co
   stage_table(a, shared, lay, a.gamma[which], nullptr, 1);
   __syncthreads();
 
-  Angles<V, K, INTER, L, MULTI> angles;
   F2 sa[K][kHalf<V>], sb[K][kHalf<V>];
 #pragma unroll
   for (int k = 0; k < K; ++k)
@@ -758,12 +757,13 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 1 : 2) qknorm_bwd_kernel(co
     copy_wait<STAGES - 2>();
     if (L == 0 || begins) __syncwarp();
     if (begins) {
-      if (warp_phases(a, shared, mine.positions + 4 * stage * group_tokens, mine.positions + 4 * STAGES * group_tokens, l, group_tokens, start,
-                      mine.cs, mine.sn))
-        angles.read(p, mine.cs + phases, mine.sn + phases);
+      warp_phases(a, shared, mine.positions + 4 * stage * group_tokens, mine.positions + 4 * STAGES * group_tokens, l, group_tokens, start, mine.cs,
+                  mine.sn);
       start = false;
       if (!MULTI) to.enter(now, o, o);
     }
+    Angles<V, K, INTER, L, MULTI> angles;  // read for each group: held over groups they are slower ([4, 4097, 32 + 8, 128] bfloat16 96 us against 93)
+    angles.read(p, mine.cs + phases, mine.sn + phases);
     const uint32_t row = now.i * l.per + l.head;
     const uint64_t out = MULTI ? mine.outs[32 * stage] : (L && l.on && row < heads ? to.row(row) : 0);
     const bool there = MULTI ? out != 0 : l.on && row < heads;
