@@ -93,9 +93,11 @@ cudaError_t launch_rope(int mode, int dt, RopeArgs a, void* grad_gamma_q, void* 
   a.rows_per_warp = 32 / a.lanes;
   a.inv_dim = 1.0f / (float)a.head_dim;
   a.pairs_inverse = a.pairs ? (1048576u + a.pairs - 1) / a.pairs : 0u;
-  // A group is rows of one token; or, where the tokens of some kind have fewer than a group's rows, those of several tokens.
+  // A group is rows of one token; or, where those are at most half of what a group takes, the rows of several tokens.  Where
+  // the norms' backward has many query heads, few key heads alone do not call for it: groups of several tokens walk the sequences
+  // for every row, and [1, 8654, 32 + 1, 64] takes 68 us with them and 32 us without, [1, 4298, 8 + 1, 96] 30 and 17 us (binary32).
   const auto few = [&](uint32_t rows) { return rows != 0 && 2 * rows <= a.rows_per_warp; };
-  const bool multi = mode == kRopeBwdNorm ? few(a.heads[0]) || few(a.heads[1]) : few(heads);
+  const bool multi = mode == kRopeBwdNorm ? few(a.heads[0]) && (a.heads[1] == 0 || few(a.heads[1])) : few(heads);
   // A warp each for the groups, until the GPU is full; then shares.  `which`: the forward kernels (and queries), keys.
   uint64_t items[2] = {0, 0};
   const auto group = [&](uint32_t rows, int which) {
