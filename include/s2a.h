@@ -414,11 +414,11 @@ typedef struct {
   const void *grad_q, *grad_k;     /* backward of the norm: the outputs' gradients              */
   void *grad_gamma_q, *grad_gamma_k, *scratch;
   int64_t first;
+  float scale, eps;
+  int interleaved, dt, wdt;
   size_t pos_batch_stride, pos_axis_stride, axes;
   size_t batch, tokens, heads_q, heads_k, head_dim, rot_dim;
   size_t q_stride[3], k_stride[3], out_q_stride[3], out_k_stride[3], grad_q_stride[3], grad_k_stride[3];
-  float scale, eps;
-  int interleaved, dt, wdt;
 } s2a_rope_args;
 
 /* Forward: with the angle w = position * frequency of its pair, (a, b) -> (a cos w - b sin w, a sin w + b cos w). */

@@ -601,8 +601,10 @@ def log_buckets(first_distance: int, count: int, n_buckets: int, max_distance: i
 
 # ------------------------------------------- rotary positions, norms of queries and keys with them
 _SCALINGS = {"none": 0, "linear": 1, "base": 2, "parts": 3}
-_rope_args = struct.Struct("@13Pq27Q2f3i0q").pack   # s2a_rope_args
-
+# s2a_rope_args in two parts: addresses and scalars of a call, and sizes and strides
+_rope_call = struct.Struct("@13Pq2f3i0q").pack
+_rope_sizes = struct.Struct("@27Q").pack
+_rope_layouts = {}   # the second part, with what else is known of it, by the shapes, strides and dtypes of a call's tensors
 
 def rope_table(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_length: float = 0.0,
                slow: float = 1.0, fast: float = 32.0, axes: int = 1) -> torch.Tensor:
@@ -622,27 +624,24 @@ def _heads(t, shape, dtype, what: str):
     stride = t.stride()
     if stride[3] != 1 and shape[3] != 1:
         raise S2AError("%s: the elements of a head's row must be contiguous" % what)
-    return stride
+    return stride[:3]
 
 
 def _address(t):
     return 0 if t is None else t.data_ptr()
 
 
-_NONE = (0, 0, 0, 0)
-
-
-def _rope(call, q, k, out_q, out_k, positions, table, scale, interleaved, first, dev, eps=0.0, wdt=F32, gamma_q=0, gamma_k=0,
-          grad_q=None, grad_k=None, sum_q=0, sum_k=0, scratch=0):
+def _rope_layout(q, k, out_q, out_k, positions, table, grad_q, grad_k, params):
+    """What the shapes, strides and dtypes of a call's tensors come to, checked: the sizes' part of the arguments, the codes of
+    the dtype and of the weights', and the bytes of scratch that the weights' gradients need."""
     shape, dtype = q.shape, q.dtype
     if len(shape) != 4:
         raise S2AError("queries and keys must be [batch, tokens, heads, head_dim]")
     batch, tokens, heads_q, dim = shape
-    a, b = _heads(q, shape, dtype, "q"), _heads(out_q, shape, dtype, "the queries' output")
-    c, d, e, f, heads_k = _NONE, _NONE, _NONE, _NONE, 0
-    k_at = out_k_at = grad_q_at = grad_k_at = 0
+    none, heads_k, rot = (0, 0, 0), 0, 0
+    strides = [_heads(q, shape, dtype, "q"), none, _heads(out_q, shape, dtype, "the queries' output"), none, none, none]
     if grad_q is not None:
-        e, grad_q_at = _heads(grad_q, shape, dtype, "grad_q"), grad_q.data_ptr()
+        strides[4] = _heads(grad_q, shape, dtype, "grad_q")
     if k is not None:
         other = k.shape
         if len(other) != 4 or other[0] != batch or other[1] != tokens or other[3] != dim:
@@ -650,16 +649,16 @@ def _rope(call, q, k, out_q, out_k, positions, table, scale, interleaved, first,
         if out_k is None or (grad_q is not None and grad_k is None):
             raise S2AError("the keys' tensors are needed")
         heads_k = other[2]
-        c, d, k_at, out_k_at = _heads(k, other, dtype, "k"), _heads(out_k, other, dtype, "the keys' output"), k.data_ptr(), out_k.data_ptr()
+        strides[1], strides[3] = _heads(k, other, dtype, "k"), _heads(out_k, other, dtype, "the keys' output")
         if grad_k is not None:
-            f, grad_k_at = _heads(grad_k, other, dtype, "grad_k"), grad_k.data_ptr()
-    rot = where = pos = per_batch = per_axis = 0
+            strides[5] = _heads(grad_k, other, dtype, "grad_k")
+    per_batch = per_axis = 0
     axes = 1
     if table is not None:
         size = table.shape
         if table.dtype is not torch.int64 or len(size) != 2 or size[1] != 2 or not table.is_contiguous():
             raise S2AError("the table must be contiguous int64 [rot_dim / 2, 2]")
-        rot, where = 2 * size[0], table.data_ptr()
+        rot = 2 * size[0]
         if positions is not None:
             size, stride = positions.shape, positions.stride()
             n = len(size)
@@ -667,20 +666,63 @@ def _rope(call, q, k, out_q, out_k, positions, table, scale, interleaved, first,
                 raise S2AError("positions must be int32 [tokens], [batch, tokens] or [axes, batch, tokens]")
             if tokens > 1 and stride[-1] != 1:
                 raise S2AError("the positions of a sequence's tokens must be contiguous")
-            pos = positions.data_ptr()
             if n > 1:
                 per_batch = stride[-2]
                 if n > 2:
                     per_axis, axes = stride[0], size[0]
-    code = _CODES.get(dtype)
+    for t, what in zip(params, ("gamma_q", "gamma_k", "grad_gamma_q", "grad_gamma_k")):
+        _param(t, dim, what)
+    need = qknorm_rope_scratch_bytes(batch, tokens, heads_q, heads_k, dim) if any(t is not None for t in params[2:]) else None
+    return (_rope_sizes(per_batch, per_axis, axes, batch, tokens, heads_q, heads_k, dim, rot, *(x for s in strides for x in s)),
+            _code(q), _param_dtype(*params), need)
+
+
+def _rope(call, q, k, out_q, out_k, positions, table, scale, interleaved, first, dev, eps=0.0, grad_q=None, grad_k=None, params=(),
+          scratch=None):
+    # A call's tensors are looked up by all that is checked of them but their addresses, which the library checks each time.
+    key = (q.shape, q.stride(), q.dtype, out_q.shape, out_q.stride(), out_q.dtype)
+    q_at, out_q_at = q.data_ptr(), out_q.data_ptr()
+    k_at = out_k_at = grad_q_at = grad_k_at = gamma_q = gamma_k = sum_q = sum_k = where = pos = room = 0
+    if k is None:
+        key += (None,)
+    elif out_k is None:
+        raise S2AError("the keys' tensors are needed")
+    else:
+        key += (k.shape, k.stride(), k.dtype, out_k.shape, out_k.stride(), out_k.dtype)
+        k_at, out_k_at = k.data_ptr(), out_k.data_ptr()
+    if table is None:
+        key += (None,)
+    else:
+        key += (table.shape, table.stride(), table.dtype)
+        where = table.data_ptr()
+        if positions is not None:
+            key += (positions.shape, positions.stride(), positions.dtype)
+            pos = positions.data_ptr()
+    if params:
+        for t in params:
+            key += (None,) if t is None else (t.numel(), t.is_contiguous(), t.dtype)
+        gamma_q, gamma_k, sum_q, sum_k = [0 if t is None else t.data_ptr() for t in params]
+        if grad_q is not None:
+            key += (grad_q.shape, grad_q.stride(), grad_q.dtype)
+            grad_q_at = grad_q.data_ptr()
+            if grad_k is not None and k is not None:
+                key += (grad_k.shape, grad_k.stride(), grad_k.dtype)
+                grad_k_at = grad_k.data_ptr()
+    found = _rope_layouts.get(key)
+    if found is None:
+        found = _rope_layout(q, k, out_q, out_k, positions, table, grad_q, grad_k, params)
+        if len(_rope_layouts) >= 1024:
+            _rope_layouts.clear()
+        _rope_layouts[key] = found
+    sizes, dt, wdt, need = found
+    if need is not None:
+        room = _scratch(scratch, need)
     try:
-        packed = _rope_args(
-            q.data_ptr(), k_at, out_q.data_ptr(), out_k_at, pos, where, gamma_q, gamma_k, grad_q_at, grad_k_at, sum_q, sum_k, scratch, first, per_batch, per_axis, axes, batch, tokens, heads_q, heads_k, dim, rot, a[0],
-            a[1], a[2], c[0], c[1], c[2], b[0], b[1], b[2], d[0], d[1], d[2], e[0], e[1], e[2], f[0], f[1], f[2], scale, eps, interleaved,
-            dtype_code(q) if code is None else code, wdt)
+        packed = _rope_call(q_at, k_at, out_q_at, out_k_at, pos, where, gamma_q, gamma_k, grad_q_at, grad_k_at, sum_q, sum_k, room, first, scale,
+                            eps, interleaved, dt, wdt)
     except (struct.error, OverflowError) as error:
         raise S2AError("scale, eps, interleaved and first must be plain numbers: %s" % error)
-    status = call(packed, _stream_on(dev))
+    status = call(packed + sizes, _stream_on(dev))
     if status:
         check(status)
 
@@ -708,10 +750,8 @@ def s2a_qknorm_rope_fwd(q, k, gamma_q, gamma_k, out_q, out_k, positions, table, 
                         interleaved: bool = False, first: int = 0) -> None:
     """The norm of each head's row (by its root mean square; gamma_q, gamma_k [head_dim] or None) and the rotation in one pass.
     table None: the norm alone.  The rest as for s2a_rope_fwd."""
-    dev = _on_device(q, k, gamma_q, gamma_k, out_q, out_k, positions, table)
-    dim = q.shape[-1]
-    _rope((_lib or lib()).s2a_qknorm_rope_fwd, q, k, out_q, out_k, positions, table, scale, interleaved, first, dev, eps,
-          _param_dtype(gamma_q, gamma_k), _param(gamma_q, dim, "gamma_q") or 0, _param(gamma_k, dim, "gamma_k") or 0)
+    _rope((_lib or lib()).s2a_qknorm_rope_fwd, q, k, out_q, out_k, positions, table, scale, interleaved, first,
+          _on_device(q, k, gamma_q, gamma_k, out_q, out_k, positions, table), eps, params=(gamma_q, gamma_k, None, None))
 
 
 def qknorm_rope_scratch_bytes(batch: int, tokens: int, heads_q: int, heads_k: int, head_dim: int) -> int:
@@ -723,17 +763,11 @@ def s2a_qknorm_rope_bwd(grad_q, grad_k, q, k, gamma_q, gamma_k, grad_in_q, grad_
     """The backward pass of s2a_qknorm_rope_fwd from its inputs q and k.  grad_gamma_q and grad_gamma_k may be None (frozen
     weights; without both, scratch may be None too); scratch holds qknorm_rope_scratch_bytes(...) bytes.  grad_in_q may be
     grad_q or q, grad_in_k grad_k or k."""
-    dev = _on_device(q, grad_q, grad_k, k, gamma_q, gamma_k, grad_in_q, grad_in_k, grad_gamma_q, grad_gamma_k, scratch, positions,
-                     table)
-    dim, room = q.shape[-1], 0
-    if grad_gamma_q is not None or grad_gamma_k is not None:
-        room = _scratch(scratch, qknorm_rope_scratch_bytes(0, 0, 0, 0, dim))
     if grad_q is None:
         raise S2AError("grad_q is needed")
-    _rope((_lib or lib()).s2a_qknorm_rope_bwd, q, k, grad_in_q, grad_in_k, positions, table, scale, interleaved, first, dev, eps,
-          _param_dtype(gamma_q, gamma_k, grad_gamma_q, grad_gamma_k), _param(gamma_q, dim, "gamma_q") or 0,
-          _param(gamma_k, dim, "gamma_k") or 0, grad_q, grad_k, _param(grad_gamma_q, dim, "grad_gamma_q") or 0,
-          _param(grad_gamma_k, dim, "grad_gamma_k") or 0, room)
+    _rope((_lib or lib()).s2a_qknorm_rope_bwd, q, k, grad_in_q, grad_in_k, positions, table, scale, interleaved, first,
+          _on_device(q, grad_q, grad_k, k, gamma_q, gamma_k, grad_in_q, grad_in_k, grad_gamma_q, grad_gamma_k, scratch, positions, table),
+          eps, grad_q, grad_k, (gamma_q, gamma_k, grad_gamma_q, grad_gamma_k), scratch)
 
 
 # --------------------------------------------------- the AdamW step over many tensors, the gradients' norm

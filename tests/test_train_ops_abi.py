@@ -16,8 +16,9 @@ OK, NULL, SHAPE, ALIGN, DTYPE, CUDA, OVERLAP, VALUE = 0, 1, 2, 3, 4, 5, 8, 9
 A, B, C, D, E, F, G = (0x10000000 * i for i in range(1, 8))   # far apart, never dereferenced
 NO_GPU = pytest.mark.skipif(torch.cuda.is_available(), reason="calls that pass every check would be launched on addresses that do not exist")
 
-FIELDS = ("q k out_q out_k positions table gamma_q gamma_k grad_q grad_k grad_gamma_q grad_gamma_k scratch first pos_batch pos_axis axes batch "
-          "tokens heads_q heads_k head_dim rot_dim").split()
+FIELDS = ("q k out_q out_k positions table gamma_q gamma_k grad_q grad_k grad_gamma_q grad_gamma_k scratch first "
+          "scale eps interleaved dt wdt").split()
+SIZES = "pos_batch pos_axis axes batch tokens heads_q heads_k head_dim rot_dim".split()
 STRIDES = ("q_stride", "k_stride", "out_q_stride", "out_k_stride", "grad_q_stride", "grad_k_stride")
 
 
@@ -34,8 +35,7 @@ def _args(**changes):
     v |= {"q_stride": (8 * 256, 256, 64), "out_q_stride": (8 * 256, 256, 64), "grad_q_stride": (8 * 256, 256, 64)}
     v |= {"k_stride": (8 * 128, 128, 64), "out_k_stride": (8 * 128, 128, 64), "grad_k_stride": (8 * 128, 128, 64)}
     v |= changes
-    flat = [v[n] for n in FIELDS] + [s for n in STRIDES for s in v[n]] + [v[n] for n in ("scale", "eps", "interleaved", "dt", "wdt")]
-    return binding._rope_args(*flat)
+    return binding._rope_call(*(v[n] for n in FIELDS)) + binding._rope_sizes(*(v[n] for n in SIZES), *(s for n in STRIDES for s in v[n]))
 
 
 CALLS = ("s2a_rope_fwd", "s2a_rope_bwd", "s2a_qknorm_rope_fwd", "s2a_qknorm_rope_bwd")
