@@ -775,7 +775,7 @@ class AdamWPlan:
     """The tensors of a step, checked and laid out once (adamw_plan); it keeps them alive and is good as long as they stay
     where they are: with other gradient tensors, make another plan."""
 
-    __slots__ = ("plan", "address", "image", "device", "tensors")
+    __slots__ = ("plan", "address", "image", "device", "tensors", "room")
 
 
 def _state_bits(m, v) -> int:
@@ -854,6 +854,7 @@ def adamw_plan(params, grads, exp_avgs, exp_avg_sqs, exp_avg_scales=None, exp_av
     self.device = torch.cuda.current_device() if dev is None else dev
     self.image = host[start:start + max(need, 16) // 8 + 1].to(torch.device("cuda", self.device))
     self.address = ctypes.addressof(self.plan)
+    self.room = int(lib().s2a_grad_norm_scratch_bytes(self.address))
     self.tensors = (list(grads),) + tuple(None if ts is None else list(ts) for ts in lists.values())
     return self
 
@@ -880,7 +881,7 @@ def s2a_adamw_step(plan: AdamWPlan, control, beta1: float = 0.9, beta2: float = 
 
 
 def grad_norm_scratch_bytes(plan: AdamWPlan) -> int:
-    return int(lib().s2a_grad_norm_scratch_bytes(plan.address))
+    return plan.room
 
 
 def s2a_grad_norm(plan: AdamWPlan, control, max_norm: float, clip, scratch) -> None:
@@ -888,7 +889,7 @@ def s2a_grad_norm(plan: AdamWPlan, control, max_norm: float, clip, scratch) -> N
     (float32, two elements).  scratch holds grad_norm_scratch_bytes(plan) bytes."""
     dev = _on_device(plan.image, control, clip, scratch)
     status = (_lib or lib()).s2a_grad_norm(plan.address, plan.image.data_ptr(), _float_words(control, 3, "control"), max_norm,
-                                           _float_words(clip, 2, "clip"), _scratch(scratch, grad_norm_scratch_bytes(plan)),
+                                           _float_words(clip, 2, "clip"), _scratch(scratch, plan.room),
                                            _stream_on(dev))
     if status:
         check(status)

@@ -276,6 +276,27 @@ def test_gradients_norm(gdt):
             assert abs(float(clip[1]) - factor) <= 8 * U * factor + TINY
 
 
+@pytest.mark.parametrize("gdt", ["f32", "bf16"])
+@pytest.mark.parametrize("blocks", [2047, 2048, 2049, 11839, 11840, 12200])
+def test_gradients_norm_of_many_blocks(gdt, blocks):
+    """Around the sizes at which the work is split in another way: tensors at odd places, a last block of one element.  The tolerance as above."""
+    flat = _normal((256 * blocks + 64,), torch.float32, "many", blocks).to(DT[gdt])
+    sizes, left, at, gs = [256 * 40, 256 * 7 + 1, 0, 255, 2, 256 * 500], blocks, 0, []
+    left -= sum((n + 255) // 256 for n in sizes)
+    for i, n in enumerate(sizes + [256 * (left - 1) + 1]):
+        gs.append(flat[at + i: at + i + n])
+        at += n
+    plan = s2a.adamw_plan(None, gs, None, None)
+    assert int(plan.plan.n_tensors) == len(gs) and sum((g.numel() + 255) // 256 for g in gs) == blocks
+    clip = torch.full((2,), 9.0, device="cuda")
+    scratch = torch.empty(s2a.grad_norm_scratch_bytes(plan), dtype=torch.uint8, device="cuda").fill_(0xFF)
+    s2a.s2a_grad_norm(plan, torch.tensor([0.0, 0.0, 1.0], device="cuda"), 2.0, clip, scratch)
+    _done()
+    norm = math.sqrt(sum(float(g.double().square().sum()) for g in gs))
+    assert abs(float(clip[0]) - norm) <= 8 * U * norm
+    assert abs(float(clip[1]) - 2.0 / (norm + 1e-6)) <= 8 * U
+
+
 def test_gradients_that_overflowed_change_nothing():
     for poison in (float("nan"), float("inf"), -float("inf")):
         ts = _tensors([1000, 30], torch.float32, torch.float32, 8, random.Random(1), "over", False)
