@@ -9,9 +9,11 @@
 // less than half a step of its code a step stays where it is (with b2 = 0.999 sqrt(v) moves by 0.05 %, a code's step is 6 to 12 %);
 // rounded at random, by the 16 bits of a counter-based generator, it moves as it should on average.
 //
-// Bound by memory: a warp takes 256 elements at a time, eight neighbouring ones a lane, everything of them in registers between
+// A warp takes 256 elements at a time, eight neighbouring ones a lane, everything of them in registers between
 // one load and one store, the block's largest magnitudes by two warp reductions.  What a warp takes from the plan
-// at a time is a chunk of such blocks; the plan has the tensor of each chunk, so that no warp searches.
+// at a time is a chunk of such blocks; the plan has the tensor of each chunk, so that no warp searches.  32-bit states are bound by
+// memory (302 M weights with bfloat16 gradients and copies 1.33 ms, 0.97 of a copy's rate); 8-bit states rounded at random by
+// the instructions of rounding and generator, some 400 a block and warp (the same weights in bfloat16 625 us, 0.74 of it).
 #include "s2a_launch.h"
 #include "s2a_oct.cuh"
 #include "s2a_philox.cuh"
@@ -402,8 +404,7 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const StepTensor& 
   }
 }
 
-// CTAs of an SM.  8-bit states: five, and two blocks of a warp's in registers at once (302 M weights: 664 us; 778 with four CTAs, 736 with six, 778 with
-// seven and one block).  32-bit states: a block is 128 bytes a lane already, and six CTAs with one block each take 10.6 M weights at odd places
+// CTAs of an SM.  8-bit states: five, and two blocks of a warp's in registers at once (302 M weights: 625 us; 645 with four CTAs, 647 with six).  32-bit states: a block is 128 bytes a lane already, and six CTAs with one block each take 10.6 M weights at odd places
 // in 49.6 us, four with two 56.
 template <int BITS> constexpr int kStepCtas = BITS == 8 ? 5 : 6;
 
