@@ -509,6 +509,58 @@ __device__ __forceinline__ float square_sum(const Raw<Io<GDT>::kBytes>& raw, dou
 
 constexpr uint32_t kAhead = 4;  // blocks in flight
 
+// A warp's part of the squares in plans whose chunks are single blocks: chunk `first` and those `stride` apart, eight at most.  They are looked up at
+// once, by a lane each (2.9 M gradients 4.3 us; one chunk after another, each a chain of three reads, 8.1).
+constexpr int kFewChunks = 8;
+
+template <int GDT>
+__device__ __forceinline__ double single_blocks_sum(const StepArgs& a, uint32_t first, uint32_t stride) {
+  constexpr int ES = Io<GDT>::kBytes;
+  constexpr bool QUAD = ES == 4;
+  const uint32_t lane = threadIdx.x & 31u, c = first + lane * stride;
+  const bool mine = lane < kFewChunks && c < a.n_chunks;
+  uint64_t at = 0;
+  int32_t left = 0, head = 0, before = 0;  // elements of the chunk, before the grid, and of these in the tensor
+  bool vec = false;
+  if (mine) {
+    const StepTensor& t = a.tensors[a.owner[c]];
+    vec = t.head != kStepScalar;
+    head = vec ? t.head : 0;
+    const uint64_t from = head + (uint64_t)(c - t.chunk0) * kStepBlock;
+    at = (uint64_t)t.g + from * ES;
+    left = from >= t.n ? 0 : (t.n - from < kStepBlock ? (int32_t)(t.n - from) : (int32_t)kStepBlock);
+    if (c == t.chunk0) before = t.n < (uint64_t)head ? (int32_t)t.n : head;
+  }
+  const int chunks = __popc(__ballot_sync(0xffffffffu, mine));
+  const int32_t place = (QUAD ? 4 : 8) * lane;
+  double sum = 0.0;
+#pragma unroll 1
+  for (int k = 0; k < chunks; k += kAhead) {
+    Raw<ES> raw[kAhead];
+#pragma unroll
+    for (int i = 0; i < (int)kAhead; ++i) {
+      const int32_t n = __shfl_sync(0xffffffffu, left, k + i) - place;
+      const uint64_t from = __shfl_sync(0xffffffffu, at, k + i);
+      const bool wide = __shfl_sync(0xffffffffu, (int)vec, k + i) != 0;
+      raw[i].load((const void*)from, Spot<QUAD>{(uint64_t)place, n < 0 ? 0 : n}, wide);
+    }
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < (int)kAhead; ++i) s += square_sum<GDT>(raw[i], sum);
+    sum += (double)s;
+  }
+  for (uint32_t rest = __ballot_sync(0xffffffffu, before > 0); rest; rest &= rest - 1) {  // the elements before the grid, at most seven
+    const int i = __ffs(rest) - 1;
+    const int32_t n = __shfl_sync(0xffffffffu, before, i) - (int32_t)(4 * lane);
+    const uint64_t from = __shfl_sync(0xffffffffu, at, i) - (uint64_t)__shfl_sync(0xffffffffu, head, i) * ES;
+    Raw<ES> front;
+    front.load((const void*)from, Spot<true>{4 * lane, n < 0 ? 0 : (n < 4 ? n : 4)}, false);
+    const float s = square_sum<GDT>(front, sum);
+    sum += (double)s;
+  }
+  return sum;
+}
+
 template <int GDT>
 __global__ void __launch_bounds__(kNormThreads, 4) grad_norm_kernel(const __grid_constant__ StepArgs a, double* partials) {
   __shared__ double buf[kNormWarps];
@@ -517,8 +569,9 @@ __global__ void __launch_bounds__(kNormThreads, 4) grad_norm_kernel(const __grid
   enter_grid();
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
   double sum = 0.0;
-  const uint32_t blocks = a.chunk_blocks;
-  for (uint64_t c = (uint64_t)blockIdx.x * kNormWarps + warp; c < a.n_chunks; c += (uint64_t)gridDim.x * kNormWarps) {
+  const uint32_t blocks = a.chunk_blocks, stride = gridDim.x * kNormWarps;
+  if (blocks == 1 && a.n_chunks <= kFewChunks * stride) sum = single_blocks_sum<GDT>(a, blockIdx.x * kNormWarps + warp, stride);
+  else for (uint64_t c = (uint64_t)blockIdx.x * kNormWarps + warp; c < a.n_chunks; c += stride) {
     const StepTensor& tensor = a.tensors[a.owner[c]];
     const void* const grad = tensor.g;
     const uint64_t from = (c - tensor.chunk0) * blocks * kStepBlock;
@@ -596,60 +649,18 @@ __global__ void __launch_bounds__(kFinishThreads) grad_norm_finish_kernel(const 
 }
 
 // Plans of few chunks, of one block each: one cluster, whose CTAs leave their sums in the first one's shared memory, in the place of a second
-// launch.  All chunks of a warp are looked up at once, by a lane each.  Up to 2048 chunks are faster so (16 384 gradients 2.6 us, two kernels
+// launch.  Up to 2048 chunks are faster so (16 384 gradients 2.6 us, two kernels
 // 3.1; 0.5 M 3.4, 3.9), and the host saves a launch; at 4090 both take 4.4 us.  Clusters of eight, the portable size, take 4.3 us for 0.5 M.
-constexpr int kFewCtas = 16, kFewWarps = 16, kFewChunks = 8;  // chunks: of a warp, at most
+constexpr int kFewCtas = 16, kFewWarps = 16;
 
 template <int GDT>
 __global__ void __cluster_dims__(kFewCtas) __launch_bounds__(kFewWarps * 32)
     grad_norm_few_kernel(const __grid_constant__ StepArgs a, float max_norm, float* out) {
   __shared__ double buf[kFewWarps], all[kFewCtas];
-  constexpr int ES = Io<GDT>::kBytes;
-  constexpr bool QUAD = ES == 4;
   enter_grid();
   const float scale = a.control[2];
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-  const uint32_t c = warp * kFewCtas + blockIdx.x + lane * (kFewCtas * kFewWarps);
-  const bool mine = lane < kFewChunks && c < a.n_chunks;
-  uint64_t at = 0;
-  int32_t left = 0, head = 0, before = 0;  // elements of the chunk, before the grid, and of these in the tensor
-  bool vec = false;
-  if (mine) {
-    const StepTensor& t = a.tensors[a.owner[c]];
-    vec = t.head != kStepScalar;
-    head = vec ? t.head : 0;
-    const uint64_t from = head + (uint64_t)(c - t.chunk0) * kStepBlock;
-    at = (uint64_t)t.g + from * ES;
-    left = from >= t.n ? 0 : (t.n - from < kStepBlock ? (int32_t)(t.n - from) : (int32_t)kStepBlock);
-    if (c == t.chunk0) before = t.n < (uint64_t)head ? (int32_t)t.n : head;
-  }
-  const int chunks = __popc(__ballot_sync(0xffffffffu, mine));
-  const int32_t place = (QUAD ? 4 : 8) * lane;
-  double sum = 0.0;
-#pragma unroll 1
-  for (int k = 0; k < chunks; k += kAhead) {
-    Raw<ES> raw[kAhead];
-#pragma unroll
-    for (int i = 0; i < (int)kAhead; ++i) {
-      const int32_t n = __shfl_sync(0xffffffffu, left, k + i) - place;
-      const uint64_t from = __shfl_sync(0xffffffffu, at, k + i);
-      const bool wide = __shfl_sync(0xffffffffu, (int)vec, k + i) != 0;
-      raw[i].load((const void*)from, Spot<QUAD>{(uint64_t)place, n < 0 ? 0 : n}, wide);
-    }
-    float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < (int)kAhead; ++i) s += square_sum<GDT>(raw[i], sum);
-    sum += (double)s;
-  }
-  for (uint32_t rest = __ballot_sync(0xffffffffu, before > 0); rest; rest &= rest - 1) {  // the elements before the grid, at most seven
-    const int i = __ffs(rest) - 1;
-    const int32_t n = __shfl_sync(0xffffffffu, before, i) - (int32_t)(4 * lane);
-    const uint64_t from = __shfl_sync(0xffffffffu, at, i) - (uint64_t)__shfl_sync(0xffffffffu, head, i) * ES;
-    Raw<ES> front;
-    front.load((const void*)from, Spot<true>{4 * lane, n < 0 ? 0 : (n < 4 ? n : 4)}, false);
-    const float s = square_sum<GDT>(front, sum);
-    sum += (double)s;
-  }
+  double sum = single_blocks_sum<GDT>(a, warp * kFewCtas + blockIdx.x, kFewCtas * kFewWarps);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) buf[warp] = sum;
