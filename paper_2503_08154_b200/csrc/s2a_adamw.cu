@@ -12,8 +12,8 @@
 // A warp takes 256 elements at a time, eight neighbouring ones a lane, everything of them in registers between
 // one load and one store, the block's largest magnitudes by two warp reductions.  What a warp takes from the plan
 // at a time is a chunk of such blocks; the plan has the tensor of each chunk, so that no warp searches.  32-bit states are bound by
-// memory (302 M weights with bfloat16 gradients and copies 1.33 ms, 0.97 of a copy's rate); 8-bit states rounded at random by
-// the instructions of rounding and generator, some 400 a block and warp (the same weights in bfloat16 625 us, 0.74 of it).
+// memory (302 M weights with bfloat16 gradients and copies 1.30 ms, a copy's rate); 8-bit states rounded at random by
+// the instructions of rounding and generator, some 400 a block and warp (the same weights in bfloat16 607 us, 0.76 of it).
 #include "s2a_launch.h"
 #include "s2a_oct.cuh"
 #include "s2a_philox.cuh"
@@ -404,7 +404,7 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const StepTensor& 
   }
 }
 
-// CTAs of an SM.  8-bit states: five, and two blocks of a warp's in registers at once (302 M weights: 625 us; 645 with four CTAs, 647 with six).  32-bit states: a block is 128 bytes a lane already, and six CTAs with one block each take 10.6 M weights at odd places
+// CTAs of an SM.  8-bit states: five, and two blocks of a warp's in registers at once (302 M weights, with four times as many CTAs as fit: 625 us; 645 with four an SM, 647 with six).  32-bit states: a block is 128 bytes a lane already, and six CTAs with one block each take 10.6 M weights at odd places
 // in 49.6 us, four with two 56.
 template <int BITS> constexpr int kStepCtas = BITS == 8 ? 5 : 6;
 
@@ -439,10 +439,12 @@ __global__ void __launch_bounds__(kStepThreads, kStepCtas<BITS>) adamw_kernel(co
   k.grad1 = scale * a.one_beta1;
   k.grad2 = scale * a.root_one_beta2;
   k.count = RANDOM ? a.rng[1] + a.site : 0ull;
-  const uint32_t blocks = a.chunk_blocks;
-  for (uint64_t c = (uint64_t)blockIdx.x * kStepWarps + (threadIdx.x >> 5); c < a.n_chunks; c += (uint64_t)gridDim.x * kStepWarps) {
+  const uint32_t split = BITS == 8 ? a.split : 0u, blocks = a.chunk_blocks >> split;
+  for (uint64_t part = (uint64_t)blockIdx.x * kStepWarps + (threadIdx.x >> 5); part < (uint64_t)a.n_chunks << split;
+       part += (uint64_t)gridDim.x * kStepWarps) {
+    const uint32_t c = (uint32_t)(part >> split);
     const StepTensor t = a.tensors[a.owner[c]];
-    const uint64_t block = (c - t.chunk0) * blocks, from = block * kStepBlock;
+    const uint64_t block = (part - ((uint64_t)t.chunk0 << split)) * blocks, from = block * kStepBlock;
     const bool vec = COUNTED ? t.head == 0u : t.head != kStepScalar;
     const uint32_t head = vec ? t.head : 0u;
     if (QUAD && head && from == 0) {  // the elements before the grid, as a block of two lanes'
@@ -709,11 +711,16 @@ cudaError_t launch_adamw_types(int bits, const StepArgs& a, unsigned grid, cudaS
 
 }  // namespace
 
-cudaError_t launch_adamw(int pdt, int gdt, int state_bits, const StepArgs& a, cudaStream_t st) {
+cudaError_t launch_adamw(int pdt, int gdt, int state_bits, StepArgs a, cudaStream_t st) {
   if (a.n_chunks == 0) return cudaSuccess;
+  // 8-bit states: chunks of four blocks in halves, the two blocks that are in registers at once (8.0 M weights 24 us, whole 27.5; 28 M 71 and 77);
+  // chunks of sixteen whole (302 M weights 607 us, 698 in parts of two to eight)
+  a.split = state_bits == 8 && a.chunk_blocks == 4 ? 1 : 0;
   const uint64_t resident = (uint64_t)sm_count() * (state_bits == 8 ? kStepCtas<8> : kStepCtas<32>);  // CTAs at once
-  // four times as many CTAs as fit: the last ones even out what the SMs have left
-  const uint64_t want = ((uint64_t)a.n_chunks + kStepWarps - 1) / kStepWarps, cap = resident * 4;
+  // Sixteen times as many CTAs as fit, whose last ones even out what the SMs have left (302 M weights: 32-bit states 1298 us, 1397 with as many as
+  // fit; 8-bit states 607, 650); where 8-bit states have few blocks a CTA, its start counts for more (2.4 M weights 10.5 us, 13.6 with four times
+  // as many as fit).
+  const uint64_t want = (((uint64_t)a.n_chunks << a.split) + kStepWarps - 1) / kStepWarps, cap = resident * (state_bits == 8 && a.chunk_blocks < 16 ? 1 : 16);
   const unsigned grid = (unsigned)(want < cap ? want : cap);
   if (pdt == kF32)
     return gdt == kF32 ? launch_adamw_types<kF32, kF32>(state_bits, a, grid, st) : launch_adamw_types<kF32, kBF16>(state_bits, a, grid, st);

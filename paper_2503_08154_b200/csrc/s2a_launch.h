@@ -152,8 +152,9 @@ struct StepArgs {
   uint64_t site;
   float beta1, one_beta1, beta2, root_beta2, root_one_beta2, log_beta1, log_beta2, eps;  // root: sqrt(beta2), sqrt(1 - beta2)
   uint32_t chunk_blocks;  // blocks of a chunk, which a warp takes at a time: 1, 4 or 16
+  uint32_t split;         // or 2^-split of them (the step with 8-bit states)
 };
-cudaError_t launch_adamw(int pdt, int gdt, int state_bits, const StepArgs& a, cudaStream_t st);
+cudaError_t launch_adamw(int pdt, int gdt, int state_bits, StepArgs a, cudaStream_t st);
 uint64_t grad_norm_scratch_bytes(uint32_t n_chunks);
 cudaError_t launch_grad_norm(int gdt, const StepArgs& a, float max_norm, float* out, double* scratch, cudaStream_t st);
 
