@@ -162,8 +162,7 @@ def _clone(ts):
     return [{n: v.clone() for n, v in t.items()} for t in ts]
 
 
-def _check_step(before, after, hyper, bits, decay, rate, rng=None, site=0, clip=None, pdt=torch.float32):
-    block0 = 0
+def _check_step(before, after, hyper, bits, decay, rate, rng=None, site=0, clip=None, pdt=torch.float32, block0=0):
     for i, (b, a) in enumerate(zip(before, after)):
         n = b["p"].numel()
         if n == 0:
@@ -277,7 +276,7 @@ def test_gradients_norm(gdt):
 
 
 @pytest.mark.parametrize("gdt", ["f32", "bf16"])
-@pytest.mark.parametrize("blocks", [2047, 2048, 2049, 11839, 11840, 12200])
+@pytest.mark.parametrize("blocks", [2047, 2048, 2049, 11839, 11840, 12200, 757_760])
 def test_gradients_norm_of_many_blocks(gdt, blocks):
     """Around the sizes at which the work is split in another way: tensors at odd places, a last block of one element.  The tolerance as above."""
     flat = _normal((256 * blocks + 64,), torch.float32, "many", blocks).to(DT[gdt])
@@ -462,6 +461,55 @@ def test_many_tensors_at_once():
     for i, (a, b) in enumerate(zip(before, ts)):
         if i not in pick:
             assert not torch.equal(a["p"], b["p"])
+
+
+class _Places(random.Random):
+    """Offsets in the order given (a tensor takes its own, its gradient's, and one that is drawn between them)."""
+
+    def __init__(self, places):
+        super().__init__(8)
+        self.places = list(places)
+
+    def choice(self, among):
+        return self.places.pop(0)
+
+
+@pytest.mark.parametrize("pdt,gdt,bits,random_bits", [("bf16", "bf16", 8, True), ("f32", "bf16", 8, False), ("f32", "f32", 8, True),
+                                                      ("f32", "bf16", 32, False), ("bf16", "bf16", 32, True)])
+@pytest.mark.parametrize("blocks", [11_839, 11_840, 12_345, 757_759, 757_760])
+def test_step_of_many_blocks(pdt, gdt, bits, random_bits, blocks):
+    """On both sides of the sizes at which a warp takes more blocks at a time: tensors that begin and end inside of what it takes, on the
+    16-byte grid and beside it."""
+    ends = [1000, 256 * 1003 + 5, 300, 777]
+    sizes = ends[:2] + [256 * (blocks - 1 - sum(-(-n // 256) for n in ends)) + 9] + ends[2:]
+    assert sum(-(-n // 256) for n in sizes) == blocks
+    copies = pdt == "f32"
+    for beside in ((1, 2), (2, 4)) if blocks < 20_000 else ((1, 3),):   # the tensors that lie off the grid
+        places = []
+        for i in range(len(sizes)):
+            at = 3 if i in beside else 0
+            places += [at, 5, at]
+        ts = _tensors(sizes, DT[pdt], DT[gdt], bits, _Places(places), (pdt, gdt, bits, blocks), copies)
+        before = _clone(ts)
+        hyper = (float(torch.tensor(1e-2)), 7.0, 0.25, 0.9, 0.999, 1e-8)
+        draws = (77, 12)
+        state = torch.tensor(draws, dtype=torch.int64, device="cuda") if random_bits else None
+        s2a.s2a_adamw_step(_plan(ts, bits, copies, 0.1), torch.tensor(hyper[:3], device="cuda"), *hyper[3:], rng=state, site=3)
+        _done()
+        block0 = 0
+        for b, a, n in zip(before, ts, sizes):
+            long = 256 * 70
+            for start in sorted({0, max(0, n // 512 * 256 - long), max(0, n - long) // 256 * 256}):
+                stop = min(n, start + long + 256)
+                rows = slice(start // 256, -(-stop // 256))
+                part = [{name: t[name][rows] if name in ("ms", "vs") else t[name][start:stop] for name in t} for t in (b, a)]
+                _check_step(part[:1], part[1:], hyper, bits, [0.1], [1.0], draws if random_bits else None, 3, pdt=DT[pdt],
+                            block0=block0 + start // 256)
+            moved = a["p"] != b["p"]
+            # No block is left out: each update is some 1.6e-3 of its weight or more (the decay alone 1e-3), a fifth of a bfloat16 step at random, and 256
+            # weights stay where they are once in 0.8^-256 = 1e24 blocks; binary32 weights of 1e-3 and more all move.
+            assert bool(moved[: n // 256 * 256].view(-1, 256).any(1).all())
+            block0 += -(-n // 256)
 
 
 def test_beta_zero_and_betas_near_one():
