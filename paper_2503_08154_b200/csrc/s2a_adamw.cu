@@ -659,6 +659,7 @@ template <int GDT>
 __global__ void __cluster_dims__(kFewCtas) __launch_bounds__(kFewWarps * 32)
     grad_norm_few_kernel(const __grid_constant__ StepArgs a, float max_norm, float* out) {
   __shared__ double buf[kFewWarps], all[kFewCtas];
+  asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");  // "this CTA has started": awaited before one writes to another
   enter_grid();
   const float scale = a.control[2];
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
@@ -666,6 +667,7 @@ __global__ void __cluster_dims__(kFewCtas) __launch_bounds__(kFewWarps * 32)
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) buf[warp] = sum;
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
   __syncthreads();
   if (threadIdx.x == 0) {
 #pragma unroll
