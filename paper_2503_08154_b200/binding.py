@@ -606,6 +606,7 @@ _rope_call = struct.Struct("@13Pq2f3i0q").pack
 _rope_sizes = struct.Struct("@27Q").pack
 _rope_layouts = {}   # the second part, with what else is known of it, by the shapes, strides and dtypes of a call's tensors
 
+
 def rope_table(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, original_length: float = 0.0,
                slow: float = 1.0, fast: float = 32.0, axes: int = 1) -> torch.Tensor:
     """The turns of each pair as a CPU int64 tensor [rot_dim / 2, 2] (s2a_rope_table), to be moved to the GPU once.

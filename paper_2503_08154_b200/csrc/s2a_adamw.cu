@@ -215,8 +215,8 @@ __device__ __forceinline__ void random_bf16(const F2 (&p)[4], const uint4& bits,
 }
 
 // The e4m3 codes of eight values x / scale * 448, |x| at most the scale, with 16 random bits and half of one below the last kept bit.
-// Times 2^-120 (LARGE: apart from `inverse`, which would leave the normal range) the type's exponents are those of binary32, its subnormals too: a code is what stands from
-// bit 20 on, moved to bit 24 here, so that a code is a byte and each field of random bits lies where one byte permutation puts it.  (The
+// Times 2^-120 (LARGE: apart from `inverse`, which would leave the normal range) the type's exponents are those of binary32, its subnormals too:
+// a code is what stands from bit 20 on, moved to bit 24 here, so that a code is a byte and each field of random bits lies where one byte permutation puts it.  (The
 // largest is at most two roundings above 448, and with the bits below the code at most 0xFFFF80 cannot carry.)  SIGNED: m; otherwise sqrt(v),
 // whose fields have their bytes exchanged and which is never rounded from above zero to zero.
 template <bool SIGNED, bool LARGE>
@@ -404,7 +404,8 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const StepTensor& 
   }
 }
 
-// CTAs of an SM.  8-bit states: five, and two blocks of a warp's in registers at once (302 M weights, with four times as many CTAs as fit: 625 us; 645 with four an SM, 647 with six).  32-bit states: a block is 128 bytes a lane already, and six CTAs with one block each take 10.6 M weights at odd places
+// CTAs of an SM.  8-bit states: five, and two blocks of a warp's in registers at once (302 M weights, with four times as many CTAs as fit: 625 us;
+// 645 with four an SM, 647 with six).  32-bit states: a block is 128 bytes a lane already, and six CTAs with one block each take 10.6 M weights at odd places
 // in 49.6 us, four with two 56.
 template <int BITS> constexpr int kStepCtas = BITS == 8 ? 5 : 6;
 
@@ -511,103 +512,95 @@ __device__ __forceinline__ float square_sum(const Raw<Io<GDT>::kBytes>& raw, dou
 
 constexpr uint32_t kAhead = 4;  // blocks in flight
 
-// A warp's part of the squares in plans whose chunks are single blocks: chunk `first` and those `stride` apart, eight at most.  They are looked up at
-// once, by a lane each (2.9 M gradients 4.3 us; one chunk after another, each a chain of three reads, 8.1).
-constexpr int kFewChunks = 8;
+// A warp's part of the squares: chunk `first` and those `stride` apart.  Eight chunks are looked up at once, by a lane each (2.9 M gradients
+// 4.3 us; one chunk after another, each a chain of three reads, 8.1).
+constexpr uint32_t kLooks = 8;
 
-template <int GDT>
-__device__ __forceinline__ double single_blocks_sum(const StepArgs& a, uint32_t first, uint32_t stride) {
+// SINGLE: chunks are single blocks.
+template <int GDT, bool SINGLE>
+__device__ __forceinline__ double chunk_squares(const StepArgs& a, uint32_t first, uint32_t stride) {
   constexpr int ES = Io<GDT>::kBytes;
   constexpr bool QUAD = ES == 4;
-  const uint32_t lane = threadIdx.x & 31u, c = first + lane * stride;
-  const bool mine = lane < kFewChunks && c < a.n_chunks;
-  uint64_t at = 0;
-  int32_t left = 0, head = 0, before = 0;  // elements of the chunk, before the grid, and of these in the tensor
-  bool vec = false;
-  if (mine) {
-    const StepTensor& t = a.tensors[a.owner[c]];
-    vec = t.head != kStepScalar;
-    head = vec ? t.head : 0;
-    const uint64_t from = head + (uint64_t)(c - t.chunk0) * kStepBlock;
-    at = (uint64_t)t.g + from * ES;
-    left = from >= t.n ? 0 : (t.n - from < kStepBlock ? (int32_t)(t.n - from) : (int32_t)kStepBlock);
-    if (c == t.chunk0) before = t.n < (uint64_t)head ? (int32_t)t.n : head;
-  }
-  const int chunks = __popc(__ballot_sync(0xffffffffu, mine));
-  const int32_t place = (QUAD ? 4 : 8) * lane;
+  const uint32_t lane = threadIdx.x & 31u;
+  const int32_t place = (QUAD ? 4 : 8) * lane, chunk = (SINGLE ? 1 : a.chunk_blocks) * kStepBlock;
   double sum = 0.0;
-#pragma unroll 1
-  for (int k = 0; k < chunks; k += kAhead) {
-    Raw<ES> raw[kAhead];
-#pragma unroll
-    for (int i = 0; i < (int)kAhead; ++i) {
-      const int32_t n = __shfl_sync(0xffffffffu, left, k + i) - place;
-      const uint64_t from = __shfl_sync(0xffffffffu, at, k + i);
-      const bool wide = __shfl_sync(0xffffffffu, (int)vec, k + i) != 0;
-      raw[i].load((const void*)from, Spot<QUAD>{(uint64_t)place, n < 0 ? 0 : n}, wide);
+  for (uint32_t base = first; base < a.n_chunks; base += kLooks * stride) {  // (chunks are fewer than 2^31)
+    const uint32_t c = base + lane * stride;
+    const bool mine = lane < kLooks && c < a.n_chunks;
+    uint64_t at = 0;
+    int32_t left = 0, head = 0, before = 0;  // elements of the chunk, before the grid, and of these in the tensor
+    bool vec = false;
+    if (mine) {
+      const StepTensor& t = a.tensors[a.owner[c]];
+      vec = t.head != kStepScalar;
+      head = vec ? t.head : 0;
+      const uint64_t from = head + (uint64_t)(c - t.chunk0) * chunk;
+      at = (uint64_t)t.g + from * ES;
+      left = from >= t.n ? 0 : (t.n - from < (uint64_t)chunk ? (int32_t)(t.n - from) : chunk);
+      if (c == t.chunk0) before = t.n < (uint64_t)head ? (int32_t)t.n : head;
     }
-    float s = 0.0f;
-#pragma unroll
-    for (int i = 0; i < (int)kAhead; ++i) s += square_sum<GDT>(raw[i], sum);
-    sum += (double)s;
-  }
-  for (uint32_t rest = __ballot_sync(0xffffffffu, before > 0); rest; rest &= rest - 1) {  // the elements before the grid, at most seven
-    const int i = __ffs(rest) - 1;
-    const int32_t n = __shfl_sync(0xffffffffu, before, i) - (int32_t)(4 * lane);
-    const uint64_t from = __shfl_sync(0xffffffffu, at, i) - (uint64_t)__shfl_sync(0xffffffffu, head, i) * ES;
-    Raw<ES> front;
-    front.load((const void*)from, Spot<true>{4 * lane, n < 0 ? 0 : (n < 4 ? n : 4)}, false);
-    const float s = square_sum<GDT>(front, sum);
-    sum += (double)s;
-  }
-  return sum;
-}
-
-template <int GDT>
-__global__ void __launch_bounds__(kNormThreads, 4) grad_norm_kernel(const __grid_constant__ StepArgs a, double* partials) {
-  __shared__ double buf[kNormWarps];
-  constexpr int ES = Io<GDT>::kBytes;
-  constexpr bool QUAD = ES == 4;
-  enter_grid();
-  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-  double sum = 0.0;
-  const uint32_t blocks = a.chunk_blocks, stride = gridDim.x * kNormWarps;
-  if (blocks == 1 && a.n_chunks <= kFewChunks * stride) sum = single_blocks_sum<GDT>(a, blockIdx.x * kNormWarps + warp, stride);
-  else for (uint64_t c = (uint64_t)blockIdx.x * kNormWarps + warp; c < a.n_chunks; c += stride) {
-    const StepTensor& tensor = a.tensors[a.owner[c]];
-    const void* const grad = tensor.g;
-    const uint64_t from = (c - tensor.chunk0) * blocks * kStepBlock;
-    const bool vec = tensor.head != kStepScalar;
-    const uint32_t head = vec ? tensor.head : 0u;
-    const uint64_t base = head + from + (QUAD ? 4 : 8) * lane, end = head + from + (uint64_t)blocks * kStepBlock;
-    const uint64_t n = tensor.n < end ? tensor.n : end;  // where the chunk ends
-    if (head && from == 0) {  // the elements before the grid
-      const uint64_t before = n < head ? n : head;
-      Raw<ES> front;
-      front.load(grad, Spot<true>{4 * lane, (int32_t)(before > 4 * lane ? (before - 4 * lane < 4 ? before - 4 * lane : 4) : 0)}, false);
-      const float s = square_sum<GDT>(front, sum);
-      sum += (double)s;
-    }
-#pragma unroll 1
-    for (uint32_t k = 0; k < blocks; k += kAhead) {
-      if (head + from + k * kStepBlock >= n) break;
-      Raw<ES> raw[kAhead];
-      if (vec && head + from + (k + kAhead) * kStepBlock <= n) {
-#pragma unroll
-        for (uint32_t i = 0; i < kAhead; ++i) raw[i].load(grad, Spot<QUAD, true>{base + (k + i) * kStepBlock, 256}, true);
-      } else {
-#pragma unroll
-        for (uint32_t i = 0; i < kAhead; ++i) {
-          const uint64_t first = base + (k + i) * kStepBlock;
-          raw[i].load(grad, Spot<QUAD>{first, first >= n ? 0 : (n - first < 256 ? (int32_t)(n - first) : 256)}, vec);
-        }
-      }
+    const int chunks = __popc(__ballot_sync(0xffffffffu, mine));
+    const auto add = [&](const Raw<ES> (&raw)[kAhead]) {
       float s = 0.0f;
 #pragma unroll
       for (uint32_t i = 0; i < kAhead; ++i) s += square_sum<GDT>(raw[i], sum);
       sum += (double)s;  // of 32 elements, each eight from 2^-80 to 2^100
+    };
+    if constexpr (SINGLE) {  // blocks of several chunks in flight
+#pragma unroll 1
+      for (int k = 0; k < chunks; k += kAhead) {
+        Raw<ES> raw[kAhead];
+#pragma unroll
+        for (int i = 0; i < (int)kAhead; ++i) {
+          const int32_t n = __shfl_sync(0xffffffffu, left, k + i) - place;
+          const uint64_t from = __shfl_sync(0xffffffffu, at, k + i);
+          const bool wide = __shfl_sync(0xffffffffu, (int)vec, k + i) != 0;
+          raw[i].load((const void*)from, Spot<QUAD>{(uint64_t)place, n < 0 ? 0 : n}, wide);
+        }
+        add(raw);
+      }
+    } else {
+#pragma unroll 1
+      for (int k = 0; k < chunks; ++k) {
+        int32_t n = __shfl_sync(0xffffffffu, left, k);
+        uint64_t from = __shfl_sync(0xffffffffu, at, k);
+        const bool wide = __shfl_sync(0xffffffffu, (int)vec, k) != 0;
+#pragma unroll 1
+        for (; n > 0; n -= kAhead * kStepBlock, from += kAhead * kStepBlock * ES) {
+          Raw<ES> raw[kAhead];
+          if (wide && n >= (int32_t)(kAhead * kStepBlock)) {
+#pragma unroll
+            for (uint32_t i = 0; i < kAhead; ++i) raw[i].load((const void*)from, Spot<QUAD, true>{place + i * kStepBlock, 256}, true);
+          } else {
+#pragma unroll
+            for (uint32_t i = 0; i < kAhead; ++i) {
+              const int32_t rest = n - (int32_t)(i * kStepBlock) - place;
+              raw[i].load((const void*)from, Spot<QUAD>{place + i * kStepBlock, rest < 0 ? 0 : (rest < 256 ? rest : 256)}, wide);
+            }
+          }
+          add(raw);
+        }
+      }
+    }
+    for (uint32_t rest = __ballot_sync(0xffffffffu, before > 0); rest; rest &= rest - 1) {  // the elements before the grid, at most seven
+      const int i = __ffs(rest) - 1;
+      const int32_t n = __shfl_sync(0xffffffffu, before, i) - (int32_t)(4 * lane);
+      const uint64_t from = __shfl_sync(0xffffffffu, at, i) - (uint64_t)__shfl_sync(0xffffffffu, head, i) * ES;
+      Raw<ES> front;
+      front.load((const void*)from, Spot<true>{4 * lane, n < 0 ? 0 : (n < 4 ? n : 4)}, false);
+      const float s = square_sum<GDT>(front, sum);
+      sum += (double)s;
     }
   }
+  return sum;
+}
+
+template <int GDT, bool SINGLE>
+__global__ void __launch_bounds__(kNormThreads, 4) grad_norm_kernel(const __grid_constant__ StepArgs a, double* partials) {
+  __shared__ double buf[kNormWarps];
+  enter_grid();
+  const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+  double sum = chunk_squares<GDT, SINGLE>(a, blockIdx.x * kNormWarps + warp, gridDim.x * kNormWarps);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) buf[warp] = sum;
@@ -663,7 +656,7 @@ __global__ void __cluster_dims__(kFewCtas) __launch_bounds__(kFewWarps * 32)
   enter_grid();
   const float scale = a.control[2];
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
-  double sum = single_blocks_sum<GDT>(a, warp * kFewCtas + blockIdx.x, kFewCtas * kFewWarps);
+  double sum = chunk_squares<GDT, true>(a, warp * kFewCtas + blockIdx.x, kFewCtas * kFewWarps);
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, o);
   if (lane == 0) buf[warp] = sum;
@@ -736,11 +729,12 @@ uint64_t grad_norm_scratch_bytes(uint32_t n_chunks) {
 }
 
 cudaError_t launch_grad_norm(int gdt, const StepArgs& a, float max_norm, float* out, double* scratch, cudaStream_t st) {
-  if (a.chunk_blocks == 1 && a.n_chunks <= kFewCtas * kFewWarps * kFewChunks)
+  if (a.chunk_blocks == 1 && a.n_chunks <= kFewCtas * kFewWarps * kLooks)
     return gdt == kF32 ? launch_grad_norm_few<kF32>(a, max_norm, out, st) : launch_grad_norm_few<kBF16>(a, max_norm, out, st);
   const unsigned grid = (unsigned)(grad_norm_scratch_bytes(a.n_chunks) / sizeof(double));
-  const cudaError_t e = gdt == kF32 ? launch_overlapped(grad_norm_kernel<kF32>, dim3(grid), kNormThreads, 0, st, a, scratch)
-                                    : launch_overlapped(grad_norm_kernel<kBF16>, dim3(grid), kNormThreads, 0, st, a, scratch);
+  const auto go = [&](void (*kernel)(const StepArgs, double*)) { return launch_overlapped(kernel, dim3(grid), kNormThreads, 0, st, a, scratch); };
+  const cudaError_t e = a.chunk_blocks == 1 ? (gdt == kF32 ? go(grad_norm_kernel<kF32, true>) : go(grad_norm_kernel<kBF16, true>))
+                                            : (gdt == kF32 ? go(grad_norm_kernel<kF32, false>) : go(grad_norm_kernel<kBF16, false>));
   if (e != cudaSuccess) return e;
   return launch_overlapped(grad_norm_finish_kernel, dim3(1), kFinishThreads, 0, st, (const double*)scratch, grid, a.control, max_norm, out);
 }
