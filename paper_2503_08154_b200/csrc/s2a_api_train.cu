@@ -125,7 +125,7 @@ int run_rope(const s2a_rope_args* args, int mode, int back, void* stream) {
   RopeArgs a = {};
   Rows wrote[2], had[4];
   const void* had_at[4];
-  int n = 0;
+  int had_by[4], n = 0;  // queries' or keys'
   for (int i = 0; i < 2 && !empty; ++i) {
     if (heads[i] == 0) continue;
     if (!in[i] || !out[i] || (bwd && !grad[i])) return S2A_ERR_NULL;
@@ -136,9 +136,11 @@ int run_rope(const s2a_rope_args* args, int mode, int back, void* stream) {
       return make_rows(s, c.batch, c.tokens, heads[i], c.head_dim, es, r);
     };
     had_at[n] = in[i];
+    had_by[n] = i;
     if (!take(in[i], in_stride[i], a.in[i], had[n++])) return S2A_ERR_SHAPE;
     if (bwd) {
       had_at[n] = grad[i];
+      had_by[n] = i;
       if (!take(grad[i], grad_stride[i], a.grad[i], had[n++])) return S2A_ERR_SHAPE;
     }
     if (!take(out[i], out_stride[i], a.out[i], wrote[i]) || folds(wrote[i])) return S2A_ERR_SHAPE;
@@ -147,8 +149,8 @@ int run_rope(const s2a_rope_args* args, int mode, int back, void* stream) {
   for (int i = 0; i < 2 && !empty; ++i) {
     if (heads[i] == 0) continue;
     for (int j = 0; j < n; ++j) {
-      const bool own = had_at[j] == in[i] || (bwd && had_at[j] == grad[i]);
-      if (own && had_at[j] == out[i] && same_rows(had[j], wrote[i])) continue;  // in place
+      // in place: a warp has read a row of the output's own input before it writes there; the other side's it reads at any time
+      if (had_by[j] == i && had_at[j] == out[i] && same_rows(had[j], wrote[i])) continue;
       if (tensors_meet(had_at[j], had[j], out[i], wrote[i])) return S2A_ERR_OVERLAP;
     }
     if (i == 1 && heads[0] && tensors_meet(out[0], wrote[0], out[1], wrote[1])) return S2A_ERR_OVERLAP;

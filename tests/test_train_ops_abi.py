@@ -256,3 +256,27 @@ def test_binding_refuses_what_is_not_on_a_gpu():
     for lists in (([x], [x, x], [x], [x]), (None, [x], [x], None), ([x], [x], None, [x])):
         with pytest.raises(binding.S2AError):
             binding.adamw_plan(*lists)
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_in_place_is_of_the_own_input_alone(lib, name):
+    """An output may be the input that it belongs to; where the same tensor is the other side's input too, that one would be read while it
+    is written."""
+    def call(**changes):
+        same = {"heads_k": 4, "k_stride": (8 * 256, 256, 64), "out_k_stride": (8 * 256, 256, 64), "grad_k_stride": (8 * 256, 256, 64)}
+        return getattr(lib, name)(_args(**same | changes), None)
+
+    for same in ({"k": A, "out_q": A}, {"k": A, "out_k": A}, {"q": B, "out_k": B}, {"q": B, "out_q": B}):
+        assert call(**same) == OVERLAP, same
+    # one head each
+    ones = {"heads_q": 1, "heads_k": 1} | {n: (8 * 64, 64, 64) for n in STRIDES}
+    assert call(k=A, out_q=A, **ones) == OVERLAP and call(k=A, out_k=A, **ones) == OVERLAP
+    if name == "s2a_qknorm_rope_bwd":
+        for same in ({"grad_k": G, "out_q": G}, {"grad_k": G, "out_k": G}, {"grad_q": B, "out_q": B}, {"k": G, "out_q": G}):
+            assert call(**same) == OVERLAP, same
+    if not torch.cuda.is_available():       # what is allowed passes every check; there is no GPU to launch on
+        for fine in ({"k": A}, {"out_q": A}, {"out_k": B}, {"out_q": A, "out_k": B}):
+            assert call(**fine) == CUDA, fine
+        if name == "s2a_qknorm_rope_bwd":
+            for fine in ({"out_q": G}, {"out_k": G + 0x100000}, {"grad_q": A, "out_q": A}, {"grad_k": G, "k": A}, {"q": G, "grad_k": A, "out_q": G}):
+                assert call(**fine) == CUDA, fine
