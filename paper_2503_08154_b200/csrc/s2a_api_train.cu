@@ -82,11 +82,9 @@ bool rows_meet(const Rows& a, int ia, const Rows& b, int ib, long long delta) {
   return true;
 }
 
-bool same_rows(const Rows& a, const Rows& b) {
-  if (a.dims != b.dims || a.row != b.row) return false;
-  for (int i = 0; i < a.dims; ++i)
-    if (a.n[i] != b.n[i] || a.s[i] != b.s[i]) return false;
-  return true;
+// Whether each row of the one is that of the other.
+bool same_place(const HeadsArg& a, const HeadsArg& b) {
+  return a.data == b.data && a.batch == b.batch && a.token == b.token && a.head == b.head;
 }
 
 bool tensors_meet(const void* pa, const Rows& a, const void* pb, const Rows& b) {
@@ -124,8 +122,8 @@ int run_rope(const s2a_rope_args* args, int mode, int back, void* stream) {
   }
   RopeArgs a = {};
   Rows wrote[2], had[4];
-  const void* had_at[4];
-  int had_by[4], n = 0;  // queries' or keys'
+  const HeadsArg* had_by[4];
+  int had_side[4], n = 0;  // queries' or keys'
   for (int i = 0; i < 2 && !empty; ++i) {
     if (heads[i] == 0) continue;
     if (!in[i] || !out[i] || (bwd && !grad[i])) return S2A_ERR_NULL;
@@ -135,12 +133,12 @@ int run_rope(const s2a_rope_args* args, int mode, int back, void* stream) {
       h = HeadsArg{p, c.batch > 1 ? s[0] : 0, c.tokens > 1 ? s[1] : 0, heads[i] > 1 ? s[2] : 0};
       return make_rows(s, c.batch, c.tokens, heads[i], c.head_dim, es, r);
     };
-    had_at[n] = in[i];
-    had_by[n] = i;
+    had_by[n] = &a.in[i];
+    had_side[n] = i;
     if (!take(in[i], in_stride[i], a.in[i], had[n++])) return S2A_ERR_SHAPE;
     if (bwd) {
-      had_at[n] = grad[i];
-      had_by[n] = i;
+      had_by[n] = &a.grad[i];
+      had_side[n] = i;
       if (!take(grad[i], grad_stride[i], a.grad[i], had[n++])) return S2A_ERR_SHAPE;
     }
     if (!take(out[i], out_stride[i], a.out[i], wrote[i]) || folds(wrote[i])) return S2A_ERR_SHAPE;
@@ -150,8 +148,8 @@ int run_rope(const s2a_rope_args* args, int mode, int back, void* stream) {
     if (heads[i] == 0) continue;
     for (int j = 0; j < n; ++j) {
       // in place: a warp has read a row of the output's own input before it writes there; the other side's it reads at any time
-      if (had_by[j] == i && had_at[j] == out[i] && same_rows(had[j], wrote[i])) continue;
-      if (tensors_meet(had_at[j], had[j], out[i], wrote[i])) return S2A_ERR_OVERLAP;
+      if (had_side[j] == i && same_place(*had_by[j], a.out[i])) continue;
+      if (tensors_meet(had_by[j]->data, had[j], out[i], wrote[i])) return S2A_ERR_OVERLAP;
     }
     if (i == 1 && heads[0] && tensors_meet(out[0], wrote[0], out[1], wrote[1])) return S2A_ERR_OVERLAP;
   }

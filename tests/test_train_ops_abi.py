@@ -280,3 +280,26 @@ def test_in_place_is_of_the_own_input_alone(lib, name):
         if name == "s2a_qknorm_rope_bwd":
             for fine in ({"out_q": G}, {"out_k": G + 0x100000}, {"grad_q": A, "out_q": A}, {"grad_k": G, "k": A}, {"q": G, "grad_k": A, "out_q": G}):
                 assert call(**fine) == CUDA, fine
+
+
+@pytest.mark.parametrize("name", CALLS)
+@pytest.mark.parametrize("swap", [(0, 1), (1, 2), (0, 2)])
+def test_in_place_has_the_same_strides_in_every_dimension(lib, name, swap):
+    """An output at its input's address with two dimensions of equal extent exchanged has the same rows, each where another one's was."""
+    whole = (16 * 64, 4 * 64, 64)                                      # 4 sequences, tokens, heads
+    swapped = list(whole)
+    swapped[swap[0]], swapped[swap[1]] = whole[swap[1]], whole[swap[0]]
+
+    def call(**changes):
+        return getattr(lib, name)(_args(**{"batch": 4, "tokens": 4, "heads_q": 4, "heads_k": 4} | {n: whole for n in STRIDES} | changes), None)
+
+    for t, at, grad in (("q", A, G), ("k", B, G + 0x100000)):
+        assert call(**{"out_" + t: at, "out_%s_stride" % t: tuple(swapped)}) == OVERLAP
+        assert call(**{"out_" + t: at, "%s_stride" % t: tuple(swapped)}) == OVERLAP
+        if name == "s2a_qknorm_rope_bwd":
+            assert call(**{"out_" + t: grad, "out_%s_stride" % t: tuple(swapped)}) == OVERLAP
+        if not torch.cuda.is_available():
+            both = {"%s_stride" % t: tuple(swapped), "out_%s_stride" % t: tuple(swapped)}
+            assert call(**{"out_" + t: at}) == CUDA and call(**{"out_" + t: at} | both) == CUDA
+            # a dimension of one has no stride
+            assert call(**{"out_" + t: at, "batch": 1, "out_%s_stride" % t: (7, *whole[1:])}) == CUDA
