@@ -382,7 +382,8 @@ int s2a_relbias_log_buckets(int32_t* buckets, int64_t first_distance, size_t cou
  * Queries q and keys k (and what belongs to them) are tensors [batch, tokens, heads, head_dim] given by
  * their strides, so that every order of the first three dimensions and slices of a packed buffer are
  * taken as they are; the elements of a row of head_dim are contiguous.  One call serves both; heads_k = 0
- * (its pointers are ignored then) serves queries alone.  These calls take their arguments in a struct, of which
+ * serves queries alone, and heads_q = 0 keys: the pointers of what is not there are ignored then, but for its grad_gamma, which gets
+ * zeros where it is not NULL.  These calls take their arguments in a struct, of which
  * a call ignores the members that are not its own.
  *   *_stride  elements from batch to batch, token to token, head to head.  Inputs may have any, 0 included (then each row
  *            has its own output, or gradient); the rows of an output must not overlap.  An output may be the

@@ -105,7 +105,8 @@ int run_rope(const s2a_rope_args* args, int mode, int back, void* stream) {
   const void* const in[2] = {c.q, c.k};
   const void* const grad[2] = {c.grad_q, c.grad_k};
   void* const out[2] = {c.out_q, c.out_k};
-  const void* const gamma[2] = {norm ? c.gamma_q : nullptr, norm ? c.gamma_k : nullptr};
+  // weights of heads that are not there are not looked at, and not read by the kernels
+  const void* const gamma[2] = {norm && c.heads_q ? c.gamma_q : nullptr, norm && c.heads_k ? c.gamma_k : nullptr};
   void* const sums[2] = {bwd ? c.grad_gamma_q : nullptr, bwd ? c.grad_gamma_k : nullptr};
   const size_t* const in_stride[2] = {c.q_stride, c.k_stride};
   const size_t* const grad_stride[2] = {c.grad_q_stride, c.grad_k_stride};

@@ -303,3 +303,16 @@ def test_in_place_has_the_same_strides_in_every_dimension(lib, name, swap):
             assert call(**{"out_" + t: at}) == CUDA and call(**{"out_" + t: at} | both) == CUDA
             # a dimension of one has no stride
             assert call(**{"out_" + t: at, "batch": 1, "out_%s_stride" % t: (7, *whole[1:])}) == CUDA
+
+
+def test_without_heads_of_a_kind_its_pointers_are_ignored(lib):
+    """heads_k = 0 or heads_q = 0: nothing of that kind is looked at, its weights included; the gradient of its weights is an output of the call."""
+    for name in ("s2a_qknorm_rope_fwd", "s2a_qknorm_rope_bwd"):
+        for side in ("q", "k"):
+            odd = {n + side: 3 for n in ("", "out_", "gamma_", "grad_")} | {"heads_" + side: 0}
+            assert getattr(lib, name)(_args(**odd, batch=0), None) == OK
+            assert getattr(lib, name)(_args(**odd, **{"heads_" + ("k" if side == "q" else "q"): 0}), None) == OK
+            if not torch.cuda.is_available():
+                assert getattr(lib, name)(_args(**odd), None) == CUDA      # passes every check
+    assert lib.s2a_qknorm_rope_bwd(_args(heads_k=0, grad_gamma_k=E + 2, scratch=F), None) == ALIGN
+    assert lib.s2a_qknorm_rope_bwd(_args(heads_k=0, grad_gamma_k=E), None) == NULL     # sums need scratch
