@@ -389,12 +389,15 @@ def _stream_on(dev: int) -> int:
 def _on_device(first: torch.Tensor, *others) -> int:
     """One device for all tensors of a call, None aside, and that device current: a launch goes to
     the current device, whatever memory its pointers name.  Returns its index."""
-    dev = first.get_device()
-    if dev < 0:
-        raise S2AError("CUDA tensors are needed")
-    for t in others:
-        if t is not None and t.get_device() != dev:
-            raise S2AError("all tensors of a call must be on one device")
+    try:
+        dev = first.get_device()
+        if dev < 0:
+            raise S2AError("CUDA tensors are needed")
+        for t in others:
+            if t is not None and t.get_device() != dev:
+                raise S2AError("all tensors of a call must be on one device")
+    except AttributeError:
+        raise S2AError("CUDA tensors are needed") from None
     if dev != _current_device():
         raise S2AError("the tensors' device must be the current one (torch.cuda.device)")
     return dev
@@ -680,6 +683,8 @@ def _rope_layout(q, k, out_q, out_k, positions, table, grad_q, grad_k, params):
 
 def _rope(call, q, k, out_q, out_k, positions, table, scale, interleaved, first, dev, eps=0.0, grad_q=None, grad_k=None, params=(),
           scratch=None):
+    if out_q is None:
+        raise S2AError("the queries' output is needed")
     # A call's tensors are looked up by all that is checked of them but their addresses, which the library checks each time.
     key = (q.shape, q.stride(), q.dtype, out_q.shape, out_q.stride(), out_q.dtype)
     q_at, out_q_at = q.data_ptr(), out_q.data_ptr()
@@ -780,6 +785,8 @@ class AdamWPlan:
 
 
 def _state_bits(m, v) -> int:
+    if not isinstance(m, torch.Tensor) or not isinstance(v, torch.Tensor):
+        raise S2AError("exp_avgs and exp_avg_sqs must be CUDA tensors of one device")
     if m.dtype is torch.float32 and v.dtype is torch.float32:
         return 32
     if m.dtype is torch.float8_e4m3fn and v.dtype is torch.float8_e4m3fn:
@@ -861,9 +868,15 @@ def adamw_plan(params, grads, exp_avgs, exp_avg_sqs, exp_avg_scales=None, exp_av
 
 
 def _float_words(t, n: int, what: str):
-    if t.dtype is not torch.float32 or t.numel() < n or not t.is_contiguous():
+    if t is None or t.dtype is not torch.float32 or t.numel() < n or not t.is_contiguous():
         raise S2AError("%s must be contiguous float32 with %d elements" % (what, n))
     return t.data_ptr()
+
+
+def _plan_device(plan, *tensors) -> int:
+    if not isinstance(plan, AdamWPlan):
+        raise S2AError("a plan of adamw_plan is needed")
+    return _on_device(plan.image, *tensors)
 
 
 def s2a_adamw_step(plan: AdamWPlan, control, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, clip=None, rng=None,
@@ -871,7 +884,7 @@ def s2a_adamw_step(plan: AdamWPlan, control, beta1: float = 0.9, beta2: float = 
     """One AdamW step over the plan's tensors, in place.  control: float32 (learning rate, number of the step from 1, scale of
     the gradients) on the device; clip: what s2a_grad_norm wrote, or None; rng: int64 (seed, offset) on the device for
     rounding at random, or None."""
-    dev = _on_device(plan.image, control, clip, rng)
+    dev = _plan_device(plan, control, clip, rng)
     if rng is not None and (rng.dtype is not torch.int64 or rng.numel() != 2 or not rng.is_contiguous()):
         raise S2AError("rng must be contiguous int64 (seed, offset)")
     status = (_lib or lib()).s2a_adamw_step(plan.address, plan.image.data_ptr(), _float_words(control, 3, "control"),
@@ -888,7 +901,7 @@ def grad_norm_scratch_bytes(plan: AdamWPlan) -> int:
 def s2a_grad_norm(plan: AdamWPlan, control, max_norm: float, clip, scratch) -> None:
     """The norm of all the plan's gradients, times control[2], and the factor that limits it to max_norm: written to clip
     (float32, two elements).  scratch holds grad_norm_scratch_bytes(plan) bytes."""
-    dev = _on_device(plan.image, control, clip, scratch)
+    dev = _plan_device(plan, control, clip, scratch)
     status = (_lib or lib()).s2a_grad_norm(plan.address, plan.image.data_ptr(), _float_words(control, 3, "control"), max_norm,
                                            _float_words(clip, 2, "clip"), _scratch(scratch, plan.room),
                                            _stream_on(dev))

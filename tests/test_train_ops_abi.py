@@ -316,3 +316,22 @@ def test_without_heads_of_a_kind_its_pointers_are_ignored(lib):
                 assert getattr(lib, name)(_args(**odd), None) == CUDA      # passes every check
     assert lib.s2a_qknorm_rope_bwd(_args(heads_k=0, grad_gamma_k=E + 2, scratch=F), None) == ALIGN
     assert lib.s2a_qknorm_rope_bwd(_args(heads_k=0, grad_gamma_k=E), None) == NULL     # sums need scratch
+
+
+def test_binding_refuses_missing_tensors():
+    """None, or a list, where a tensor is needed: an S2AError as for every other refusal."""
+    x, table = torch.zeros(1, 2, 3, 64), binding.rope_table(64)
+    for missing in (None, [1.0, 2.0, 3.0]):
+        for call in (lambda: binding.s2a_rope_fwd(missing, None, x, None, None, table), lambda: binding.s2a_rope_bwd(missing, None, x, None, None, table),
+                     lambda: binding.s2a_qknorm_rope_fwd(missing, None, None, None, x, None, None, table, 1e-6),
+                     lambda: binding.s2a_qknorm_rope_bwd(x, None, missing, None, None, None, x, None, None, None, None, None, table, 1e-6),
+                     lambda: binding.s2a_adamw_step(missing, x), lambda: binding.s2a_grad_norm(missing, x, 1.0, x, x)):
+            with pytest.raises(binding.S2AError):
+                call()
+    with pytest.raises(binding.S2AError, match="output"):       # (a call with tensors on a GPU comes here)
+        binding._rope(None, x, None, None, None, None, table, 1.0, False, 0, 0)
+    for name, n in (("control", 3), ("clip", 2)):
+        with pytest.raises(binding.S2AError, match=name):
+            binding._float_words(None, n, name)
+    with pytest.raises(binding.S2AError, match="exp_avg"):
+        binding._state_bits(None, x)

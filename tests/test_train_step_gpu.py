@@ -342,3 +342,23 @@ def test_binding_refusals():
     bad("NULL", plan(None, [g], None, None), torch.zeros(3, device="cuda"), call=s2a.s2a_adamw_step)
     bad("scratch", good, torch.zeros(3, device="cuda"), 1.0, torch.zeros(2, device="cuda"), None, call=s2a.s2a_grad_norm)
     rope._done()
+
+
+def test_binding_refuses_missing_tensors():
+    x, table = torch.zeros(2, 3, 4, 64, device="cuda"), s2a.rope_table(64).cuda()
+    p, g, m, v = (torch.zeros(300, device="cuda") for _ in range(4))
+    good, control = s2a.adamw_plan([p], [g], [m], [v]), torch.zeros(3, device="cuda")
+    clip, scratch = torch.zeros(2, device="cuda"), torch.empty(s2a.grad_norm_scratch_bytes(good), dtype=torch.uint8, device="cuda")
+    for match, call in (("output", lambda: s2a.s2a_rope_fwd(x, None, None, None, None, table)),
+                        ("output", lambda: s2a.s2a_rope_bwd(x, None, None, None, None, table)),
+                        ("output", lambda: s2a.s2a_qknorm_rope_fwd(x, None, None, None, None, None, None, table, 1e-6)),
+                        ("output", lambda: s2a.s2a_qknorm_rope_bwd(x, None, x, None, None, None, None, None, None, None, None, None, table, 1e-6)),
+                        ("CUDA", lambda: s2a.s2a_qknorm_rope_bwd(x, None, None, None, None, None, x, None, None, None, None, None, table, 1e-6)),
+                        ("control", lambda: s2a.s2a_adamw_step(good, None)), ("CUDA", lambda: s2a.s2a_adamw_step(good, [1e-3, 1.0, 1.0])),
+                        ("plan", lambda: s2a.s2a_adamw_step(None, control)), ("plan", lambda: s2a.s2a_grad_norm(None, control, 1.0, clip, scratch)),
+                        ("control", lambda: s2a.s2a_grad_norm(good, None, 1.0, clip, scratch)),
+                        ("clip", lambda: s2a.s2a_grad_norm(good, control, 1.0, None, scratch)),
+                        ("exp_avg", lambda: s2a.adamw_plan([p], [g], [None], [v]))):
+        with pytest.raises(s2a.S2AError, match=match):
+            call()
+    rope._done()
