@@ -779,9 +779,10 @@ def s2a_qknorm_rope_bwd(grad_q, grad_k, q, k, gamma_q, gamma_k, grad_in_q, grad_
 # --------------------------------------------------- the AdamW step over many tensors, the gradients' norm
 class AdamWPlan:
     """The tensors of a step, checked and laid out once (adamw_plan); it keeps them alive and is good as long as they stay
-    where they are: with other gradient tensors, make another plan."""
+    where they are: with other gradient tensors, make another plan.  It may be dropped while a stream still runs it (its tensors are the
+    caller's to keep for a stream that is not their own, as with any call); a graph that has captured its calls needs it as long as it is replayed."""
 
-    __slots__ = ("plan", "address", "image", "device", "tensors", "room")
+    __slots__ = ("plan", "address", "image", "device", "tensors", "room", "streams")
 
 
 def _state_bits(m, v) -> int:
@@ -861,6 +862,7 @@ def adamw_plan(params, grads, exp_avgs, exp_avg_sqs, exp_avg_scales=None, exp_av
     check(lib().s2a_step_plan_fill(records, count, pdt, gdt, bits, host.data_ptr() + 8 * start, ctypes.byref(self.plan)))
     self.device = torch.cuda.current_device() if dev is None else dev
     self.image = host[start:start + max(need, 16) // 8 + 1].to(torch.device("cuda", self.device))
+    self.streams = {_stream_on(self.device)}
     self.address = ctypes.addressof(self.plan)
     self.room = int(lib().s2a_grad_norm_scratch_bytes(self.address))
     self.tensors = (list(grads),) + tuple(None if ts is None else list(ts) for ts in lists.values())
@@ -879,6 +881,16 @@ def _plan_device(plan, *tensors) -> int:
     return _on_device(plan.image, *tensors)
 
 
+def _plan_stream(plan: AdamWPlan, dev: int) -> int:
+    """The current stream.  The plan's image is memory of the stream on which the plan was made; once another one reads it, that
+    memory may be given away only after its work."""
+    stream = _stream_on(dev)
+    if stream not in plan.streams:
+        plan.image.record_stream(torch.cuda.current_stream(dev))
+        plan.streams.add(stream)
+    return stream
+
+
 def s2a_adamw_step(plan: AdamWPlan, control, beta1: float = 0.9, beta2: float = 0.999, eps: float = 1e-8, clip=None, rng=None,
                    site: int = 0) -> None:
     """One AdamW step over the plan's tensors, in place.  control: float32 (learning rate, number of the step from 1, scale of
@@ -889,7 +901,7 @@ def s2a_adamw_step(plan: AdamWPlan, control, beta1: float = 0.9, beta2: float = 
         raise S2AError("rng must be contiguous int64 (seed, offset)")
     status = (_lib or lib()).s2a_adamw_step(plan.address, plan.image.data_ptr(), _float_words(control, 3, "control"),
                                             None if clip is None else _float_words(clip, 2, "clip"), _address(rng) or None, site, beta1,
-                                            beta2, eps, _stream_on(dev))
+                                            beta2, eps, _plan_stream(plan, dev))
     if status:
         check(status)
 
@@ -904,7 +916,7 @@ def s2a_grad_norm(plan: AdamWPlan, control, max_norm: float, clip, scratch) -> N
     dev = _plan_device(plan, control, clip, scratch)
     status = (_lib or lib()).s2a_grad_norm(plan.address, plan.image.data_ptr(), _float_words(control, 3, "control"), max_norm,
                                            _float_words(clip, 2, "clip"), _scratch(scratch, plan.room),
-                                           _stream_on(dev))
+                                           _plan_stream(plan, dev))
     if status:
         check(status)
 

@@ -335,3 +335,21 @@ def test_binding_refuses_missing_tensors():
             binding._float_words(None, n, name)
     with pytest.raises(binding.S2AError, match="exp_avg"):
         binding._state_bits(None, x)
+
+
+def test_a_plans_image_is_kept_for_every_stream_that_reads_it(monkeypatch):
+    """The image is memory of the stream current when the plan was made; each other stream that runs the plan is recorded with it, once."""
+    recorded = []
+
+    class Image:
+        def record_stream(self, stream):
+            recorded.append(stream)
+
+    plan = binding.AdamWPlan()
+    plan.image, plan.streams = Image(), {100}
+    now = 100
+    monkeypatch.setattr(binding, "_stream_on", lambda dev: now)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda dev=None: ("stream", now, dev))
+    for now in (100, 200, 200, 100, 300, 200, 300):
+        assert binding._plan_stream(plan, 1) == now
+    assert recorded == [("stream", 200, 1), ("stream", 300, 1)]

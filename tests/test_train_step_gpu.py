@@ -362,3 +362,37 @@ def test_binding_refuses_missing_tensors():
         with pytest.raises(s2a.S2AError, match=match):
             call()
     rope._done()
+
+
+def test_a_plan_may_be_dropped_while_another_stream_reads_it():
+    """A plan of the current stream, run by a side stream that is busy, and dropped: its image's memory goes to nobody before the side stream has
+    read it."""
+    def tensors():
+        return [rope._normal((n,), torch.float32, "dropped", n, i) for n in (3000, 17, 40_000) for i in range(2)]
+
+    p, g = tensors(), [t * 0.1 for t in tensors()]
+    q = [t.clone() for t in p]
+    states = [[torch.zeros_like(t) for t in p] for _ in range(4)]
+    control = torch.tensor([1e-2, 1.0, 1.0], device="cuda")
+    clips = [torch.empty(2, device="cuda") for _ in range(2)]
+    plan = s2a.adamw_plan(q, g, states[2], states[3])
+    scratch = [torch.empty(s2a.grad_norm_scratch_bytes(plan), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    s2a.s2a_grad_norm(plan, control, 0.5, clips[1], scratch[1])
+    s2a.s2a_adamw_step(plan, control, clip=clips[1])
+    plan = s2a.adamw_plan(p, g, states[0], states[1])
+    torch.cuda.synchronize()
+    at, size = plan.image.data_ptr(), plan.image.numel() * 8
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(400_000_000)                     # some 0.2 s
+        s2a.s2a_grad_norm(plan, control, 0.5, clips[0], scratch[0])
+        s2a.s2a_adamw_step(plan, control, clip=clips[0])
+    del plan
+    others = [torch.zeros(size, dtype=torch.uint8, device="cuda") for _ in range(8)]
+    busy = not side.query()
+    places = [t.data_ptr() for t in others]
+    rope._done()
+    assert not busy or all(x + size <= at or at + size <= x for x in places)
+    assert torch.equal(clips[0], clips[1])
+    for a, b in zip(p + states[0] + states[1], q + states[2] + states[3]):
+        assert torch.equal(a, b)
