@@ -519,3 +519,40 @@ def test_beta_zero_and_betas_near_one():
         s2a.s2a_adamw_step(_plan(ts, 32, False), torch.tensor([1e-3, 1.0, 1.0], device="cuda"), b1, b2, 1e-8)
         _done()
         _check_step(before, ts, (float(torch.tensor(1e-3)), 1.0, 1.0, b1, b2, 1e-8), 32, [0.0], [1.0])
+
+
+def test_states_rounded_at_random_follow_where_nearest_stays():
+    """Under a scale that stays 1 (the first element of each block has a state and a gradient of 1, the others none) m shrinks by 0.1 % a step and
+    sqrt(v) by 0.05 %, far less than half a code's step.  To nearest, all codes stay.  At random a state's mean is the formula's:
+    a code's step is at most 1/8 of its value, so that a step d (1e-3, 5e-4 of the value) adds a variance of at most d / 8, 400 steps 0.05
+    and 0.025, of which the mean over 65280 elements has a deviation of 8.8e-4 and 6.2e-4; five of them, 400 times the half of a
+    16-bit field's last place (2^-17 of 1/8: 3.9e-4), and 400 steps of the scale, each off by at most
+    8 u (five roundings on the way to a, two of the sum of squares, half of them in the root, and one step of the root): 2e-4."""
+    n, steps, b1, b2 = 65536, 400, 0.999, 0.999
+    gen = _gen("follow")
+    start = 0.3 + 0.4 * torch.rand(2, n, generator=gen, device="cuda")
+    start[0] *= torch.where(torch.rand(n, generator=gen, device="cuda") < 0.5, -1.0, 1.0)
+    start.view(2, -1, 256)[:, :, 0] = 1.0
+    g = torch.zeros(n, device="cuda")
+    g[::256] = 1.0
+    for random_bits in (False, True):
+        m, v = ((x * 448).to(E4) for x in start)
+        scales = [torch.ones(n // 256, device="cuda") for _ in range(2)]
+        first = [x.float().clone() for x in (m, v)]
+        p = torch.zeros(n, device="cuda")
+        plan = s2a.adamw_plan([p], [g], [m], [v], [scales[0]], [scales[1]])
+        control = torch.tensor([0.0, 1.0, 1.0], device="cuda")
+        rng = torch.tensor([11, 0], dtype=torch.int64, device="cuda")
+        for _ in range(steps):
+            s2a.s2a_adamw_step(plan, control, b1, b2, rng=rng if random_bits else None)
+            rng[1] += 1
+        _done()
+        for x, s, was, kept, deviation in ((m, scales[0], first[0], b1 ** steps, 8.8e-4), (v, scales[1], first[1], b2 ** (steps / 2), 6.2e-4)):
+            assert float((s - 1).abs().max()) <= 2e-4
+            now = x.float()
+            assert bool((now.view(-1, 256)[:, 0] == 448).all())
+            if random_bits:
+                ratio = (now * s.repeat_interleave(256) / was).view(-1, 256)[:, 1:]
+                assert abs(float(ratio.double().mean()) - kept) <= 5 * deviation + 3.9e-4 + 2e-4
+            else:
+                assert torch.equal(now, was)
