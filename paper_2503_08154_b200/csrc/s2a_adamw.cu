@@ -678,19 +678,32 @@ __global__ void __cluster_dims__(kFewCtas) __launch_bounds__(kFewWarps * 32)
   }
 }
 
+// Whether the current device has room for a cluster of sixteen: a part of a GPU, or one with SMs switched off, may not.  Asked once a device.
 template <int GDT>
-cudaError_t launch_grad_norm_few(const StepArgs& a, float max_norm, float* out, cudaStream_t st) {
-  static std::atomic<uint64_t> ready{0};  // devices on which clusters of sixteen are allowed
+bool few_fits() {
+  static std::atomic<uint64_t> asked{0}, fits{0};  // a bit for each device
   int dev = 0;
-  cudaError_t e = cudaGetDevice(&dev);
-  if (e != cudaSuccess) return e;
+  if (cudaGetDevice(&dev) != cudaSuccess) return false;
   const uint64_t bit = 1ull << (dev & 63);
-  if (dev >= 64 || !(ready.load(std::memory_order_acquire) & bit)) {
-    e = cudaFuncSetAttribute(grad_norm_few_kernel<GDT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-    if (e != cudaSuccess) return e;
-    if (dev < 64) ready.fetch_or(bit, std::memory_order_release);
+  if (dev < 64 && (asked.load(std::memory_order_acquire) & bit)) return (fits.load(std::memory_order_relaxed) & bit) != 0;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = kFewCtas;
+  attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(kFewCtas);
+  cfg.blockDim = dim3(kFewWarps * 32);
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  int n = 0;
+  const bool ok = cudaFuncSetAttribute(grad_norm_few_kernel<GDT>, cudaFuncAttributeNonPortableClusterSizeAllowed, 1) == cudaSuccess &&
+                  cudaOccupancyMaxActiveClusters(&n, grad_norm_few_kernel<GDT>, &cfg) == cudaSuccess && n > 0;
+  if (!ok) cudaGetLastError();  // the other kernels run: nobody is to find this error later
+  if (dev < 64) {
+    if (ok) fits.fetch_or(bit, std::memory_order_relaxed);
+    asked.fetch_or(bit, std::memory_order_release);
   }
-  return launch_overlapped(grad_norm_few_kernel<GDT>, dim3(kFewCtas), kFewWarps * 32, 0, st, a, max_norm, out);
+  return ok;
 }
 
 template <int PDT, int GDT>
@@ -729,8 +742,8 @@ uint64_t grad_norm_scratch_bytes(uint32_t n_chunks) {
 }
 
 cudaError_t launch_grad_norm(int gdt, const StepArgs& a, float max_norm, float* out, double* scratch, cudaStream_t st) {
-  if (a.chunk_blocks == 1 && a.n_chunks <= kFewCtas * kFewWarps * kLooks)
-    return gdt == kF32 ? launch_grad_norm_few<kF32>(a, max_norm, out, st) : launch_grad_norm_few<kBF16>(a, max_norm, out, st);
+  if (a.chunk_blocks == 1 && a.n_chunks <= kFewCtas * kFewWarps * kLooks && (gdt == kF32 ? few_fits<kF32>() : few_fits<kBF16>()))
+    return launch_overlapped(gdt == kF32 ? grad_norm_few_kernel<kF32> : grad_norm_few_kernel<kBF16>, dim3(kFewCtas), kFewWarps * 32, 0, st, a, max_norm, out);
   const unsigned grid = (unsigned)(grad_norm_scratch_bytes(a.n_chunks) / sizeof(double));
   const auto go = [&](void (*kernel)(const StepArgs, double*)) { return launch_overlapped(kernel, dim3(grid), kNormThreads, 0, st, a, scratch); };
   const cudaError_t e = a.chunk_blocks == 1 ? (gdt == kF32 ? go(grad_norm_kernel<kF32, true>) : go(grad_norm_kernel<kBF16, true>))

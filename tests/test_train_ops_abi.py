@@ -3,7 +3,10 @@ before any launch), the overlap rules against a walk over every byte, the table 
 import ctypes
 import itertools
 import math
+import os
 import random
+import shutil
+import subprocess
 from fractions import Fraction
 
 import pytest
@@ -353,3 +356,29 @@ def test_a_plans_image_is_kept_for_every_stream_that_reads_it(monkeypatch):
     for now in (100, 200, 200, 100, 300, 200, 300):
         assert binding._plan_stream(plan, 1) == now
     assert recorded == [("stream", 200, 1), ("stream", 300, 1)]
+
+
+def test_gradients_norm_where_clusters_of_sixteen_do_not_fit(lib, tmp_path):
+    """The library's own host code against a runtime of the test's: small plans take one launch of a cluster where the device has room for one,
+    and otherwise (a part of a GPU) the two launches of the others.  The device is asked once."""
+    here = os.path.dirname(os.path.abspath(__file__))
+    out = str(tmp_path / "fake.so")
+    nvcc = shutil.which(os.environ.get("NVCC", "nvcc"))
+    include = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(nvcc))), "include")
+    subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", "-Wl,-z,defs", "-Wl,-Bsymbolic", "-I", include, os.path.join(here, "fake_runtime.cpp"),
+                    os.path.join(build.OBJ, "s2a_adamw.o"), "-o", out], check=True, capture_output=True)
+    run = ctypes.CDLL(out).run_grad_norm
+    grids, asked = (ctypes.c_uint * 16)(), ctypes.c_int()
+
+    def launches(device, clusters, dtype, chunks):
+        n = run(device, clusters, dtype, chunks, grids, ctypes.byref(asked))
+        return list(grids[:n]) if n >= 0 else n
+
+    for dtype in (F32, BF16):
+        for device, clusters in ((0, 9), (1, 0), (2, -1), (3, 1), (70, 0), (71, 2)):   # (70, 71: beyond the devices that answers are kept for)
+            for chunks in (1, 240, 2048):
+                want = [16] if clusters > 0 else [-(-chunks // 8), 1]
+                for _ in range(2):
+                    assert launches(device, clusters, dtype, chunks) == want, (device, chunks)
+            assert launches(device, clusters, dtype, 2049) == [257, 1]
+        assert asked.value == (4 + 2 * 6) * (1 + (dtype == BF16))
