@@ -21,31 +21,34 @@ namespace {
 constexpr int kWarps = 8;         // as in the kernels
 constexpr int kLaneElems = 16;
 
-// grad_gamma of queries (blockIdx.y = 0) and keys: the CTAs' partial rows added in a fixed order, a column a lane, a warp's share of the rows
-// in flight at once.
+// grad_gamma of queries (blockIdx.y = 0) and keys: the CTAs' partial rows added in a fixed order and in 64 bits, a column a lane, a warp's share of
+// the rows in flight at once.
 constexpr int kReduceWarps = 16;
 constexpr int kReduceRows = (kMaxRopePartials + kReduceWarps - 1) / kReduceWarps;  // of a warp
 
 __global__ void __launch_bounds__(kReduceWarps * 32) qknorm_reduce_kernel(const float* partials, uint32_t ctas0, uint32_t ctas, uint32_t D,
                                                                          void* gq, void* gk, int wdt) {
-  __shared__ float buf[kReduceWarps][33];
+  __shared__ double buf[kReduceWarps][33];
   enter_grid();
   const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, d = blockIdx.x * 32 + lane;
   const uint32_t from = blockIdx.y ? ctas0 : 0, to = blockIdx.y ? ctas : ctas0;
   void* out = blockIdx.y ? gk : gq;
-  float s = 0.0f;
+  float p[kReduceRows];
 #pragma unroll
   for (int i = 0; i < kReduceRows; ++i) {
     const uint32_t r = from + warp + i * kReduceWarps;
-    if (d < D && r < to) s += partials[(uint64_t)r * D + d];
+    p[i] = d < D && r < to ? partials[(uint64_t)r * D + d] : 0.0f;
   }
-  buf[warp][lane] = s;
+  double s = 0.0, t = 0.0;  // an addition waits for the one before it
+#pragma unroll
+  for (int i = 0; i < kReduceRows; ++i) (i % 2 ? t : s) += (double)p[i];
+  buf[warp][lane] = s + t;
   __syncthreads();
   if (warp == 0 && d < D && out) {
-    s = 0.0f;
+    s = 0.0;
 #pragma unroll
     for (int w = 0; w < kReduceWarps; ++w) s += buf[w][lane];
-    store_param(out, d, wdt, s);
+    store_param(out, d, wdt, (float)s);
   }
 }
 

@@ -848,10 +848,26 @@ __global__ void __launch_bounds__(kThreads, V == 1 ? 1 : 2) qknorm_bwd_kernel(co
       }
   }
   __syncthreads();
-  for (uint32_t d = threadIdx.x; d < D; d += kThreads) {
-    float s = 0.0f;
-    for (uint32_t r = 0; r < all; ++r) s += sums[r * D + d];
-    a.partials[(uint64_t)blockIdx.x * D + d] = s;
+  // Over lanes and warps in 64 bits: with rows that add up rather than cancel, a chain of some 64 terms in 32 loses several units in the last place.
+  // Narrow rows leave threads for halves or quarters of the rows.
+  const uint32_t parts = 4 * D <= kThreads ? 4 : (2 * D <= kThreads ? 2 : 1), of_part = all / parts;  // (kWarps is a multiple of eight)
+  double* joined = (double*)(sums + all * D);
+  for (uint32_t i = threadIdx.x; i < parts * D; i += kThreads) {
+    const float* from = sums + i / D * of_part * D + i % D;
+    double s = 0.0, t = 0.0;  // an addition waits for the one before it
+    for (uint32_t r = 0; r < of_part; r += 2) {
+      s += (double)from[r * D];
+      t += (double)from[(r + 1) * D];
+    }
+    if (parts == 1) a.partials[(uint64_t)blockIdx.x * D + i] = (float)(s + t);
+    else joined[i] = s + t;
+  }
+  if (parts == 1) return;
+  __syncthreads();
+  if (threadIdx.x < D) {
+    double s = 0.0;
+    for (uint32_t i = 0; i < parts; ++i) s += joined[i * D + threadIdx.x];
+    a.partials[(uint64_t)blockIdx.x * D + threadIdx.x] = (float)s;
   }
 }
 
@@ -860,8 +876,8 @@ cudaError_t launch_one(int mode, const RopeArgs& a, unsigned grid, cudaStream_t 
   static std::atomic<uint64_t> ready[3] = {};
   const bool bwd = mode == kRopeBwdNorm;
   constexpr uint32_t group = Group<DT, V, W, kLaneElems / (2 * V), L, MULTI>::kGroupBytes;
-  // the sums of the backward pass take the rings' place: 16 floats a lane
-  static_assert(kBwdStages<DT> * 2 * group >= 32 * kLaneElems * sizeof(float), "the sums fit in the rings");
+  // the sums of the backward pass take the rings' place: 16 floats a lane, and one double a thread
+  static_assert(kBwdStages<DT> * 2 * group >= 32 * (kLaneElems * sizeof(float) + sizeof(double)), "the sums fit in the rings");
   const int weights = mode == kRopeFwdNorm ? 2 : (bwd ? 1 : 0);
   const uint32_t stages = bwd ? kBwdStages<DT> : 4, bytes = bwd ? 2 * group : group;
   const size_t smem = std::max(Layout(a.pairs, a.head_dim, weights, a.group_tokens[0], stages, bytes).bytes(),

@@ -470,3 +470,29 @@ def test_same_call_same_bits_other_stream_and_replay():
         _done()
         for b in kept:
             assert all(torch.equal(x, y) for x, y in zip(b[:4], want[:4]))
+
+
+@pytest.mark.parametrize("D,tokens,heads", [(64, 2368, (8, 0)), (40, 2368, (10, 0)), (64, 8 * 2368, (1, 0)), (128, 1184, (4, 4)), (2, 1500, (16, 16))])
+def test_weights_gradients_are_added_up_in_64_bits(D, tokens, heads):
+    """Rows of ones whose gradients are the same in all rows: a lane has one row (or a few, whose sums the numbers below have room for), and what is
+    added over lanes, warps and CTAs must be exact but for the last rounding.  Numbers of 20 bits: the sum of up to 16 of them is exact in binary32, a
+    CTA's sum is rounded once (1 u), and so is the result (1 u)."""
+    g = torch.randint(1 << 19, 1 << 20, (D,), generator=_gen("terms", D), device="cuda").float()
+    x = [torch.ones((1, tokens, h, D), device="cuda") for h in heads]
+    y = torch.empty_like(x[0])
+    s2a.s2a_qknorm_rope_fwd(x[0], None, None, None, y, None, None, None, 0.0)
+    _done()
+    rstd = y[0, 0, 0, 0]
+    assert bool((y == rstd).all())
+    terms = [g.expand_as(t).contiguous() for t in x]
+    out = [torch.empty_like(t) for t in x]
+    sums = [torch.empty(D, device="cuda") for _ in heads]
+    scratch = torch.empty(s2a.qknorm_rope_scratch_bytes(1, tokens, *heads, D), dtype=torch.uint8, device="cuda")
+    keys = heads[1] > 0
+    s2a.s2a_qknorm_rope_bwd(terms[0], terms[1] if keys else None, x[0], x[1] if keys else None, None, None, out[0], out[1] if keys else None, sums[0],
+                            sums[1] if keys else None, scratch, None, None, 0.0)
+    _done()
+    for s, h in zip(sums, heads):
+        if h:
+            want = (g * rstd).double() * (tokens * h)      # each term is rounded to binary32 as it is added to the lane's first
+            assert float(((s.double() - want).abs() / want).max()) <= 2.01 * U + (0 if float(rstd) == 1 else 16 * U)
