@@ -875,12 +875,6 @@ def _float_words(t, n: int, what: str):
     return t.data_ptr()
 
 
-def _plan_device(plan, *tensors) -> int:
-    if not isinstance(plan, AdamWPlan):
-        raise S2AError("a plan of adamw_plan is needed")
-    return _on_device(plan.image, *tensors)
-
-
 def _plan_stream(plan: AdamWPlan, dev: int) -> int:
     """The current stream.  The plan's image is memory of the stream on which the plan was made; once another one reads it, that
     memory may be given away only after its work."""
@@ -896,7 +890,10 @@ def s2a_adamw_step(plan: AdamWPlan, control, beta1: float = 0.9, beta2: float = 
     """One AdamW step over the plan's tensors, in place.  control: float32 (learning rate, number of the step from 1, scale of
     the gradients) on the device; clip: what s2a_grad_norm wrote, or None; rng: int64 (seed, offset) on the device for
     rounding at random, or None."""
-    dev = _plan_device(plan, control, clip, rng)
+    try:
+        dev = _on_device(plan.image, control, clip, rng)
+    except AttributeError:
+        raise S2AError("a plan of adamw_plan is needed") from None
     if rng is not None and (rng.dtype is not torch.int64 or rng.numel() != 2 or not rng.is_contiguous()):
         raise S2AError("rng must be contiguous int64 (seed, offset)")
     status = (_lib or lib()).s2a_adamw_step(plan.address, plan.image.data_ptr(), _float_words(control, 3, "control"),
@@ -913,7 +910,10 @@ def grad_norm_scratch_bytes(plan: AdamWPlan) -> int:
 def s2a_grad_norm(plan: AdamWPlan, control, max_norm: float, clip, scratch) -> None:
     """The norm of all the plan's gradients, times control[2], and the factor that limits it to max_norm: written to clip
     (float32, two elements).  scratch holds grad_norm_scratch_bytes(plan) bytes."""
-    dev = _plan_device(plan, control, clip, scratch)
+    try:
+        dev = _on_device(plan.image, control, clip, scratch)
+    except AttributeError:
+        raise S2AError("a plan of adamw_plan is needed") from None
     status = (_lib or lib()).s2a_grad_norm(plan.address, plan.image.data_ptr(), _float_words(control, 3, "control"), max_norm,
                                            _float_words(clip, 2, "clip"), _scratch(scratch, plan.room),
                                            _plan_stream(plan, dev))
