@@ -228,7 +228,6 @@ StepArgs step_args(const s2a_step_plan* plan, const void* image, const float* co
   StepArgs a = {};
   a.tensors = (const StepTensor*)image;
   a.owner = (const uint32_t*)((const char*)image + plan->n_tensors * sizeof(StepTensor));
-  a.n_tensors = (uint32_t)plan->n_tensors;
   a.n_chunks = (uint32_t)plan->n_chunks;
   a.chunk_blocks = (uint32_t)plan->chunk_blocks;
   a.control = control;

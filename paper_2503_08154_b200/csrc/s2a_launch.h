@@ -145,7 +145,7 @@ constexpr uint32_t kStepScalar = 8;
 struct StepArgs {
   const StepTensor* tensors;
   const uint32_t* owner;
-  uint32_t n_tensors, n_chunks;
+  uint32_t n_chunks;
   const float* control;   // learning rate, number of the step, scale of the gradients
   const float* clip;      // norm and factor, or NULL
   const uint64_t* rng;    // seed and offset, or NULL: round to nearest

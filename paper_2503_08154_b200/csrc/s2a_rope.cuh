@@ -15,7 +15,7 @@
 // lanes.  A warp takes 32 / L rows (L lanes a row) at a time: a group.  Where a token has as many rows (heads of queries and keys) or more,
 // its groups follow one another and its cosines and sines are computed once; where it has fewer, a group takes the rows of several tokens.  The
 // phases are computed by all lanes, each some pairs, and shared through the warp's own shared memory.  Rows come through a ring of
-// asynchronous copies of each warp's own, four groups deep.  With plain loads, addresses from scratch and the weights read per token, the norm
+// asynchronous copies of each warp's own, four groups deep (the norm's backward: kBwdStages).  With plain loads, addresses from scratch and the weights read per token, the norm
 // of [64, 197, 12 + 12, 64] bfloat16 took 581 instructions a group and 39.5 us; so it takes 17.0 (a copy of the same bytes: 13.5), the rotation of
 // [2, 16384, 32 + 8, 128] 121.5 us (0.84 of a copy's rate) and the norm's backward of [4, 4097, 32 + 8, 128] 92.4 (0.83).
 //

@@ -382,3 +382,41 @@ def test_gradients_norm_where_clusters_of_sixteen_do_not_fit(lib, tmp_path):
                     assert launches(device, clusters, dtype, chunks) == want, (device, chunks)
             assert launches(device, clusters, dtype, 2049) == [257, 1]
         assert asked.value == (4 + 2 * 6) * (1 + (dtype == BF16))
+
+
+@NO_GPU
+def test_overlap_of_any_strides(lib):
+    """Inputs, gradients and outputs with strides of their own, in any order of the dimensions, 0 among the inputs': a call that passes writes no byte that it
+    reads elsewhere, nor one byte twice."""
+    rng = random.Random(1)
+    passed = refused = 0
+    for _ in range(3000):
+        n, heads, d, bwd = (rng.randint(1, 4), rng.randint(1, 4)), (rng.randint(1, 3), rng.randint(0, 3)), rng.choice([2, 4]), rng.random() < 0.5
+
+        def strides(h, zero):
+            s, step = [0, 0, 0], d
+            for i in rng.sample(range(3), 3):
+                s[i], step = step, step * max(1, (*n, h)[i]) + rng.choice([0, 0, 0, d, 1])
+            if zero and rng.random() < 0.3:
+                s[rng.randrange(3)] = rng.choice([0, d, 1])
+            return tuple(s)
+
+        places, often = {}, strides(max(heads), False)
+        for name in ("q", "k", "out_q", "out_k") + (("grad_q", "grad_k") if bwd else ()):
+            at = rng.choice([A + 4 * rng.choice([0, d * heads[0], rng.randrange(400)]), A + 40000 * (len(places) + 1)] + [v[0] for v in places.values()])
+            places[name] = (at, rng.choice([often, strides(heads[name[-1] == "k"], not name.startswith("out"))]))
+        call = lib.s2a_qknorm_rope_bwd if bwd else lib.s2a_rope_fwd
+        status = call(_args(dt=F32, batch=n[0], tokens=n[1], heads_q=heads[0], heads_k=heads[1], head_dim=d, rot_dim=d, positions=0,
+                            **{k: v[0] for k, v in places.items()}, **{k + "_stride": v[1] for k, v in places.items()}), None)
+        size = {name: (*n, heads[name[-1] == "k"]) for name in places}
+        touched = {name: _bytes(at, size[name], [4 * x for x in s], 4 * d) for name, (at, s) in places.items()}
+        same = {name: (at, *(x for x, e in zip(s, size[name]) if e > 1)) for name, (at, s) in places.items()}
+        bad = False
+        for out in ("out_q", "out_k"):
+            bad = bad or len(touched[out]) < math.prod(size[out]) * 4 * d
+            for name in places:
+                own = name[-1] == out[-1] and not name.startswith("out") and same[name] == same[out]
+                bad = bad or (name != out and not own and bool(touched[out] & touched[name]))
+        assert not (bad and status == CUDA), (n, heads, d, places)
+        passed, refused = passed + (status == CUDA), refused + (status in (OVERLAP, SHAPE))
+    assert passed > 300 and refused > 300
