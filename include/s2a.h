@@ -462,7 +462,7 @@ int s2a_rope_table(uint64_t* table, size_t rot_dim, double base, int scaling, do
 /* ---- After the backward pass: the gradients' norm and the AdamW step over many tensors ------------------
  * Both go by a plan: the list of tensors, checked and laid out once in HOST memory (s2a_step_plan_fill), copied by the
  * caller to 16-byte aligned device memory, and good for any number of calls as long as the tensors stay where
- * they are.
+ * they are.  The calls go by the addresses in the image: a gradient that has moved is not noticed.
  */
 typedef struct {
   void* param;              /* n elements of type pdt                                                   */

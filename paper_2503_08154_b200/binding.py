@@ -779,10 +779,12 @@ def s2a_qknorm_rope_bwd(grad_q, grad_k, q, k, gamma_q, gamma_k, grad_in_q, grad_
 # --------------------------------------------------- the AdamW step over many tensors, the gradients' norm
 class AdamWPlan:
     """The tensors of a step, checked and laid out once (adamw_plan); it keeps them alive and is good as long as they stay
-    where they are: with other gradient tensors, make another plan.  It may be dropped while a stream still runs it (its tensors are the
+    where they are.  A step with gradients that have become other tensors would go on with the old ones: zero gradients in place
+    (zero_grad(set_to_none=False)), or make another plan, which costs some 6 us a tensor and a wait for the stream.  Where the parameters are leaves and
+    the gradients their .grad, each call looks at one pair in turn and refuses a plan whose gradient is no longer that.  It may be dropped while a stream still runs it (its tensors are the
     caller's to keep for a stream that is not their own, as with any call); a graph that has captured its calls needs it as long as it is replayed."""
 
-    __slots__ = ("plan", "address", "image", "device", "tensors", "room", "streams")
+    __slots__ = ("plan", "address", "image", "device", "tensors", "room", "streams", "pairs", "turn")
 
 
 def _state_bits(m, v) -> int:
@@ -865,6 +867,8 @@ def adamw_plan(params, grads, exp_avgs, exp_avg_sqs, exp_avg_scales=None, exp_av
     self.streams = {_stream_on(self.device)}
     self.address = ctypes.addressof(self.plan)
     self.room = int(lib().s2a_grad_norm_scratch_bytes(self.address))
+    self.pairs = [(p, g) for p, g in zip(params or (), grads) if p.is_leaf and p.requires_grad and p.grad is g]
+    self.turn = 0
     self.tensors = (list(grads),) + tuple(None if ts is None else list(ts) for ts in lists.values())
     return self
 
@@ -875,9 +879,20 @@ def _float_words(t, n: int, what: str):
     return t.data_ptr()
 
 
+def _plan_current(plan: AdamWPlan) -> None:
+    """Refuses a plan whose gradients have been replaced.  That happens to all at once, as a rule: one pair a call, in turn, tells."""
+    param, grad = plan.pairs[plan.turn % len(plan.pairs)]
+    plan.turn += 1
+    now = param.grad
+    if now is not grad and (now is None or now.data_ptr() != grad.data_ptr()):
+        raise S2AError("a parameter's gradient is another tensor than when the plan was made: make another plan, or zero gradients in place")
+
+
 def _plan_stream(plan: AdamWPlan, dev: int) -> int:
     """The current stream.  The plan's image is memory of the stream on which the plan was made; once another one reads it, that
     memory may be given away only after its work."""
+    if plan.pairs:
+        _plan_current(plan)
     stream = _stream_on(dev)
     if stream not in plan.streams:
         plan.image.record_stream(torch.cuda.current_stream(dev))

@@ -349,7 +349,7 @@ def test_a_plans_image_is_kept_for_every_stream_that_reads_it(monkeypatch):
             recorded.append(stream)
 
     plan = binding.AdamWPlan()
-    plan.image, plan.streams = Image(), {100}
+    plan.image, plan.streams, plan.pairs = Image(), {100}, []
     now = 100
     monkeypatch.setattr(binding, "_stream_on", lambda dev: now)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda dev=None: ("stream", now, dev))
@@ -420,3 +420,26 @@ def test_overlap_of_any_strides(lib):
         assert not (bad and status == CUDA), (n, heads, d, places)
         passed, refused = passed + (status == CUDA), refused + (status in (OVERLAP, SHAPE))
     assert passed > 300 and refused > 300
+
+
+def test_a_plan_whose_gradients_were_replaced_is_refused():
+    """One pair of parameter and gradient a call, in turn: all of them replaced is seen at once, one of them within a round."""
+    plan = binding.AdamWPlan()
+    params = [torch.zeros(3, requires_grad=True) for _ in range(3)]
+    for p in params:
+        p.grad = torch.ones(3)
+    plan.pairs, plan.turn = [(p, p.grad) for p in params], 0
+    for _ in range(4):
+        binding._plan_current(plan)
+    params[1].grad.zero_()
+    params[2].grad = params[2].grad.detach()        # the same memory
+    for _ in range(3):
+        binding._plan_current(plan)
+    params[0].grad = None
+    with pytest.raises(binding.S2AError, match="another"):
+        for _ in range(3):
+            binding._plan_current(plan)
+    for p in params:
+        p.grad = torch.ones(3)
+    with pytest.raises(binding.S2AError, match="another"):
+        binding._plan_current(plan)

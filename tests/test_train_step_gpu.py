@@ -396,3 +396,56 @@ def test_a_plan_may_be_dropped_while_another_stream_reads_it():
     assert torch.equal(clips[0], clips[1])
     for a, b in zip(p + states[0] + states[1], q + states[2] + states[3]):
         assert torch.equal(a, b)
+
+
+def test_training_with_gradients_that_stay():
+    """Gradients of automatic differentiation that are zeroed in place stay where they are, and one plan serves all steps; with replaced ones (set to
+    None) the old plan is refused, in place of a step with the old gradients, and a new one is right."""
+    torch.backends.cuda.matmul.allow_tf32 = False
+    sizes = [(40, 24), (24,), (24, 7)]
+    params = [rope._normal(s, torch.float32, "stay", s, scale=0.3).requires_grad_() for s in sizes]
+    x, w = rope._normal((50, 40), torch.float32, "x"), rope._normal((50, 7), torch.float32, "w", scale=0.1)
+    states = [[torch.zeros(s, device="cuda") for s in sizes] for _ in range(2)]
+    control = torch.tensor([1e-2, 0.0, 1.0], device="cuda")
+
+    def backward():
+        ((torch.tanh(x @ params[0] + params[1]) @ params[2]) * w).sum().backward()
+
+    def update(number, plan):
+        """The step, checked against the formula with the gradients that the parameters have now."""
+        control[1] = number
+        before = [{"p": p.detach().clone(), "g": p.grad.clone(), "m": m.clone(), "v": v.clone()} for p, m, v in zip(params, *states)]
+        s2a.s2a_adamw_step(plan, control)
+        rope._done()
+        after = [{"p": p.detach(), "m": m, "v": v} for p, m, v in zip(params, *states)]
+        flat = lambda ts: [{n: t.reshape(-1) for n, t in d.items()} for d in ts]  # noqa: E731
+        step._check_step(flat(before), flat(after), (float(control[0]), float(number), 1.0, 0.9, 0.999, 1e-8), 32, [0.1] * 3, [1.0] * 3)
+
+    def make():
+        return s2a.adamw_plan(params, [p.grad for p in params], *states, weight_decay=0.1)
+
+    backward()
+    plan, places = make(), [p.grad.data_ptr() for p in params]
+    update(1, plan)
+    for number in (2, 3, 4):
+        for p in params:
+            p.grad.zero_()                      # optimizer.zero_grad(set_to_none=False)
+        backward()
+        assert [p.grad.data_ptr() for p in params] == places
+        update(number, plan)
+    for p in params:
+        p.grad = None                           # optimizer.zero_grad()
+    scratch, clip = torch.empty(s2a.grad_norm_scratch_bytes(plan), dtype=torch.uint8, device="cuda"), torch.empty(2, device="cuda")
+    for again in (False, True):                 # nothing in their place yet, and others
+        was = [t.detach().clone() for t in params + states[0] + states[1]]
+        with pytest.raises(s2a.S2AError, match="another"):
+            s2a.s2a_adamw_step(plan, control)
+        with pytest.raises(s2a.S2AError, match="another"):
+            s2a.s2a_grad_norm(plan, control, 1.0, clip, scratch)
+        rope._done()
+        assert all(torch.equal(a, b) for a, b in zip(was, params + states[0] + states[1]))
+        backward()
+    for p in params:
+        p.grad = None
+    backward()
+    update(5, make())
