@@ -13,7 +13,8 @@
 // one load and one store, the block's largest magnitudes by two warp reductions.  What a warp takes from the plan
 // at a time is a chunk of such blocks; the plan has the tensor of each chunk, so that no warp searches.  32-bit states are bound by
 // memory (302 M weights with bfloat16 gradients and copies 1.30 ms, a copy's rate); 8-bit states rounded at random by
-// the instructions of rounding and generator, some 400 a block and warp (the same weights in bfloat16 607 us, 0.76 of it).
+// the instructions of rounding and generator, some 400 a block and warp: the same weights in bfloat16 take 608 us
+// (0.76 of a copy's rate) in runs of some ms, and 680 (0.68) in longer ones, in which the power limit takes the clock from 1.97 to 1.7 GHz.
 #include "s2a_launch.h"
 #include "s2a_oct.cuh"
 #include "s2a_philox.cuh"
@@ -404,7 +405,7 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const StepTensor& 
   }
 }
 
-// CTAs of an SM.  8-bit states: five, and two blocks of a warp's in registers at once (302 M weights, with four times as many CTAs as fit: 625 us;
+// CTAs of an SM (times here and below are of short runs, at the full clock).  8-bit states: five, and two blocks of a warp's in registers at once (302 M weights, with four times as many CTAs as fit: 625 us;
 // 645 with four an SM, 647 with six).  32-bit states: a block is 128 bytes a lane already, and six CTAs with one block each take 10.6 M weights at odd places
 // in 49.6 us, four with two 56.
 template <int BITS> constexpr int kStepCtas = BITS == 8 ? 5 : 6;
@@ -722,11 +723,11 @@ cudaError_t launch_adamw_types(int bits, const StepArgs& a, unsigned grid, cudaS
 cudaError_t launch_adamw(int pdt, int gdt, int state_bits, StepArgs a, cudaStream_t st) {
   if (a.n_chunks == 0) return cudaSuccess;
   // 8-bit states: chunks of four blocks in halves, the two blocks that are in registers at once (8.0 M weights 24 us, whole 27.5; 28 M 71 and 77);
-  // chunks of sixteen whole (302 M weights 607 us, 698 in parts of two to eight)
+  // chunks of sixteen whole (302 M weights 608 us, 698 in parts of two to eight)
   a.split = state_bits == 8 && a.chunk_blocks == 4 ? 1 : 0;
   const uint64_t resident = (uint64_t)sm_count() * (state_bits == 8 ? kStepCtas<8> : kStepCtas<32>);  // CTAs at once
   // Sixteen times as many CTAs as fit, whose last ones even out what the SMs have left (302 M weights: 32-bit states 1298 us, 1397 with as many as
-  // fit; 8-bit states 607, 650); where 8-bit states have few blocks a CTA, its start counts for more (2.4 M weights 10.5 us, 13.6 with four times
+  // fit; 8-bit states 608, 650); where 8-bit states have few blocks a CTA, its start counts for more (2.4 M weights 10.5 us, 13.6 with four times
   // as many as fit).
   const uint64_t want = (((uint64_t)a.n_chunks << a.split) + kStepWarps - 1) / kStepWarps, cap = resident * (state_bits == 8 && a.chunk_blocks < 16 ? 1 : 16);
   const unsigned grid = (unsigned)(want < cap ? want : cap);

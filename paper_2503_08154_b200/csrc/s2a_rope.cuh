@@ -17,7 +17,8 @@
 // phases are computed by all lanes, each some pairs, and shared through the warp's own shared memory.  Rows come through a ring of
 // asynchronous copies of each warp's own, four groups deep (the norm's backward: kBwdStages).  With plain loads, addresses from scratch and the weights read per token, the norm
 // of [64, 197, 12 + 12, 64] bfloat16 took 581 instructions a group and 39.5 us; so it takes 17.0 (a copy of the same bytes: 13.5), the rotation of
-// [2, 16384, 32 + 8, 128] 121.5 us (0.84 of a copy's rate) and the norm's backward of [4, 4097, 32 + 8, 128] 92.4 (0.83).
+// [2, 16384, 32 + 8, 128] 121 to 123 us (0.84 of a copy's rate) and the norm's backward of [4, 4097, 32 + 8, 128] 92 (0.83), or 100 to 102 (0.76) in runs of a
+// second, at the 1.77 GHz that the power limit leaves.
 //
 // Rows that turn as a whole and are 2, 4, 6, 8, 10, 12 or 16 lanes (heads of 32 to 256, whose halves are whole 32-byte sectors) have kernels of their
 // own (L > 0), in which every slot exists and each lane copies for itself; the others (L = 0) ask for each slot and copy by vectors of W elements in order.
