@@ -382,7 +382,7 @@ int s2a_adamw_step(const s2a_step_plan* plan, const void* image, const float* co
   a.beta1 = (float)beta1;
   a.beta2 = (float)beta2;
   a.one_beta1 = (float)(1.0 - beta1);
-  a.root_beta2 = (float)sqrt(beta2);
+  a.one_beta2 = (float)(1.0 - beta2);
   a.root_one_beta2 = (float)sqrt(1.0 - beta2);
   a.log_beta1 = (float)log(beta1);
   a.log_beta2 = (float)log(beta2);

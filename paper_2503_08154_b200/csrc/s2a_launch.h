@@ -150,7 +150,7 @@ struct StepArgs {
   const float* clip;      // norm and factor, or NULL
   const uint64_t* rng;    // seed and offset, or NULL: round to nearest
   uint64_t site;
-  float beta1, one_beta1, beta2, root_beta2, root_one_beta2, log_beta1, log_beta2, eps;  // root: sqrt(beta2), sqrt(1 - beta2)
+  float beta1, one_beta1, beta2, one_beta2, root_one_beta2, log_beta1, log_beta2, eps;  // one: 1 - beta, root: its root
   uint32_t chunk_blocks;  // blocks of a chunk, which a warp takes at a time: 1, 4 or 16
   uint32_t split;         // or 2^-split of them (the step with 8-bit states)
 };

@@ -556,3 +556,68 @@ def test_states_rounded_at_random_follow_where_nearest_stays():
                 assert abs(float(ratio.double().mean()) - kept) <= 5 * deviation + 3.9e-4 + 2e-4
             else:
                 assert torch.equal(now, was)
+
+
+@pytest.mark.parametrize("gdt,random_bits", [("f32", False), ("f32", True), ("bf16", False), ("bf16", True)])
+def test_8_bit_states_are_the_formulas_bit_for_bit(gdt, random_bits):
+    """Four steps by elementary operations, each rounded to binary32: m + (1 - b1)(g' - m), b2 v + ((1 - b2) g') g', the root, the largest of a block,
+    448 times its reciprocal, the product with that and the code.  No code and no scale differs; so none differs in the steps after."""
+    n, b1, b2 = 40_000, 0.9, 0.999
+    f = lambda x: torch.tensor(x, dtype=torch.float32, device="cuda")  # noqa: E731
+    blocks = -(-n // 256)
+    grow = 10 ** (20 * torch.rand(blocks, generator=_gen("grow"), device="cuda") - 12)       # a block's magnitudes, 1e-12 to 1e8
+    per = lambda s: s.repeat_interleave(256)[:n]  # noqa: E731
+    rows = lambda x: torch.nn.functional.pad(x, (0, -n % 256)).view(-1, 256)  # noqa: E731
+    g = (_normal((n,), torch.float32, "bits", gdt) * per(grow)).to(DT[gdt])
+    g[1000:1300] = 0
+    p = torch.zeros(n, device="cuda")
+    m, v = (torch.zeros(n, dtype=torch.uint8, device="cuda").view(E4) for _ in range(2))
+    ms, vs = torch.zeros(blocks, device="cuda"), torch.zeros(blocks, device="cuda")
+    plan = s2a.adamw_plan([p], [g], [m], [v], [ms], [vs])
+    control = torch.tensor([1e-3, 0.0, 0.37], device="cuda")
+    words = torch.tensor([123456789, 77], dtype=torch.int64, device="cuda")
+    code_m, code_v, top_m, top_v = (t.clone() for t in (m, v, ms, vs))
+    scaled = g.float() * control[2]
+    for number in range(1, 5):
+        control[1] = number
+        words[1] += 1
+        s2a.s2a_adamw_step(plan, control, b1, b2, rng=words if random_bits else None, site=5)
+        o = code_m.float() * per(top_m * f(1 / 448))
+        r = code_v.float() * per(top_v * f(1 / 448))
+        want_m = o + f(1 - b1) * (scaled - o)
+        root = (f(b2) * (r * r) + (f(1 - b2) * scaled) * scaled).double().sqrt().float()
+        bits = _fields(n, 0, words.tolist(), 5, False) if random_bits else None
+        codes = []
+        for x, draws in ((want_m, bits), (root, None if bits is None else (bits % 256) * 256 + bits // 256)):
+            top = rows(x.abs()).amax(1)
+            codes.append(top)
+            magnitude = x.abs() * per(torch.where(top > 0, (1 / top.double()).float() * 448, 0.0))
+            if bits is None:
+                codes.append(magnitude.to(E4).view(torch.uint8).int())
+            else:
+                codes.append((((magnitude * 2.0 ** -120).view(torch.int32) + ((draws.int() << 4) | 8)) >> 20).clamp(max=0x7E))
+        top_m, code_m, top_v, code_v = codes
+        code_m = (code_m | ((want_m < 0).int() << 7)).to(torch.uint8).view(E4)
+        code_v = torch.where(root > 0, code_v.clamp(min=1), code_v).to(torch.uint8).view(E4)
+        _done()
+        assert torch.equal(ms, top_m) and torch.equal(vs, top_v)
+        # (a code of zero may have either sign)
+        assert torch.equal(m.float(), code_m.float()) and torch.equal(v.view(torch.uint8), code_v.view(torch.uint8))
+    assert int((v.view(torch.uint8) == 0).sum()) == 300
+
+
+def test_roots_beyond_the_range():
+    """A finite gradient whose square is beyond binary32 leaves its weight (an update of m over an infinity) and the others; zeros and squares below the
+    normal range have the root zero."""
+    n = 512
+    for random_bits in (False, True):
+        p, g = torch.ones(n, device="cuda"), torch.full((n,), 1e-3, device="cuda")
+        g[3], g[300], g[301] = 1e25, 0.0, 1e-22
+        m, v = (torch.zeros(n, dtype=torch.uint8, device="cuda").view(E4) for _ in range(2))
+        scales = [torch.zeros(n // 256, device="cuda") for _ in range(2)]
+        words = torch.tensor([5, 6], dtype=torch.int64, device="cuda") if random_bits else None
+        s2a.s2a_adamw_step(s2a.adamw_plan([p], [g], [m], [v], [scales[0]], [scales[1]]), torch.tensor([1e-2, 1.0, 1.0], device="cuda"), rng=words)
+        _done()
+        assert bool(torch.isfinite(p).all()) and float(p[3]) == 1.0 and float(p[300]) == 1.0 and bool((p[:3] < 1).all())
+        assert float(scales[1][0]) == math.inf and math.isfinite(float(scales[1][1]))
+        assert not v.view(torch.uint8)[300:302].any() and int((v.view(torch.uint8)[256:] == 0).sum()) == 2
