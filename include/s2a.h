@@ -506,7 +506,8 @@ int s2a_step_plan_fill(const s2a_step_tensor* tensors, size_t n_tensors, int pdt
  *   rng      DEVICE, (seed, offset) as for s2a_dropout_fwd, or NULL: round to nearest
  *   site     as for s2a_dropout_fwd
  * 8-bit states hold m and sqrt(v) as e4m3 codes, 448 standing for the largest magnitude of each 256 elements, counted from the tensor's first; the
- * step itself uses the unrounded m and v.  A sqrt(v) above zero never gets the code zero.  A block of which the largest magnitude is below
+ * step itself uses the unrounded m and v, each operation above rounded to binary32 in the order written, v's last term as ((1 - beta2) g') g', so that
+ * states are the same bits wherever this formula is followed.  A sqrt(v) above zero never gets the code zero.  A block of which the largest magnitude is below
  * 2^-110 is stored as zeros.  With rng, 8-bit states and bfloat16 parameters are rounded at random, up with the probability of
  * what lies above the lower neighbour (binary32 ones need no rounding, copies are rounded to nearest): element e of a tensor that starts at block b of 256 in the
  * plan (each tensor takes whole blocks) owns 16 bits of Philox4x32-10 under key rng[0] at counter (32 b + e / 8, rng[1] + site),

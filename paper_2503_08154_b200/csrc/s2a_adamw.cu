@@ -13,8 +13,8 @@
 // one load and one store, the block's largest magnitudes by two warp reductions.  What a warp takes from the plan
 // at a time is a chunk of such blocks; the plan has the tensor of each chunk, so that no warp searches.  32-bit states are bound by
 // memory (302 M weights with bfloat16 gradients and copies 1.30 ms, a copy's rate); 8-bit states rounded at random by
-// the instructions of rounding and generator, some 400 a block and warp: the same weights in bfloat16 take 608 us
-// (0.76 of a copy's rate) in runs of some ms, and 680 (0.68) in longer ones, in which the power limit takes the clock from 1.97 to 1.7 GHz.
+// the instructions of the formula step by step, rounding and generator, some 460 a block and warp: the same weights in bfloat16 take 684 us
+// (0.68 of a copy's rate) in runs of some ms, and 750 (0.62) in longer ones, in which the power limit takes the clock from 1.97 to 1.78 GHz.
 #include "s2a_launch.h"
 #include "s2a_oct.cuh"
 #include "s2a_philox.cuh"
@@ -435,7 +435,8 @@ __device__ __forceinline__ void step_block(const StepArgs& a, const StepTensor& 
   }
 }
 
-// CTAs of an SM (times here and below are of short runs, at the full clock).  8-bit states: five, and two blocks of a warp's in registers at once (302 M weights, with four times as many CTAs as fit: 625 us;
+// CTAs of an SM (times here and below are of short runs, at the full clock, and those of 8-bit states of when the 302 M weights took 608 us, before
+// `moments` rounded each operation; now five 684, four 698).  8-bit states: five, and two blocks of a warp's in registers at once (302 M weights, with four times as many CTAs as fit: 625 us;
 // 645 with four an SM, 647 with six).  32-bit states: a block is 128 bytes a lane already, and six CTAs with one block each take 10.6 M weights at odd places
 // in 49.6 us, four with two 56.
 template <int BITS> constexpr int kStepCtas = BITS == 8 ? 5 : 6;

@@ -183,8 +183,8 @@ struct Span {
 size_t blocks_of(size_t n) { return (n + kStepBlock - 1) / kStepBlock; }
 
 // Blocks of a chunk: one where the plan is small, so that every warp gets one; four where every warp gets a chunk all the same, and sixteen where it
-// gets sixteen, as each chunk costs a look at the plan and a wait for its first block (302 M weights with 8-bit states: 608 us with 16 blocks,
-// 698 with 4; their gradients' norm 90 and 105).
+// gets sixteen, as each chunk costs a look at the plan and a wait for its first block (302 M weights with 8-bit states, before each operation was rounded: 608 us with
+// 16 blocks, 698 with 4; their gradients' norm 90 and 105).
 size_t chunk_blocks_of(size_t blocks) {
   const size_t warps = 148 * 20;
   return blocks >= 256 * warps ? 16 : (blocks >= 4 * warps ? 4 : 1);
