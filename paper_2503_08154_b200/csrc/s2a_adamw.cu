@@ -184,8 +184,8 @@ __device__ __forceinline__ F2 sub_rounded(F2 a, F2 b) {
   return f2_pack(__fsub_rn(x, u), __fsub_rn(y, v));
 }
 
-// The roots of two numbers, as __fsqrt_rn gives them (which costs 4 % more of the whole step): v times the approximate reciprocal root, and one step of
-// Newton's iteration on the remainder.  That makes NaN of zeros (what is below the normal range among them) and infinities, and v 2^-64, which is
+// The rounded roots of two numbers: v times the approximate reciprocal root, and one step of Newton's iteration on the remainder (Markstein, "Computation
+// of elementary functions on the IBM RISC System/6000 processor", 1990); __fsqrt_rn has the same bits and costs 4 % more of the step rounded at random.  That makes NaN of zeros (what is below the normal range among them) and infinities, and v 2^-64, which is
 // never above the root, takes their place.
 __device__ __forceinline__ F2 roots(F2 v) {
   float x, y, u, w;
