@@ -185,8 +185,9 @@ __device__ __forceinline__ F2 sub_rounded(F2 a, F2 b) {
 }
 
 // The rounded roots of two numbers: v times the approximate reciprocal root, and one step of Newton's iteration on the remainder (Markstein, "Computation
-// of elementary functions on the IBM RISC System/6000 processor", 1990); __fsqrt_rn has the same bits and costs 4 % more of the step rounded at random.  That makes NaN of zeros (what is below the normal range among them) and infinities, and v 2^-64, which is
-// never above the root, takes their place.
+// of elementary functions on the IBM RISC System/6000 processor", 1990); with __fsqrt_rn the codes of 302 M weights are the same, and the step that rounds at
+// random takes 4 % longer.  The iteration makes NaN of infinities and of zeros (what is below the normal range among them); v 2^-64, which is never
+// above the root, takes their place.
 __device__ __forceinline__ F2 roots(F2 v) {
   float x, y, u, w;
   f2_unpack(v, x, y);
